@@ -325,7 +325,7 @@ def _plain_update(s):
         m.copy_(m2)
         v.copy_(v2)
     else:
-        h = (s["index"].to(torch.int64) * 0x9E3779B1 + t * 0x7F4A7C15) & 0xFFFFFFFF
+        h = (s["index"].to(torch.int64) * 0x6A09E667 + t * 0x9E3779B9) & 0xFFFFFFFF
         u = (h >> 12).float() * 2.0 ** -20
         mq, ms = _plain_store(m2, u, False)
         u = ((h ^ 0x80000000) >> 12).float() * 2.0 ** -20

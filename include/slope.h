@@ -54,7 +54,8 @@ typedef enum {
     SLOPE_ERR_ALIGN = -3,       /* a pointer is not 16-byte aligned                    */
     SLOPE_ERR_UNSUPPORTED = -4, /* N:M other than 2:4, adapter rank not supported      */
     SLOPE_ERR_HIP = -5,         /* a launch failed; see slope_last_hip_error()         */
-    SLOPE_ERR_WORKSPACE = -6    /* the scratch buffer is smaller than the call needs   */
+    SLOPE_ERR_WORKSPACE = -6,   /* the scratch buffer is smaller than the call needs   */
+    SLOPE_ERR_VALUE = -7        /* a scalar argument is outside its range              */
 } slope_status;
 
 /* Library version (major*100 + minor) and the last hipError_t seen by this thread. */
@@ -80,7 +81,9 @@ typedef enum {
     SLOPE_CALL_SPMM_BWD_X_ADAPTER = 7,
     SLOPE_CALL_WGRAD_ADAPTER = 8,
     SLOPE_CALL_WGRAD_MASKED_T = 9,
-    SLOPE_CALL_SPMM_BWD_X_WS = 10
+    SLOPE_CALL_SPMM_BWD_X_WS = 10,
+    SLOPE_CALL_RMSNORM_BWD = 11,       /* d_in: the width d; d_out and r are not looked at */
+    SLOPE_CALL_SPMM_FWD_Q8 = 12        /* r is not looked at                                */
 } slope_call_id;
 
 /* Bytes of scratch memory a call wants for b tokens, a d_out x d_in layer and adapter rank r (0: none);
@@ -307,6 +310,110 @@ slope_status slope_sparse_add(const void* A_vals, const void* B_vals, int64_t ro
  */
 slope_status slope_update_sparse(const void* Wnew_vals, const void* Wr_meta, int64_t d_out, int64_t d_in,
                                  void* Wr_vals, const void* WrcT_meta, void* WrcT_vals, void* stream);
+
+/*
+ * ---- the layer's surroundings: norm, 8-bit product, optimizer ----
+ *
+ * 8-bit values are OCP e4m3 (largest 448) with an fp32 scale for each row: code = value / scale rounded to nearest even,
+ * scale = largest magnitude of the row * (1 / 448).  A row whose largest magnitude is below 1e-30 has scale 0 and codes 0; a
+ * row that holds an infinity or NaN has a scale that is not finite.
+ *
+ * slope_rmsnorm_fwd - residual addition and root-mean-square norm over the d elements of each of b tokens:
+ *     H = bf16(X + residual) (H is X without a residual)    r = 1 / sqrt(mean(H^2) + eps)    y = H r weight
+ * The statistics are those of H as it is stored; all sums are fp32.
+ *   X, residual_or_null in bf16[b, d]    weight in bf16[d]
+ *   H_or_null     out bf16[b, d]  the summed stream; required with a residual, NULL without; may be X or the residual.
+ *                     No other output may overlap an input.
+ *   Y_or_null     out bf16[b, d]  y
+ *   rstd_or_null  out fp32[b]     r, which slope_rmsnorm_bwd wants
+ *   Q_or_null, scale_or_null out e4m3[b, d], fp32[b]   y in 8 bits with a scale per token, what slope_spmm_fwd_q8 reads;
+ *                     both or neither.  At least one of Y and Q is wanted.
+ *   d % 8 == 0, d < 2^24; eps > 0 and finite (SLOPE_ERR_VALUE)
+ *
+ * slope_rmsnorm_bwd - its gradient:
+ *     g = dY weight    c = mean(g H r)    dX = r (g - H r c) + dH    dweight = sum over tokens of dY H r
+ * dX is the gradient of X and of the residual alike; sums are fp32 and added in a fixed order.
+ *   dY, H in bf16[b, d]   weight in bf16[d]   rstd in fp32[b]
+ *   dH_or_null in bf16[b, d]  the gradient that reaches H beside the norm (the residual stream's); may be dX
+ *   dX out bf16[b, d] (may be dY or dH, not H)   dweight out bf16[d]
+ *   workspace  slope_rmsnorm_bwd_workspace_bytes(b, d) bytes, 256-byte aligned
+ */
+slope_status slope_rmsnorm_fwd(const void* X, const void* residual_or_null, const void* weight, int64_t b, int64_t d,
+                               double eps, void* H_or_null, void* Y_or_null, void* rstd_or_null, void* Q_or_null,
+                               void* scale_or_null, void* stream);
+size_t slope_rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d);
+slope_status slope_rmsnorm_bwd(const void* dY, const void* H, const void* weight, const void* rstd, const void* dH_or_null,
+                               int64_t b, int64_t d, void* dX, void* dweight, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * slope_quantize_packed - packed values of W^R to 8 bits with a scale per weight row, once per weight; the metadata serves
+ * both forms.
+ *   Wr_vals in bf16[d_out, d_in/2]   Wq_vals out e4m3[d_out, d_in/2]   w_scale out fp32[d_out]     d_in % 8 == 0
+ *
+ * slope_spmm_fwd_q8 - the forward product on 8-bit operands (inference; Eq. 4):
+ *     Y[i, j] = bf16(x_scale[i] w_scale[j] sum_k Xq[i, k] W^R[j, k] + add[i, j])
+ *   Xq in e4m3[b, d_in], x_scale in fp32[b]     Wq_vals in e4m3[d_out, d_in/2], Wr_meta in u8[d_out, d_in/8], w_scale in fp32[d_out]
+ *   add_or_null in bf16[b, d_out]  a residual stream or an adapter's product; may be Y
+ *   Y out bf16[b, d_out]; fp32 accumulation over instructions of 64 products each
+ *   workspace_or_null  slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out) bytes (may be 0), 256-byte aligned: lets the call
+ *       split the contraction where tiles alone would leave much of the chip idle.  NULL: no split; too small a buffer:
+ *       SLOPE_ERR_WORKSPACE
+ */
+slope_status slope_quantize_packed(const void* Wr_vals, int64_t d_out, int64_t d_in, void* Wq_vals, void* w_scale, void* stream);
+size_t slope_spmm_fwd_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out);
+slope_status slope_spmm_fwd_q8(const void* Xq, const void* x_scale, int64_t b, const void* Wq_vals, const void* Wr_meta,
+                               const void* w_scale, int64_t d_out, int64_t d_in, const void* add_or_null, void* Y,
+                               void* workspace_or_null, size_t workspace_bytes, void* stream);
+
+/*
+ * slope_adamw_step - AdamW on any number of tensors in one launch (the optimizer of Algorithm 1 between slope_wgrad_masked and
+ * slope_update_sparse: packed values are a tensor like any other, their pattern does not matter here):
+ *     g = c grad    m = beta1 m + (1 - beta1) g    v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * A set of tensors is described once:
+ */
+#define SLOPE_ADAMW_BLOCK 128
+typedef struct {
+    void* param;          /* bf16[n], written; also the value that is updated if there is no master; NULL with a master */
+    void* master;         /* fp32[n], the value that is updated, or NULL                                               */
+    const void* grad;     /* bf16[n] or fp32[n]                                                                        */
+    void* m;              /* first moment: fp32[n]; 8-bit states: e4m3[n]                                              */
+    void* v;              /* second moment: fp32[n]; 8-bit states: its square root, e4m3[n]                            */
+    float* m_scale;       /* 8-bit states: fp32[(n + 127) / 128], value = code * scale; else not looked at              */
+    float* v_scale;
+    int64_t n;            /* elements; 0: left alone                                                                   */
+    float weight_decay;
+    int32_t grad_bits;    /* 16 or 32                                                                                  */
+} slope_adamw_tensor;
+/*
+ *   All pointers 16-byte aligned (the scales: 4-byte); no two tensors may overlap.
+ * slope_adamw_table checks `count` descriptions and lays out the table of a set in HOST memory, slope_adamw_table_bytes bytes;
+ * the caller copies it to device memory (16-byte aligned) as it is and passes both to the calls below: the host copy says what
+ * to launch, the device copy which memory to work on.  A table is good as long as the memory it names; it holds no state.
+ *   state_bits  32 or 8
+ *
+ * With 8-bit states new codes are rounded up or down according to a threshold that moves with the step, so that averages of
+ * slow decay are tracked without bias; the update itself uses m and v before they are rounded.  States start as zeros.
+ *
+ * slope_grad_norm - the global norm of a set's gradients, for clipping and for leaving out steps that are not finite:
+ *     norm = inv_scale sqrt(sum grad^2)    c = inv_scale min(1, max_norm / (norm + 1e-6))
+ *   control  in/out fp32[4], device: {norm, c (0 if norm is not finite), steps taken (incremented if norm is finite), unused};
+ *            starts as zeros
+ *   inv_scale  1 / loss scale, > 0;  max_norm  > 0, infinity: no clipping
+ *   workspace  slope_grad_norm_workspace_bytes(table) bytes, 256-byte aligned
+ * slope_adamw_step
+ *   control_or_null  as written by slope_grad_norm: c, t and whether the step is left out (nothing is written then) come from
+ *            there, so that the host need not wait; NULL: c = grad_scale and t = step >= 1
+ *   lr >= 0; 0 <= beta < 1; eps > 0; all finite (SLOPE_ERR_VALUE)
+ */
+size_t slope_adamw_table_bytes(const slope_adamw_tensor* tensors, int64_t count);
+slope_status slope_adamw_table(const slope_adamw_tensor* tensors, int64_t count, int state_bits, void* table, size_t table_bytes);
+size_t slope_grad_norm_workspace_bytes(const void* table);
+slope_status slope_grad_norm(const void* table, const void* device_table, double inv_scale, double max_norm, void* control,
+                             void* workspace, size_t workspace_bytes, void* stream);
+slope_status slope_adamw_step(const void* table, const void* device_table, double lr, double beta1, double beta2, double eps,
+                              double grad_scale, int64_t step, const void* control_or_null, void* stream);
 
 /*
  * slope_spmm_fwd_plan - diagnostics, host only (no GPU call): which kernels slope_spmm_fwd (Eq. 4, 11)

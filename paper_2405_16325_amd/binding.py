@@ -21,13 +21,14 @@ SLOPE_ERR_ALIGN = -3
 SLOPE_ERR_UNSUPPORTED = -4
 SLOPE_ERR_HIP = -5
 SLOPE_ERR_WORKSPACE = -6
+SLOPE_ERR_VALUE = -7
 SLOPE_STATIC_SCRATCH_BYTES = 72 << 20      # include/slope.h
 # slope_call_id
 (SLOPE_CALL_PRUNE_ROWS, SLOPE_CALL_DOUBLE_PRUNE, SLOPE_CALL_SPMM_FWD, SLOPE_CALL_SPMM_BWD_X, SLOPE_CALL_WGRAD_MASKED,
  SLOPE_CALL_WGRAD_MASKED_WS, SLOPE_CALL_SPMM_BWD_X_ADAPTER, SLOPE_CALL_WGRAD_ADAPTER,
- SLOPE_CALL_WGRAD_MASKED_T, SLOPE_CALL_SPMM_BWD_X_WS) = range(1, 11)
+ SLOPE_CALL_WGRAD_MASKED_T, SLOPE_CALL_SPMM_BWD_X_WS, SLOPE_CALL_RMSNORM_BWD, SLOPE_CALL_SPMM_FWD_Q8) = range(1, 13)
 
-_P, _I64, _INT, _SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+_P, _I64, _INT, _SZ, _DBL = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_double
 
 # name -> (restype, argtypes); mirrors include/slope.h one to one
 SIGNATURES = {
@@ -60,6 +61,17 @@ SIGNATURES = {
     "slope_gemm_tn": (_INT, [_P, _I64, _P, _I64, _I64, _P, _P]),
     "slope_sparse_add": (_INT, [_P, _P, _I64, _I64, ctypes.c_float, ctypes.c_float, _P, _P]),
     "slope_update_sparse": (_INT, [_P, _P, _I64, _I64, _P, _P, _P, _P]),
+    "slope_rmsnorm_fwd": (_INT, [_P, _P, _P, _I64, _I64, _DBL, _P, _P, _P, _P, _P, _P]),
+    "slope_rmsnorm_bwd_workspace_bytes": (_SZ, [_I64, _I64]),
+    "slope_rmsnorm_bwd": (_INT, [_P, _P, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "slope_quantize_packed": (_INT, [_P, _I64, _I64, _P, _P, _P]),
+    "slope_spmm_fwd_q8_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "slope_spmm_fwd_q8": (_INT, [_P, _P, _I64, _P, _P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
+    "slope_adamw_table_bytes": (_SZ, [_P, _I64]),
+    "slope_adamw_table": (_INT, [_P, _I64, _INT, _P, _SZ]),
+    "slope_grad_norm_workspace_bytes": (_SZ, [_P]),
+    "slope_grad_norm": (_INT, [_P, _P, _DBL, _DBL, _P, _P, _SZ, _P]),
+    "slope_adamw_step": (_INT, [_P, _P, _DBL, _DBL, _DBL, _DBL, _DBL, _I64, _P, _P]),
     "slope_ceiling_min_bytes": (_SZ, []),
     "slope_ceiling": (_INT, [_INT, _P, _SZ, _INT, _P, _P]),
     "slope_tile_order": (_I64, [_I64, _I64, _P, _P, _I64]),
@@ -439,6 +451,180 @@ def slope_update_sparse(Wnew_vals: torch.Tensor, meta: torch.Tensor, vals: torch
     _check("slope_update_sparse", lib().slope_update_sparse(_ptr(Wnew_vals), _ptr(meta), d_out, d_in, _ptr(vals),
                                                             _ptr(meta_t), _ptr(vals_t), _stream()))
     return vals, vals_t
+
+
+# ---------------------------------------------------------------- the layer's surroundings: norm, 8-bit product, optimizer
+F32, E4M3 = torch.float32, torch.float8_e4m3fn
+SLOPE_ADAMW_BLOCK = 128
+
+
+def slope_rmsnorm_fwd(X: torch.Tensor, weight: torch.Tensor, eps: float, residual=None, want_y: bool = True,
+                      want_rstd: bool = False, want_q8: bool = False, out=None):
+    """RMS norm of X (+ residual) bf16[b, d]: (Y bf16[b, d], H bf16[b, d], rstd fp32[b], Q e4m3[b, d], scale fp32[b]); what was
+    not asked for is None, and H (the summed stream) without a residual.  out: the same five, to write into; H may be X or
+    the residual."""
+    if X is None or X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    b, d = X.shape
+    _want(X, BF16, (b, d), "X")
+    _want(weight, BF16, (d,), "weight")
+    if residual is not None:
+        _want(residual, BF16, (b, d), "residual")
+    if out is None:
+        new = lambda shape, dtype, asked: torch.empty(shape, dtype=dtype, device=X.device) if asked else None   # noqa: E731
+        Y, H = new((b, d), BF16, want_y), new((b, d), BF16, residual is not None)
+        rstd, Q, scale = new((b,), F32, want_rstd), new((b, d), E4M3, want_q8), new((b,), F32, want_q8)
+    else:
+        Y, H, rstd, Q, scale = out
+        for t, dtype, shape, what in ((Y, BF16, (b, d), "Y"), (H, BF16, (b, d), "H"), (rstd, F32, (b,), "rstd"),
+                                      (Q, E4M3, (b, d), "Q"), (scale, F32, (b,), "scale")):
+            if t is not None:
+                _want(t, dtype, shape, what)
+    _check("slope_rmsnorm_fwd", lib().slope_rmsnorm_fwd(_ptr(X), _ptr(residual), _ptr(weight), b, d, eps, _ptr(H), _ptr(Y),
+                                                        _ptr(rstd), _ptr(Q), _ptr(scale), _stream()))
+    return Y, H, rstd, Q, scale
+
+
+def slope_rmsnorm_bwd(dY: torch.Tensor, H: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dh=None, out=None,
+                      workspace=None):
+    """Gradient of slope_rmsnorm_fwd at the normed stream H: (dX bf16[b, d], dweight bf16[d]).  dh bf16[b, d]: the gradient that
+    reaches H beside the norm, added to dX.  out: (dX, dweight); dX may be dY or dh.
+    workspace: a uint8 device tensor of slope_workspace_bytes(SLOPE_CALL_RMSNORM_BWD, b, d, 0) bytes, or None (allocated here)."""
+    if dY is None or dY.dim() != 2:
+        raise ValueError("dY must be a matrix")
+    b, d = dY.shape
+    _want(dY, BF16, (b, d), "dY")
+    _want(H, BF16, (b, d), "H")
+    _want(weight, BF16, (d,), "weight")
+    _want(rstd, F32, (b,), "rstd")
+    if dh is not None:
+        _want(dh, BF16, (b, d), "dh")
+    if out is None:
+        dX, dw = torch.empty((b, d), dtype=BF16, device=dY.device), torch.empty((d,), dtype=BF16, device=dY.device)
+    else:
+        dX, dw = _want(out[0], BF16, (b, d), "dX"), _want(out[1], BF16, (d,), "dweight")
+    workspace = _scratch(workspace, int(lib().slope_rmsnorm_bwd_workspace_bytes(b, d)), dY.device, "workspace")
+    _check("slope_rmsnorm_bwd", lib().slope_rmsnorm_bwd(_ptr(dY), _ptr(H), _ptr(weight), _ptr(rstd), _ptr(dh), b, d, _ptr(dX),
+                                                        _ptr(dw), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return dX, dw
+
+
+def slope_quantize_packed(vals: torch.Tensor, out=None):
+    """Packed values bf16[d_out, d_in/2] -> (e4m3[d_out, d_in/2], scale fp32[d_out]); the metadata serves both."""
+    if vals is None or vals.dim() != 2:
+        raise ValueError("vals must be a matrix")
+    d_out, half = vals.shape
+    _want(vals, BF16, (d_out, half), "vals")
+    if out is None:
+        q, scale = torch.empty((d_out, half), dtype=E4M3, device=vals.device), torch.empty((d_out,), dtype=F32, device=vals.device)
+    else:
+        q, scale = _want(out[0], E4M3, (d_out, half), "values"), _want(out[1], F32, (d_out,), "scale")
+    _check("slope_quantize_packed", lib().slope_quantize_packed(_ptr(vals), d_out, 2 * half, _ptr(q), _ptr(scale), _stream()))
+    return q, scale
+
+
+def slope_spmm_fwd_q8(Xq: torch.Tensor, x_scale: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, w_scale: torch.Tensor,
+                      add=None, out=None, workspace="auto"):
+    """Y = X (W^R)^T (+ add) on 8-bit operands: Xq e4m3[b, d_in] with x_scale fp32[b] (slope_rmsnorm_fwd), vals
+    e4m3[d_out, d_in/2] with w_scale fp32[d_out] (slope_quantize_packed), meta as for slope_spmm_fwd; add bf16[b, d_out] (may be
+    out).  workspace: "auto" (allocated here when the shape wants one), None (the contraction is not split) or a uint8 device
+    tensor of slope_workspace_bytes(SLOPE_CALL_SPMM_FWD_Q8, b, d_in, d_out) bytes."""
+    if Xq is None or Xq.dim() != 2 or vals is None or vals.dim() != 2:
+        raise ValueError("Xq and vals must be matrices")
+    b, d_in = Xq.shape
+    d_out = vals.shape[0]
+    _want(Xq, E4M3, (b, d_in), "Xq")
+    _want(x_scale, F32, (b,), "x_scale")
+    _want(vals, E4M3, (d_out, d_in // 2), "vals")
+    _want(meta, U8, (d_out, d_in // 8), "meta")
+    _want(w_scale, F32, (d_out,), "w_scale")
+    if add is not None:
+        _want(add, BF16, (b, d_out), "add")
+    Y = _want(out, BF16, (b, d_out), "out") if out is not None else torch.empty((b, d_out), dtype=BF16, device=Xq.device)
+    if workspace is not None:
+        need = int(lib().slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out))
+        workspace = _scratch(None if isinstance(workspace, str) else workspace, need, Xq.device, "workspace") if need else None
+    _check("slope_spmm_fwd_q8", lib().slope_spmm_fwd_q8(_ptr(Xq), _ptr(x_scale), b, _ptr(vals), _ptr(meta), _ptr(w_scale), d_out,
+                                                        d_in, _ptr(add), _ptr(Y), _ptr(workspace),
+                                                        0 if workspace is None else workspace.numel(), _stream()))
+    return Y
+
+
+class AdamWTensor(ctypes.Structure):                                     # slope_adamw_tensor
+    _fields_ = [("param", _P), ("master", _P), ("grad", _P), ("m", _P), ("v", _P), ("m_scale", _P), ("v_scale", _P), ("n", _I64),
+                ("weight_decay", ctypes.c_float), ("grad_bits", ctypes.c_int32)]
+
+
+class AdamWPlan:
+    """A set of tensors that slope_grad_norm and slope_adamw_step work on in place.  Holds on to them; they must stay where
+    they are (a gradient is read from the buffer it had when the plan was made)."""
+
+    def __init__(self, tensors, state_bits, table, device_table):
+        self.tensors, self.state_bits = tensors, state_bits
+        self.table, self.device_table = table, device_table
+        self.workspace_bytes = int(lib().slope_grad_norm_workspace_bytes(table))
+
+
+def slope_adamw_plan(params, grads, m, v, masters=None, m_scales=None, v_scales=None, weight_decay=0.0) -> AdamWPlan:
+    """Lists with an entry per tensor.  params: bf16, or None where there is only a master; masters: fp32 or None; grads: bf16 or
+    fp32; m, v: fp32, or e4m3 (8-bit states; v holds roots) with m_scales, v_scales fp32[(n + 127) // 128].  All tensors of a set
+    have states of one type.  weight_decay: a number for all or a list."""
+    count = len(grads)
+    decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+    lists = [list(x) if x is not None else [None] * count for x in (params, masters, m, v, m_scales, v_scales)]
+    if count == 0 or len(decay) != count or any(len(x) != count for x in lists):
+        raise ValueError("the lists must have an entry for every tensor, and at least one")
+    params, masters, m, v, m_scales, v_scales = lists
+    bits = 8 if m[0] is not None and m[0].dtype == E4M3 else 32
+    state = E4M3 if bits == 8 else F32
+    table, device = (AdamWTensor * count)(), None
+    for i, g in enumerate(grads):
+        if g is None or g.dtype not in (BF16, F32):
+            raise ValueError("grads[%d] must be a bf16 or fp32 tensor" % i)
+        if params[i] is None and masters[i] is None:
+            raise ValueError("params[%d] and masters[%d] are both missing" % (i, i))
+        shape, n, blocks = g.shape, g.numel(), (g.numel() + SLOPE_ADAMW_BLOCK - 1) // SLOPE_ADAMW_BLOCK
+        _want(g, g.dtype, shape, "grads[%d]" % i)
+        for t, dtype, size, what in ((params[i], BF16, shape, "params"), (masters[i], F32, shape, "masters")):
+            if t is not None:
+                _want(t, dtype, size, "%s[%d]" % (what, i))
+        _want(m[i], state, shape, "m[%d]" % i)
+        _want(v[i], state, shape, "v[%d]" % i)
+        if bits == 8:
+            _want(m_scales[i], F32, (blocks,), "m_scales[%d]" % i)
+            _want(v_scales[i], F32, (blocks,), "v_scales[%d]" % i)
+        device = g.device if device is None else device
+        if any(t is not None and t.device != device for t in (g, params[i], masters[i], m[i], v[i], m_scales[i], v_scales[i])):
+            raise ValueError("all tensors of a plan must be on one device")
+        table[i] = AdamWTensor(_ptr(params[i]), _ptr(masters[i]), _ptr(g), _ptr(m[i]), _ptr(v[i]),
+                               _ptr(m_scales[i]) if bits == 8 else None, _ptr(v_scales[i]) if bits == 8 else None, n, decay[i],
+                               32 if g.dtype == F32 else 16)
+    need = int(lib().slope_adamw_table_bytes(table, count))
+    host = torch.empty(max(need, 64), dtype=U8)
+    _check("slope_adamw_table", lib().slope_adamw_table(table, count, bits, host.data_ptr(), host.numel()))
+    plan = AdamWPlan([params, masters, list(grads), m, v, m_scales, v_scales], bits, host.data_ptr(), host.to(device))
+    plan.host = host
+    return plan
+
+
+def slope_grad_norm(plan: AdamWPlan, control: torch.Tensor, inv_scale: float = 1.0, max_norm: float = float("inf"), workspace=None):
+    """Global norm of the plan's gradients into control fp32[4] = {norm, factor for the gradients, steps taken, unused} (starts as
+    zeros); nothing is copied to the host."""
+    _want(control, F32, (4,), "control")
+    workspace = _scratch(workspace, plan.workspace_bytes, control.device, "workspace")
+    _check("slope_grad_norm", lib().slope_grad_norm(plan.table, _ptr(plan.device_table), inv_scale, max_norm, _ptr(control),
+                                                    _ptr(workspace), workspace.numel(), _stream()))
+    return control
+
+
+def slope_adamw_step(plan: AdamWPlan, lr: float, beta1: float, beta2: float, eps: float, step: int = 0, grad_scale: float = 1.0,
+                     control=None):
+    """One AdamW step on the plan's tensors.  control (written by slope_grad_norm): the gradients' factor, the step's number and
+    whether the step is left out come from there; else grad_scale and step >= 1."""
+    if control is not None:
+        _want(control, F32, (4,), "control")
+    _check("slope_adamw_step", lib().slope_adamw_step(plan.table, _ptr(plan.device_table), lr, beta1, beta2, eps, grad_scale, step,
+                                                      _ptr(control), _stream()))
 
 
 (SLOPE_CEILING_SPARSE_MFMA, SLOPE_CEILING_DENSE_MFMA, SLOPE_CEILING_READ, SLOPE_CEILING_COPY,

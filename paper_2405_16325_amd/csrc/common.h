@@ -140,6 +140,26 @@ hipError_t launch_wgrad_adapter(const bf16_t* dY, const bf16_t* X, int64_t b, co
                                 int64_t d_in, const bf16_t* L, const bf16_t* R, int64_t r, bf16_t* gvals, bf16_t* dL,
                                 bf16_t* dR, void* workspace, hipStream_t s);
 
+// the layer's surroundings (rmsnorm.hip, spmm_q8.hip, adamw.hip)
+hipError_t launch_rmsnorm_fwd(const bf16_t* x, const bf16_t* res, const bf16_t* w, int64_t b, int64_t d, float eps, bf16_t* h,
+                              bf16_t* y, float* rstd, uint8_t* q, float* scale, hipStream_t s);
+size_t rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d);
+hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w, const float* rstd, const bf16_t* dh, int64_t b,
+                              int64_t d, bf16_t* dx, bf16_t* dw, float* part, hipStream_t s);
+hipError_t launch_quantize_packed(const bf16_t* vals, int64_t rows, int64_t cols, uint8_t* q, float* scale, hipStream_t s);
+size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K);
+hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,
+                          int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* partial_or_null, hipStream_t s);
+int64_t adamw_chunks(const slope_adamw_tensor* tensors, int64_t count);
+size_t adamw_table_bytes(int64_t count, int64_t chunks);
+void adamw_fill_table(const slope_adamw_tensor* tensors, int64_t count, int state_bits, void* table);
+bool adamw_table_ok(const void* table);
+size_t grad_norm_workspace_bytes(const void* table);
+hipError_t launch_grad_norm(const void* table, const void* device_table, float inv_scale, float max_norm, float* control,
+                            float* part, hipStream_t s);
+hipError_t launch_adamw(const void* table, const void* device_table, double lr, double beta1, double beta2, double eps,
+                        double grad_scale, int64_t step, const float* control, hipStream_t s);
+
 // Launches of any number of workgroups as rows of 2^20: a dimension of a grid holds fewer than 2^32 work items, and a launch
 // beyond that runs a part of them without an error.  A kernel takes flat_block() and leaves when it is past the last.
 constexpr int64_t GRID_ROW = (int64_t)1 << 20;

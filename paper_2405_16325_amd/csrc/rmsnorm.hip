@@ -1,0 +1,400 @@
+// Root-mean-square norm with the residual's addition, its 8-bit output, and its gradient.
+//
+//     h = bf16(x + res)      r = 1 / sqrt(mean_j h_j^2 + eps)      y_j = h_j r w_j
+//     q = e4m3(y / s), s = max_j |y_j| / 448                        (one scale per token, for the 8-bit product)
+//     g_j = dy_j w_j,  c = mean_j g_j h_j r:   dx_j = r (g_j - h_j r c) + dh_j      dw_j = sum over tokens of dy_j h_j r
+//
+// The statistics are those of the stream as it is stored, rounded: the gradient is taken at that h.  All sums are fp32.
+// Memory bounds both directions.  A row is read once and stays in registers: LPR lanes (8 to 64) of a wavefront share a
+// short one, `wpr` wavefronts a longer one; a lane holds VPT pieces of 8 neighbouring elements, so that every load and
+// store of a wavefront covers whole 128-byte lines.
+#include "wave.h"
+
+namespace {
+
+constexpr int MAX_THREADS = 1024;
+constexpr int MAX_WAVES = MAX_THREADS / 64;
+
+// The threads of one row: `lane` of `threads`, piece p of the row is lane + p * threads
+struct RowThreads { int row, lane, threads; };
+template <int LPR>
+__device__ __forceinline__ RowThreads row_threads(int wpr) {
+    const int t = threadIdx.x;
+    if constexpr (LPR < 64) return {t / LPR, t % LPR, LPR};
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), row = wpr == 1 ? wave : wave / wpr;
+    return {row, (wave - row * wpr) * 64 + (t & 63), wpr * 64};
+}
+
+// Sum (or largest) over a row's threads.  part: MAX_WAVES floats of LDS that nothing else uses until the next barrier but one.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v, int wpr, float* part) {
+    v = lanes_sum<LPR>(v);
+    if (LPR < 64 || wpr == 1) return v;
+    const int wave = threadIdx.x >> 6, first = wave / wpr * wpr;
+    if ((threadIdx.x & 63) == 0) part[wave] = v;
+    __syncthreads();
+    v = part[first];
+    for (int i = 1; i < wpr; ++i) v += part[first + i];
+    return v;
+}
+template <int LPR>
+__device__ __forceinline__ float row_max(float v, int wpr, float* part) {
+    v = lanes_max_abs<LPR>(v);
+    if (LPR < 64 || wpr == 1) return v;
+    const int wave = threadIdx.x >> 6, first = wave / wpr * wpr;
+    if ((threadIdx.x & 63) == 0) part[wave] = v;
+    __syncthreads();
+    v = part[first];
+    for (int i = 1; i < wpr; ++i) v = max_abs(v, part[first + i]);
+    return v;
+}
+
+struct NormFwd {
+    const bf16_t *x, *res, *w;                 // res: or null
+    int64_t b;
+    int d;
+    float eps;
+    bf16_t *h, *y;                             // y: or null
+    float* rstd;                               // or null
+    uint8_t* q;                                // or null
+    float* scale;
+};
+
+template <int LPR, int VPT>
+__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int wpr) {
+    __shared__ float part[2][MAX_WAVES];
+    const RowThreads rt = row_threads<LPR>(wpr);
+    const int64_t row = flat_block() * (blockDim.x / rt.threads) + rt.row;
+    const bool live = row < a.b;
+    const int pieces = a.d / 8;
+    const size_t at = (size_t)row * a.d;
+
+    F8 h[VPT];
+    u32x4 w[VPT];
+    float sum = 0.0f;
+    u32x4 px[VPT], pr[VPT];
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        px[p] = pr[p] = w[p] = (u32x4){0, 0, 0, 0};
+        if (live && i < pieces) {
+            px[p] = *(const u32x4*)(a.x + at + 8 * (size_t)i);
+            if (a.res) pr[p] = *(const u32x4*)(a.res + at + 8 * (size_t)i);
+            w[p] = *(const u32x4*)(a.w + 8 * (size_t)i);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        if (a.res) {
+            F8 s = unpack_bf16(px[p]);
+            const F8 r = unpack_bf16(pr[p]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s.v[k] += r.v[k];
+            px[p] = pack_bf16(s);
+            if (live && i < pieces) *(u32x4*)(a.h + at + 8 * (size_t)i) = px[p];
+        }
+        h[p] = unpack_bf16(px[p]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(h[p].v[k], h[p].v[k], sum);
+    }
+    sum = row_sum<LPR>(sum, wpr, part[0]);
+    const float r = 1.0f / sqrtf(sum / (float)a.d + a.eps);
+    if (a.rstd && live && rt.lane == 0) a.rstd[row] = r;
+
+    float top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        const F8 f = unpack_bf16(w[p]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            h[p].v[k] = h[p].v[k] * r * f.v[k];
+            top = max_abs(top, h[p].v[k]);
+        }
+        if (a.y && live && i < pieces) *(u32x4*)(a.y + at + 8 * (size_t)i) = pack_bf16(h[p]);
+    }
+    if (!a.q) return;
+    const Q8Scale s = q8_scale(row_max<LPR>(top, wpr, part[1]));
+    if (live && rt.lane == 0) a.scale[row] = s.scale;
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) h[p].v[k] *= s.inv;
+        if (live && i < pieces) *(u32x2*)(a.q + at + 8 * (size_t)i) = pack_e4m3(h[p]);
+    }
+}
+
+// Rows too long for registers: the row is read once for the sum and again, from the caches, for the output (twice for an
+// 8-bit one).  A thread reads back only what it wrote itself.
+__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_wide_kernel(NormFwd a) {
+    __shared__ float part[2][MAX_WAVES];
+    const int64_t row = flat_block();
+    if (row >= a.b) return;                                     // the whole workgroup
+    const int pieces = a.d / 8, t = threadIdx.x;
+    const size_t at = (size_t)row * a.d;
+    const bf16_t* from = a.res ? a.h : a.x;
+    float sum = 0.0f;
+    for (int i = t; i < pieces; i += MAX_THREADS) {
+        u32x4 p = *(const u32x4*)(a.x + at + 8 * (size_t)i);
+        if (a.res) {
+            F8 s = unpack_bf16(p);
+            const F8 r = unpack_bf16(*(const u32x4*)(a.res + at + 8 * (size_t)i));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s.v[k] += r.v[k];
+            p = pack_bf16(s);
+            *(u32x4*)(a.h + at + 8 * (size_t)i) = p;
+        }
+        const F8 h = unpack_bf16(p);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fmaf(h.v[k], h.v[k], sum);
+    }
+    sum = row_sum<64>(sum, MAX_WAVES, part[0]);
+    const float r = 1.0f / sqrtf(sum / (float)a.d + a.eps);
+    if (a.rstd && t == 0) a.rstd[row] = r;
+    float top = 0.0f, inv = 0.0f;
+    for (int pass = 0; pass < (a.q ? 2 : 1); ++pass) {
+        for (int i = t; i < pieces; i += MAX_THREADS) {
+            F8 y = unpack_bf16(*(const u32x4*)(from + at + 8 * (size_t)i));
+            const F8 f = unpack_bf16(*(const u32x4*)(a.w + 8 * (size_t)i));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                y.v[k] = y.v[k] * r * f.v[k];
+                top = max_abs(top, y.v[k]);
+            }
+            if (pass == 0) {
+                if (a.y) *(u32x4*)(a.y + at + 8 * (size_t)i) = pack_bf16(y);
+                continue;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y.v[k] *= inv;
+            *(u32x2*)(a.q + at + 8 * (size_t)i) = pack_e4m3(y);
+        }
+        if (pass == 0 && a.q) {
+            const Q8Scale s = q8_scale(row_max<64>(top, MAX_WAVES, part[1]));
+            inv = s.inv;
+            if (t == 0) a.scale[row] = s.scale;
+        }
+    }
+}
+
+struct NormBwd {
+    const bf16_t *dy, *h, *w;
+    const float* rstd;
+    const bf16_t* dh;                          // or null
+    int64_t b;
+    int d;
+    bf16_t* dx;
+    float* part;                               // fp32[groups][d]: each workgroup's share of dw
+};
+
+// Workgroup g takes rows g R .. g R + R - 1, then those `groups` R later, and keeps its share of dw in registers; the R row
+// slots' shares are added through LDS.
+template <int LPR, int VPT>
+__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_kernel(NormBwd a, int wpr) {
+    extern __shared__ float lds[];                              // 2 x MAX_WAVES, then R - 1 rows of d
+    const RowThreads rt = row_threads<LPR>(wpr);
+    const int slots = blockDim.x / rt.threads, pieces = a.d / 8;
+    F8 w[VPT], dw[VPT];
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        w[p] = unpack_bf16(i < pieces ? *(const u32x4*)(a.w + 8 * (size_t)i) : (u32x4){0, 0, 0, 0});
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dw[p].v[k] = 0.0f;
+    }
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * slots; first < a.b; first += (int64_t)gridDim.x * slots, turn ^= 1) {
+        const int64_t row = first + rt.row;
+        const bool live = row < a.b;
+        const size_t at = (size_t)row * a.d;
+        const float r = live ? a.rstd[row] : 0.0f;
+        u32x4 pdy[VPT], ph[VPT], pdh[VPT];
+#pragma unroll
+        for (int p = 0; p < VPT; ++p) {
+            const int i = rt.lane + p * rt.threads;
+            pdy[p] = ph[p] = pdh[p] = (u32x4){0, 0, 0, 0};
+            if (live && i < pieces) {
+                pdy[p] = *(const u32x4*)(a.dy + at + 8 * (size_t)i);
+                ph[p] = *(const u32x4*)(a.h + at + 8 * (size_t)i);
+                if (a.dh) pdh[p] = *(const u32x4*)(a.dh + at + 8 * (size_t)i);
+            }
+        }
+        float c = 0.0f;
+#pragma unroll
+        for (int p = 0; p < VPT; ++p) {
+            const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float t = dy.v[k] * (h.v[k] * r);
+                c = fmaf(t, w[p].v[k], c);
+                dw[p].v[k] += t;
+            }
+        }
+        c = row_sum<LPR>(c, wpr, lds + turn * MAX_WAVES) / (float)a.d;
+#pragma unroll
+        for (int p = 0; p < VPT; ++p) {
+            const int i = rt.lane + p * rt.threads;
+            const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]), dh = unpack_bf16(pdh[p]);
+            F8 o;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w[p].v[k] - h.v[k] * r * c, dh.v[k]);
+            if (live && i < pieces) *(u32x4*)(a.dx + at + 8 * (size_t)i) = pack_bf16(o);
+        }
+    }
+    float* const sums = lds + 2 * MAX_WAVES;
+    if (rt.row > 0)
+#pragma unroll
+        for (int p = 0; p < VPT; ++p) {
+            const int i = rt.lane + p * rt.threads;
+            if (i < pieces)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sums[(size_t)(rt.row - 1) * a.d + 8 * i + k] = dw[p].v[k];
+        }
+    __syncthreads();
+    if (rt.row > 0) return;
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        if (i >= pieces) continue;
+        for (int s = 1; s < slots; ++s)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dw[p].v[k] += sums[(size_t)(s - 1) * a.d + 8 * i + k];
+        f32x4* const o = (f32x4*)(a.part + (size_t)blockIdx.x * a.d + 8 * (size_t)i);
+        o[0] = (f32x4){dw[p].v[0], dw[p].v[1], dw[p].v[2], dw[p].v[3]};
+        o[1] = (f32x4){dw[p].v[4], dw[p].v[5], dw[p].v[6], dw[p].v[7]};
+    }
+}
+
+// Rows too long for registers: dx row by row, reading the row twice, and dw's shares column by column
+__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_wide_kernel(NormBwd a) {
+    __shared__ float part[MAX_WAVES];
+    const int64_t row = flat_block();
+    if (row >= a.b) return;
+    const int pieces = a.d / 8;
+    const size_t at = (size_t)row * a.d;
+    const float r = a.rstd[row];
+    float c = 0.0f;
+    for (int i = threadIdx.x; i < pieces; i += MAX_THREADS) {
+        const F8 dy = unpack_bf16(*(const u32x4*)(a.dy + at + 8 * (size_t)i)), h = unpack_bf16(*(const u32x4*)(a.h + at + 8 * (size_t)i));
+        const F8 w = unpack_bf16(*(const u32x4*)(a.w + 8 * (size_t)i));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c = fmaf(dy.v[k] * (h.v[k] * r), w.v[k], c);
+    }
+    c = row_sum<64>(c, MAX_WAVES, part) / (float)a.d;
+    for (int i = threadIdx.x; i < pieces; i += MAX_THREADS) {
+        const F8 dy = unpack_bf16(*(const u32x4*)(a.dy + at + 8 * (size_t)i)), h = unpack_bf16(*(const u32x4*)(a.h + at + 8 * (size_t)i));
+        const F8 w = unpack_bf16(*(const u32x4*)(a.w + 8 * (size_t)i));
+        const F8 dh = unpack_bf16(a.dh ? *(const u32x4*)(a.dh + at + 8 * (size_t)i) : (u32x4){0, 0, 0, 0});
+        F8 o;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w.v[k] - h.v[k] * r * c, dh.v[k]);
+        *(u32x4*)(a.dx + at + 8 * (size_t)i) = pack_bf16(o);
+    }
+}
+// grid: (pieces / 256 rounded up) x groups
+__global__ void __launch_bounds__(256) rmsnorm_dw_wide_kernel(NormBwd a) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.d / 8) return;
+    F8 s;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s.v[k] = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.b; row += gridDim.y) {
+        const size_t at = (size_t)row * a.d + 8 * (size_t)i;
+        const float r = a.rstd[row];
+        const F8 dy = unpack_bf16(*(const u32x4*)(a.dy + at)), h = unpack_bf16(*(const u32x4*)(a.h + at));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s.v[k] += dy.v[k] * (h.v[k] * r);
+    }
+    f32x4* const o = (f32x4*)(a.part + (size_t)blockIdx.y * a.d + 8 * (size_t)i);
+    o[0] = (f32x4){s.v[0], s.v[1], s.v[2], s.v[3]};
+    o[1] = (f32x4){s.v[4], s.v[5], s.v[6], s.v[7]};
+}
+
+// dw = bf16(sum of the groups' shares), in a fixed order.  A workgroup: 32 columns, 8 lanes of 4 each, 32 rows at a time
+__global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict__ part, int groups, int d, bf16_t* __restrict__ dw) {
+    __shared__ f32x4 sums[32][8];
+    const int lane = threadIdx.x & 7, slot = threadIdx.x >> 3, col = blockIdx.x * 32 + lane * 4;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < d)
+        for (int g = slot; g < groups; g += 32) s += *(const f32x4*)(part + (size_t)g * d + col);
+    sums[slot][lane] = s;
+    __syncthreads();
+    if (slot != 0 || col >= d) return;
+    for (int i = 1; i < 32; ++i) s += sums[i][lane];
+    union { __bf16 h[4]; u32x2 u; } o;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o.h[k] = (__bf16)s[k];
+    *(u32x2*)(dw + col) = o.u;
+}
+
+// How the threads of a workgroup share rows of d elements: lanes per row below 64, or `wpr` wavefronts per row, VPT pieces a lane
+struct RowShape { int lpr, wpr, vpt, threads; };
+RowShape row_shape(int64_t b, int64_t d, int most) {
+    const int64_t pieces = d / 8;
+    if (pieces > (int64_t)MAX_THREADS * most) return {64, 0, 0, MAX_THREADS};
+    if (pieces <= 32) return {pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32, 1, 1, 256};
+    int vpt = 1;
+    while (vpt < most && pieces > (int64_t)64 * vpt && (b >= 2048 || pieces > (int64_t)MAX_THREADS * vpt)) vpt *= 2;
+    const int wpr = (int)((pieces + 64 * vpt - 1) / (64 * vpt));
+    return {64, wpr, vpt, wpr >= 4 ? wpr * 64 : 4 / wpr * wpr * 64};
+}
+
+constexpr int FWD_MOST = 8, BWD_MOST = 4;
+constexpr int BWD_GROUPS = 512;
+
+int bwd_groups(int64_t b, int64_t d) {
+    const RowShape s = row_shape(b, d, BWD_MOST);
+    const int64_t slots = s.wpr == 0 ? 1 : s.lpr < 64 ? s.threads / s.lpr : s.threads / (64 * s.wpr);
+    const int64_t turns = (b + slots - 1) / slots;
+    return (int)(turns < BWD_GROUPS ? turns : BWD_GROUPS);
+}
+
+}  // namespace
+
+hipError_t launch_rmsnorm_fwd(const bf16_t* x, const bf16_t* res, const bf16_t* w, int64_t b, int64_t d, float eps, bf16_t* h,
+                              bf16_t* y, float* rstd, uint8_t* q, float* scale, hipStream_t s) {
+    const NormFwd a = {x, res, w, b, (int)d, eps, h, y, rstd, q, scale};
+    const RowShape rs = row_shape(b, d, FWD_MOST);
+    const int64_t slots = rs.wpr == 0 ? 1 : rs.lpr < 64 ? rs.threads / rs.lpr : rs.threads / (64 * rs.wpr);
+    const dim3 grid = grid_of((b + slots - 1) / slots);
+#define FWD(L, V) rmsnorm_fwd_kernel<L, V><<<grid, rs.threads, 0, s>>>(a, rs.wpr)
+    if (rs.wpr == 0) rmsnorm_fwd_wide_kernel<<<grid, MAX_THREADS, 0, s>>>(a);
+    else if (rs.lpr == 8) FWD(8, 1);
+    else if (rs.lpr == 16) FWD(16, 1);
+    else if (rs.lpr == 32) FWD(32, 1);
+    else if (rs.vpt == 1) FWD(64, 1);
+    else if (rs.vpt == 2) FWD(64, 2);
+    else if (rs.vpt == 4) FWD(64, 4);
+    else FWD(64, 8);
+#undef FWD
+    return hipGetLastError();
+}
+
+size_t rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d) { return (size_t)bwd_groups(b, d) * (size_t)d * 4; }
+
+hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w, const float* rstd, const bf16_t* dh, int64_t b,
+                              int64_t d, bf16_t* dx, bf16_t* dw, float* part, hipStream_t s) {
+    const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, part};
+    const RowShape rs = row_shape(b, d, BWD_MOST);
+    const int groups = bwd_groups(b, d);
+    if (rs.wpr == 0) {
+        // dw first: dx may be written over dy
+        rmsnorm_dw_wide_kernel<<<dim3((unsigned)((d / 8 + 255) / 256), (unsigned)groups), 256, 0, s>>>(a);
+        rmsnorm_bwd_wide_kernel<<<grid_of(b), MAX_THREADS, 0, s>>>(a);
+    } else {
+        const int slots = rs.lpr < 64 ? rs.threads / rs.lpr : rs.threads / (64 * rs.wpr);
+        const size_t lds = 2 * MAX_WAVES * 4 + (size_t)(slots - 1) * d * 4;
+#define BWD(L, V) rmsnorm_bwd_kernel<L, V><<<groups, rs.threads, lds, s>>>(a, rs.wpr)
+        if (rs.lpr == 8) BWD(8, 1);
+        else if (rs.lpr == 16) BWD(16, 1);
+        else if (rs.lpr == 32) BWD(32, 1);
+        else if (rs.vpt == 1) BWD(64, 1);
+        else if (rs.vpt == 2) BWD(64, 2);
+        else BWD(64, 4);
+#undef BWD
+    }
+    rmsnorm_dw_kernel<<<(unsigned)((d + 31) / 32), 256, 0, s>>>(part, groups, (int)d, dw);
+    return hipGetLastError();
+}

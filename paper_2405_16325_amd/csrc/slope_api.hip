@@ -1,6 +1,8 @@
 // C ABI of the double-pruned 2:4 sparse linear layer (declared in include/slope.h):
 // argument checks on the host, then the launchers.  No allocation, no synchronisation; the only
 // state is the per-device address of the static scratch array of slope_spmm_fwd_static.
+#include <math.h>
+
 #include <atomic>
 
 #include "pipeline.h"
@@ -101,6 +103,7 @@ const char* slope_status_string(int status) {
         case SLOPE_ERR_UNSUPPORTED: return "unsupported N:M pattern or adapter rank";
         case SLOPE_ERR_HIP: return "a HIP launch failed";
         case SLOPE_ERR_WORKSPACE: return "the call needs more scratch memory than the buffer it was given holds";
+        case SLOPE_ERR_VALUE: return "a scalar argument is outside its range";
         default: return "unknown status";
     }
 }
@@ -157,6 +160,8 @@ size_t slope_workspace_bytes(int call_id, int64_t b, int64_t d_in, int64_t d_out
         case SLOPE_CALL_SPMM_BWD_X_ADAPTER: return slope_spmm_bwd_x_adapter_workspace_bytes(b, r);
         case SLOPE_CALL_SPMM_BWD_X_WS: return slope_spmm_fwd_workspace_bytes(b, d_out, d_in, 0);   // the forward's product
         case SLOPE_CALL_WGRAD_ADAPTER: return slope_wgrad_adapter_workspace_bytes(b, d_in, d_out, r);
+        case SLOPE_CALL_RMSNORM_BWD: return slope_rmsnorm_bwd_workspace_bytes(b, d_in);
+        case SLOPE_CALL_SPMM_FWD_Q8: return slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out);
         default: return 0;      // prune_rows, double_prune, spmm_bwd_x, wgrad_masked need no scratch; unknown ids
     }
 }
@@ -486,6 +491,138 @@ slope_status slope_update_sparse(const void* Wnew_vals, const void* Wr_meta, int
     return finish(launch_update_transposed((const bf16_t*)Wnew_vals, (const uint8_t*)Wr_meta, d_out, d_in,
                                            Wr_vals != Wnew_vals ? (bf16_t*)Wr_vals : nullptr, (const uint8_t*)WrcT_meta,
                                            (bf16_t*)WrcT_vals, (hipStream_t)stream));
+}
+
+constexpr int64_t NORM_EXTENT_MAX = (int64_t)1 << 24;
+static bool bad_norm(int64_t b, int64_t d) { return bad_extent(b, 1) || bad_extent(d, 8) || d >= NORM_EXTENT_MAX; }
+
+slope_status slope_rmsnorm_fwd(const void* X, const void* residual_or_null, const void* weight, int64_t b, int64_t d,
+                               double eps, void* H_or_null, void* Y_or_null, void* rstd_or_null, void* Q_or_null,
+                               void* scale_or_null, void* stream) {
+    if (!X || !weight || (!Y_or_null && !Q_or_null) || !residual_or_null != !H_or_null || !Q_or_null != !scale_or_null)
+        return SLOPE_ERR_NULL;
+    if (bad_norm(b, d)) return SLOPE_ERR_SHAPE;
+    if (misaligned(X, 16) || misaligned(residual_or_null, 16) || misaligned(weight, 16) || misaligned(H_or_null, 16) ||
+        misaligned(Y_or_null, 16) || misaligned(rstd_or_null, 16) || misaligned(Q_or_null, 16) || misaligned(scale_or_null, 16))
+        return SLOPE_ERR_ALIGN;
+    if (!((float)eps > 0.0f && (float)eps < INFINITY)) return SLOPE_ERR_VALUE;
+    return finish(launch_rmsnorm_fwd((const bf16_t*)X, (const bf16_t*)residual_or_null, (const bf16_t*)weight, b, d, (float)eps,
+                                     (bf16_t*)H_or_null, (bf16_t*)Y_or_null, (float*)rstd_or_null, (uint8_t*)Q_or_null,
+                                     (float*)scale_or_null, (hipStream_t)stream));
+}
+
+size_t slope_rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d) {
+    return bad_norm(b, d) ? 0 : round256(rmsnorm_bwd_workspace_bytes(b, d));
+}
+
+slope_status slope_rmsnorm_bwd(const void* dY, const void* H, const void* weight, const void* rstd, const void* dH_or_null,
+                               int64_t b, int64_t d, void* dX, void* dweight, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    if (!dY || !H || !weight || !rstd || !dX || !dweight || !workspace) return SLOPE_ERR_NULL;
+    if (bad_norm(b, d)) return SLOPE_ERR_SHAPE;
+    if (misaligned(dY, 16) || misaligned(H, 16) || misaligned(weight, 16) || misaligned(rstd, 16) || misaligned(dH_or_null, 16) ||
+        misaligned(dX, 16) || misaligned(dweight, 16) || misaligned(workspace, 256))
+        return SLOPE_ERR_ALIGN;
+    if (workspace_bytes < slope_rmsnorm_bwd_workspace_bytes(b, d)) return SLOPE_ERR_WORKSPACE;
+    return finish(launch_rmsnorm_bwd((const bf16_t*)dY, (const bf16_t*)H, (const bf16_t*)weight, (const float*)rstd,
+                                     (const bf16_t*)dH_or_null, b, d, (bf16_t*)dX, (bf16_t*)dweight, (float*)workspace,
+                                     (hipStream_t)stream));
+}
+
+slope_status slope_quantize_packed(const void* Wr_vals, int64_t d_out, int64_t d_in, void* Wq_vals, void* w_scale, void* stream) {
+    if (!Wr_vals || !Wq_vals || !w_scale) return SLOPE_ERR_NULL;
+    if (bad_extent(d_out, 1) || bad_extent(d_in, 8)) return SLOPE_ERR_SHAPE;
+    if (misaligned(Wr_vals, 16) || misaligned(Wq_vals, 16) || misaligned(w_scale, 16)) return SLOPE_ERR_ALIGN;
+    return finish(launch_quantize_packed((const bf16_t*)Wr_vals, d_out, d_in, (uint8_t*)Wq_vals, (float*)w_scale, (hipStream_t)stream));
+}
+
+size_t slope_spmm_fwd_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out) {
+    return bad_layer(b, d_out, d_in) ? 0 : round256(spmm_q8_workspace_bytes(b, d_out, d_in));
+}
+
+slope_status slope_spmm_fwd_q8(const void* Xq, const void* x_scale, int64_t b, const void* Wq_vals, const void* Wr_meta,
+                               const void* w_scale, int64_t d_out, int64_t d_in, const void* add_or_null, void* Y,
+                               void* workspace_or_null, size_t workspace_bytes, void* stream) {
+    if (!Xq || !x_scale || !Wq_vals || !Wr_meta || !w_scale || !Y) return SLOPE_ERR_NULL;
+    if (bad_layer(b, d_out, d_in)) return SLOPE_ERR_SHAPE;
+    if (misaligned(Xq, 16) || misaligned(x_scale, 16) || misaligned(Wq_vals, 16) || misaligned(Wr_meta, 16) ||
+        misaligned(w_scale, 16) || misaligned(add_or_null, 16) || misaligned(Y, 16) || misaligned(workspace_or_null, 256))
+        return SLOPE_ERR_ALIGN;
+    if (workspace_or_null && workspace_bytes < slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out)) return SLOPE_ERR_WORKSPACE;
+    return finish(launch_spmm_q8((const uint8_t*)Xq, (const float*)x_scale, b, (const uint8_t*)Wq_vals, (const uint8_t*)Wr_meta,
+                                 (const float*)w_scale, d_out, d_in, (const bf16_t*)add_or_null, (bf16_t*)Y,
+                                 (float*)workspace_or_null, (hipStream_t)stream));
+}
+
+// a set's tensors have 32-bit numbers, and so do a tensor's chunks
+constexpr int64_t ADAMW_TENSORS_MAX = (int64_t)1 << 24, ADAMW_ELEMENTS_MAX = (int64_t)1 << 40;
+
+static slope_status adamw_check(const slope_adamw_tensor* tensors, int64_t count, int state_bits) {
+    if (!tensors) return SLOPE_ERR_NULL;
+    if (count <= 0 || count > ADAMW_TENSORS_MAX) return SLOPE_ERR_SHAPE;
+    int64_t total = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const slope_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > ADAMW_ELEMENTS_MAX || (total += t.n) > ADAMW_ELEMENTS_MAX) return SLOPE_ERR_SHAPE;
+        if (state_bits == 0 || t.n == 0) continue;                 // sizes only, or nothing to do
+        if ((!t.param && !t.master) || !t.grad || !t.m || !t.v || (state_bits == 8 && (!t.m_scale || !t.v_scale))) return SLOPE_ERR_NULL;
+        if (misaligned(t.param, 16) || misaligned(t.master, 16) || misaligned(t.grad, 16) || misaligned(t.m, 16) || misaligned(t.v, 16) ||
+            (state_bits == 8 && (misaligned(t.m_scale, 4) || misaligned(t.v_scale, 4))))
+            return SLOPE_ERR_ALIGN;
+        if (t.grad_bits != 16 && t.grad_bits != 32) return SLOPE_ERR_UNSUPPORTED;
+        if (!(fabsf(t.weight_decay) < INFINITY)) return SLOPE_ERR_VALUE;
+    }
+    return SLOPE_OK;
+}
+
+size_t slope_adamw_table_bytes(const slope_adamw_tensor* tensors, int64_t count) {
+    return adamw_check(tensors, count, 0) == SLOPE_OK ? adamw_table_bytes(count, adamw_chunks(tensors, count)) : 0;
+}
+
+slope_status slope_adamw_table(const slope_adamw_tensor* tensors, int64_t count, int state_bits, void* table, size_t table_bytes) {
+    if (state_bits != 8 && state_bits != 32) return SLOPE_ERR_UNSUPPORTED;
+    if (!table) return SLOPE_ERR_NULL;
+    const slope_status e = adamw_check(tensors, count, state_bits);
+    if (e != SLOPE_OK) return e;
+    if (misaligned(table, 8)) return SLOPE_ERR_ALIGN;
+    if (table_bytes < adamw_table_bytes(count, adamw_chunks(tensors, count))) return SLOPE_ERR_WORKSPACE;
+    adamw_fill_table(tensors, count, state_bits, table);
+    return SLOPE_OK;
+}
+
+size_t slope_grad_norm_workspace_bytes(const void* table) {
+    return table && !misaligned(table, 8) && adamw_table_ok(table) ? round256(grad_norm_workspace_bytes(table)) : 0;
+}
+
+static slope_status adamw_table_check(const void* table, const void* device_table) {
+    if (!table || !device_table) return SLOPE_ERR_NULL;
+    if (misaligned(table, 8) || misaligned(device_table, 16)) return SLOPE_ERR_ALIGN;
+    return adamw_table_ok(table) ? SLOPE_OK : SLOPE_ERR_UNSUPPORTED;
+}
+
+slope_status slope_grad_norm(const void* table, const void* device_table, double inv_scale, double max_norm, void* control,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    const slope_status e = adamw_table_check(table, device_table);
+    if (e != SLOPE_OK) return e;
+    if (!control || !workspace) return SLOPE_ERR_NULL;
+    if (misaligned(control, 16) || misaligned(workspace, 256)) return SLOPE_ERR_ALIGN;
+    if (!((float)inv_scale > 0.0f && (float)inv_scale < INFINITY && (float)max_norm > 0.0f)) return SLOPE_ERR_VALUE;
+    if (workspace_bytes < slope_grad_norm_workspace_bytes(table)) return SLOPE_ERR_WORKSPACE;
+    return finish(launch_grad_norm(table, device_table, (float)inv_scale, (float)max_norm, (float*)control, (float*)workspace,
+                                   (hipStream_t)stream));
+}
+
+slope_status slope_adamw_step(const void* table, const void* device_table, double lr, double beta1, double beta2, double eps,
+                              double grad_scale, int64_t step, const void* control_or_null, void* stream) {
+    const slope_status e = adamw_table_check(table, device_table);
+    if (e != SLOPE_OK) return e;
+    if (misaligned(control_or_null, 16)) return SLOPE_ERR_ALIGN;
+    const bool betas = beta1 >= 0.0 && (float)beta1 < 1.0f && beta2 >= 0.0 && (float)beta2 < 1.0f;
+    if (!betas || !(lr >= 0.0 && (float)lr < INFINITY) || !((float)eps > 0.0f && (float)eps < INFINITY)) return SLOPE_ERR_VALUE;
+    // steps are counted in fp32
+    if (!control_or_null && (step < 1 || step > (1 << 24) || !(fabs(grad_scale) < INFINITY))) return SLOPE_ERR_VALUE;
+    return finish(launch_adamw(table, device_table, lr, beta1, beta2, eps, grad_scale, step, (const float*)control_or_null,
+                               (hipStream_t)stream));
 }
 
 slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t r, int with_workspace, int32_t* plan) {

@@ -1,0 +1,147 @@
+"""The 2:4 product on 8-bit operands and the weights' 8-bit form: HIP path vs the oracle.
+
+Bound of an element: rounding to bf16 (2^-8 of the value), what the matrix instruction leaves off when it adds its 64 products
+(2^-14 of the largest of them, taken twice, so 2^-13 of the terms' magnitudes at most) and fp32 sums over instructions.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import slope_oracle as so
+from oracle import surroundings_oracle as oo
+from paper_2405_16325_amd import binding as sl
+from paper_2405_16325_amd import inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+def make(b, d_out, d_in, seed):
+    t = inputs.layer_inputs(b, d_out, d_in, seed=seed)
+    vals, meta, _ = so.prune_rows_packed(t["W"])
+    wq, ws = sl.slope_quantize_packed(sl.bf16_to_device(vals))
+    x = so.bf16_to_f64(t["X"])
+    xs, inv = oo.q8_scale(np.abs(x).max(1))
+    q = oo.e4m3_nearest(x * inv[:, None].astype(np.float64))
+    dev = {"q": torch.from_numpy(q).cuda().view(sl.E4M3), "xs": torch.from_numpy(xs).cuda(), "wq": wq, "ws": ws,
+           "meta": torch.from_numpy(meta).cuda()}
+    return t, vals, meta, q, xs, dev
+
+
+def codes(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def check(y, q, xs, dev, meta, add=None):
+    want, terms = oo.product_q8(q, xs, codes(dev["wq"]), meta, dev["ws"].cpu().numpy(), add)
+    got = so.bf16_to_f64(sl.bf16_to_host(y))
+    bound = 2.0 ** -8 * 1.01 * np.abs(want) + 2.0 ** -13 * terms + 1e-38
+    bad = np.abs(got - want) > bound
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
+
+
+@pytest.mark.parametrize("d_out,d_in", [(1, 8), (8, 64), (100, 264), (768, 3072), (129, 9216)])
+def test_quantized_rows(d_out, d_in):
+    say(f"quantize_packed {d_out} x {d_in}")
+    bits = inputs.gaussian_bf16((d_out, d_in // 2), 0.02, d_out, 3)
+    if d_out > 2:
+        bits[1] = 0
+    q, s = sl.slope_quantize_packed(sl.bf16_to_device(bits))
+    v = so.bf16_to_f64(bits)
+    want_s, inv = oo.q8_scale(np.abs(v).max(1))
+    assert (s.cpu().numpy() == want_s).all()
+    # the product with the reciprocal is rounded to fp32 before the code is chosen, here too
+    want = oo.e4m3_nearest((v.astype(np.float32) * inv[:, None]).astype(np.float32))
+    assert (codes(q) == want).all()
+
+
+# one token to many; multiples of 256, of 128, of 8 only; a contraction of one step, of part of one; few rows
+SHAPES = [(1, 8, 8), (1, 256, 128), (3, 72, 136), (1, 520, 1024), (5, 64, 2048), (16, 768, 512), (17, 1000, 200), (31, 264, 1160),
+          (33, 128, 384), (64, 256, 256), (100, 1000, 1000), (128, 512, 4096), (130, 200, 4096), (200, 1032, 640), (257, 264, 896),
+          (300, 512, 128), (520, 768, 768), (777, 640, 1280), (1000, 1000, 1000), (1030, 520, 2176)]
+
+
+@pytest.mark.parametrize("b,d_out,d_in", SHAPES)
+@pytest.mark.parametrize("with_add", [False, True])
+def test_product(b, d_out, d_in, with_add):
+    say(f"spmm_fwd_q8 b={b} d_out={d_out} d_in={d_in} add={with_add}")
+    _, _, meta, q, xs, dev = make(b, d_out, d_in, seed=b + d_out + d_in)
+    add_bits = inputs.gaussian_bf16((b, d_out), 1.0, b, 9) if with_add else None
+    add = sl.bf16_to_device(add_bits) if with_add else None
+    args = (dev["q"], dev["xs"], dev["wq"], dev["meta"], dev["ws"])
+    y = sl.slope_spmm_fwd_q8(*args, add=add)
+    again = sl.slope_spmm_fwd_q8(*args, add=add)
+    alone = sl.slope_spmm_fwd_q8(*args, add=add, workspace=None)
+    torch.cuda.synchronize()
+    add_v = so.bf16_to_f64(add_bits) if with_add else None
+    check(y, q, xs, dev, meta, add_v)
+    check(alone, q, xs, dev, meta, add_v)
+    assert torch.equal(y, again)
+
+
+def test_the_added_term_in_place_and_nothing_outside_is_written():
+    b, d_out, d_in = 70, 264, 512
+    _, _, meta, q, xs, dev = make(b, d_out, d_in, seed=1)
+    bits = inputs.gaussian_bf16((b, d_out), 1.0, 1, 9)
+    buf = torch.full((b * d_out + 8192,), 7.0, dtype=sl.BF16, device="cuda")
+    y = buf[4096:4096 + b * d_out].view(b, d_out)
+    y.copy_(sl.bf16_to_device(bits))
+    sl.slope_spmm_fwd_q8(dev["q"], dev["xs"], dev["wq"], dev["meta"], dev["ws"], add=y, out=y)
+    torch.cuda.synchronize()
+    check(y, q, xs, dev, meta, so.bf16_to_f64(bits))
+    assert (buf[:4096] == 7).all() and (buf[4096 + b * d_out:] == 7).all()
+
+
+@pytest.mark.parametrize("b", [4, 20, 300])
+def test_a_token_of_zeros_and_one_that_is_not_finite(b):
+    d_out, d_in = 256, 512
+    say(f"spmm_fwd_q8 special tokens b={b}")
+    _, _, meta, q, xs, dev = make(b, d_out, d_in, seed=2)
+    dev["q"].view(torch.uint8)[1] = 0
+    dev["xs"][1] = 0.0
+    dev["q"].view(torch.uint8)[2] = 0x7F
+    dev["xs"][2] = float("nan")
+    y = sl.slope_spmm_fwd_q8(dev["q"], dev["xs"], dev["wq"], dev["meta"], dev["ws"])
+    torch.cuda.synchronize()
+    assert (y[1] == 0).all() and torch.isnan(y[2]).all()
+    rest = [i for i in range(b) if i not in (1, 2)]
+    check(y[rest], q[rest], xs[rest], dev, meta)
+
+
+@pytest.mark.parametrize("b,d_out,d_in", [(1, 36864, 9216), (16, 9216, 36864), (300, 2560, 10240), (2048, 5120, 5120)])
+def test_layers_at_full_size_against_a_library_product(b, d_out, d_in):
+    """Every element against an fp32 product of the same values; the bound's middle term from the rows' norms, which is what
+    the terms' magnitudes add up to at most."""
+    say(f"spmm_fwd_q8 full size b={b} d_out={d_out} d_in={d_in}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(inputs.SEED_BASE + b)
+    W = (torch.randn(d_out, d_in, generator=gen, device="cuda") * 0.02).to(sl.BF16)
+    vals, meta, mask = sl.slope_prune_rows(W, want_mask=True)
+    wq, ws = sl.slope_quantize_packed(vals)
+    x = torch.randn(b, d_in, generator=gen, device="cuda").to(sl.BF16)
+    ones = torch.ones(d_in, dtype=sl.BF16, device="cuda")
+    _, _, _, q, xs = sl.slope_rmsnorm_fwd(x, ones, 1e-5, want_y=False, want_q8=True)
+    y = sl.slope_spmm_fwd_q8(q, xs, wq, meta, ws).float()
+    bits = (mask.unsqueeze(-1) >> torch.arange(8, device="cuda", dtype=torch.uint8)) & 1
+    dense = torch.zeros(d_out, d_in, device="cuda")
+    dense[bits.view(d_out, d_in).bool()] = (wq.float() * ws[:, None]).view(-1)
+    xf = q.float() * xs[:, None]
+    want = torch.matmul(xf, dense.t().contiguous())
+    terms = xf.norm(dim=1)[:, None] * dense.norm(dim=1)[None]
+    assert ((y - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -13 * terms).all()
+
+
+def test_norm_and_product_agree_with_the_16_bit_path():
+    """The 8-bit path against the bf16 path of the same layer: each operand is off by at most 2^-4 of its value, and the errors
+    of thousands of terms are independent: 2^-4 / sqrt(3) for each operand bounds the relative norm of the difference."""
+    b, d_out, d_in = 40, 512, 1024
+    t = inputs.layer_inputs(b, d_out, d_in, seed=5)
+    vals, meta, _ = sl.slope_prune_rows(sl.bf16_to_device(t["W"]))
+    w = torch.ones(d_in, dtype=sl.BF16, device="cuda")
+    yn, _, _, q, s = sl.slope_rmsnorm_fwd(sl.bf16_to_device(t["X"]), w, 1e-5, want_q8=True)
+    want = sl.slope_spmm_fwd(yn, vals, meta).float()
+    got = sl.slope_spmm_fwd_q8(q, s, *(lambda wq, ws: (wq, meta, ws))(*sl.slope_quantize_packed(vals))).float()
+    assert float((got - want).norm() / want.norm()) < 2.0 ** -4 / 3 ** 0.5 * 2 ** 0.5

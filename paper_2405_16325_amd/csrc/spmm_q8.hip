@@ -9,6 +9,8 @@
 //     of D  token l % 16, rows 4 (l / 16) .. + 3.
 // The instruction adds its 64 products with fewer bits than fp32 has: a sum is off by up to about 2^-14 of its largest
 // product (measured), below what rounding the operands to 8 bits costs.  Sums over instructions are fp32.
+#include <type_traits>
+
 #include "pipeline.h"
 #include "wave.h"
 
@@ -16,6 +18,7 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 union AQ { i32x4 v; u32x4 u; uint32_t w[4]; };
 union BQ { i32x8 v; u32x4 u[2]; u32x2 h[4]; };
 
@@ -101,6 +104,233 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// q8_tile_kernel: whole tiles of BM rows x BN tokens, K % 128 == 0.  Four wavefronts, one per SIMD, 2 x 2, each BM / 2 x BN / 2 on
+// v_smfmac_f32_32x32x64_fp8_fp8, whose lane l holds
+//     of W  row l % 32, packed bytes 16 (l / 32) .. + 15 and the 4 metadata bytes of that stretch,
+//     of X  token l % 32, k 16 (l / 32) .. + 15 and 32 + that,
+//     of D  token l % 32, rows 8 i + 4 (l / 32) .. + 3, i = 0 .. 3.
+// A k-step is 128 logical k: 64 bytes of a packed row, 16 of its metadata, 128 of a token.  Operands come through a ring of three
+// k-steps in LDS by global -> LDS loads, metadata by pairs of k-steps in two buffers.  A wavefront reads the fragments of half a
+// k-step while it multiplies the half before; one barrier a k-step, after which the ring's stage that everybody has left is
+// refilled for the third k-step on.
+// LDS bounds the loop: with wavefront tiles of 128 x 128 a k-step reads 104 KB and writes 52 KB of it, 1250 cycles at 128 bytes
+// each, while its products take 1024.
+template <int BM, int BN>
+struct Q8Smem {
+    static constexpr int A = BM * 64, B = BN * 128, STAGE = A + B, M = BM * 32;
+    static constexpr int M_OFF = 3 * STAGE, TOTAL = M_OFF + 2 * M;
+    static constexpr int OUT_PITCH = BM * 2 + 16;
+    static constexpr int LOADS = BM / 64 + BN / 32, META = BM / 128;    // a wavefront's, per k-step and per pair
+};
+
+// where a workgroup's slab of k-steps lies; slabs > 1: fp32 sums to part[slab][token][row]
+struct Q8Split { int steps, total; float* part; };
+
+template <int BM, int BN>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, BM * BN > 128 * 128 ? 1 : 2)))
+q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
+    using S = Q8Smem<BM, BN>;
+    constexpr int MF = BM / 64, NF = BN / 64;
+    extern __shared__ __align__(16) uint8_t smem[];
+    int tm, tn;
+    if (!tile_of_block(tiles_m, tiles_n, tm, tn)) return;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int l32 = lane & 31, lq = lane >> 5, wm = wave & 1, wn = wave >> 1;
+    const int first = (int)blockIdx.y * split.steps;
+    const int steps = min(split.steps, split.total - first);
+    const int K = (int)p.K;
+
+    // loader lanes.  Rows past the end read the tile's rows again: they feed sums that are not stored.
+    const int rows = (int)min((int64_t)BM, p.m - m0), toks = (int)min((int64_t)BN, p.n - n0);
+    uint32_t a_off[BM / 64], b_off[BN / 32], m_off[S::META];
+#pragma unroll
+    for (int i = 0; i < BM / 64; ++i) {
+        const int r = (wave * (BM / 64) + i) * 16 + (lane >> 2);
+        a_off[i] = (uint32_t)wrap_row(r, rows) * (uint32_t)(K / 2) + 16 * ((lane & 3) ^ ((r >> 2) & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < BN / 32; ++i) {
+        const int r = (wave * (BN / 32) + i) * 8 + (lane >> 3);
+        b_off[i] = (uint32_t)wrap_row(r, toks) * (uint32_t)K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+    }
+    int m_piece[S::META];
+#pragma unroll
+    for (int i = 0; i < S::META; ++i) {
+        const int r = (wave * S::META + i) * 32 + (lane >> 1);
+        m_off[i] = (uint32_t)wrap_row(r, rows) * (uint32_t)(K / 8);
+        m_piece[i] = 16 * ((lane & 1) ^ ((r >> 3) & 1));
+    }
+    const uint8_t* const a0 = p.a + m0 * (K / 2) + (int64_t)first * 64;
+    const uint8_t* const b0 = p.x + n0 * K + (int64_t)first * KSTEP;
+    const uint8_t* const e0 = p.am + m0 * (K / 8) + (int64_t)first * 16;
+    const int last = steps - 1;
+
+    auto issue = [&](int k, int stage) {                        // operands of k-step k (clamped) into ring stage `stage`
+        const int kc = k < last ? k : last;
+        uint8_t* const to = smem + stage * S::STAGE;
+#pragma unroll
+        for (int i = 0; i < BM / 64; ++i) dma16(a0 + kc * 64 + a_off[i], to + (wave * (BM / 64) + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i) dma16(b0 + (int64_t)kc * KSTEP + b_off[i], to + S::A + (wave * (BN / 32) + i) * 1024);
+    };
+    auto issue_meta = [&](int pair) {                           // the second half of an odd last pair: the first again
+#pragma unroll
+        for (int i = 0; i < S::META; ++i) {
+            const int at = pair * 32 + m_piece[i];
+            dma16(e0 + (at < 16 * last ? at : 16 * last) + m_off[i], smem + S::M_OFF + (pair & 1) * S::M + (wave * S::META + i) * 1024);
+        }
+    };
+
+    // reader lanes
+    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32;
+    const int a_rd = a_row * 64, a_sw = (l32 >> 2) & 3, b_rd = S::A + b_row * 128, b_sw = (l32 >> 1) & 7;
+    const int m_rd = S::M_OFF + a_row * 32 + lq * 4, m_sw = (l32 >> 3) & 1;
+    struct Frags { AQ a[MF]; BQ b[NF]; uint32_t e[MF]; };
+    auto read = [&](Frags& f, int stage, int k, auto half) {    // half h of k-step k
+        constexpr int h = decltype(half)::value;
+        const uint8_t* const at = smem + stage * S::STAGE;
+        const uint8_t* const pa = at + a_rd + (((2 * h + lq) ^ a_sw) * 16);
+        const uint8_t* const pb0 = at + b_rd + (((4 * h + lq) ^ b_sw) * 16);
+        const uint8_t* const pb1 = at + b_rd + (((4 * h + 2 + lq) ^ b_sw) * 16);
+        const uint8_t* const pe = smem + m_rd + ((k >> 1) & 1) * S::M + (((k & 1) ^ m_sw) * 16) + 8 * h;
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            f.b[j].u[0] = *(const u32x4*)(pb0 + j * 32 * 128);
+            f.b[j].u[1] = *(const u32x4*)(pb1 + j * 32 * 128);
+        }
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            f.a[i].u = *(const u32x4*)(pa + i * 32 * 64);
+            f.e[i] = *(const uint32_t*)(pe + i * 32 * 32);
+        }
+    };
+    f32x16 acc[MF][NF];
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    auto multiply = [&](const Frags& f) {
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int j = 0; j < NF; ++j)
+                acc[i][j] = __builtin_amdgcn_smfmac_f32_32x32x64_fp8_fp8(f.a[i].v, f.b[j].v, acc[i][j], (int)f.e[i], 0, 0);
+    };
+
+    issue_meta(0);
+    issue(0, 0);
+    issue(1, 1);
+    issue_meta(1);
+    issue(2, 2);
+    WAIT_HERE(waitcnt_imm(2 * S::LOADS + S::META, 15));
+    wg_barrier();
+    Frags f0, f1;
+    read(f0, 0, 0, std::integral_constant<int, 0>());
+    int stage = 0;
+    // one k-step; EVEN: k is
+    auto step = [&](int k, auto even) {
+        constexpr bool EVEN = decltype(even)::value;
+        const int next = stage == 2 ? 0 : stage + 1;
+        read(f1, stage, k, std::integral_constant<int, 1>());
+        multiply(f0);
+        // of the loads still under way, those of step k + 2 may stay so
+        WAIT_HERE(waitcnt_imm(S::LOADS + (EVEN ? S::META : 0), 0));
+        wg_barrier();
+        if (!EVEN) issue_meta((k + 3) >> 1);
+        issue(k + 3, stage);
+        read(f0, next, k + 1, std::integral_constant<int, 0>());
+        multiply(f1);
+        stage = next;
+    };
+    int k = 0;
+    for (; k + 1 < steps; k += 2) {
+        step(k, std::true_type());
+        step(k + 1, std::false_type());
+    }
+    if (k < steps) step(k, std::true_type());
+    WAIT_HERE(waitcnt_imm(0, 0));                               // the look-ahead loads
+
+    // ---- results
+    const int f_base = wm * (BM / 2) + 4 * lq, t_base = wn * (BN / 2) + l32;
+    if (split.part) {
+        float* const to = split.part + (int64_t)blockIdx.y * p.n * p.m;
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t tok = n0 + t_base + 32 * j, f = m0 + f_base + 32 * i + 8 * q;
+                    if (tok < p.n && f < p.m)
+                        *(f32x4*)(to + tok * p.m + f) = (f32x4){acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                }
+        return;
+    }
+    // The tile leaves in whole rows by way of LDS, and a term that is added comes the same way before.
+    constexpr int PIECES = BN * (BM / 8), PER = PIECES / 256;
+    __syncthreads();
+    if (p.add) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
+            if (tok < toks && f < rows) *(u32x4*)(smem + tok * S::OUT_PITCH + f * 2) = *(const u32x4*)(p.add + (n0 + tok) * p.m + m0 + f);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+        const int64_t tok = n0 + t_base + 32 * j;
+        const float xs = p.xs[tok < p.n ? tok : p.n - 1];
+#pragma unroll
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t f = m0 + f_base + 32 * i + 8 * q;
+                const f32x4 ws = *(const f32x4*)(p.as + (f < p.m ? f : 0));
+                u32x2* const at = (u32x2*)(smem + (t_base + 32 * j) * S::OUT_PITCH + (f_base + 32 * i + 8 * q) * 2);
+                const u32x2 add = p.add ? *at : (u32x2){0, 0};
+                union { __bf16 h[4]; u32x2 u; } o;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
+                    const float v = acc[i][j][4 * q + r] * xs;
+                    o.h[r] = (__bf16)(p.add ? fmaf(v, ws[r], t) : v * ws[r]);
+                }
+                *at = o.u;
+            }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int u = 0; u < PER; ++u) {
+        const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
+        if (tok < toks && f < rows) *(u32x4*)(p.y + (n0 + tok) * p.m + m0 + f) = *(const u32x4*)(smem + tok * S::OUT_PITCH + f * 2);
+    }
+}
+
+// Y from the slabs' sums, added in order
+__global__ void __launch_bounds__(256) q8_reduce_kernel(Q8Product p, const float* __restrict__ part, int slabs) {
+    const int64_t quads = p.m / 4, i = (flat_block() * 256 + threadIdx.x);
+    if (i >= p.n * quads) return;
+    const int64_t tok = i / quads, f = (i - tok * quads) * 4;
+    f32x4 s = *(const f32x4*)(part + tok * p.m + f);
+    for (int k = 1; k < slabs; ++k) s += *(const f32x4*)(part + ((int64_t)k * p.n + tok) * p.m + f);
+    const f32x4 ws = *(const f32x4*)(p.as + f);
+    const float xs = p.xs[tok];
+    u32x2 add = {0, 0};
+    if (p.add) add = *(const u32x2*)(p.add + tok * p.m + f);
+    union { __bf16 h[4]; u32x2 u; } o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
+        o.h[r] = (__bf16)(p.add ? fmaf(s[r] * xs, ws[r], t) : s[r] * xs * ws[r]);
+    }
+    *(u32x2*)(p.y + tok * p.m + f) = o.u;
+}
+
 // One wavefront a row: packed bf16 values to e4m3 with the row's scale.  half = d_in / 2, a multiple of 4.
 __global__ void __launch_bounds__(256) quantize_packed_kernel(const bf16_t* __restrict__ vals, int64_t rows, int64_t half,
                                                               uint8_t* __restrict__ q, float* __restrict__ scale) {
@@ -131,17 +361,68 @@ hipError_t launch_quantize_packed(const bf16_t* vals, int64_t rows, int64_t cols
     return hipGetLastError();
 }
 
+namespace {
+
+// 32-bit offsets inside a tile's rows, and a grid of fewer than 2^32 work items
+bool tile_fits(int64_t n, int64_t m, int64_t K) {
+    return K % KSTEP == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < ((int64_t)1 << 23);
+}
+
+template <int BM, int BN>
+hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+    using S = Q8Smem<BM, BN>;
+    constexpr int LDS = S::TOTAL > BN * S::OUT_PITCH ? S::TOTAL : BN * S::OUT_PITCH;
+    const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN>>(LDS);
+    if (e != hipSuccess) return e;
+    const int tiles_m = (int)((p.m + BM - 1) / BM), tiles_n = (int)((p.n + BN - 1) / BN);
+    q8_tile_kernel<BM, BN><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
+    return hipGetLastError();
+}
+
+// tile and slabs of a product
+struct Q8Plan { int bm, bn, slabs, steps; };
+Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
+    if (!tile_fits(n, m, K)) return {0, 0, 1, 0};
+    const int total = (int)(K / KSTEP);
+    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
+    Q8Plan plan = {128, 64, 1, total};
+    if (n > 128 && tiles(256, 256) >= 192) plan.bm = plan.bn = 256;
+    else if (n > 64) plan.bn = 128;
+    const int64_t t = tiles(plan.bm, plan.bn);
+    if (room && t < 256) {
+        int slabs = (int)(512 / t);
+        if (slabs > total / 4) slabs = total / 4;
+        if (slabs > 1) {
+            plan.steps = ((total + slabs - 1) / slabs + 1) / 2 * 2;      // whole pairs of metadata
+            plan.slabs = (total + plan.steps - 1) / plan.steps;
+        }
+    }
+    return plan;
+}
+
+}  // namespace
+
 size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K) {
-    (void)n; (void)m; (void)K;
-    return 0;
+    const Q8Plan plan = q8_plan(n, m, K, true);
+    return plan.slabs > 1 ? (size_t)plan.slabs * (size_t)n * (size_t)m * 4 : 0;
 }
 
 hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,
                           int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* partial_or_null, hipStream_t s) {
-    (void)partial_or_null;
     const Q8Product p = {x, xs, n, a, am, as, m, K, add, y};
-    const int64_t tiles_m = (m + 63) / 64, tiles = tiles_m * ((n + 63) / 64);
-    if (!grid_fits(tiles)) return hipErrorInvalidConfiguration;
-    q8_generic_kernel<<<grid_of(tiles), 256, 0, s>>>(p, tiles_m);
+    const Q8Plan plan = q8_plan(n, m, K, partial_or_null != nullptr);
+    if (plan.bm == 0) {
+        const int64_t tiles_m = (m + 63) / 64, tiles = tiles_m * ((n + 63) / 64);
+        if (!grid_fits(tiles)) return hipErrorInvalidConfiguration;
+        q8_generic_kernel<<<grid_of(tiles), 256, 0, s>>>(p, tiles_m);
+        return hipGetLastError();
+    }
+    const Q8Split split = {plan.steps, (int)(K / KSTEP), plan.slabs > 1 ? partial_or_null : nullptr};
+    hipError_t e;
+    if (plan.bm == 256) e = launch_tiles<256, 256>(p, split, plan.slabs, s);
+    else if (plan.bn == 128) e = launch_tiles<128, 128>(p, split, plan.slabs, s);
+    else e = launch_tiles<128, 64>(p, split, plan.slabs, s);
+    if (e != hipSuccess || plan.slabs == 1) return e;
+    q8_reduce_kernel<<<grid_of((n * (m / 4) + 255) / 256), 256, 0, s>>>(p, partial_or_null, plan.slabs);
     return hipGetLastError();
 }

@@ -35,6 +35,16 @@ struct Q8Product {
 };
 
 constexpr int KSTEP = 128;
+// a raw buffer descriptor over `bytes` bytes; loads at offsets past them give zeros
+typedef __amdgpu_buffer_rsrc_t buffer_t;
+constexpr uint32_t NOWHERE = 0x80000000u;
+__device__ __forceinline__ buffer_t tile_buffer(const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000);
+}
+// 64 lanes x 16 bytes: lane l's bytes land at lds_dst + 16 * l; lds_dst and step are the same for all lanes
+__device__ __forceinline__ void buffer_dma16(buffer_t from, uint8_t* lds_dst, uint32_t offset, int step) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (void __attribute__((address_space(3)))*)lds_dst, 16, (int)offset, step, 0, 0);
+}
 constexpr uint32_t META_NONE = 0x44444444u;                    // a legal pair in every group
 
 // Any extents (K % 8 == 0).  Four wavefronts of 32 rows x 32 tokens, operands straight from memory in pieces of 8 logical k,
@@ -142,68 +152,67 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     const int steps = min(split.steps, split.total - first);
     const int K = (int)p.K;
 
-    // loader lanes.  Rows past the end read the tile's rows again: they feed sums that are not stored.
+    // loader lanes, through buffer descriptors of the tile's rows: rows past the end read zeros and no memory
     const int rows = (int)min((int64_t)BM, p.m - m0), toks = (int)min((int64_t)BN, p.n - n0);
+    const uint32_t a_pitch = (uint32_t)K / 2, b_pitch = (uint32_t)K, m_pitch = (uint32_t)K / 8;
+    const buffer_t a_buf = tile_buffer(p.a + m0 * a_pitch, rows * a_pitch);
+    const buffer_t b_buf = tile_buffer(p.x + n0 * b_pitch, toks * b_pitch);
+    const buffer_t m_buf = tile_buffer(p.am + m0 * m_pitch, rows * m_pitch);
     uint32_t a_off[BM / 64], b_off[BN / 32], m_off[S::META];
+    int m_piece[S::META];
 #pragma unroll
     for (int i = 0; i < BM / 64; ++i) {
         const int r = (wave * (BM / 64) + i) * 16 + (lane >> 2);
-        a_off[i] = (uint32_t)wrap_row(r, rows) * (uint32_t)(K / 2) + 16 * ((lane & 3) ^ ((r >> 2) & 3));
+        a_off[i] = r < rows ? r * a_pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
     }
 #pragma unroll
     for (int i = 0; i < BN / 32; ++i) {
         const int r = (wave * (BN / 32) + i) * 8 + (lane >> 3);
-        b_off[i] = (uint32_t)wrap_row(r, toks) * (uint32_t)K + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+        b_off[i] = r < toks ? r * b_pitch + 16 * ((lane & 7) ^ ((r >> 1) & 7)) : NOWHERE;
     }
-    int m_piece[S::META];
 #pragma unroll
     for (int i = 0; i < S::META; ++i) {
         const int r = (wave * S::META + i) * 32 + (lane >> 1);
-        m_off[i] = (uint32_t)wrap_row(r, rows) * (uint32_t)(K / 8);
+        m_off[i] = r < rows ? r * m_pitch : NOWHERE;
         m_piece[i] = 16 * ((lane & 1) ^ ((r >> 3) & 1));
     }
-    const uint8_t* const a0 = p.a + m0 * (K / 2) + (int64_t)first * 64;
-    const uint8_t* const b0 = p.x + n0 * K + (int64_t)first * KSTEP;
-    const uint8_t* const e0 = p.am + m0 * (K / 8) + (int64_t)first * 16;
-    const int last = steps - 1;
+    const int last = first + steps - 1;
 
-    auto issue = [&](int k, int stage) {                        // operands of k-step k (clamped) into ring stage `stage`
-        const int kc = k < last ? k : last;
+    // load i of k-step k (clamped) into ring stage `stage`
+    auto issue = [&](int k, int stage, int i) {
+        const int kc = min(first + k, last);
         uint8_t* const to = smem + stage * S::STAGE;
-#pragma unroll
-        for (int i = 0; i < BM / 64; ++i) dma16(a0 + kc * 64 + a_off[i], to + (wave * (BM / 64) + i) * 1024);
-#pragma unroll
-        for (int i = 0; i < BN / 32; ++i) dma16(b0 + (int64_t)kc * KSTEP + b_off[i], to + S::A + (wave * (BN / 32) + i) * 1024);
+        if (i < BM / 64) buffer_dma16(a_buf, to + (wave * (BM / 64) + i) * 1024, a_off[i], kc * 64);
+        else buffer_dma16(b_buf, to + S::A + (wave * (BN / 32) + i - BM / 64) * 1024, b_off[i - BM / 64], kc * KSTEP);
     };
     auto issue_meta = [&](int pair) {                           // the second half of an odd last pair: the first again
 #pragma unroll
-        for (int i = 0; i < S::META; ++i) {
-            const int at = pair * 32 + m_piece[i];
-            dma16(e0 + (at < 16 * last ? at : 16 * last) + m_off[i], smem + S::M_OFF + (pair & 1) * S::M + (wave * S::META + i) * 1024);
-        }
+        for (int i = 0; i < S::META; ++i)
+            buffer_dma16(m_buf, smem + S::M_OFF + (pair & 1) * S::M + (wave * S::META + i) * 1024,
+                         m_off[i] + (uint32_t)min(first * 16 + pair * 32 + m_piece[i], 16 * last), 0);
     };
 
-    // reader lanes
-    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32;
-    const int a_rd = a_row * 64, a_sw = (l32 >> 2) & 3, b_rd = S::A + b_row * 128, b_sw = (l32 >> 1) & 7;
-    const int m_rd = S::M_OFF + a_row * 32 + lq * 4, m_sw = (l32 >> 3) & 1;
-    struct Frags { AQ a[MF]; BQ b[NF]; uint32_t e[MF]; };
-    auto read = [&](Frags& f, int stage, int k, auto half) {    // half h of k-step k
-        constexpr int h = decltype(half)::value;
+    // reader lanes: offsets inside a stage (W: of each half's chunk; X: of each half's two), inside the metadata
+    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32, a_sw = (l32 >> 2) & 3, b_sw = (l32 >> 1) & 7;
+    const int a_rd = a_row * 64, b_rd = S::A + b_row * 128, m_rd = S::M_OFF + a_row * 32 + lq * 4, m_sw = (l32 >> 3) & 1;
+    struct Reader { const uint8_t *a, *b[2], *e; };
+    auto reader = [&](int stage, int k, int h) {
         const uint8_t* const at = smem + stage * S::STAGE;
-        const uint8_t* const pa = at + a_rd + (((2 * h + lq) ^ a_sw) * 16);
-        const uint8_t* const pb0 = at + b_rd + (((4 * h + lq) ^ b_sw) * 16);
-        const uint8_t* const pb1 = at + b_rd + (((4 * h + 2 + lq) ^ b_sw) * 16);
-        const uint8_t* const pe = smem + m_rd + ((k >> 1) & 1) * S::M + (((k & 1) ^ m_sw) * 16) + 8 * h;
-#pragma unroll
-        for (int j = 0; j < NF; ++j) {
-            f.b[j].u[0] = *(const u32x4*)(pb0 + j * 32 * 128);
-            f.b[j].u[1] = *(const u32x4*)(pb1 + j * 32 * 128);
-        }
-#pragma unroll
-        for (int i = 0; i < MF; ++i) {
-            f.a[i].u = *(const u32x4*)(pa + i * 32 * 64);
-            f.e[i] = *(const uint32_t*)(pe + i * 32 * 32);
+        return Reader{at + a_rd + (((2 * h + lq) ^ a_sw) * 16), {at + b_rd + (((4 * h + lq) ^ b_sw) * 16), at + b_rd + (((4 * h + 2 + lq) ^ b_sw) * 16)},
+                      smem + m_rd + ((k >> 1) & 1) * S::M + (((k & 1) ^ m_sw) * 16) + 8 * h};
+    };
+    struct Frags { AQ a[MF]; BQ b[NF]; uint32_t e[MF]; };
+    constexpr int READS = 2 * (MF + NF);
+    // read i of a half's fragments, in the order in which the products want them
+    auto read = [&](Frags& f, const Reader& r, int i) {
+        if (i == 0 || i > 2 * NF + 1) {
+            const int q = i == 0 ? 0 : (i - 2 * NF) / 2;
+            if (i % 2 == 0) f.a[q].u = *(const u32x4*)(r.a + q * 32 * 64);
+            else f.e[q] = *(const uint32_t*)(r.e + q * 32 * 32);
+        } else if (i == 1) {
+            f.e[0] = *(const uint32_t*)r.e;
+        } else {
+            f.b[(i - 2) / 2].u[i & 1] = *(const u32x4*)(r.b[i & 1] + (i - 2) / 2 * 32 * 128);
         }
     };
     f32x16 acc[MF][NF];
@@ -213,37 +222,66 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    auto multiply = [&](const Frags& f) {
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-            for (int j = 0; j < NF; ++j)
-                acc[i][j] = __builtin_amdgcn_smfmac_f32_32x32x64_fp8_fp8(f.a[i].v, f.b[j].v, acc[i][j], (int)f.e[i], 0, 0);
+    // Product i of a half.  With 16 fragments the accumulators fill all accumulation registers; left to itself the compiler keeps
+    // some of them in the others and moves them back and forth, two hundred moves a k-step.  (The instruction is written out for
+    // that; its wait states: two after a write of an operand by a vector instruction, here in front, and those of a read of the
+    // result by one, after the loop.)
+    auto multiply = [&](const Frags& f, int i) {
+        f32x16& c = acc[i / NF][i % NF];
+        if constexpr (MF * NF == 16) {
+#ifdef __HIP_DEVICE_COMPILE__
+            asm volatile("s_nop 1\n\tv_smfmac_f32_32x32x64_fp8_fp8 %0, %1, %2, %3" : "+a"(c) : "v"(f.a[i / NF].v), "v"(f.b[i % NF].v), "v"(f.e[i / NF]));
+#endif
+        } else {
+            c = __builtin_amdgcn_smfmac_f32_32x32x64_fp8_fp8(f.a[i / NF].v, f.b[i % NF].v, c, (int)f.e[i / NF], 0, 0);
+        }
+    };
+    // The products of a half with a share of n other things after each; the order is kept
+    constexpr int PRODUCTS = MF * NF;
+    auto share = [&](int i, int n, int over, auto&& f) {
+        for (int u = (n * i + over - 1) / over; u < (n * (i + 1) + over - 1) / over && u < n; ++u) f(u);
     };
 
+    // loads of a k-step: the first EARLY after the barrier that frees their stage, the others with the next half's products
+    constexpr int EARLY = S::LOADS / 2;
     issue_meta(0);
-    issue(0, 0);
-    issue(1, 1);
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) issue(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < S::LOADS; ++i) issue(1, 1, i);
     issue_meta(1);
-    issue(2, 2);
-    WAIT_HERE(waitcnt_imm(2 * S::LOADS + S::META, 15));
+#pragma unroll
+    for (int i = 0; i < EARLY; ++i) issue(2, 2, i);
+    WAIT_HERE(waitcnt_imm(S::LOADS + S::META + EARLY, 15));
     wg_barrier();
     Frags f0, f1;
-    read(f0, 0, 0, std::integral_constant<int, 0>());
+#pragma unroll
+    for (int i = 0; i < READS; ++i) read(f0, reader(0, 0, 0), i);
     int stage = 0;
     // one k-step; EVEN: k is
     auto step = [&](int k, auto even) {
         constexpr bool EVEN = decltype(even)::value;
-        const int next = stage == 2 ? 0 : stage + 1;
-        read(f1, stage, k, std::integral_constant<int, 1>());
-        multiply(f0);
+        const int next = stage == 2 ? 0 : stage + 1, before = stage == 0 ? 2 : stage - 1;
+        const Reader r1 = reader(stage, k, 1);
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(f0, i);
+            share(i, READS, (PRODUCTS + 1) / 2, [&](int u) { read(f1, r1, u); });
+            share(i, S::LOADS - EARLY, PRODUCTS, [&](int u) { issue(k + 2, before, EARLY + u); });
+        }
         // of the loads still under way, those of step k + 2 may stay so
         WAIT_HERE(waitcnt_imm(S::LOADS + (EVEN ? S::META : 0), 0));
         wg_barrier();
         if (!EVEN) issue_meta((k + 3) >> 1);
-        issue(k + 3, stage);
-        read(f0, next, k + 1, std::integral_constant<int, 0>());
-        multiply(f1);
+        const Reader r0 = reader(next, k + 1, 0);
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(f1, i);
+            share(i, READS, PRODUCTS, [&](int u) { read(f0, r0, u); });
+            share(i, EARLY, PRODUCTS, [&](int u) { issue(k + 3, stage, u); });
+        }
         stage = next;
     };
     int k = 0;
@@ -253,6 +291,14 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     }
     if (k < steps) step(k, std::true_type());
     WAIT_HERE(waitcnt_imm(0, 0));                               // the look-ahead loads
+#ifdef __HIP_DEVICE_COMPILE__
+    if constexpr (MF * NF == 16) {
+        asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[0][0]), "+a"(acc[0][1]), "+a"(acc[0][2]), "+a"(acc[0][3]), "+a"(acc[1][0]),
+                     "+a"(acc[1][1]), "+a"(acc[1][2]), "+a"(acc[1][3]));
+        asm volatile("" : "+a"(acc[2][0]), "+a"(acc[2][1]), "+a"(acc[2][2]), "+a"(acc[2][3]), "+a"(acc[3][0]), "+a"(acc[3][1]),
+                     "+a"(acc[3][2]), "+a"(acc[3][3]));
+    }
+#endif
 
     // ---- results
     const int f_base = wm * (BM / 2) + 4 * lq, t_base = wn * (BN / 2) + l32;

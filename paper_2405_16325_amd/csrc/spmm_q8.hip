@@ -120,18 +120,21 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
 //     of W  row l % 32, packed bytes 16 (l / 32) .. + 15 and the 4 metadata bytes of that stretch,
 //     of X  token l % 32, k 16 (l / 32) .. + 15 and 32 + that,
 //     of D  token l % 32, rows 8 i + 4 (l / 32) .. + 3, i = 0 .. 3.
-// A k-step is 128 logical k: 64 bytes of a packed row, 16 of its metadata, 128 of a token.  Operands come through a ring of three
-// k-steps in LDS by global -> LDS loads, metadata by pairs of k-steps in two buffers.  A wavefront reads the fragments of half a
-// k-step while it multiplies the half before; one barrier a k-step, after which the ring's stage that everybody has left is
-// refilled for the third k-step on.
-// LDS bounds the loop: with wavefront tiles of 128 x 128 a k-step reads 104 KB and writes 52 KB of it, 1250 cycles at 128 bytes
-// each, while its products take 1024.
+// A k-step is 128 logical k: 64 bytes of a packed row, 16 of its metadata, 128 of a token.  Operands come by global -> LDS loads
+// of whole 128-byte lines where they can: a compute unit has a fixed number of requests in flight, whatever their size, and that
+// bounds the loop (requests of 64 bytes of W and 32 of metadata, in a ring of three k-steps: 1.61 ms for 8192 tokens, 36864 x 9216).
+// So W comes by pairs of k-steps and metadata by four, two buffers of each, tokens by k-steps in two stages.  A wavefront reads the
+// fragments of half a k-step while it multiplies the half before.  One barrier a k-step, between its halves' products: then
+// everybody has left the k-step's buffers.  Loads of a wavefront, by k mod 4 (k: the k-step in work):
+//     first half        0, 2: half of the pair of W after next      1: the metadata block after next
+//     second half       tokens of k-step k + 2, a quarter of the pair of W after next
+// What was queued before the first half has landed at the barrier that ends it.
 template <int BM, int BN>
 struct Q8Smem {
-    static constexpr int A = BM * 64, B = BN * 128, STAGE = A + B, M = BM * 32;
-    static constexpr int M_OFF = 3 * STAGE, TOTAL = M_OFF + 2 * M;
+    static constexpr int A = BM * 128, B = BN * 128, M = BM * 64;         // a pair of W, a k-step of tokens, a block of metadata
+    static constexpr int B_OFF = 2 * A, M_OFF = B_OFF + 2 * B, TOTAL = M_OFF + 2 * M;
     static constexpr int OUT_PITCH = BM * 2 + 16;
-    static constexpr int LOADS = BM / 64 + BN / 32, META = BM / 128;    // a wavefront's, per k-step and per pair
+    static constexpr int A_LOADS = BM / 32, B_LOADS = BN / 32, M_LOADS = BM / 64;    // a wavefront's
 };
 
 // where a workgroup's slab of k-steps lies; slabs > 1: fp32 sums to part[slab][token][row]
@@ -158,48 +161,42 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     const buffer_t a_buf = tile_buffer(p.a + m0 * a_pitch, rows * a_pitch);
     const buffer_t b_buf = tile_buffer(p.x + n0 * b_pitch, toks * b_pitch);
     const buffer_t m_buf = tile_buffer(p.am + m0 * m_pitch, rows * m_pitch);
-    uint32_t a_off[BM / 64], b_off[BN / 32], m_off[S::META];
-    int m_piece[S::META];
+    uint32_t a_off[S::A_LOADS], b_off[S::B_LOADS], m_off[S::M_LOADS];
 #pragma unroll
-    for (int i = 0; i < BM / 64; ++i) {
-        const int r = (wave * (BM / 64) + i) * 16 + (lane >> 2);
-        a_off[i] = r < rows ? r * a_pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
+    for (int i = 0; i < S::A_LOADS; ++i) {                      // 8 rows a load, the 16-byte pieces of a row rotated
+        const int r = (wave * S::A_LOADS + i) * 8 + (lane >> 3);
+        a_off[i] = r < rows ? r * a_pitch + 16 * ((lane & 7) ^ ((r >> 1) & 7)) : NOWHERE;
     }
 #pragma unroll
-    for (int i = 0; i < BN / 32; ++i) {
-        const int r = (wave * (BN / 32) + i) * 8 + (lane >> 3);
+    for (int i = 0; i < S::B_LOADS; ++i) {
+        const int r = (wave * S::B_LOADS + i) * 8 + (lane >> 3);
         b_off[i] = r < toks ? r * b_pitch + 16 * ((lane & 7) ^ ((r >> 1) & 7)) : NOWHERE;
     }
 #pragma unroll
-    for (int i = 0; i < S::META; ++i) {
-        const int r = (wave * S::META + i) * 32 + (lane >> 1);
-        m_off[i] = r < rows ? r * m_pitch : NOWHERE;
-        m_piece[i] = 16 * ((lane & 1) ^ ((r >> 3) & 1));
+    for (int i = 0; i < S::M_LOADS; ++i) {                      // 16 rows a load
+        const int r = (wave * S::M_LOADS + i) * 16 + (lane >> 2);
+        m_off[i] = r < rows ? r * m_pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
     }
-    const int last = first + steps - 1;
-
-    // load i of k-step k (clamped) into ring stage `stage`
-    auto issue = [&](int k, int stage, int i) {
-        const int kc = min(first + k, last);
-        uint8_t* const to = smem + stage * S::STAGE;
-        if (i < BM / 64) buffer_dma16(a_buf, to + (wave * (BM / 64) + i) * 1024, a_off[i], kc * 64);
-        else buffer_dma16(b_buf, to + S::A + (wave * (BN / 32) + i - BM / 64) * 1024, b_off[i - BM / 64], kc * KSTEP);
+    // Past the last k-step the last of each is loaded again.  The pieces that a last pair or block has too many are the next row's
+    // (the last row's: zeros) and not used.
+    auto issue_a = [&](int pair, int i) {
+        buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, a_off[i], first * 64 + min(pair, (steps - 1) >> 1) * 128);
     };
-    auto issue_meta = [&](int pair) {                           // the second half of an odd last pair: the first again
-#pragma unroll
-        for (int i = 0; i < S::META; ++i)
-            buffer_dma16(m_buf, smem + S::M_OFF + (pair & 1) * S::M + (wave * S::META + i) * 1024,
-                         m_off[i] + (uint32_t)min(first * 16 + pair * 32 + m_piece[i], 16 * last), 0);
+    auto issue_b = [&](int k, int i) {
+        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, b_off[i], (first + min(k, steps - 1)) * KSTEP);
+    };
+    auto issue_m = [&](int block, int i) {
+        buffer_dma16(m_buf, smem + S::M_OFF + (block & 1) * S::M + (wave * S::M_LOADS + i) * 1024, m_off[i], first * 16 + min(block, (steps - 1) >> 2) * 64);
     };
 
-    // reader lanes: offsets inside a stage (W: of each half's chunk; X: of each half's two), inside the metadata
-    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32, a_sw = (l32 >> 2) & 3, b_sw = (l32 >> 1) & 7;
-    const int a_rd = a_row * 64, b_rd = S::A + b_row * 128, m_rd = S::M_OFF + a_row * 32 + lq * 4, m_sw = (l32 >> 3) & 1;
+    // reader lanes
+    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32, sw = (l32 >> 1) & 7, m_sw = (l32 >> 2) & 3;
+    const int a_rd = a_row * 128, b_rd = S::B_OFF + b_row * 128, m_rd = S::M_OFF + a_row * 64 + lq * 4;
     struct Reader { const uint8_t *a, *b[2], *e; };
-    auto reader = [&](int stage, int k, int h) {
-        const uint8_t* const at = smem + stage * S::STAGE;
-        return Reader{at + a_rd + (((2 * h + lq) ^ a_sw) * 16), {at + b_rd + (((4 * h + lq) ^ b_sw) * 16), at + b_rd + (((4 * h + 2 + lq) ^ b_sw) * 16)},
-                      smem + m_rd + ((k >> 1) & 1) * S::M + (((k & 1) ^ m_sw) * 16) + 8 * h};
+    auto reader = [&](int k, int h) {                           // half h of k-step k
+        const uint8_t *const pa = smem + ((k >> 1) & 1) * S::A + a_rd, *const pb = smem + (k & 1) * S::B + b_rd;
+        return Reader{pa + (((4 * (k & 1) + 2 * h + lq) ^ sw) * 16), {pb + (((4 * h + lq) ^ sw) * 16), pb + (((4 * h + 2 + lq) ^ sw) * 16)},
+                      smem + m_rd + ((k >> 2) & 1) * S::M + (((k & 3) ^ m_sw) * 16) + 8 * h};
     };
     struct Frags { AQ a[MF]; BQ b[NF]; uint32_t e[MF]; };
     constexpr int READS = 2 * (MF + NF);
@@ -207,8 +204,8 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     auto read = [&](Frags& f, const Reader& r, int i) {
         if (i == 0 || i > 2 * NF + 1) {
             const int q = i == 0 ? 0 : (i - 2 * NF) / 2;
-            if (i % 2 == 0) f.a[q].u = *(const u32x4*)(r.a + q * 32 * 64);
-            else f.e[q] = *(const uint32_t*)(r.e + q * 32 * 32);
+            if (i % 2 == 0) f.a[q].u = *(const u32x4*)(r.a + q * 32 * 128);
+            else f.e[q] = *(const uint32_t*)(r.e + q * 32 * 64);
         } else if (i == 1) {
             f.e[0] = *(const uint32_t*)r.e;
         } else {
@@ -242,54 +239,64 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         for (int u = (n * i + over - 1) / over; u < (n * (i + 1) + over - 1) / over && u < n; ++u) f(u);
     };
 
-    // loads of a k-step: the first EARLY after the barrier that frees their stage, the others with the next half's products
-    constexpr int EARLY = S::LOADS / 2;
-    issue_meta(0);
+    constexpr int QUARTER = S::A_LOADS / 4, HALF = S::A_LOADS / 2;
 #pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) issue(0, 0, i);
+    for (int i = 0; i < S::M_LOADS; ++i) issue_m(0, i);
 #pragma unroll
-    for (int i = 0; i < S::LOADS; ++i) issue(1, 1, i);
-    issue_meta(1);
+    for (int i = 0; i < S::A_LOADS; ++i) issue_a(0, i);
 #pragma unroll
-    for (int i = 0; i < EARLY; ++i) issue(2, 2, i);
-    WAIT_HERE(waitcnt_imm(S::LOADS + S::META + EARLY, 15));
+    for (int i = 0; i < S::B_LOADS; ++i) issue_b(0, i);
+#pragma unroll
+    for (int i = 0; i < S::B_LOADS; ++i) issue_b(1, i);
+#pragma unroll
+    for (int i = 0; i < QUARTER; ++i) issue_a(1, i);
+    WAIT_HERE(waitcnt_imm(S::B_LOADS + QUARTER, 15));
     wg_barrier();
     Frags f0, f1;
+    {
+        const Reader r = reader(0, 0);
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read(f0, reader(0, 0, 0), i);
-    int stage = 0;
-    // one k-step; EVEN: k is
-    auto step = [&](int k, auto even) {
-        constexpr bool EVEN = decltype(even)::value;
-        const int next = stage == 2 ? 0 : stage + 1, before = stage == 0 ? 2 : stage - 1;
-        const Reader r1 = reader(stage, k, 1);
+        for (int i = 0; i < READS; ++i) read(f0, r, i);
+    }
+    auto step = [&](int k, auto mod4) {
+        constexpr int K4 = decltype(mod4)::value;
+        constexpr int LOADS1 = K4 % 2 == 0 ? HALF : K4 == 1 ? S::M_LOADS : 0;
+        const Reader r1 = reader(k, 1);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             multiply(f0, i);
             share(i, READS, (PRODUCTS + 1) / 2, [&](int u) { read(f1, r1, u); });
-            share(i, S::LOADS - EARLY, PRODUCTS, [&](int u) { issue(k + 2, before, EARLY + u); });
+            share(i, LOADS1, PRODUCTS, [&](int u) {
+                if (K4 % 2 == 0) issue_a((k >> 1) + 1, QUARTER + u);
+                else issue_m((k >> 2) + 1, u);
+            });
         }
-        // of the loads still under way, those of step k + 2 may stay so
-        WAIT_HERE(waitcnt_imm(S::LOADS + (EVEN ? S::META : 0), 0));
+        WAIT_HERE(waitcnt_imm(LOADS1, 0));
         wg_barrier();
-        if (!EVEN) issue_meta((k + 3) >> 1);
-        const Reader r0 = reader(next, k + 1, 0);
+        const Reader r0 = reader(k + 1, 0);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             multiply(f1, i);
-            share(i, READS, PRODUCTS, [&](int u) { read(f0, r0, u); });
-            share(i, EARLY, PRODUCTS, [&](int u) { issue(k + 3, stage, u); });
+            share(i, READS, PRODUCTS - PRODUCTS / 4, [&](int u) { read(f0, r0, u); });
+            share(i, S::B_LOADS + QUARTER, PRODUCTS, [&](int u) {
+                if (u < S::B_LOADS) issue_b(k + 2, u);
+                else if (K4 % 2 == 0) issue_a((k >> 1) + 1, QUARTER + HALF + u - S::B_LOADS);
+                else issue_a((k >> 1) + 2, u - S::B_LOADS);
+            });
         }
-        stage = next;
     };
     int k = 0;
-    for (; k + 1 < steps; k += 2) {
-        step(k, std::true_type());
-        step(k + 1, std::false_type());
+    for (; k + 3 < steps; k += 4) {
+        step(k, std::integral_constant<int, 0>());
+        step(k + 1, std::integral_constant<int, 1>());
+        step(k + 2, std::integral_constant<int, 2>());
+        step(k + 3, std::integral_constant<int, 3>());
     }
-    if (k < steps) step(k, std::true_type());
+    if (k < steps) step(k, std::integral_constant<int, 0>());
+    if (k + 1 < steps) step(k + 1, std::integral_constant<int, 1>());
+    if (k + 2 < steps) step(k + 2, std::integral_constant<int, 2>());
     WAIT_HERE(waitcnt_imm(0, 0));                               // the look-ahead loads
 #ifdef __HIP_DEVICE_COMPILE__
     if constexpr (MF * NF == 16) {

@@ -8,6 +8,7 @@
 // Memory bounds both directions.  A row is read once and stays in registers: LPR lanes (8 to 64) of a wavefront share a
 // short one, `wpr` wavefronts a longer one; a lane holds VPT pieces of 8 neighbouring elements, so that every load and
 // store of a wavefront covers whole 128-byte lines.
+#include "pipeline.h"
 #include "wave.h"
 
 namespace {
@@ -49,6 +50,16 @@ __device__ __forceinline__ float row_max(float v, int wpr, float* part) {
     return v;
 }
 
+// STREAM: a call that moves more than the last-level cache holds, of which nothing would be found there by the next one
+// (16384 x 9216, 1.2 GB: forward 205 -> 197 us, gradient 227 -> 201; 4096 x 2560, 84 MB, would take 15.4 -> 17.0 and 22.6 -> 22.9)
+template <bool STREAM, class T>
+__device__ __forceinline__ T load(const void* p) { return STREAM ? __builtin_nontemporal_load((const T*)p) : *(const T*)p; }
+template <bool STREAM, class T>
+__device__ __forceinline__ void store(void* p, T v) {
+    if (STREAM) __builtin_nontemporal_store(v, (T*)p);
+    else *(T*)p = v;
+}
+
 struct NormFwd {
     const bf16_t *x, *res, *w;                 // res: or null
     int64_t b;
@@ -60,7 +71,7 @@ struct NormFwd {
     float* scale;
 };
 
-template <int LPR, int VPT>
+template <int LPR, int VPT, bool STREAM = false>
 __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int wpr) {
     __shared__ float part[2][MAX_WAVES];
     const RowThreads rt = row_threads<LPR>(wpr);
@@ -78,8 +89,8 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int
         const int i = rt.lane + p * rt.threads;
         px[p] = pr[p] = w[p] = (u32x4){0, 0, 0, 0};
         if (live && i < pieces) {
-            px[p] = *(const u32x4*)(a.x + at + 8 * (size_t)i);
-            if (a.res) pr[p] = *(const u32x4*)(a.res + at + 8 * (size_t)i);
+            px[p] = load<STREAM, u32x4>(a.x + at + 8 * (size_t)i);
+            if (a.res) pr[p] = load<STREAM, u32x4>(a.res + at + 8 * (size_t)i);
             w[p] = *(const u32x4*)(a.w + 8 * (size_t)i);
         }
     }
@@ -92,7 +103,7 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int
 #pragma unroll
             for (int k = 0; k < 8; ++k) s.v[k] += r.v[k];
             px[p] = pack_bf16(s);
-            if (live && i < pieces) *(u32x4*)(a.h + at + 8 * (size_t)i) = px[p];
+            if (live && i < pieces) store<STREAM>(a.h + at + 8 * (size_t)i, px[p]);
         }
         h[p] = unpack_bf16(px[p]);
 #pragma unroll
@@ -112,7 +123,7 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int
             h[p].v[k] = h[p].v[k] * r * f.v[k];
             top = max_abs(top, h[p].v[k]);
         }
-        if (a.y && live && i < pieces) *(u32x4*)(a.y + at + 8 * (size_t)i) = pack_bf16(h[p]);
+        if (a.y && live && i < pieces) store<STREAM>(a.y + at + 8 * (size_t)i, pack_bf16(h[p]));
     }
     if (!a.q) return;
     const Q8Scale s = q8_scale(row_max<LPR>(top, wpr, part[1]));
@@ -122,7 +133,7 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_fwd_kernel(NormFwd a, int
         const int i = rt.lane + p * rt.threads;
 #pragma unroll
         for (int k = 0; k < 8; ++k) h[p].v[k] *= s.inv;
-        if (live && i < pieces) *(u32x2*)(a.q + at + 8 * (size_t)i) = pack_e4m3(h[p]);
+        if (live && i < pieces) store<STREAM>(a.q + at + 8 * (size_t)i, pack_e4m3(h[p]));
     }
 }
 
@@ -191,44 +202,66 @@ struct NormBwd {
 
 // Workgroup g takes rows g R .. g R + R - 1, then those `groups` R later, and keeps its share of dw in registers; the R row
 // slots' shares are added through LDS.
-template <int LPR, int VPT>
-__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_kernel(NormBwd a, int wpr) {
+constexpr int bwd_threads(int vpt) { return vpt == 1 ? MAX_THREADS : 512; }   // more would leave fewer registers than they take
+
+template <int LPR, int VPT, bool STREAM = false>
+__global__ void __launch_bounds__(bwd_threads(VPT)) rmsnorm_bwd_kernel(NormBwd a, int wpr) {
+    constexpr bool AHEAD = VPT <= 4;                            // longer rows keep enough loads on their way one at a time,
+                                                                // and registers only for them and dw
     extern __shared__ float lds[];                              // 2 x MAX_WAVES, then R - 1 rows of d
     const RowThreads rt = row_threads<LPR>(wpr);
     const int slots = blockDim.x / rt.threads, pieces = a.d / 8;
-    F8 w[VPT], dw[VPT];
+    struct Row { u32x4 dy[VPT], h[VPT], dh[VPT]; float r; };
+    auto fetch = [&](Row& o, int64_t row) {
+        const bool live = row < a.b;
+        const size_t at = (size_t)row * a.d;
+        o.r = live ? a.rstd[row] : 0.0f;
+#pragma unroll
+        for (int p = 0; p < VPT; ++p) {
+            const int i = rt.lane + p * rt.threads;
+            o.dy[p] = o.h[p] = o.dh[p] = (u32x4){0, 0, 0, 0};
+            if (live && i < pieces) {
+                o.dy[p] = load<STREAM, u32x4>(a.dy + at + 8 * (size_t)i);
+                o.h[p] = load<STREAM, u32x4>(a.h + at + 8 * (size_t)i);
+                if (a.dh) o.dh[p] = load<STREAM, u32x4>(a.dh + at + 8 * (size_t)i);
+            }
+        }
+    };
+    u32x4 w[AHEAD ? VPT : 1];
+    auto weight = [&](int p) {
+        const int i = rt.lane + p * rt.threads;
+        return i < pieces ? *(const u32x4*)(a.w + 8 * (size_t)i) : (u32x4){0, 0, 0, 0};
+    };
+    F8 dw[VPT];
 #pragma unroll
     for (int p = 0; p < VPT; ++p) {
-        const int i = rt.lane + p * rt.threads;
-        w[p] = unpack_bf16(i < pieces ? *(const u32x4*)(a.w + 8 * (size_t)i) : (u32x4){0, 0, 0, 0});
+        if (AHEAD) w[p] = weight(p);
 #pragma unroll
         for (int k = 0; k < 8; ++k) dw[p].v[k] = 0.0f;
     }
     int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * slots; first < a.b; first += (int64_t)gridDim.x * slots, turn ^= 1) {
+    const int64_t stride = (int64_t)gridDim.x * slots;
+    Row now, next;
+    if (AHEAD) fetch(next, (int64_t)blockIdx.x * slots + rt.row);
+    for (int64_t first = (int64_t)blockIdx.x * slots; first < a.b; first += stride, turn ^= 1) {
         const int64_t row = first + rt.row;
         const bool live = row < a.b;
         const size_t at = (size_t)row * a.d;
-        const float r = live ? a.rstd[row] : 0.0f;
-        u32x4 pdy[VPT], ph[VPT], pdh[VPT];
-#pragma unroll
-        for (int p = 0; p < VPT; ++p) {
-            const int i = rt.lane + p * rt.threads;
-            pdy[p] = ph[p] = pdh[p] = (u32x4){0, 0, 0, 0};
-            if (live && i < pieces) {
-                pdy[p] = *(const u32x4*)(a.dy + at + 8 * (size_t)i);
-                ph[p] = *(const u32x4*)(a.h + at + 8 * (size_t)i);
-                if (a.dh) pdh[p] = *(const u32x4*)(a.dh + at + 8 * (size_t)i);
-            }
+        if (AHEAD) {
+            now = next;
+            fetch(next, row + stride);                           // on its way while this row is worked on
+        } else {
+            fetch(now, row);
         }
         float c = 0.0f;
 #pragma unroll
         for (int p = 0; p < VPT; ++p) {
-            const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]);
+            if (!AHEAD) __builtin_amdgcn_sched_barrier(0);      // no pieces of the weight in advance
+            const F8 dy = unpack_bf16(now.dy[p]), h = unpack_bf16(now.h[p]), f = unpack_bf16(AHEAD ? w[AHEAD ? p : 0] : weight(p));
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float t = dy.v[k] * (h.v[k] * r);
-                c = fmaf(t, w[p].v[k], c);
+                const float t = dy.v[k] * (h.v[k] * now.r);
+                c = fmaf(t, f.v[k], c);
                 dw[p].v[k] += t;
             }
         }
@@ -236,11 +269,15 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_kernel(NormBwd a, int
 #pragma unroll
         for (int p = 0; p < VPT; ++p) {
             const int i = rt.lane + p * rt.threads;
-            const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]), dh = unpack_bf16(pdh[p]);
+            // packed again from here: twice the registers would be taken by the values as they were unpacked above
+            if (!AHEAD) __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+v"(now.dy[p]), "+v"(now.h[p]));
+            const F8 dy = unpack_bf16(now.dy[p]), h = unpack_bf16(now.h[p]), dh = unpack_bf16(now.dh[p]),
+                     f = unpack_bf16(AHEAD ? w[AHEAD ? p : 0] : weight(p));
             F8 o;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w[p].v[k] - h.v[k] * r * c, dh.v[k]);
-            if (live && i < pieces) *(u32x4*)(a.dx + at + 8 * (size_t)i) = pack_bf16(o);
+            for (int k = 0; k < 8; ++k) o.v[k] = fmaf(now.r, dy.v[k] * f.v[k] - h.v[k] * now.r * c, dh.v[k]);
+            if (live && i < pieces) store<STREAM>(a.dx + at + 8 * (size_t)i, pack_bf16(o));
         }
     }
     float* const sums = lds + 2 * MAX_WAVES;
@@ -312,43 +349,60 @@ __global__ void __launch_bounds__(256) rmsnorm_dw_wide_kernel(NormBwd a) {
     o[1] = (f32x4){s.v[4], s.v[5], s.v[6], s.v[7]};
 }
 
-// dw = bf16(sum of the groups' shares), in a fixed order.  A workgroup: 32 columns, 8 lanes of 4 each, 32 rows at a time
-__global__ void __launch_bounds__(256) rmsnorm_dw_kernel(const float* __restrict__ part, int groups, int d, bf16_t* __restrict__ dw) {
-    __shared__ f32x4 sums[32][8];
-    const int lane = threadIdx.x & 7, slot = threadIdx.x >> 3, col = blockIdx.x * 32 + lane * 4;
+// dw = bf16(sum of the groups' shares), in a fixed order.  A workgroup: 32 columns, 8 lanes of 4 each, 128 shares at a time
+__global__ void __launch_bounds__(1024) rmsnorm_dw_kernel(const float* __restrict__ part, int groups, int d, bf16_t* __restrict__ dw) {
+    __shared__ f32x4 sums[16][8];
+    const int lane = threadIdx.x & 7, wave = threadIdx.x >> 6, col = blockIdx.x * 32 + lane * 4;
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     if (col < d)
-        for (int g = slot; g < groups; g += 32) s += *(const f32x4*)(part + (size_t)g * d + col);
-    sums[slot][lane] = s;
+#pragma unroll 4
+        for (int g = threadIdx.x >> 3; g < groups; g += 128) s += *(const f32x4*)(part + (size_t)g * d + col);
+#pragma unroll
+    for (int x = 8; x < 64; x *= 2)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] += __shfl_xor(s[k], x);
+    if ((threadIdx.x & 63) < 8) sums[wave][lane] = s;
     __syncthreads();
-    if (slot != 0 || col >= d) return;
-    for (int i = 1; i < 32; ++i) s += sums[i][lane];
+    if (threadIdx.x >= 8 || col >= d) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += sums[i][lane];
     union { __bf16 h[4]; u32x2 u; } o;
 #pragma unroll
     for (int k = 0; k < 4; ++k) o.h[k] = (__bf16)s[k];
     *(u32x2*)(dw + col) = o.u;
 }
 
-// How the threads of a workgroup share rows of d elements: lanes per row below 64, or `wpr` wavefronts per row, VPT pieces a lane
-struct RowShape { int lpr, wpr, vpt, threads; };
-RowShape row_shape(int64_t b, int64_t d, int most) {
-    const int64_t pieces = d / 8;
-    if (pieces > (int64_t)MAX_THREADS * most) return {64, 0, 0, MAX_THREADS};
+// How the threads of a workgroup share rows of d elements: `lpr` lanes a row (below 64), or `wpr` wavefronts, vpt pieces a lane
+struct RowShape {
+    int lpr, wpr, vpt, threads;
+    int64_t slots() const { return lpr < 64 ? threads / lpr : threads / (64 * wpr); }
+};
+RowShape row_shape(int64_t pieces, int vpt) {
     if (pieces <= 32) return {pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32, 1, 1, 256};
-    int vpt = 1;
-    while (vpt < most && pieces > (int64_t)64 * vpt && (b >= 2048 || pieces > (int64_t)MAX_THREADS * vpt)) vpt *= 2;
     const int wpr = (int)((pieces + 64 * vpt - 1) / (64 * vpt));
     return {64, wpr, vpt, wpr >= 4 ? wpr * 64 : 4 / wpr * wpr * 64};
 }
+// Few rows: as many threads as there are pieces, up to MAX_THREADS.  Many: two pieces a lane keep enough loads on their way
+// (16384 x 9216: 207 us with 2, 3 or 4, with 8, whose registers leave a wavefront per SIMD, 296).  vpt 0: the row stays in memory.
+constexpr int64_t MANY_ROWS = 2048;
+RowShape fwd_shape(int64_t b, int64_t d) {
+    const int64_t pieces = d / 8;
+    if (pieces > 4 * MAX_THREADS) return {64, 1, 0, MAX_THREADS};
+    return row_shape(pieces, pieces > 2 * MAX_THREADS ? 4 : b >= MANY_ROWS || pieces > MAX_THREADS ? 2 : 1);
+}
+RowShape bwd_shape(int64_t b, int64_t d) {
+    const int64_t pieces = d / 8;
+    if (pieces > 6 * 512) return {64, 1, 0, MAX_THREADS};
+    if (b < MANY_ROWS && pieces <= MAX_THREADS) return row_shape(pieces, 1);
+    return row_shape(pieces, pieces <= 2 * 512 ? 2 : pieces <= 3 * 512 ? 3 : pieces <= 4 * 512 ? 4 : 6);
+}
 
-constexpr int FWD_MOST = 8, BWD_MOST = 4;
-constexpr int BWD_GROUPS = 512;
-
+// workgroups of the gradient: as many as are resident together (eight wavefronts on a compute unit), so that each makes one share of dw
 int bwd_groups(int64_t b, int64_t d) {
-    const RowShape s = row_shape(b, d, BWD_MOST);
-    const int64_t slots = s.wpr == 0 ? 1 : s.lpr < 64 ? s.threads / s.lpr : s.threads / (64 * s.wpr);
-    const int64_t turns = (b + slots - 1) / slots;
-    return (int)(turns < BWD_GROUPS ? turns : BWD_GROUPS);
+    const RowShape s = bwd_shape(b, d);
+    const int64_t turns = s.vpt == 0 ? b : (b + s.slots() - 1) / s.slots();
+    const int64_t most = RESIDENT * (s.threads >= 8 * 64 ? 1 : 8 * 64 / s.threads);
+    return (int)(turns < most ? turns : most);
 }
 
 }  // namespace
@@ -356,18 +410,19 @@ int bwd_groups(int64_t b, int64_t d) {
 hipError_t launch_rmsnorm_fwd(const bf16_t* x, const bf16_t* res, const bf16_t* w, int64_t b, int64_t d, float eps, bf16_t* h,
                               bf16_t* y, float* rstd, uint8_t* q, float* scale, hipStream_t s) {
     const NormFwd a = {x, res, w, b, (int)d, eps, h, y, rstd, q, scale};
-    const RowShape rs = row_shape(b, d, FWD_MOST);
-    const int64_t slots = rs.wpr == 0 ? 1 : rs.lpr < 64 ? rs.threads / rs.lpr : rs.threads / (64 * rs.wpr);
-    const dim3 grid = grid_of((b + slots - 1) / slots);
-#define FWD(L, V) rmsnorm_fwd_kernel<L, V><<<grid, rs.threads, 0, s>>>(a, rs.wpr)
-    if (rs.wpr == 0) rmsnorm_fwd_wide_kernel<<<grid, MAX_THREADS, 0, s>>>(a);
+    const RowShape rs = fwd_shape(b, d);
+    const dim3 grid = grid_of((b + rs.slots() - 1) / rs.slots());
+    const bool stream = (size_t)b * (size_t)d * (2 + (res ? 4 : 0) + (y ? 2 : 0) + (q ? 1 : 0)) > LAST_LEVEL_CACHE_BYTES;
+#define FWD(...) rmsnorm_fwd_kernel<__VA_ARGS__><<<grid, rs.threads, 0, s>>>(a, rs.wpr)
+    if (rs.vpt == 0) rmsnorm_fwd_wide_kernel<<<grid_of(b), MAX_THREADS, 0, s>>>(a);
     else if (rs.lpr == 8) FWD(8, 1);
     else if (rs.lpr == 16) FWD(16, 1);
     else if (rs.lpr == 32) FWD(32, 1);
     else if (rs.vpt == 1) FWD(64, 1);
+    else if (rs.vpt == 2 && stream) FWD(64, 2, true);
     else if (rs.vpt == 2) FWD(64, 2);
-    else if (rs.vpt == 4) FWD(64, 4);
-    else FWD(64, 8);
+    else if (stream) FWD(64, 4, true);
+    else FWD(64, 4);
 #undef FWD
     return hipGetLastError();
 }
@@ -377,24 +432,30 @@ size_t rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d) { return (size_t)bwd_gr
 hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w, const float* rstd, const bf16_t* dh, int64_t b,
                               int64_t d, bf16_t* dx, bf16_t* dw, float* part, hipStream_t s) {
     const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, part};
-    const RowShape rs = row_shape(b, d, BWD_MOST);
+    const RowShape rs = bwd_shape(b, d);
     const int groups = bwd_groups(b, d);
-    if (rs.wpr == 0) {
+    if (rs.vpt == 0) {
         // dw first: dx may be written over dy
         rmsnorm_dw_wide_kernel<<<dim3((unsigned)((d / 8 + 255) / 256), (unsigned)groups), 256, 0, s>>>(a);
         rmsnorm_bwd_wide_kernel<<<grid_of(b), MAX_THREADS, 0, s>>>(a);
     } else {
-        const int slots = rs.lpr < 64 ? rs.threads / rs.lpr : rs.threads / (64 * rs.wpr);
-        const size_t lds = 2 * MAX_WAVES * 4 + (size_t)(slots - 1) * d * 4;
-#define BWD(L, V) rmsnorm_bwd_kernel<L, V><<<groups, rs.threads, lds, s>>>(a, rs.wpr)
+        const size_t lds = 2 * MAX_WAVES * 4 + (size_t)(rs.slots() - 1) * d * 4;
+        const bool stream = (size_t)b * (size_t)d * (dh ? 8 : 6) > LAST_LEVEL_CACHE_BYTES;
+#define BWD(...) rmsnorm_bwd_kernel<__VA_ARGS__><<<groups, rs.threads, lds, s>>>(a, rs.wpr)
         if (rs.lpr == 8) BWD(8, 1);
         else if (rs.lpr == 16) BWD(16, 1);
         else if (rs.lpr == 32) BWD(32, 1);
         else if (rs.vpt == 1) BWD(64, 1);
+        else if (rs.vpt == 2 && stream) BWD(64, 2, true);
         else if (rs.vpt == 2) BWD(64, 2);
-        else BWD(64, 4);
+        else if (rs.vpt == 3 && stream) BWD(64, 3, true);
+        else if (rs.vpt == 3) BWD(64, 3);
+        else if (rs.vpt == 4 && stream) BWD(64, 4, true);
+        else if (rs.vpt == 4) BWD(64, 4);
+        else if (stream) BWD(64, 6, true);
+        else BWD(64, 6);
 #undef BWD
     }
-    rmsnorm_dw_kernel<<<(unsigned)((d + 31) / 32), 256, 0, s>>>(part, groups, (int)d, dw);
+    rmsnorm_dw_kernel<<<(unsigned)((d + 31) / 32), 1024, 0, s>>>(part, groups, (int)d, dw);
     return hipGetLastError();
 }

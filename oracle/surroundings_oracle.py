@@ -90,9 +90,7 @@ def dithered(a, u):
     a = np.asarray(a, F32)
     e = np.maximum(np.frexp(a)[1] - 1, -6).astype(np.float64)
     ulp = 2.0 ** (e - 3)
-    low = np.where(a < F32(2.0 ** -6), 8.0, 0.0)
-    t = (a.astype(np.float64) / ulp + low).astype(F32).astype(np.float64)      # below 2^-6: in steps of 2^-20 of a code
-    return (np.floor(t + u) - low) * ulp
+    return np.floor(a.astype(np.float64) / ulp + u) * ulp
 
 
 def store_states(x, step, root):

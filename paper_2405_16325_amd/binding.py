@@ -471,9 +471,11 @@ def slope_rmsnorm_fwd(X: torch.Tensor, weight: torch.Tensor, eps: float, residua
     if residual is not None:
         _want(residual, BF16, (b, d), "residual")
     if out is None:
-        new = lambda shape, dtype, asked: torch.empty(shape, dtype=dtype, device=X.device) if asked else None   # noqa: E731
-        Y, H = new((b, d), BF16, want_y), new((b, d), BF16, residual is not None)
-        rstd, Q, scale = new((b,), F32, want_rstd), new((b, d), E4M3, want_q8), new((b,), F32, want_q8)
+        Y = torch.empty_like(X) if want_y else None
+        H = torch.empty_like(X) if residual is not None else None
+        rstd = torch.empty(b, dtype=F32, device=X.device) if want_rstd else None
+        Q = torch.empty_like(X, dtype=E4M3) if want_q8 else None
+        scale = torch.empty(b, dtype=F32, device=X.device) if want_q8 else None
     else:
         Y, H, rstd, Q, scale = out
         for t, dtype, shape, what in ((Y, BF16, (b, d), "Y"), (H, BF16, (b, d), "H"), (rstd, F32, (b,), "rstd"),
@@ -500,7 +502,7 @@ def slope_rmsnorm_bwd(dY: torch.Tensor, H: torch.Tensor, weight: torch.Tensor, r
     if dh is not None:
         _want(dh, BF16, (b, d), "dh")
     if out is None:
-        dX, dw = torch.empty((b, d), dtype=BF16, device=dY.device), torch.empty((d,), dtype=BF16, device=dY.device)
+        dX, dw = torch.empty_like(dY), torch.empty_like(weight)
     else:
         dX, dw = _want(out[0], BF16, (b, d), "dX"), _want(out[1], BF16, (d,), "dweight")
     workspace = _scratch(workspace, int(lib().slope_rmsnorm_bwd_workspace_bytes(b, d)), dY.device, "workspace")
@@ -556,13 +558,14 @@ class AdamWTensor(ctypes.Structure):                                     # slope
 
 
 class AdamWPlan:
-    """A set of tensors that slope_grad_norm and slope_adamw_step work on in place.  Holds on to them; they must stay where
-    they are (a gradient is read from the buffer it had when the plan was made)."""
+    """A set of tensors that slope_grad_norm and slope_adamw_step work on in place, and the norm's scratch memory.  Holds on to
+    them; they must stay where they are (a gradient is read from the buffer it had when the plan was made).  One call at a time."""
 
-    def __init__(self, tensors, state_bits, table, device_table):
+    def __init__(self, tensors, state_bits, host, device):
         self.tensors, self.state_bits = tensors, state_bits
-        self.table, self.device_table = table, device_table
-        self.workspace_bytes = int(lib().slope_grad_norm_workspace_bytes(table))
+        self.host, self.device_table = host, host.to(device)
+        self.table = host.data_ptr()
+        self.workspace = torch.empty(int(lib().slope_grad_norm_workspace_bytes(self.table)), dtype=U8, device=device)
 
 
 def slope_adamw_plan(params, grads, m, v, masters=None, m_scales=None, v_scales=None, weight_decay=0.0) -> AdamWPlan:
@@ -602,16 +605,14 @@ def slope_adamw_plan(params, grads, m, v, masters=None, m_scales=None, v_scales=
     need = int(lib().slope_adamw_table_bytes(table, count))
     host = torch.empty(max(need, 64), dtype=U8)
     _check("slope_adamw_table", lib().slope_adamw_table(table, count, bits, host.data_ptr(), host.numel()))
-    plan = AdamWPlan([params, masters, list(grads), m, v, m_scales, v_scales], bits, host.data_ptr(), host.to(device))
-    plan.host = host
-    return plan
+    return AdamWPlan([params, masters, list(grads), m, v, m_scales, v_scales], bits, host, device)
 
 
-def slope_grad_norm(plan: AdamWPlan, control: torch.Tensor, inv_scale: float = 1.0, max_norm: float = float("inf"), workspace=None):
-    """Global norm of the plan's gradients into control fp32[4] = {norm, factor for the gradients, steps taken, unused} (starts as
-    zeros); nothing is copied to the host."""
+def slope_grad_norm(plan: AdamWPlan, control: torch.Tensor, inv_scale: float = 1.0, max_norm: float = float("inf")):
+    """Global norm of the plan's gradients into control fp32[4] = {norm, factor for the gradients, steps taken, unused} (starts
+    as zeros); nothing is copied to the host."""
     _want(control, F32, (4,), "control")
-    workspace = _scratch(workspace, plan.workspace_bytes, control.device, "workspace")
+    workspace = plan.workspace
     _check("slope_grad_norm", lib().slope_grad_norm(plan.table, _ptr(plan.device_table), inv_scale, max_norm, _ptr(control),
                                                     _ptr(workspace), workspace.numel(), _stream()))
     return control

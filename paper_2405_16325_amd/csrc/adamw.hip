@@ -28,7 +28,7 @@
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;                                    // of the norm's workgroups, and of the step's on large sets
 constexpr int CHUNK = 4096;
 constexpr int Q8_BLOCK = SLOPE_ADAMW_BLOCK;
 constexpr uint32_t DITHER_INDEX = 0x6A09E667u, DITHER_STEP = 0x9E3779B9u;   // 2^32 of sqrt(2) - 1, of the golden ratio - 1
@@ -189,7 +189,7 @@ __device__ __forceinline__ Raw<8, W> to_codes(const Vec<W>& x, uint32_t u, float
 struct Rates { float coef, rate, inv_root2, keep, t; };
 
 // One chunk of a tensor, whole (FULL) or its last part
-template <bool STATE8, bool MASTER, bool GRAD32, bool FULL, bool STREAM>
+template <int THREADS, bool STATE8, bool MASTER, bool GRAD32, bool FULL, bool STREAM>
 __device__ __forceinline__ void adamw_chunk(const StepArgs& a, const slope_adamw_tensor& tensor, int64_t start, const Rates& c) {
 #pragma clang fp contract(off)
     constexpr int W = STATE8 && !MASTER && !GRAD32 ? 8 : 4, BLOCK_LANES = Q8_BLOCK / W;
@@ -250,7 +250,7 @@ __device__ __forceinline__ void adamw_chunk(const StepArgs& a, const slope_adamw
     }
 }
 
-template <bool STATE8, bool STREAM>
+template <int THREADS, bool STATE8, bool STREAM>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(StepArgs a) {
     if (flat_block() >= a.chunks) return;
     const Chunk chunk = chunks_of(a.table, a.count)[flat_block()];
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(StepArgs a) {
     c.keep = 1.0f - a.lr * tensor.weight_decay;
     const int64_t start = (int64_t)chunk.part * CHUNK;
     const bool full = tensor.n - start >= CHUNK;
-#define CHUNK_OF(M, G) full ? adamw_chunk<STATE8, M, G, true, STREAM>(a, tensor, start, c) : adamw_chunk<STATE8, M, G, false, false>(a, tensor, start, c)
+#define CHUNK_OF(M, G) full ? adamw_chunk<THREADS, STATE8, M, G, true, STREAM>(a, tensor, start, c) : adamw_chunk<THREADS, STATE8, M, G, false, false>(a, tensor, start, c)
     if (tensor.master) {
         if (tensor.grad_bits == 32) CHUNK_OF(true, true);
         else CHUNK_OF(true, false);
@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(StepArgs a) {
 }
 
 // Sum of squares of a workgroup's run of chunks, one partial sum a workgroup.  (157 M elements, us: chunk w, w + 2048, ... 96; runs of
-// neighbours, whose table entries come together, 55; 8192 shorter runs 50, and 11 for the sum of that many.)
+// neighbours, whose table entries come together, 55; 8192 shorter runs 50, and 11 for the sum of that many.  The last workgroup to be
+// done as the one that adds them, in one launch: 244, the release of 4096 partial sums to all dies one after the other.)
 constexpr int NORM_GROUPS = 4096, FINISH_THREADS = 1024;
 __device__ __forceinline__ float block_sum(float v) {
     __shared__ float part[THREADS / 64];
@@ -409,9 +410,13 @@ hipError_t launch_adamw(const void* table, const void* device_table, double lr, 
     // a set that the last-level cache does not hold goes past it (us, through it / past it: 157 M elements with masters, 32-bit states
     // 900 / 779, 8-bit states 488 / 427; 510 M, 8-bit states, bf16 weights 1050 / 964)
     const bool stream = (size_t)h->chunks * CHUNK * (h->state_bits == 8 ? 8 : 16) > LAST_LEVEL_CACHE_BYTES;
-    if (h->state_bits == 8 && stream) adamw_kernel<true, true><<<grid, THREADS, 0, s>>>(a);
-    else if (h->state_bits == 8) adamw_kernel<true, false><<<grid, THREADS, 0, s>>>(a);
-    else if (stream) adamw_kernel<false, true><<<grid, THREADS, 0, s>>>(a);
-    else adamw_kernel<false, false><<<grid, THREADS, 0, s>>>(a);
+    // few chunks: more wavefronts on each, so that all of its loads are under way at once (0.9 M elements with masters: 9.0 -> 8.4 us)
+    const bool few = h->chunks < 4 * RESIDENT;
+    if (h->state_bits == 8 && stream) adamw_kernel<THREADS, true, true><<<grid, THREADS, 0, s>>>(a);
+    else if (h->state_bits == 8 && few) adamw_kernel<512, true, false><<<grid, 512, 0, s>>>(a);
+    else if (h->state_bits == 8) adamw_kernel<THREADS, true, false><<<grid, THREADS, 0, s>>>(a);
+    else if (stream) adamw_kernel<THREADS, false, true><<<grid, THREADS, 0, s>>>(a);
+    else if (few) adamw_kernel<512, false, false><<<grid, 512, 0, s>>>(a);
+    else adamw_kernel<THREADS, false, false><<<grid, THREADS, 0, s>>>(a);
     return hipGetLastError();
 }

@@ -202,12 +202,11 @@ def test_another_stream_and_graph_replays():
     """Graph replays take the step's number and the clipping factor from the device: they equal eager steps one by one."""
     sets = [Set(SIZES, 8, True, 16, seed=9) for _ in range(2)]
     controls = [torch.zeros(4, device="cuda") for _ in range(2)]
-    ws = torch.empty(sets[0].plan.workspace_bytes, dtype=torch.uint8, device="cuda")
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
 
     def step(i):
-        sl.slope_grad_norm(sets[i].plan, controls[i], 1.0, 0.05, workspace=ws)
+        sl.slope_grad_norm(sets[i].plan, controls[i], 1.0, 0.05)
         sl.slope_adamw_step(sets[i].plan, LR, B1, B2, EPS, control=controls[i])
 
     with torch.cuda.stream(stream):

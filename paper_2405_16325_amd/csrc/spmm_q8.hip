@@ -34,6 +34,21 @@ struct Q8Product {
     bf16_t* y;
 };
 
+// four rows' sums of a token to Y: scales, the added term, one rounding
+__device__ __forceinline__ void store_quad(const Q8Product& p, int64_t tok, int64_t f, f32x4 s) {
+    const f32x4 ws = *(const f32x4*)(p.as + f);
+    const float xs = p.xs[tok];
+    u32x2 add = {0, 0};
+    if (p.add) add = *(const u32x2*)(p.add + tok * p.m + f);
+    union { __bf16 h[4]; u32x2 u; } o;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
+        o.h[r] = (__bf16)(p.add ? fmaf(s[r] * xs, ws[r], t) : s[r] * xs * ws[r]);
+    }
+    *(u32x2*)(p.y + tok * p.m + f) = o.u;
+}
+
 constexpr int KSTEP = 128;
 // a raw buffer descriptor over `bytes` bytes; loads at offsets past them give zeros
 typedef __amdgpu_buffer_rsrc_t buffer_t;
@@ -94,28 +109,16 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
     for (int j = 0; j < 2; ++j) {
         const int64_t tok = n0 + j * 16 + l16;
         if (tok >= p.n) continue;
-        const float xs = p.xs[tok];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int64_t row = m0 + i * 16 + lq * 4;
-            if (row >= p.m) continue;                            // m is a multiple of 8: four rows are inside or outside
-            const f32x4 ws = *(const f32x4*)(p.as + row);
-            u32x2 add = {0, 0};
-            if (p.add) add = *(const u32x2*)(p.add + tok * p.m + row);
-            union { __bf16 h[4]; u32x2 u; } o;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t half = add[k >> 1];
-                const float t = __uint_as_float((k & 1) ? half & 0xFFFF0000u : half << 16);
-                o.h[k] = (__bf16)(p.add ? fmaf(acc[i][j][k] * xs, ws[k], t) : acc[i][j][k] * xs * ws[k]);
-            }
-            *(u32x2*)(p.y + tok * p.m + row) = o.u;
+            if (row < p.m) store_quad(p, tok, row, acc[i][j]);  // m is a multiple of 8: four rows are inside or outside
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------
-// q8_tile_kernel: whole tiles of BM rows x BN tokens, K % 128 == 0.  Four wavefronts, one per SIMD, 2 x 2, each BM / 2 x BN / 2 on
+// q8_tile_kernel: tiles of BM rows x BN tokens, K % 64 == 0 (TAIL: not of 128).  Four wavefronts, one per SIMD, WM along the rows, on
 // v_smfmac_f32_32x32x64_fp8_fp8, whose lane l holds
 //     of W  row l % 32, packed bytes 16 (l / 32) .. + 15 and the 4 metadata bytes of that stretch,
 //     of X  token l % 32, k 16 (l / 32) .. + 15 and 32 + that,
@@ -140,17 +143,17 @@ struct Q8Smem {
 // where a workgroup's slab of k-steps lies; slabs > 1: fp32 sums to part[slab][token][row]
 struct Q8Split { int steps, total; float* part; };
 
-template <int BM, int BN>
+template <int BM, int BN, int WM, bool TAIL>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, BM * BN > 128 * 128 ? 1 : 2)))
 q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     using S = Q8Smem<BM, BN>;
-    constexpr int MF = BM / 64, NF = BN / 64;
+    constexpr int WN = 4 / WM, MF = BM / (32 * WM), NF = BN / (32 * WN);
     extern __shared__ __align__(16) uint8_t smem[];
     int tm, tn;
     if (!tile_of_block(tiles_m, tiles_n, tm, tn)) return;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int l32 = lane & 31, lq = lane >> 5, wm = wave & 1, wn = wave >> 1;
+    const int l32 = lane & 31, lq = lane >> 5, wm = wave % WM, wn = wave / WM;
     const int first = (int)blockIdx.y * split.steps;
     const int steps = min(split.steps, split.total - first);
     const int K = (int)p.K;
@@ -177,20 +180,32 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         const int r = (wave * S::M_LOADS + i) * 16 + (lane >> 2);
         m_off[i] = r < rows ? r * m_pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
     }
+    // TAIL: the contraction ends inside a k-step; pieces past a row's end read zeros.  Pieces of a row, as its rows give them (rows
+    // 16 apart alike): of an even and of an odd load.
+    int piece[2];
+    if (TAIL)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) piece[i] = (lane & 7) ^ ((4 * i + (lane >> 4)) & 7);
     // Past the last k-step the last of each is loaded again.  The pieces that a last pair or block has too many are the next row's
     // (the last row's: zeros) and not used.
     auto issue_a = [&](int pair, int i) {
-        buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, a_off[i], first * 64 + min(pair, (steps - 1) >> 1) * 128);
+        const int at = min(pair, (steps - 1) >> 1);
+        uint32_t off = a_off[i];
+        if (TAIL) off |= piece[(wave * S::A_LOADS + i) & 1] * 32 >= K - (first + 2 * at) * KSTEP ? NOWHERE : 0;
+        buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, off, first * 64 + at * 128);
     };
     auto issue_b = [&](int k, int i) {
-        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, b_off[i], (first + min(k, steps - 1)) * KSTEP);
+        const int at = first + min(k, steps - 1);
+        uint32_t off = b_off[i];
+        if (TAIL) off |= piece[(wave * S::B_LOADS + i) & 1] * 16 >= K - at * KSTEP ? NOWHERE : 0;
+        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, off, at * KSTEP);
     };
     auto issue_m = [&](int block, int i) {
         buffer_dma16(m_buf, smem + S::M_OFF + (block & 1) * S::M + (wave * S::M_LOADS + i) * 1024, m_off[i], first * 16 + min(block, (steps - 1) >> 2) * 64);
     };
 
     // reader lanes
-    const int a_row = wm * (BM / 2) + l32, b_row = wn * (BN / 2) + l32, sw = (l32 >> 1) & 7, m_sw = (l32 >> 2) & 3;
+    const int a_row = wm * (BM / WM) + l32, b_row = wn * (BN / WN) + l32, sw = (l32 >> 1) & 7, m_sw = (l32 >> 2) & 3;
     const int a_rd = a_row * 128, b_rd = S::B_OFF + b_row * 128, m_rd = S::M_OFF + a_row * 64 + lq * 4;
     struct Reader { const uint8_t *a, *b[2], *e; };
     auto reader = [&](int k, int h) {                           // half h of k-step k
@@ -240,6 +255,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     };
 
     constexpr int QUARTER = S::A_LOADS / 4, HALF = S::A_LOADS / 2;
+    static_assert(QUARTER * 4 == S::A_LOADS && S::B_LOADS > 0 && S::M_LOADS > 0, "whole loads");
 #pragma unroll
     for (int i = 0; i < S::M_LOADS; ++i) issue_m(0, i);
 #pragma unroll
@@ -308,7 +324,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
 #endif
 
     // ---- results
-    const int f_base = wm * (BM / 2) + 4 * lq, t_base = wn * (BN / 2) + l32;
+    const int f_base = wm * (BM / WM) + 4 * lq, t_base = wn * (BN / WN) + l32;
     if (split.part) {
         float* const to = split.part + (int64_t)blockIdx.y * p.n * p.m;
 #pragma unroll
@@ -364,6 +380,115 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     }
 }
 
+// ------------------------------------------------------------------------------------------
+// q8_stream_kernel: up to TOK <= 32 tokens, K % 32 == 0: one pass over the packed weight, bound by memory.  A workgroup owns 32 rows
+// and all tokens; its wavefronts take the stretches of 256 logical k in turn, each through a ring of its own in LDS, without a
+// barrier, and add their sums through LDS at the end, in order.  Loads are of whole 128-byte lines of W: with operands straight to
+// registers, where a load takes 16 bytes from each of 64 places, the address unit is the bound (1 token, 36864 x 9216: 54.6 us).
+template <int TOK>
+struct Q8Ring {
+    static constexpr int M_OFF = 4096, X_OFF = M_OFF + 1024, STAGE = X_OFF + TOK * 256;
+    static constexpr int X_LOADS = TOK / 4, LOADS = 5 + X_LOADS;
+};
+template <int TOK, int WAVES, int STAGES>
+__global__ void __launch_bounds__(64 * WAVES) q8_stream_kernel(Q8Product p, Q8Split split) {
+    using S = Q8Ring<TOK>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l32 = lane & 31, lq = lane >> 5;
+    const int64_t m0 = (int64_t)blockIdx.x * 32;
+    const int rows = (int)min((int64_t)32, p.m - m0), toks = (int)p.n;
+    const int K = (int)p.K;
+    const buffer_t a_buf = tile_buffer(p.a + m0 * (K / 2), rows * (K / 2));
+    const buffer_t m_buf = tile_buffer(p.am + m0 * (K / 8), rows * (K / 8));
+    const buffer_t x_buf = tile_buffer(p.x, toks * K);
+    uint8_t* const ring = smem + wave * STAGES * S::STAGE;
+
+    // loads: 8 rows of W, 32 rows' metadata, 4 tokens each; pieces of 16 bytes, a row's rotated
+    uint32_t a_off[4], x_off[S::X_LOADS];
+    int a_piece[2];                                             // of an even load, of an odd one
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+        if (i < 2) a_piece[i] = c;
+        a_off[i] = r < rows ? r * (K / 2) + 16 * c : NOWHERE;
+    }
+    const uint32_t m_off = (lane >> 1) < rows ? (lane >> 1) * (K / 8) + 16 * (lane & 1) : NOWHERE;
+#pragma unroll
+    for (int i = 0; i < S::X_LOADS; ++i) {
+        const int t = 4 * i + (lane >> 4);
+        x_off[i] = t < toks ? t * K + 16 * ((lane & 15) ^ (t & 15)) : NOWHERE;
+    }
+    const int first = (int)blockIdx.y * split.steps, last = min(first + split.steps, split.total);
+    auto issue = [&](int s, int stage) {                        // zeros past the row's end and past the last stretch
+        uint8_t* const to = ring + stage * S::STAGE;
+        const int left = s < last ? K - s * 256 : 0;
+        if (left >= 256) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) buffer_dma16(a_buf, to + i * 1024, a_off[i], s * 128);
+            buffer_dma16(m_buf, to + S::M_OFF, m_off, s * 32);
+#pragma unroll
+            for (int i = 0; i < S::X_LOADS; ++i) buffer_dma16(x_buf, to + S::X_OFF + i * 1024, x_off[i], s * 256);
+        } else {
+            const int at = left > 0 ? s : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) buffer_dma16(a_buf, to + i * 1024, a_piece[i & 1] * 32 < left ? a_off[i] : NOWHERE, at * 128);
+            buffer_dma16(m_buf, to + S::M_OFF, left > 0 ? m_off : NOWHERE, at * 32);
+#pragma unroll
+            for (int i = 0; i < S::X_LOADS; ++i) {
+                const int c = (lane & 15) ^ ((4 * i + (lane >> 4)) & 15);
+                buffer_dma16(x_buf, to + S::X_OFF + i * 1024, c * 16 < left ? x_off[i] : NOWHERE, at * 256);
+            }
+        }
+    };
+    const int tok = l32 < TOK ? l32 : TOK - 1;                  // lanes without a token: any one's values, not stored
+    const int a_rd = l32 * 128, sw = (l32 >> 1) & 7, m_rd = S::M_OFF + l32 * 32 + 4 * lq, x_rd = S::X_OFF + tok * 256, x_sw = tok & 15;
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+
+    int s = first + wave, stage = 0;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) issue(s + i * WAVES, i);
+    for (; s < last; s += WAVES) {
+        WAIT_HERE(waitcnt_imm((STAGES - 2) * S::LOADS, 15));
+        const uint8_t* const at = ring + stage * S::STAGE;
+        AQ a[4];
+        BQ x[4];
+        uint32_t e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            a[u].u = *(const u32x4*)(at + a_rd + (((2 * u + lq) ^ sw) * 16));
+            e[u] = *(const uint32_t*)(at + m_rd + 8 * u);
+            x[u].u[0] = *(const u32x4*)(at + x_rd + (((4 * u + lq) ^ x_sw) * 16));
+            x[u].u[1] = *(const u32x4*)(at + x_rd + (((4 * u + 2 + lq) ^ x_sw) * 16));
+        }
+        issue(s + (STAGES - 1) * WAVES, stage == 0 ? STAGES - 1 : stage - 1);    // where the stretch before was
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc = __builtin_amdgcn_smfmac_f32_32x32x64_fp8_fp8(a[u].v, x[u].v, acc, (int)e[u], 0, 0);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+        WAIT_HERE(waitcnt_imm(63, 0));                          // read before it is loaded into again
+    }
+    WAIT_HERE(waitcnt_imm(0, 0));
+    __syncthreads();
+
+    // lane: token l32, rows 8 q + 4 lq .. + 3
+    constexpr int PITCH = 36;
+    float (*const sums)[TOK][PITCH] = (float (*)[TOK][PITCH])smem;
+    if (l32 < TOK)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *(f32x4*)&sums[wave][l32][8 * q + 4 * lq] = (f32x4){acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    for (int i = threadIdx.x; i < TOK * 8; i += 64 * WAVES) {
+        const int t = i >> 3, r = (i & 7) * 4;
+        if (t >= toks || r >= rows) continue;
+        f32x4 v = *(const f32x4*)&sums[0][t][r];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += *(const f32x4*)&sums[w][t][r];
+        if (split.part) *(f32x4*)(split.part + ((int64_t)blockIdx.y * p.n + t) * p.m + m0 + r) = v;
+        else store_quad(p, t, m0 + r, v);
+    }
+}
+
 // Y from the slabs' sums, added in order
 __global__ void __launch_bounds__(256) q8_reduce_kernel(Q8Product p, const float* __restrict__ part, int slabs) {
     const int64_t quads = p.m / 4, i = (flat_block() * 256 + threadIdx.x);
@@ -371,17 +496,21 @@ __global__ void __launch_bounds__(256) q8_reduce_kernel(Q8Product p, const float
     const int64_t tok = i / quads, f = (i - tok * quads) * 4;
     f32x4 s = *(const f32x4*)(part + tok * p.m + f);
     for (int k = 1; k < slabs; ++k) s += *(const f32x4*)(part + ((int64_t)k * p.n + tok) * p.m + f);
-    const f32x4 ws = *(const f32x4*)(p.as + f);
-    const float xs = p.xs[tok];
-    u32x2 add = {0, 0};
-    if (p.add) add = *(const u32x2*)(p.add + tok * p.m + f);
-    union { __bf16 h[4]; u32x2 u; } o;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
-        o.h[r] = (__bf16)(p.add ? fmaf(s[r] * xs, ws[r], t) : s[r] * xs * ws[r]);
+    store_quad(p, tok, f, s);
+}
+
+// Operands with rows of whole k-steps' halves: K to Kp = a multiple of 64.  A thread: 8 logical k of a row of W or of a token.
+__global__ void __launch_bounds__(256) q8_pad_kernel(Q8Product p, int64_t Kp, uint8_t* __restrict__ a, uint8_t* __restrict__ am, uint8_t* __restrict__ x) {
+    const int64_t pieces = Kp / 8, i = flat_block() * 256 + threadIdx.x, row = i / pieces, k = (i - row * pieces) * 8;
+    if (row >= p.m + p.n) return;
+    const bool in = k < p.K;
+    if (row < p.m) {
+        *(uint32_t*)(a + (row * Kp + k) / 2) = in ? *(const uint32_t*)(p.a + (row * p.K + k) / 2) : 0u;
+        am[(row * Kp + k) / 8] = in ? p.am[(row * p.K + k) / 8] : (uint8_t)META_NONE;
+    } else {
+        const int64_t t = row - p.m;
+        *(u32x2*)(x + t * Kp + k) = in ? *(const u32x2*)(p.x + t * p.K + k) : (u32x2){0, 0};
     }
-    *(u32x2*)(p.y + tok * p.m + f) = o.u;
 }
 
 // One wavefront a row: packed bf16 values to e4m3 with the row's scale.  half = d_in / 2, a multiple of 4.
@@ -418,29 +547,59 @@ namespace {
 
 // 32-bit offsets inside a tile's rows, and a grid of fewer than 2^32 work items
 bool tile_fits(int64_t n, int64_t m, int64_t K) {
-    return K % KSTEP == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < ((int64_t)1 << 23);
+    return K % 64 == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < ((int64_t)1 << 23);
 }
 
-template <int BM, int BN>
-hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+template <int BM, int BN, int WM, bool TAIL>
+hipError_t launch_tiles_of(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
     using S = Q8Smem<BM, BN>;
     constexpr int LDS = S::TOTAL > BN * S::OUT_PITCH ? S::TOTAL : BN * S::OUT_PITCH;
-    const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN>>(LDS);
+    const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN, WM, TAIL>>(LDS);
     if (e != hipSuccess) return e;
     const int tiles_m = (int)((p.m + BM - 1) / BM), tiles_n = (int)((p.n + BN - 1) / BN);
-    q8_tile_kernel<BM, BN><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
+    q8_tile_kernel<BM, BN, WM, TAIL><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
+    return hipGetLastError();
+}
+template <int BM, int BN, int WM>
+hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+    return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, false>(p, split, slabs, s) : launch_tiles_of<BM, BN, WM, true>(p, split, slabs, s);
+}
+
+constexpr int64_t PAD_WORK = (int64_t)1 << 24;
+constexpr int STREAM_WAVES = 4, STREAM_STAGES = 3, STREAM_GROUPS = 1024, STREAM_TOKENS = 8;
+bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && m < ((int64_t)1 << 29); }
+
+template <int TOK>
+hipError_t launch_stream(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+    constexpr int RING = STREAM_WAVES * STREAM_STAGES * Q8Ring<TOK>::STAGE, SUMS = STREAM_WAVES * TOK * 36 * 4, LDS = RING > SUMS ? RING : SUMS;
+    const hipError_t e = allow_dynamic_lds<q8_stream_kernel<TOK, STREAM_WAVES, STREAM_STAGES>>(LDS);
+    if (e != hipSuccess) return e;
+    q8_stream_kernel<TOK, STREAM_WAVES, STREAM_STAGES><<<dim3((unsigned)((p.m + 31) / 32), (unsigned)slabs), 64 * STREAM_WAVES, LDS, s>>>(p, split);
     return hipGetLastError();
 }
 
-// tile and slabs of a product
-struct Q8Plan { int bm, bn, slabs, steps; };
+// kernel of a product: stream (bn: tokens), tiles of bm x bn, or neither (the general one); the contraction in `slabs`
+// slabs of `steps` k-steps (stream: stretches)
+struct Q8Plan { bool stream; int bm, bn, slabs, steps, total; };
 Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
-    if (!tile_fits(n, m, K)) return {0, 0, 1, 0};
-    const int total = (int)(K / KSTEP);
+    if (stream_fits(n, m, K)) {
+        Q8Plan plan = {true, 32, n <= 4 ? 4 : 8, 1, 0, (int)((K + 255) / 256)};
+        plan.steps = plan.total;
+        const int64_t groups = (m + 31) / 32;
+        int slabs = room ? (int)min((int64_t)STREAM_GROUPS / groups, (int64_t)plan.total / (2 * STREAM_WAVES)) : 1;
+        if (slabs > 1) {
+            plan.steps = (plan.total + slabs - 1) / slabs;
+            plan.slabs = (plan.total + plan.steps - 1) / plan.steps;
+        }
+        return plan;
+    }
+    if (!tile_fits(n, m, K)) return {false, 0, 0, 1, 0, 0};
+    const int total = (int)((K + KSTEP - 1) / KSTEP);
     auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
-    Q8Plan plan = {128, 64, 1, total};
+    Q8Plan plan = {false, 128, 64, 1, total, total};
     if (n > 128 && tiles(256, 256) >= 192) plan.bm = plan.bn = 256;
     else if (n > 64) plan.bn = 128;
+    else if (n <= 32) plan.bn = 32;
     const int64_t t = tiles(plan.bm, plan.bn);
     if (room && t < 256) {
         int slabs = (int)(512 / t);
@@ -455,27 +614,60 @@ Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
 
 }  // namespace
 
+namespace {
+
+size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// Copies with longer rows for the kernels above, where rows are no multiple of 64 (nor, for few tokens, of 32) and the product is
+// worth two launches
+struct Q8Pad { int64_t Kp; size_t a, am, x; };
+Q8Pad q8_pad(int64_t n, int64_t m, int64_t K) {
+    const int64_t Kp = (K + 63) / 64 * 64;
+    if (stream_fits(n, m, K) || K % 64 == 0 || !tile_fits(n, m, Kp) || n * m * K < PAD_WORK) return {0, 0, 0, 0};
+    return {Kp, round256((size_t)m * (size_t)(Kp / 2)), round256((size_t)m * (size_t)(Kp / 8)), round256((size_t)n * (size_t)Kp)};
+}
+
+}  // namespace
+
+// [ padded copies | slabs' sums ]
 size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K) {
-    const Q8Plan plan = q8_plan(n, m, K, true);
-    return plan.slabs > 1 ? (size_t)plan.slabs * (size_t)n * (size_t)m * 4 : 0;
+    const Q8Pad pad = q8_pad(n, m, K);
+    const Q8Plan plan = q8_plan(n, m, pad.Kp ? pad.Kp : K, true);
+    return pad.a + pad.am + pad.x + (plan.slabs > 1 ? (size_t)plan.slabs * (size_t)n * (size_t)m * 4 : 0);
 }
 
 hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,
-                          int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* partial_or_null, hipStream_t s) {
-    const Q8Product p = {x, xs, n, a, am, as, m, K, add, y};
-    const Q8Plan plan = q8_plan(n, m, K, partial_or_null != nullptr);
+                          int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* workspace_or_null, hipStream_t s) {
+    Q8Product p = {x, xs, n, a, am, as, m, K, add, y};
+    uint8_t* room = (uint8_t*)workspace_or_null;
+    const Q8Pad pad = room ? q8_pad(n, m, K) : Q8Pad{0, 0, 0, 0};
+    if (pad.Kp) {
+        uint8_t *const a2 = room, *const am2 = a2 + pad.a, *const x2 = am2 + pad.am;
+        room = x2 + pad.x;
+        q8_pad_kernel<<<grid_of(((m + n) * (pad.Kp / 8) + 255) / 256), 256, 0, s>>>(p, pad.Kp, a2, am2, x2);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        p.a = a2;
+        p.am = am2;
+        p.x = x2;
+        p.K = pad.Kp;
+    }
+    const Q8Plan plan = q8_plan(n, m, p.K, room != nullptr);
     if (plan.bm == 0) {
         const int64_t tiles_m = (m + 63) / 64, tiles = tiles_m * ((n + 63) / 64);
         if (!grid_fits(tiles)) return hipErrorInvalidConfiguration;
         q8_generic_kernel<<<grid_of(tiles), 256, 0, s>>>(p, tiles_m);
         return hipGetLastError();
     }
-    const Q8Split split = {plan.steps, (int)(K / KSTEP), plan.slabs > 1 ? partial_or_null : nullptr};
+    float* const part = plan.slabs > 1 ? (float*)room : nullptr;
+    const Q8Split split = {plan.steps, plan.total, part};
     hipError_t e;
-    if (plan.bm == 256) e = launch_tiles<256, 256>(p, split, plan.slabs, s);
-    else if (plan.bn == 128) e = launch_tiles<128, 128>(p, split, plan.slabs, s);
-    else e = launch_tiles<128, 64>(p, split, plan.slabs, s);
+    if (plan.stream) e = plan.bn == 4 ? launch_stream<4>(p, split, plan.slabs, s) : launch_stream<8>(p, split, plan.slabs, s);
+    else if (plan.bm == 256) e = launch_tiles<256, 256, 2>(p, split, plan.slabs, s);
+    else if (plan.bn == 128) e = launch_tiles<128, 128, 2>(p, split, plan.slabs, s);
+    else if (plan.bn == 64) e = launch_tiles<128, 64, 2>(p, split, plan.slabs, s);
+    else e = launch_tiles<128, 32, 4>(p, split, plan.slabs, s);
     if (e != hipSuccess || plan.slabs == 1) return e;
-    q8_reduce_kernel<<<grid_of((n * (m / 4) + 255) / 256), 256, 0, s>>>(p, partial_or_null, plan.slabs);
+    q8_reduce_kernel<<<grid_of((n * (m / 4) + 255) / 256), 256, 0, s>>>(p, part, plan.slabs);
     return hipGetLastError();
 }

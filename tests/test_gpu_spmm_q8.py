@@ -61,7 +61,7 @@ def test_quantized_rows(d_out, d_in):
 # one token to many; multiples of 256, of 128, of 8 only; a contraction of one step, of part of one; few rows
 SHAPES = [(1, 8, 8), (1, 256, 128), (3, 72, 136), (1, 520, 1024), (5, 64, 2048), (16, 768, 512), (17, 1000, 200), (31, 264, 1160),
           (33, 128, 384), (64, 256, 256), (100, 1000, 1000), (128, 512, 4096), (130, 200, 4096), (200, 1032, 640), (257, 264, 896),
-          (300, 512, 128), (520, 768, 768), (777, 640, 1280), (1000, 1000, 1000), (1030, 520, 2176)]
+          (1, 64, 32), (2, 40, 96), (7, 104, 160), (40, 72, 224), (33, 200, 416), (64, 264, 2080), (30, 136, 64), (20, 264, 448), (70, 200, 320), (300, 264, 192), (777, 512, 4160), (300, 264, 1000), (2048, 1000, 2056), (9, 2056, 1992), (300, 512, 128), (520, 768, 768), (777, 640, 1280), (1000, 1000, 1000), (1030, 520, 2176)]
 
 
 @pytest.mark.parametrize("b,d_out,d_in", SHAPES)

@@ -62,17 +62,19 @@ __device__ __forceinline__ void buffer_dma16(buffer_t from, uint8_t* lds_dst, ui
 }
 constexpr uint32_t META_NONE = 0x44444444u;                    // a legal pair in every group
 
-// Any extents (K % 8 == 0).  Four wavefronts of 32 rows x 32 tokens, operands straight from memory in pieces of 8 logical k,
-// each of which is inside its row as a whole.
-__global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t tiles_m) {
+// Any extents (K % 8 == 0): 32 rows x 32 tokens, whose k-steps four wavefronts take in turn, operands straight from memory in pieces
+// of 8 logical k, each of which is inside its row as a whole; the sums are added through LDS, in order.  Latency bounds it where it
+// is meant to be used: a wavefront's loads of a k-step are all under way together, and no second launch is needed.
+__global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t tiles_m, int64_t tiles) {
+    __shared__ f32x4 sums[4][32][9];                            // [wavefront][token][four rows]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lq = lane >> 4;
     const int64_t block = flat_block();
-    const int64_t m0 = block % tiles_m * 64 + (wave & 1) * 32, n0 = block / tiles_m * 64 + (wave >> 1) * 32;
-    if (m0 >= p.m || n0 >= p.n) return;
+    if (block >= tiles) return;
+    const int64_t m0 = block % tiles_m * 32, n0 = block / tiles_m * 32;
     f32x4 acc[2][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i >> 1][i & 1] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t k0 = 0; k0 < p.K; k0 += KSTEP) {
+    for (int64_t k0 = wave * KSTEP; k0 < p.K; k0 += 4 * KSTEP) {
         AQ af[2];
         uint32_t meta[2];
         BQ bf[2];
@@ -106,15 +108,16 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
                 acc[i][j] = __builtin_amdgcn_smfmac_f32_16x16x128_fp8_fp8(af[i].v, bf[j].v, acc[i][j], (int)meta[i], 0, 0);
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int64_t tok = n0 + j * 16 + l16;
-        if (tok >= p.n) continue;
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t row = m0 + i * 16 + lq * 4;
-            if (row < p.m) store_quad(p, tok, row, acc[i][j]);  // m is a multiple of 8: four rows are inside or outside
-        }
-    }
+        for (int i = 0; i < 2; ++i) sums[wave][j * 16 + l16][i * 4 + lq] = acc[i][j];
+    __syncthreads();
+    const int t = threadIdx.x >> 3, q = threadIdx.x & 7;
+    if (n0 + t >= p.n || m0 + 4 * q >= p.m) return;             // m is a multiple of 8: four rows are inside or outside
+    f32x4 v = sums[0][t][q];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) v += sums[w][t][q];
+    store_quad(p, n0 + t, m0 + 4 * q, v);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -565,7 +568,10 @@ hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hip
     return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, false>(p, split, slabs, s) : launch_tiles_of<BM, BN, WM, true>(p, split, slabs, s);
 }
 
-constexpr int64_t PAD_WORK = (int64_t)1 << 24;
+// below it the general kernel's one launch is faster (us, general / copies and tiles: 200 tokens, 2056 x 2056 15.8 / 17; 600, 1000 x 1000
+// 11.8 / 13; 2048, 2056 x 2056 106 / 30)
+constexpr int64_t PAD_WORK = (int64_t)1 << 30;
+constexpr int STEPS_WHOLE = 40, STEPS_SLAB = 16;
 constexpr int STREAM_WAVES = 4, STREAM_STAGES = 3, STREAM_GROUPS = 1024, STREAM_TOKENS = 8;
 bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && m < ((int64_t)1 << 29); }
 
@@ -596,16 +602,29 @@ Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
     if (!tile_fits(n, m, K)) return {false, 0, 0, 1, 0, 0};
     const int total = (int)((K + KSTEP - 1) / KSTEP);
     auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
-    Q8Plan plan = {false, 128, 64, 1, total, total};
-    if (n > 128 && tiles(256, 256) >= 192) plan.bm = plan.bn = 256;
-    else if (n > 64) plan.bn = 128;
-    else if (n <= 32) plan.bn = 32;
+    // Tile by the time of a k-step of the whole grid, us.  256 x 256 goes by whole rounds of the chip; of the others two are on a
+    // compute unit, and rounds overlap.  (us, 256 x 256 / 128 x 128 / 128 x 64: 777 tokens, 20480 x 5120 105 / 95 / 120; 2048, 5120 x 5120
+    // 50 / 58 / 68; 512, 5120 x 5120 46 / 26 / 25; 256, 9216 x 9216 67 / 41 / 37; 1200, 14336 x 4096 80 / 71 / 92; 8192, 36864 x 9216
+    // 1550 / 2250 / 2930)
+    auto shared = [&](int bn, double one, double two) {        // one tile on a compute unit, 512 tiles on the chip
+        const int64_t t = tiles(128, bn);
+        const double all = two * (double)t / 512.0;
+        return t <= RESIDENT ? one : all > 0.75 * two ? all : 0.75 * two;
+    };
+    Q8Plan plan = {false, 128, 32, 1, total, total};
+    double best = shared(32, 0.40, 0.50);
+    const double t64 = shared(64, 0.42, 0.67), t128 = shared(128, 0.60, 1.08), t256 = 1.24 * (double)((tiles(256, 256) + RESIDENT - 1) / RESIDENT);
+    if (n > 32 && t64 < best) best = t64, plan.bn = 64;
+    if (n > 64 && t128 < best) best = t128, plan.bn = 128;
+    if (n > 128 && t256 < best) plan.bm = plan.bn = 256;
+    // A slab less than STEPS_WHOLE k-steps long is not worth a second launch, and more than two workgroups a compute unit give nothing
+    // (us, whole / slabs: 128 tokens, 5120 x 5120 16 / 18 with 6; 300, 4096 x 4096 15 / 20 with 2; 60, 9216 x 9216 34 / 20 with 7;
+    // 60, 2560 x 10240 21 / 14 with 12, 20 with 20; 300, 9216 x 36864 145 / 100 with 2)
     const int64_t t = tiles(plan.bm, plan.bn);
-    if (room && t < 256) {
-        int slabs = (int)(512 / t);
-        if (slabs > total / 4) slabs = total / 4;
+    if (room && total > STEPS_WHOLE) {
+        const int slabs = (int)min(2 * (int64_t)RESIDENT / t, (int64_t)(total + STEPS_SLAB - 1) / STEPS_SLAB);
         if (slabs > 1) {
-            plan.steps = ((total + slabs - 1) / slabs + 1) / 2 * 2;      // whole pairs of metadata
+            plan.steps = ((total + slabs - 1) / slabs + 1) / 2 * 2;      // whole pairs of k-steps
             plan.slabs = (total + plan.steps - 1) / plan.steps;
         }
     }
@@ -654,9 +673,9 @@ hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const ui
     }
     const Q8Plan plan = q8_plan(n, m, p.K, room != nullptr);
     if (plan.bm == 0) {
-        const int64_t tiles_m = (m + 63) / 64, tiles = tiles_m * ((n + 63) / 64);
+        const int64_t tiles_m = (m + 31) / 32, tiles = tiles_m * ((n + 31) / 32);
         if (!grid_fits(tiles)) return hipErrorInvalidConfiguration;
-        q8_generic_kernel<<<grid_of(tiles), 256, 0, s>>>(p, tiles_m);
+        q8_generic_kernel<<<grid_of(tiles), 256, 0, s>>>(p, tiles_m, tiles);
         return hipGetLastError();
     }
     float* const part = plan.slabs > 1 ? (float*)room : nullptr;

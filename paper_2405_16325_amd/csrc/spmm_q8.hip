@@ -130,37 +130,34 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
 // of whole 128-byte lines where they can: a compute unit has a fixed number of requests in flight, whatever their size, and that
 // bounds the loop (requests of 64 bytes of W and 32 of metadata, in a ring of three k-steps: 1.61 ms for 8192 tokens, 36864 x 9216).
 // So W comes by pairs of k-steps and metadata by four, two buffers of each, tokens by k-steps in two stages.  A wavefront reads the
-// fragments of half a k-step while it multiplies the half before.  One barrier a k-step, between its halves' products: then
-// everybody has left the k-step's buffers.  Loads of a wavefront, by k mod 4 (k: the k-step in work):
-//     first half        0, 2: half of the pair of W after next      1: the metadata block after next
-//     second half       tokens of k-step k + 2, a quarter of the pair of W after next
-// What was queued before the first half has landed at the barrier that ends it.
-//
-// DEEP, the 256 x 192 tile: what bounds the loop at 256 x 256 is that its loads have one k-step for their way.  With fewer tokens
-// there is room for a third stage of them, and, metadata by pairs, for loads that are queued two k-steps before the barrier at
-// which they have landed:
-//     after the barrier of k-step k     tokens of k-step k + 3; k odd: also W and metadata of the pair after next
-template <int BM, int BN, bool DEEP>
+// fragments of half a k-step while it multiplies the half before.  One barrier a k-step, as soon as the fragments of its second half
+// are read: then everybody has left its buffers.  After it a wavefront queues, by k mod 4 (k: the k-step in work),
+//     the tokens of k-step k + 2 and a quarter of a pair of W, which have landed at the next barrier, and then
+//     1, 3: half of the pair of W after next      0: the next metadata block, which have not to.
+// What bounds it: 52 KB of operands a k-step, which reach a compute unit at about 30 bytes a cycle in all variants tried (a ring of three
+// k-steps with smaller requests, 256 x 192 tiles with two k-steps of look-ahead 13 % slower), at the 1.46 GHz that the power management
+// leaves: 1.05 us a k-step, against 0.70 of products; and 11 us before and after the loop of every tile.
+template <int BM, int BN>
 struct Q8Smem {
-    static constexpr int A = BM * 128, B = BN * 128, M = BM * (DEEP ? 32 : 64);   // a pair of W, a k-step of tokens, a block of metadata
-    static constexpr int B_STAGES = DEEP ? 3 : 2;
-    static constexpr int B_OFF = 2 * A, M_OFF = B_OFF + B_STAGES * B, TOTAL = M_OFF + 2 * M;
+    static constexpr int A = BM * 128, B = BN * 128, M = BM * 64;         // a pair of W, a k-step of tokens, a block of metadata
+    static constexpr int B_OFF = 2 * A, M_OFF = B_OFF + 2 * B, TOTAL = M_OFF + 2 * M;
     static constexpr int OUT_PITCH = BM * 2 + 16;
-    static constexpr int A_LOADS = BM / 32, B_LOADS = BN / 32, M_LOADS = M / 4096;    // a wavefront's
-    static constexpr int QUARTER = A_LOADS / 4, HALF = A_LOADS / 2, PAIR = A_LOADS + M_LOADS;
-    // loads after the barrier of a k-step, k4 = k mod 4, and how many of them may still be under way at the next barrier
-    static constexpr int loads(int k4) { return DEEP ? B_LOADS + (k4 % 2 ? PAIR : 0) : B_LOADS + QUARTER + late(k4); }
-    static constexpr int late(int k4) { return DEEP ? loads(k4) : k4 % 2 ? HALF : k4 == 0 ? M_LOADS : 0; }
+    static constexpr int A_LOADS = BM / 32, B_LOADS = BN / 32, M_LOADS = BM / 64;    // a wavefront's
+    static constexpr int QUARTER = A_LOADS / 4, HALF = A_LOADS / 2;
+    // loads after the barrier of a k-step, k4 = k mod 4, and how many of them, the last, may still be under way at the next barrier
+    static constexpr int loads(int k4) { return B_LOADS + QUARTER + late(k4); }
+    static constexpr int late(int k4) { return k4 % 2 ? HALF : k4 == 0 ? M_LOADS : 0; }
     static_assert(TOTAL <= 160 * 1024 && BN * OUT_PITCH <= 160 * 1024, "fits");
+    static_assert(QUARTER * 4 == A_LOADS && B_LOADS > 0 && M_LOADS > 0, "whole loads");
 };
 
 // where a workgroup's slab of k-steps lies; slabs > 1: fp32 sums to part[slab][token][row]
 struct Q8Split { int steps, total; float* part; };
 
-template <int BM, int BN, int WM, bool DEEP, bool TAIL>
+template <int BM, int BN, int WM, bool TAIL>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, BM * BN > 128 * 128 ? 1 : 2)))
 q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
-    using S = Q8Smem<BM, BN, DEEP>;
+    using S = Q8Smem<BM, BN>;
     constexpr int WN = 4 / WM, MF = BM / (32 * WM), NF = BN / (32 * WN);
     extern __shared__ __align__(16) uint8_t smem[];
     int tm, tn;
@@ -190,9 +187,9 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         b_off[i] = r < toks ? r * b_pitch + 16 * ((lane & 7) ^ ((r >> 1) & 7)) : NOWHERE;
     }
 #pragma unroll
-    for (int i = 0; i < S::M_LOADS; ++i) {                      // 16 rows a load, or 32
-        const int r = DEEP ? (wave * S::M_LOADS + i) * 32 + (lane >> 1) : (wave * S::M_LOADS + i) * 16 + (lane >> 2);
-        m_off[i] = r < rows ? r * m_pitch + 16 * (DEEP ? (lane & 1) ^ ((r >> 3) & 1) : (lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
+    for (int i = 0; i < S::M_LOADS; ++i) {                      // 16 rows a load
+        const int r = (wave * S::M_LOADS + i) * 16 + (lane >> 2);
+        m_off[i] = r < rows ? r * m_pitch + 16 * ((lane & 3) ^ ((r >> 2) & 3)) : NOWHERE;
     }
     // TAIL: the contraction ends inside a k-step; pieces past a row's end read zeros.  Pieces of a row, as its rows give them (rows
     // 16 apart alike): of an even and of an odd load.
@@ -208,25 +205,25 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         if (TAIL) off |= piece[(wave * S::A_LOADS + i) & 1] * 32 >= K - (first + 2 * at) * KSTEP ? NOWHERE : 0;
         buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, off, first * 64 + at * 128);
     };
-    auto issue_b = [&](int k, int stage, int i) {
+    auto issue_b = [&](int k, int i) {
         const int at = first + min(k, steps - 1);
         uint32_t off = b_off[i];
         if (TAIL) off |= piece[(wave * S::B_LOADS + i) & 1] * 16 >= K - at * KSTEP ? NOWHERE : 0;
-        buffer_dma16(b_buf, smem + S::B_OFF + stage * S::B + (wave * S::B_LOADS + i) * 1024, off, at * KSTEP);
+        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, off, at * KSTEP);
     };
     auto issue_m = [&](int block, int i) {
         buffer_dma16(m_buf, smem + S::M_OFF + (block & 1) * S::M + (wave * S::M_LOADS + i) * 1024, m_off[i],
-                     first * 16 + (DEEP ? min(block, (steps - 1) >> 1) * 32 : min(block, (steps - 1) >> 2) * 64));
+                     first * 16 + min(block, (steps - 1) >> 2) * 64);
     };
 
     // reader lanes
-    const int a_row = wm * (BM / WM) + l32, b_row = wn * (BN / WN) + l32, sw = (l32 >> 1) & 7, m_sw = DEEP ? (l32 >> 3) & 1 : (l32 >> 2) & 3;
-    const int a_rd = a_row * 128, b_rd = S::B_OFF + b_row * 128, m_rd = S::M_OFF + a_row * (DEEP ? 32 : 64) + lq * 4;
+    const int a_row = wm * (BM / WM) + l32, b_row = wn * (BN / WN) + l32, sw = (l32 >> 1) & 7, m_sw = (l32 >> 2) & 3;
+    const int a_rd = a_row * 128, b_rd = S::B_OFF + b_row * 128, m_rd = S::M_OFF + a_row * 64 + lq * 4;
     struct Reader { const uint8_t *a, *b[2], *e; };
-    auto reader = [&](int k, int stage, int h) {                // half h of k-step k, its tokens in `stage`
-        const uint8_t *const pa = smem + ((k >> 1) & 1) * S::A + a_rd, *const pb = smem + stage * S::B + b_rd;
+    auto reader = [&](int k, int h) {                           // half h of k-step k
+        const uint8_t *const pa = smem + ((k >> 1) & 1) * S::A + a_rd, *const pb = smem + (k & 1) * S::B + b_rd;
         return Reader{pa + (((4 * (k & 1) + 2 * h + lq) ^ sw) * 16), {pb + (((4 * h + lq) ^ sw) * 16), pb + (((4 * h + 2 + lq) ^ sw) * 16)},
-                      smem + m_rd + (DEEP ? ((k >> 1) & 1) * S::M + (((k & 1) ^ m_sw) * 16) : ((k >> 2) & 1) * S::M + (((k & 3) ^ m_sw) * 16)) + 8 * h};
+                      smem + m_rd + ((k >> 2) & 1) * S::M + (((k & 3) ^ m_sw) * 16) + 8 * h};
     };
     struct Frags { AQ a[MF]; BQ b[NF]; uint32_t e[MF]; };
     constexpr int READS = 2 * (MF + NF);
@@ -235,7 +232,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         if (i == 0 || i > 2 * NF + 1) {
             const int q = i == 0 ? 0 : (i - 2 * NF) / 2;
             if (i % 2 == 0) f.a[q].u = *(const u32x4*)(r.a + q * 32 * 128);
-            else f.e[q] = *(const uint32_t*)(r.e + q * 32 * (DEEP ? 32 : 64));
+            else f.e[q] = *(const uint32_t*)(r.e + q * 32 * 64);
         } else if (i == 1) {
             f.e[0] = *(const uint32_t*)r.e;
         } else {
@@ -249,13 +246,13 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         for (int j = 0; j < NF; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    // Product i of a half.  With 12 or 16 fragments the accumulators belong into the accumulation registers; left to itself the compiler keeps
+    // Product i of a half.  With 16 fragments the accumulators fill all accumulation registers; left to itself the compiler keeps
     // some of them in the others and moves them back and forth, two hundred moves a k-step.  (The instruction is written out for
     // that; its wait states: two after a write of an operand by a vector instruction, here in front, and those of a read of the
     // result by one, after the loop.)
     auto multiply = [&](const Frags& f, int i) {
         f32x16& c = acc[i / NF][i % NF];
-        if constexpr (MF * NF >= 12) {
+        if constexpr (MF * NF == 16) {
 #ifdef __HIP_DEVICE_COMPILE__
             asm volatile("s_nop 1\n\tv_smfmac_f32_32x32x64_fp8_fp8 %0, %1, %2, %3" : "+a"(c) : "v"(f.a[i / NF].v), "v"(f.b[i % NF].v), "v"(f.e[i / NF]));
 #endif
@@ -270,20 +267,12 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     };
 
     constexpr int QUARTER = S::QUARTER, HALF = S::HALF;
-    static_assert(QUARTER * 4 == S::A_LOADS && S::B_LOADS > 0 && S::M_LOADS > 0, "whole loads");
-    // load u after the barrier of k-step k, k4 = k mod 4; `stage`: of its tokens
-    constexpr int PAIR = S::PAIR;
-    auto load = [&](int k, int k4, int stage, int u) {
-        if (DEEP) {
-            if (k4 % 2 && u < S::A_LOADS) issue_a((k >> 1) + 2, u);
-            else if (k4 % 2 && u < PAIR) issue_m((k >> 1) + 2, u - S::A_LOADS);
-            else issue_b(k + 3, stage, u - (k4 % 2 ? PAIR : 0));
-        } else {
-            if (u < S::B_LOADS) issue_b(k + 2, stage, u);
-            else if (k4 % 2 == 0 && u < S::B_LOADS + QUARTER) issue_a((k >> 1) + 1, QUARTER + HALF + u - S::B_LOADS);
-            else if (k4 % 2 == 0) issue_m((k >> 2) + 1, u - S::B_LOADS - QUARTER);
-            else issue_a((k >> 1) + 2, u - S::B_LOADS);
-        }
+    // load u after the barrier of k-step k, k4 = k mod 4
+    auto load = [&](int k, int k4, int u) {
+        if (u < S::B_LOADS) issue_b(k + 2, u);
+        else if (k4 % 2 == 0 && u < S::B_LOADS + QUARTER) issue_a((k >> 1) + 1, QUARTER + HALF + u - S::B_LOADS);
+        else if (k4 % 2 == 0) issue_m((k >> 2) + 1, u - S::B_LOADS - QUARTER);
+        else issue_a((k >> 1) + 2, u - S::B_LOADS);
     };
     // what the k-steps before the first would have queued
 #pragma unroll
@@ -291,32 +280,23 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
 #pragma unroll
     for (int i = 0; i < S::A_LOADS; ++i) issue_a(0, i);
 #pragma unroll
-    for (int i = 0; i < S::B_LOADS; ++i) issue_b(0, 0, i);
-    if (DEEP) {
+    for (int i = 0; i < S::B_LOADS; ++i) issue_b(0, i);
 #pragma unroll
-        for (int i = 0; i < S::B_LOADS; ++i) issue_b(1, 1, i);
-#pragma unroll
-        for (int i = 0; i < PAIR + S::B_LOADS; ++i) load(-1, 3, 2, i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < S::B_LOADS + QUARTER + HALF; ++i) load(-1, 3, 1, i);
-    }
-    WAIT_HERE(waitcnt_imm(DEEP ? 2 * S::B_LOADS + PAIR : S::B_LOADS + QUARTER + HALF, 15));
+    for (int i = 0; i < S::loads(3); ++i) load(-1, 3, i);
+    WAIT_HERE(waitcnt_imm(S::loads(3), 15));
     wg_barrier();
     Frags f0, f1;
     {
-        const Reader r = reader(0, 0, 0);
+        const Reader r = reader(0, 0);
 #pragma unroll
         for (int i = 0; i < READS; ++i) read(f0, r, i);
     }
     // the barrier comes as soon as the fragments of the second half are read
     constexpr int BARRIER = PRODUCTS > 1 ? PRODUCTS * 5 / 8 : 1;
-    int stage = 0;
     auto step = [&](int k, auto mod4) {
         constexpr int K4 = decltype(mod4)::value;
         constexpr int MINE = S::loads(K4), AT_ONCE = PRODUCTS - BARRIER < MINE ? PRODUCTS - BARRIER : MINE;   // one a product, then evenly
-        const int next = stage == S::B_STAGES - 1 ? 0 : stage + 1;
-        const Reader r1 = reader(k, stage, 1);
+        const Reader r1 = reader(k, 1);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
             if (i == BARRIER) {
@@ -326,21 +306,20 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
             __builtin_amdgcn_sched_barrier(0);
             multiply(f0, i);
             if (i < BARRIER) share(i, READS, BARRIER > 2 ? BARRIER - 2 : 1, [&](int u) { read(f1, r1, u); });
-            else if (i - BARRIER < AT_ONCE) load(k, K4, stage, i - BARRIER);
+            else if (i - BARRIER < AT_ONCE) load(k, K4, i - BARRIER);
         }
         if (BARRIER == PRODUCTS) {
             WAIT_HERE(waitcnt_imm(S::late((K4 + 3) % 4), 0));
             wg_barrier();
         }
-        const Reader r0 = reader(k + 1, next, 0);
+        const Reader r0 = reader(k + 1, 0);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             multiply(f1, i);
             share(i, READS, PRODUCTS - PRODUCTS / 4, [&](int u) { read(f0, r0, u); });
-            share(i, MINE - AT_ONCE, PRODUCTS, [&](int u) { load(k, K4, stage, AT_ONCE + u); });
+            share(i, MINE - AT_ONCE, PRODUCTS, [&](int u) { load(k, K4, AT_ONCE + u); });
         }
-        stage = next;
     };
     int k = 0;
     for (; k + 3 < steps; k += 4) {
@@ -354,7 +333,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     if (k + 2 < steps) step(k + 2, std::integral_constant<int, 2>());
     WAIT_HERE(waitcnt_imm(0, 0));                               // the look-ahead loads
 #ifdef __HIP_DEVICE_COMPILE__
-    if constexpr (MF * NF >= 12) {
+    if constexpr (MF * NF == 16) {
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
         for (int i = 0; i < MF; ++i)
@@ -390,33 +369,46 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
         }
         __syncthreads();
     }
+    // (with and without that term apart: a choice at every value cost 4 us of every tile)
+    float xs[NF];
 #pragma unroll
-    for (int j = 0; j < NF; ++j) {
-        const int64_t tok = n0 + t_base + 32 * j;
-        const float xs = p.xs[tok < p.n ? tok : p.n - 1];
+    for (int j = 0; j < NF; ++j) xs[j] = p.xs[min(n0 + t_base + 32 * j, p.n - 1)];
+    auto scale = [&](auto with_add) {
+        constexpr bool ADD = decltype(with_add)::value;
 #pragma unroll
         for (int i = 0; i < MF; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t f = m0 + f_base + 32 * i + 8 * q;
                 const f32x4 ws = *(const f32x4*)(p.as + (f < p.m ? f : 0));
-                u32x2* const at = (u32x2*)(smem + (t_base + 32 * j) * S::OUT_PITCH + (f_base + 32 * i + 8 * q) * 2);
-                const u32x2 add = p.add ? *at : (u32x2){0, 0};
-                union { __bf16 h[4]; u32x2 u; } o;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
-                    const float v = acc[i][j][4 * q + r] * xs;
-                    o.h[r] = (__bf16)(p.add ? fmaf(v, ws[r], t) : v * ws[r]);
+                for (int j = 0; j < NF; ++j) {
+                    u32x2* const at = (u32x2*)(smem + (t_base + 32 * j) * S::OUT_PITCH + (f_base + 32 * i + 8 * q) * 2);
+                    const u32x2 add = ADD ? *at : (u32x2){0, 0};
+                    union { __bf16 h[4]; u32x2 u; } o;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
+                        const float v = acc[i][j][4 * q + r] * xs[j];
+                        o.h[r] = (__bf16)(ADD ? fmaf(v, ws[r], t) : v * ws[r]);
+                    }
+                    *at = o.u;
                 }
-                *at = o.u;
             }
-    }
+    };
+    if (p.add) scale(std::true_type());
+    else scale(std::false_type());
     __syncthreads();
-#pragma unroll 4
+    // a Y that the dies' second-level caches would not hold goes past them (777 tokens, 20480 x 5120 110 -> 105 us)
+    const bool stream = p.n * p.m > ((int64_t)8 << 20);
+#pragma unroll 8
     for (int u = 0; u < PER; ++u) {
         const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
-        if (tok < toks && f < rows) *(u32x4*)(p.y + (n0 + tok) * p.m + m0 + f) = *(const u32x4*)(smem + tok * S::OUT_PITCH + f * 2);
+        if (tok >= toks || f >= rows) continue;
+        u32x4* const to = (u32x4*)(p.y + (n0 + tok) * p.m + m0 + f);
+        const u32x4 v = *(const u32x4*)(smem + tok * S::OUT_PITCH + f * 2);
+        if (stream) __builtin_nontemporal_store(v, to);
+        else *to = v;
     }
 }
 
@@ -590,19 +582,19 @@ bool tile_fits(int64_t n, int64_t m, int64_t K) {
     return K % 64 == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < ((int64_t)1 << 23);
 }
 
-template <int BM, int BN, int WM, bool DEEP, bool TAIL>
+template <int BM, int BN, int WM, bool TAIL>
 hipError_t launch_tiles_of(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
-    using S = Q8Smem<BM, BN, DEEP>;
+    using S = Q8Smem<BM, BN>;
     constexpr int LDS = S::TOTAL > BN * S::OUT_PITCH ? S::TOTAL : BN * S::OUT_PITCH;
-    const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN, WM, DEEP, TAIL>>(LDS);
+    const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN, WM, TAIL>>(LDS);
     if (e != hipSuccess) return e;
     const int tiles_m = (int)((p.m + BM - 1) / BM), tiles_n = (int)((p.n + BN - 1) / BN);
-    q8_tile_kernel<BM, BN, WM, DEEP, TAIL><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
+    q8_tile_kernel<BM, BN, WM, TAIL><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
     return hipGetLastError();
 }
-template <int BM, int BN, int WM, bool DEEP = false>
+template <int BM, int BN, int WM>
 hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
-    return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, DEEP, false>(p, split, slabs, s) : launch_tiles_of<BM, BN, WM, DEEP, true>(p, split, slabs, s);
+    return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, false>(p, split, slabs, s) : launch_tiles_of<BM, BN, WM, true>(p, split, slabs, s);
 }
 
 // below it the general kernel's one launch is faster (us, general / copies and tiles: 200 tokens, 2056 x 2056 15.8 / 17; 600, 1000 x 1000
@@ -719,8 +711,7 @@ hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const ui
     const Q8Split split = {plan.steps, plan.total, part};
     hipError_t e;
     if (plan.stream) e = plan.bn == 4 ? launch_stream<4>(p, split, plan.slabs, s) : launch_stream<8>(p, split, plan.slabs, s);
-    else if (plan.bm == 256 && plan.bn == 256) e = launch_tiles<256, 256, 2>(p, split, plan.slabs, s);
-    else if (plan.bm == 256) e = launch_tiles<256, 192, 2, true>(p, split, plan.slabs, s);
+    else if (plan.bm == 256) e = launch_tiles<256, 256, 2>(p, split, plan.slabs, s);
     else if (plan.bn == 128) e = launch_tiles<128, 128, 2>(p, split, plan.slabs, s);
     else if (plan.bn == 64) e = launch_tiles<128, 64, 2>(p, split, plan.slabs, s);
     else e = launch_tiles<128, 32, 4>(p, split, plan.slabs, s);

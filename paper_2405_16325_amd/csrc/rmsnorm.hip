@@ -196,8 +196,8 @@ struct NormBwd {
     const bf16_t* dh;                          // or null
     int64_t b;
     int d;
-    bf16_t* dx;
-    float* part;                               // fp32[groups][d]: each workgroup's share of dw
+    bf16_t *dx, *dw;
+    float* part;                               // fp32[groups][d]: each workgroup's share of dw; one workgroup writes dw itself
 };
 
 // Workgroup g takes rows g R .. g R + R - 1, then those `groups` R later, and keeps its share of dw in registers; the R row
@@ -298,6 +298,10 @@ __global__ void __launch_bounds__(bwd_threads(VPT)) rmsnorm_bwd_kernel(NormBwd a
         for (int s = 1; s < slots; ++s)
 #pragma unroll
             for (int k = 0; k < 8; ++k) dw[p].v[k] += sums[(size_t)(s - 1) * a.d + 8 * i + k];
+        if (gridDim.x == 1) {
+            *(u32x4*)(a.dw + 8 * (size_t)i) = pack_bf16(dw[p]);
+            continue;
+        }
         f32x4* const o = (f32x4*)(a.part + (size_t)blockIdx.x * a.d + 8 * (size_t)i);
         o[0] = (f32x4){dw[p].v[0], dw[p].v[1], dw[p].v[2], dw[p].v[3]};
         o[1] = (f32x4){dw[p].v[4], dw[p].v[5], dw[p].v[6], dw[p].v[7]};
@@ -397,10 +401,12 @@ RowShape bwd_shape(int64_t b, int64_t d) {
     return row_shape(pieces, pieces <= 2 * 512 ? 2 : pieces <= 3 * 512 ? 3 : pieces <= 4 * 512 ? 4 : 6);
 }
 
-// workgroups of the gradient: as many as are resident together (eight wavefronts on a compute unit), so that each makes one share of dw
+// workgroups of the gradient: as many as are resident together (eight wavefronts on a compute unit), so that each makes one share of
+// dw; for a few rows one, which saves the second launch
 int bwd_groups(int64_t b, int64_t d) {
     const RowShape s = bwd_shape(b, d);
     const int64_t turns = s.vpt == 0 ? b : (b + s.slots() - 1) / s.slots();
+    if (s.vpt != 0 && turns <= 4) return 1;
     const int64_t most = RESIDENT * (s.threads >= 8 * 64 ? 1 : 8 * 64 / s.threads);
     return (int)(turns < most ? turns : most);
 }
@@ -431,7 +437,7 @@ size_t rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d) { return (size_t)bwd_gr
 
 hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w, const float* rstd, const bf16_t* dh, int64_t b,
                               int64_t d, bf16_t* dx, bf16_t* dw, float* part, hipStream_t s) {
-    const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, part};
+    const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, dw, part};
     const RowShape rs = bwd_shape(b, d);
     const int groups = bwd_groups(b, d);
     if (rs.vpt == 0) {
@@ -455,6 +461,7 @@ hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w
         else if (stream) BWD(64, 6, true);
         else BWD(64, 6);
 #undef BWD
+        if (groups == 1) return hipGetLastError();
     }
     rmsnorm_dw_kernel<<<(unsigned)((d + 31) / 32), 1024, 0, s>>>(part, groups, (int)d, dw);
     return hipGetLastError();

@@ -32,6 +32,7 @@ struct Q8Product {
     int64_t m, K;
     const bf16_t* add;         // or null
     bf16_t* y;
+    int64_t ldy;               // of y and add: m, or that of the whole of which this is a part
 };
 
 // four rows' sums of a token to Y: scales, the added term, one rounding
@@ -39,14 +40,14 @@ __device__ __forceinline__ void store_quad(const Q8Product& p, int64_t tok, int6
     const f32x4 ws = *(const f32x4*)(p.as + f);
     const float xs = p.xs[tok];
     u32x2 add = {0, 0};
-    if (p.add) add = *(const u32x2*)(p.add + tok * p.m + f);
+    if (p.add) add = *(const u32x2*)(p.add + tok * p.ldy + f);
     union { __bf16 h[4]; u32x2 u; } o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const float t = __uint_as_float((r & 1) ? add[r >> 1] & 0xFFFF0000u : add[r >> 1] << 16);
         o.h[r] = (__bf16)(p.add ? fmaf(s[r] * xs, ws[r], t) : s[r] * xs * ws[r]);
     }
-    *(u32x2*)(p.y + tok * p.m + f) = o.u;
+    *(u32x2*)(p.y + tok * p.ldy + f) = o.u;
 }
 
 constexpr int KSTEP = 128;
@@ -365,7 +366,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
-            if (tok < toks && f < rows) *(u32x4*)(smem + tok * S::OUT_PITCH + f * 2) = *(const u32x4*)(p.add + (n0 + tok) * p.m + m0 + f);
+            if (tok < toks && f < rows) *(u32x4*)(smem + tok * S::OUT_PITCH + f * 2) = *(const u32x4*)(p.add + (n0 + tok) * p.ldy + m0 + f);
         }
         __syncthreads();
     }
@@ -400,12 +401,12 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     else scale(std::false_type());
     __syncthreads();
     // a Y that the dies' second-level caches would not hold goes past them (777 tokens, 20480 x 5120 110 -> 105 us)
-    const bool stream = p.n * p.m > ((int64_t)8 << 20);
+    const bool stream = p.n * p.ldy > ((int64_t)8 << 20);
 #pragma unroll 8
     for (int u = 0; u < PER; ++u) {
         const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
         if (tok >= toks || f >= rows) continue;
-        u32x4* const to = (u32x4*)(p.y + (n0 + tok) * p.m + m0 + f);
+        u32x4* const to = (u32x4*)(p.y + (n0 + tok) * p.ldy + m0 + f);
         const u32x4 v = *(const u32x4*)(smem + tok * S::OUT_PITCH + f * 2);
         if (stream) __builtin_nontemporal_store(v, to);
         else *to = v;
@@ -615,10 +616,11 @@ hipError_t launch_stream(const Q8Product& p, const Q8Split& split, int slabs, hi
 
 // kernel of a product: stream (bn: tokens), tiles of bm x bn, or neither (the general one); the contraction in `slabs`
 // slabs of `steps` k-steps (stream: stretches)
-struct Q8Plan { bool stream; int bm, bn, slabs, steps, total; };
+// rows0: the first rows, on 256 x 256 tiles in whole rounds of the chip, where the others go to bm x bn
+struct Q8Plan { bool stream; int bm, bn, slabs, steps, total; int64_t rows0; };
 Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
     if (stream_fits(n, m, K)) {
-        Q8Plan plan = {true, 32, n <= 4 ? 4 : 8, 1, 0, (int)((K + 255) / 256)};
+        Q8Plan plan = {true, 32, n <= 4 ? 4 : 8, 1, 0, (int)((K + 255) / 256), 0};
         plan.steps = plan.total;
         const int64_t groups = (m + 31) / 32;
         int slabs = room ? (int)min((int64_t)STREAM_GROUPS / groups, (int64_t)plan.total / (2 * STREAM_WAVES)) : 1;
@@ -628,28 +630,45 @@ Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
         }
         return plan;
     }
-    if (!tile_fits(n, m, K)) return {false, 0, 0, 1, 0, 0};
+    if (!tile_fits(n, m, K)) return {false, 0, 0, 1, 0, 0, 0};
     const int total = (int)((K + KSTEP - 1) / KSTEP);
-    auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
+    auto tiles = [&](int bm, int bn, int64_t rows) { return (rows + bm - 1) / bm * ((n + bn - 1) / bn); };
     // Tile by the time of a k-step of the whole grid, us.  256 x 256 goes by whole rounds of the chip; of the others two are on a
     // compute unit, and rounds overlap.  (us, 256 x 256 / 128 x 128 / 128 x 64: 777 tokens, 20480 x 5120 105 / 95 / 120; 2048, 5120 x 5120
     // 50 / 58 / 68; 512, 5120 x 5120 46 / 26 / 25; 256, 9216 x 9216 67 / 41 / 37; 1200, 14336 x 4096 80 / 71 / 92; 8192, 36864 x 9216
     // 1550 / 2250 / 2930)
-    auto shared = [&](int bn, double one, double two) {        // one tile on a compute unit, 512 tiles on the chip
-        const int64_t t = tiles(128, bn);
+    auto shared = [&](int bn, double one, double two, int64_t rows) {        // one tile on a compute unit, 512 tiles on the chip
+        const int64_t t = tiles(128, bn, rows);
         const double all = two * (double)t / 512.0;
         return t <= RESIDENT ? one : all > 0.75 * two ? all : 0.75 * two;
     };
-    Q8Plan plan = {false, 128, 32, 1, total, total};
-    double best = shared(32, 0.40, 0.50);
-    const double t64 = shared(64, 0.42, 0.67), t128 = shared(128, 0.60, 1.08), t256 = 1.24 * (double)((tiles(256, 256) + RESIDENT - 1) / RESIDENT);
-    if (n > 32 && t64 < best) best = t64, plan.bn = 64;
-    if (n > 64 && t128 < best) best = t128, plan.bn = 128;
-    if (n > 128 && t256 < best) plan.bm = plan.bn = 256;
+    auto smaller = [&](int64_t rows, int& bn) {                  // the best tile of 128 rows
+        double best = shared(bn = 32, 0.40, 0.50, rows);
+        const double t64 = shared(64, 0.42, 0.67, rows), t128 = shared(128, 0.60, 1.08, rows);
+        if (n > 32 && t64 < best) best = t64, bn = 64;
+        if (n > 64 && t128 < best) best = t128, bn = 128;
+        return best;
+    };
+    Q8Plan plan = {false, 128, 32, 1, total, total, 0};
+    double best = smaller(m, plan.bn);
+    const int64_t t256 = tiles(256, 256, m), rounds = t256 / RESIDENT;
+    if (n > 128 && 1.24 * (double)((t256 + RESIDENT - 1) / RESIDENT) < best) {
+        best = 1.24 * (double)((t256 + RESIDENT - 1) / RESIDENT);
+        plan.bm = plan.bn = 256;
+    }
+    // Or whole rounds of 256 x 256 and the rows that are left on smaller tiles, in a second launch.  (us, one tile / both: 777 tokens, 20480 x 5120, 320
+    // tiles of 256 x 256: 110 / 103; 4096, 5120 x 5120, 320 tiles: 92 / 81; 6000, 9216 x 9216, 864: 333 / 327.  The leftover tiles of the first
+    // in four slabs each, whose 64 MB of sums are written and read once more: 124.)
+    const int64_t rows0 = rounds * RESIDENT / ((n + 255) / 256) * 256;
+    if (n > 128 && rows0 > 0 && rows0 < m) {
+        int bn;
+        const double t = 1.24 * (double)rounds + smaller(m - rows0, bn) + 5.0 / total;
+        if (t < best) return {false, 128, bn, 1, total, total, rows0};
+    }
     // A slab less than STEPS_WHOLE k-steps long is not worth a second launch, and more than two workgroups a compute unit give nothing
     // (us, whole / slabs: 128 tokens, 5120 x 5120 16 / 18 with 6; 300, 4096 x 4096 15 / 20 with 2; 60, 9216 x 9216 34 / 20 with 7;
     // 60, 2560 x 10240 21 / 14 with 12, 20 with 20; 300, 9216 x 36864 145 / 100 with 2)
-    const int64_t t = tiles(plan.bm, plan.bn);
+    const int64_t t = tiles(plan.bm, plan.bn, m);
     if (room && total > STEPS_WHOLE) {
         const int slabs = (int)min(2 * (int64_t)RESIDENT / t, (int64_t)(total + STEPS_SLAB - 1) / STEPS_SLAB);
         if (slabs > 1) {
@@ -686,7 +705,7 @@ size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K) {
 
 hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,
                           int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* workspace_or_null, hipStream_t s) {
-    Q8Product p = {x, xs, n, a, am, as, m, K, add, y};
+    Q8Product p = {x, xs, n, a, am, as, m, K, add, y, m};
     uint8_t* room = (uint8_t*)workspace_or_null;
     const Q8Pad pad = room ? q8_pad(n, m, K) : Q8Pad{0, 0, 0, 0};
     if (pad.Kp) {
@@ -710,6 +729,18 @@ hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const ui
     float* const part = plan.slabs > 1 ? (float*)room : nullptr;
     const Q8Split split = {plan.steps, plan.total, part};
     hipError_t e;
+    if (plan.rows0 > 0) {
+        Q8Product first = p;
+        first.m = plan.rows0;
+        e = launch_tiles<256, 256, 2>(first, split, 1, s);
+        if (e != hipSuccess) return e;
+        p.a += plan.rows0 * (p.K / 2);
+        p.am += plan.rows0 * (p.K / 8);
+        p.as += plan.rows0;
+        p.y += plan.rows0;
+        if (p.add) p.add += plan.rows0;
+        p.m -= plan.rows0;
+    }
     if (plan.stream) e = plan.bn == 4 ? launch_stream<4>(p, split, plan.slabs, s) : launch_stream<8>(p, split, plan.slabs, s);
     else if (plan.bm == 256) e = launch_tiles<256, 256, 2>(p, split, plan.slabs, s);
     else if (plan.bn == 128) e = launch_tiles<128, 128, 2>(p, split, plan.slabs, s);

@@ -111,7 +111,8 @@ def test_a_token_of_zeros_and_one_that_is_not_finite(b):
     check(y[rest], q[rest], xs[rest], dev, meta)
 
 
-@pytest.mark.parametrize("b,d_out,d_in", [(1, 36864, 9216), (16, 9216, 36864), (300, 2560, 10240), (2048, 5120, 5120)])
+@pytest.mark.parametrize("b,d_out,d_in", [(1, 36864, 9216), (16, 9216, 36864), (300, 2560, 10240), (2048, 5120, 5120), (777, 20480, 5120),
+                                           (1100, 14080, 4160)])
 def test_layers_at_full_size_against_a_library_product(b, d_out, d_in):
     """Every element against an fp32 product of the same values; the bound's middle term from the rows' norms, which is what
     the terms' magnitudes add up to at most."""

@@ -54,15 +54,17 @@ __device__ __forceinline__ const Chunk* chunks_of(const void* table, int64_t cou
 // everywhere, 32 bytes a lane in two loads, streaming past the caches made 157 M elements with masters 20 % slower, not faster).
 // Values are kept as they are in memory until all of a lane's loads are on their way.
 template <int W> struct Vec { float v[W]; };
+// The tensors' addresses come out of memory, where the compiler cannot see that they are global: said here.
+#define GLOBAL __attribute__((address_space(1)))
 template <int BITS, int W> struct Raw { uint32_t u[BITS * W / 32]; };
 
 template <bool STREAM, int DWORDS>
 __device__ __forceinline__ void load_dwords(const void* p, uint32_t (&u)[DWORDS]) {
     typedef uint32_t V __attribute__((ext_vector_type(DWORDS == 1 ? 2 : DWORDS)));
     if constexpr (DWORDS == 1) {
-        u[0] = STREAM ? __builtin_nontemporal_load((const uint32_t*)p) : *(const uint32_t*)p;
+        u[0] = STREAM ? __builtin_nontemporal_load((const GLOBAL uint32_t*)p) : *(const GLOBAL uint32_t*)p;
     } else {
-        const V x = STREAM ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
+        const V x = STREAM ? __builtin_nontemporal_load((const GLOBAL V*)p) : *(const GLOBAL V*)p;
 #pragma unroll
         for (int k = 0; k < DWORDS; ++k) u[k] = x[k];
     }
@@ -71,14 +73,14 @@ template <bool STREAM, int DWORDS>
 __device__ __forceinline__ void store_dwords(void* p, const uint32_t (&u)[DWORDS]) {
     typedef uint32_t V __attribute__((ext_vector_type(DWORDS == 1 ? 2 : DWORDS)));
     if constexpr (DWORDS == 1) {
-        if (STREAM) __builtin_nontemporal_store(u[0], (uint32_t*)p);
-        else *(uint32_t*)p = u[0];
+        if (STREAM) __builtin_nontemporal_store(u[0], (GLOBAL uint32_t*)p);
+        else *(GLOBAL uint32_t*)p = u[0];
     } else {
         V x;
 #pragma unroll
         for (int k = 0; k < DWORDS; ++k) x[k] = u[k];
-        if (STREAM) __builtin_nontemporal_store(x, (V*)p);
-        else *(V*)p = x;
+        if (STREAM) __builtin_nontemporal_store(x, (GLOBAL V*)p);
+        else *(GLOBAL V*)p = x;
     }
 }
 template <int BITS, int W, bool FULL, bool STREAM>
@@ -94,7 +96,8 @@ __device__ __forceinline__ Raw<BITS, W> load(const void* base, int64_t i, int li
 #pragma unroll
         for (int k = 0; k < W; ++k)
             if (k < live)
-                o.u[k / PER] |= (BITS == 32 ? *(const uint32_t*)(p + 4 * k) : BITS == 16 ? *(const uint16_t*)(p + 2 * k) : p[k]) << (BITS % 32 * (k % PER));
+                o.u[k / PER] |= (BITS == 32 ? *(const GLOBAL uint32_t*)(p + 4 * k) : BITS == 16 ? *(const GLOBAL uint16_t*)(p + 2 * k)
+                                                                                    : *(const GLOBAL uint8_t*)(p + k)) << (BITS % 32 * (k % PER));
     }
     return o;
 }
@@ -109,9 +112,9 @@ __device__ __forceinline__ void store(void* base, int64_t i, int live, const Raw
         for (int k = 0; k < W; ++k)
             if (k < live) {
                 const uint32_t v = x.u[k / PER] >> (BITS % 32 * (k % PER));
-                if (BITS == 32) *(uint32_t*)(p + 4 * k) = v;
-                else if (BITS == 16) *(uint16_t*)(p + 2 * k) = (uint16_t)v;
-                else p[k] = (uint8_t)v;
+                if (BITS == 32) *(GLOBAL uint32_t*)(p + 4 * k) = v;
+                else if (BITS == 16) *(GLOBAL uint16_t*)(p + 2 * k) = (uint16_t)v;
+                else *(GLOBAL uint8_t*)(p + k) = (uint8_t)v;
             }
     }
 }
@@ -161,11 +164,11 @@ struct StepArgs {
 // The W values of each of 128 / W lanes to codes, with the block's scale to *scale.  The conversion takes a value to one of its e4m3
 // neighbours: up where the part of the way from the lower one, in magnitude, plus u (its upper 20 bits, as a fraction) reaches 1.
 template <bool ROOT, int W>
-__device__ __forceinline__ Raw<8, W> to_codes(const Vec<W>& x, uint32_t u, float* scale, bool writes) {
+__device__ __forceinline__ Raw<8, W> to_codes(const Vec<W>& x, uint32_t u, GLOBAL float* scale, bool writes) {
 #pragma clang fp contract(off)
     float top = 0.0f;
 #pragma unroll
-    for (int k = 0; k < W; ++k) top = max_abs(top, x.v[k]);
+    for (int k = 0; k < W; ++k) top = ROOT ? __uint_as_float(max(__float_as_uint(top), __float_as_uint(x.v[k]))) : max_abs(top, x.v[k]);
     const Q8Scale s = q8_scale(lanes_max_abs<Q8_BLOCK / W>(top));
     if (writes) *scale = s.scale;
     // a root below the smallest code becomes that code, whatever u is
@@ -182,6 +185,29 @@ __device__ __forceinline__ Raw<8, W> to_codes(const Vec<W>& x, uint32_t u, float
         c = __builtin_amdgcn_cvt_sr_fp8_f32(held(x.v[k + 2]), (int)(u + (uint32_t)(k + 2) * DITHER_INDEX), c, 2);
         c = __builtin_amdgcn_cvt_sr_fp8_f32(held(x.v[k + 3]), (int)(u + (uint32_t)(k + 3) * DITHER_INDEX), c, 3);
         o.u[k / 4] = s.scale < INFINITY ? (uint32_t)c : 0x7F7F7F7Fu;    // else the block holds an infinity or NaN
+    }
+    return o;
+}
+
+// Square roots, exactly rounded: the hardware's is off by one unit at most, and the residuals of its neighbours tell.  (Zeros, infinities
+// and NaN stay as they are: their residuals are no numbers, or zero.)  Below 2^-96 residuals would vanish: the compiler's form for all then.
+template <int W>
+__device__ __forceinline__ Vec<W> roots(const Vec<W>& x) {
+    Vec<W> o;
+    bool tiny = false;
+#pragma unroll
+    for (int k = 0; k < W; ++k) tiny |= x.v[k] < 0x1p-96f && x.v[k] != 0.0f;
+    if (__builtin_expect(__any(tiny), 0)) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) o.v[k] = sqrtf(x.v[k]);
+        return o;
+    }
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        const float s = __builtin_amdgcn_sqrtf(x.v[k]);
+        const float down = __uint_as_float(__float_as_uint(s) - 1), up = __uint_as_float(__float_as_uint(s) + 1);
+        const float below = fmaf(-down, s, x.v[k]), above = fmaf(-up, s, x.v[k]);
+        o.v[k] = above > 0.0f ? up : below <= 0.0f ? down : s;
     }
     return o;
 }
@@ -213,8 +239,8 @@ __device__ __forceinline__ void adamw_chunk(const StepArgs& a, const slope_adamw
         mraw[t] = load<S, W, FULL, STREAM>(tensor.m, i, live);
         vraw[t] = load<S, W, FULL, STREAM>(tensor.v, i, live);
         if (STATE8) {
-            ms[t] = tensor.m_scale[i / Q8_BLOCK];
-            vs[t] = tensor.v_scale[i / Q8_BLOCK];
+            ms[t] = ((const GLOBAL float*)tensor.m_scale)[i / Q8_BLOCK];
+            vs[t] = ((const GLOBAL float*)tensor.v_scale)[i / Q8_BLOCK];
         }
     }
 #pragma unroll
@@ -234,15 +260,17 @@ __device__ __forceinline__ void adamw_chunk(const StepArgs& a, const slope_adamw
             const float x = g.v[k] * c.coef;
             m.v[k] = m.v[k] * a.b1 + x * a.c1;
             v.v[k] = v.v[k] * a.b2 + x * x * a.c2;
-            r.v[k] = sqrtf(v.v[k]);
-            p.v[k] = p.v[k] * c.keep - c.rate * (m.v[k] * __builtin_amdgcn_rcpf(r.v[k] * c.inv_root2 + a.eps));
         }
+        r = roots(v);
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+            p.v[k] = fmaf(-c.rate, m.v[k] * __builtin_amdgcn_rcpf(fmaf(r.v[k], c.inv_root2, a.eps)), p.v[k] * c.keep);
         if constexpr (MASTER) store<32, W, FULL, STREAM>(tensor.master, i, live, raw_f32(p));
         if (!MASTER || tensor.param) store<16, W, FULL, STREAM>(tensor.param, i, live, raw_bf16(p));
         if constexpr (STATE8) {
             const uint32_t u = (uint32_t)i * DITHER_INDEX + (uint32_t)(int)c.t * DITHER_STEP;
-            store<8, W, FULL, STREAM>(tensor.m, i, live, to_codes<false>(m, u, tensor.m_scale + i / Q8_BLOCK, lane == 0));
-            store<8, W, FULL, STREAM>(tensor.v, i, live, to_codes<true>(r, u + 0x80000000u, tensor.v_scale + i / Q8_BLOCK, lane == 0));
+            store<8, W, FULL, STREAM>(tensor.m, i, live, to_codes<false>(m, u, (GLOBAL float*)tensor.m_scale + i / Q8_BLOCK, lane == 0));
+            store<8, W, FULL, STREAM>(tensor.v, i, live, to_codes<true>(r, u + 0x80000000u, (GLOBAL float*)tensor.v_scale + i / Q8_BLOCK, lane == 0));
         } else {
             store<32, W, FULL, STREAM>(tensor.m, i, live, raw_f32(m));
             store<32, W, FULL, STREAM>(tensor.v, i, live, raw_f32(v));

@@ -152,8 +152,26 @@ struct Q8Smem {
     static_assert(QUARTER * 4 == A_LOADS && B_LOADS > 0 && M_LOADS > 0, "whole loads");
 };
 
-// where a workgroup's slab of k-steps lies; slabs > 1: fp32 sums to part[slab][token][row]
-struct Q8Split { int steps, total; float* part; };
+// slabs of `steps` of the `total` k-steps; more than one: fp32 sums to part[slab][token][row]
+struct Q8Split { int slabs, steps, total; float* part; };
+
+// A workgroup's tile and slab.  Slabs come one after the other, each XCD takes an equal run of all their tiles (32 tiles of 256 x 256 at
+// most, the compute units it has), and so shares the k-steps of one slab or two in its cache.
+inline unsigned q8_grid(int tiles_m, int tiles_n, int slabs) {
+    return slabs > 1 ? (unsigned)((tiles_m * tiles_n * slabs + XCDS - 1) / XCDS * XCDS) : (unsigned)super_grid(tiles_m, tiles_n);
+}
+__device__ __forceinline__ bool q8_tile_of_block(int tiles_m, int tiles_n, int slabs, int& tm, int& tn, int& slab) {
+    slab = 0;
+    if (slabs == 1) return tile_of_block(tiles_m, tiles_n, tm, tn);
+    const int tiles = tiles_m * tiles_n, count = tiles * slabs, b = (int)blockIdx.x;
+    int t = b % XCDS * ((count + XCDS - 1) / XCDS) + b / XCDS;
+    if (t >= count) return false;
+    slab = t / tiles;
+    t -= slab * tiles;
+    if (tiles_m <= tiles_n) { tm = t % tiles_m; tn = t / tiles_m; }
+    else { tn = t % tiles_n; tm = t / tiles_n; }
+    return true;
+}
 
 template <int BM, int BN, int WM, bool TAIL>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, BM * BN > 128 * 128 ? 1 : 2)))
@@ -161,12 +179,12 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     using S = Q8Smem<BM, BN>;
     constexpr int WN = 4 / WM, MF = BM / (32 * WM), NF = BN / (32 * WN);
     extern __shared__ __align__(16) uint8_t smem[];
-    int tm, tn;
-    if (!tile_of_block(tiles_m, tiles_n, tm, tn)) return;
+    int tm, tn, slab;
+    if (!q8_tile_of_block(tiles_m, tiles_n, split.slabs, tm, tn, slab)) return;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int l32 = lane & 31, lq = lane >> 5, wm = wave % WM, wn = wave / WM;
-    const int first = (int)blockIdx.y * split.steps;
+    const int first = slab * split.steps;
     const int steps = min(split.steps, split.total - first);
     const int K = (int)p.K;
 
@@ -198,23 +216,21 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     if (TAIL)
 #pragma unroll
         for (int i = 0; i < 2; ++i) piece[i] = (lane & 7) ^ ((4 * i + (lane >> 4)) & 7);
-    // Past the last k-step the last of each is loaded again.  The pieces that a last pair or block has too many are the next row's
-    // (the last row's: zeros) and not used.
+    // Past the last k-step loads read zeros and no memory: they are counted upon.  The pieces that a last pair or block has too many
+    // are the next row's (the last row's: zeros) and not used.
     auto issue_a = [&](int pair, int i) {
-        const int at = min(pair, (steps - 1) >> 1);
-        uint32_t off = a_off[i];
-        if (TAIL) off |= piece[(wave * S::A_LOADS + i) & 1] * 32 >= K - (first + 2 * at) * KSTEP ? NOWHERE : 0;
-        buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, off, first * 64 + at * 128);
+        uint32_t off = a_off[i] | (2 * pair >= steps ? NOWHERE : 0);
+        if (TAIL) off |= piece[(wave * S::A_LOADS + i) & 1] * 32 >= K - (first + 2 * pair) * KSTEP ? NOWHERE : 0;
+        buffer_dma16(a_buf, smem + (pair & 1) * S::A + (wave * S::A_LOADS + i) * 1024, off, first * 64 + pair * 128);
     };
     auto issue_b = [&](int k, int i) {
-        const int at = first + min(k, steps - 1);
-        uint32_t off = b_off[i];
-        if (TAIL) off |= piece[(wave * S::B_LOADS + i) & 1] * 16 >= K - at * KSTEP ? NOWHERE : 0;
-        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, off, at * KSTEP);
+        uint32_t off = b_off[i] | (k >= steps ? NOWHERE : 0);
+        if (TAIL) off |= piece[(wave * S::B_LOADS + i) & 1] * 16 >= K - (first + k) * KSTEP ? NOWHERE : 0;
+        buffer_dma16(b_buf, smem + S::B_OFF + (k & 1) * S::B + (wave * S::B_LOADS + i) * 1024, off, (first + k) * KSTEP);
     };
     auto issue_m = [&](int block, int i) {
-        buffer_dma16(m_buf, smem + S::M_OFF + (block & 1) * S::M + (wave * S::M_LOADS + i) * 1024, m_off[i],
-                     first * 16 + min(block, (steps - 1) >> 2) * 64);
+        buffer_dma16(m_buf, smem + S::M_OFF + (block & 1) * S::M + (wave * S::M_LOADS + i) * 1024, m_off[i] | (4 * block >= steps ? NOWHERE : 0),
+                     first * 16 + block * 64);
     };
 
     // reader lanes
@@ -332,7 +348,6 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     if (k < steps) step(k, std::integral_constant<int, 0>());
     if (k + 1 < steps) step(k + 1, std::integral_constant<int, 1>());
     if (k + 2 < steps) step(k + 2, std::integral_constant<int, 2>());
-    WAIT_HERE(waitcnt_imm(0, 0));                               // the look-ahead loads
 #ifdef __HIP_DEVICE_COMPILE__
     if constexpr (MF * NF == 16) {
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -346,7 +361,8 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
     // ---- results
     const int f_base = wm * (BM / WM) + 4 * lq, t_base = wn * (BN / WN) + l32;
     if (split.part) {
-        float* const to = split.part + (int64_t)blockIdx.y * p.n * p.m;
+        WAIT_HERE(waitcnt_imm(0, 0));                           // the look-ahead loads
+        float* const to = split.part + (int64_t)slab * p.n * p.m;
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -359,29 +375,54 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
                 }
         return;
     }
-    // The tile leaves in whole rows by way of LDS, and a term that is added comes the same way before.
-    constexpr int PIECES = BN * (BM / 8), PER = PIECES / 256;
-    __syncthreads();
-    if (p.add) {
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
-            if (tok < toks && f < rows) *(u32x4*)(smem + tok * S::OUT_PITCH + f * 2) = *(const u32x4*)(p.add + (n0 + tok) * p.ldy + m0 + f);
-        }
-        __syncthreads();
-    }
-    // (with and without that term apart: a choice at every value cost 4 us of every tile)
+    // The tile leaves in whole rows by way of LDS, and a term that is added comes the same way before.  Everything that is loaded is
+    // under way together, from places clamped into the operands: with a branch around each of them the loads of the added term
+    // came one after the other (777 tokens, 20480 x 5120: 27 us more than without the term).
+    constexpr int PIECES = BN * (BM / 8), PER = PIECES / 256, BATCH = PER < 16 ? PER : 16;
     float xs[NF];
 #pragma unroll
     for (int j = 0; j < NF; ++j) xs[j] = p.xs[min(n0 + t_base + 32 * j, p.n - 1)];
+    const int piece_f = (int)threadIdx.x % (BM / 8) * 8, piece_tok = (int)threadIdx.x / (BM / 8);       // of the first piece; the next ones:
+    constexpr int TOKS_ON = 256 / (BM / 8);                                                             // so many tokens on
+    uint8_t* const piece_at = smem + piece_tok * S::OUT_PITCH + piece_f * 2;
+    auto barrier = [&] {
+        WAIT_HERE(waitcnt_imm(63, 0));
+        wg_barrier();
+    };
+    if (p.add) {
+        const bf16_t* const from = p.add + n0 * p.ldy + m0 + (piece_f < rows ? piece_f : 0);
+#pragma unroll
+        for (int b = 0; b < PER; b += BATCH) {
+            u32x4 v[BATCH];
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) v[u] = *(const u32x4*)(from + min(piece_tok + (b + u) * TOKS_ON, toks - 1) * p.ldy);
+            if (b == 0) {
+                WAIT_HERE(waitcnt_imm(0, 0));                   // the look-ahead loads too
+                wg_barrier();
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) *(u32x4*)(piece_at + (b + u) * TOKS_ON * S::OUT_PITCH) = v[u];
+        }
+        barrier();
+    } else {
+        WAIT_HERE(waitcnt_imm(0, 0));
+        wg_barrier();
+    }
+    // (with and without that term apart: a choice at every value cost 4 us of every tile; all scales of the rows ahead of that, 64 registers
+    // more, 2 %)
     auto scale = [&](auto with_add) {
         constexpr bool ADD = decltype(with_add)::value;
 #pragma unroll
-        for (int i = 0; i < MF; ++i)
+        for (int i = 0; i < MF; ++i) {
+            f32x4 wq[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int64_t f = m0 + f_base + 32 * i + 8 * q;
-                const f32x4 ws = *(const f32x4*)(p.as + (f < p.m ? f : 0));
+                wq[q] = *(const f32x4*)(p.as + (f < p.m ? f : 0));
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 ws = wq[q];
 #pragma unroll
                 for (int j = 0; j < NF; ++j) {
                     u32x2* const at = (u32x2*)(smem + (t_base + 32 * j) * S::OUT_PITCH + (f_base + 32 * i + 8 * q) * 2);
@@ -396,20 +437,26 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
                     *at = o.u;
                 }
             }
+        }
     };
     if (p.add) scale(std::true_type());
     else scale(std::false_type());
-    __syncthreads();
+    barrier();
     // a Y that the dies' second-level caches would not hold goes past them (777 tokens, 20480 x 5120 110 -> 105 us)
     const bool stream = p.n * p.ldy > ((int64_t)8 << 20);
-#pragma unroll 8
-    for (int u = 0; u < PER; ++u) {
-        const int idx = (int)threadIdx.x + u * 256, tok = idx / (BM / 8), f = idx % (BM / 8) * 8;
-        if (tok >= toks || f >= rows) continue;
-        u32x4* const to = (u32x4*)(p.y + (n0 + tok) * p.ldy + m0 + f);
-        const u32x4 v = *(const u32x4*)(smem + tok * S::OUT_PITCH + f * 2);
-        if (stream) __builtin_nontemporal_store(v, to);
-        else *to = v;
+    bf16_t* const to = p.y + n0 * p.ldy + m0 + piece_f;
+#pragma unroll
+    for (int b = 0; b < PER; b += BATCH) {
+        u32x4 v[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) v[u] = *(const u32x4*)(piece_at + (b + u) * TOKS_ON * S::OUT_PITCH);
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int tok = piece_tok + (b + u) * TOKS_ON;
+            if (tok >= toks || piece_f >= rows) continue;
+            if (stream) __builtin_nontemporal_store(v[u], (u32x4*)(to + tok * p.ldy));
+            else *(u32x4*)(to + tok * p.ldy) = v[u];
+        }
     }
 }
 
@@ -584,34 +631,56 @@ bool tile_fits(int64_t n, int64_t m, int64_t K) {
 }
 
 template <int BM, int BN, int WM, bool TAIL>
-hipError_t launch_tiles_of(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+hipError_t launch_tiles_of(const Q8Product& p, const Q8Split& split, hipStream_t s) {
     using S = Q8Smem<BM, BN>;
     constexpr int LDS = S::TOTAL > BN * S::OUT_PITCH ? S::TOTAL : BN * S::OUT_PITCH;
     const hipError_t e = allow_dynamic_lds<q8_tile_kernel<BM, BN, WM, TAIL>>(LDS);
     if (e != hipSuccess) return e;
     const int tiles_m = (int)((p.m + BM - 1) / BM), tiles_n = (int)((p.n + BN - 1) / BN);
-    q8_tile_kernel<BM, BN, WM, TAIL><<<dim3((unsigned)super_grid(tiles_m, tiles_n), (unsigned)slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
+    q8_tile_kernel<BM, BN, WM, TAIL><<<q8_grid(tiles_m, tiles_n, split.slabs), 256, LDS, s>>>(p, tiles_m, tiles_n, split);
     return hipGetLastError();
 }
 template <int BM, int BN, int WM>
-hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
-    return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, false>(p, split, slabs, s) : launch_tiles_of<BM, BN, WM, true>(p, split, slabs, s);
+hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, hipStream_t s) {
+    return p.K % KSTEP == 0 ? launch_tiles_of<BM, BN, WM, false>(p, split, s) : launch_tiles_of<BM, BN, WM, true>(p, split, s);
 }
 
 // below it the general kernel's one launch is faster (us, general / copies and tiles: 200 tokens, 2056 x 2056 15.8 / 17; 600, 1000 x 1000
 // 11.8 / 13; 2048, 2056 x 2056 106 / 30)
 constexpr int64_t PAD_WORK = (int64_t)1 << 30;
-constexpr int STEPS_WHOLE = 40, STEPS_SLAB = 16;
 constexpr int STREAM_WAVES = 4, STREAM_STAGES = 3, STREAM_GROUPS = 1024, STREAM_TOKENS = 8;
 bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && m < ((int64_t)1 << 29); }
 
 template <int TOK>
-hipError_t launch_stream(const Q8Product& p, const Q8Split& split, int slabs, hipStream_t s) {
+hipError_t launch_stream(const Q8Product& p, const Q8Split& split, hipStream_t s) {
     constexpr int RING = STREAM_WAVES * STREAM_STAGES * Q8Ring<TOK>::STAGE, SUMS = STREAM_WAVES * TOK * 36 * 4, LDS = RING > SUMS ? RING : SUMS;
     const hipError_t e = allow_dynamic_lds<q8_stream_kernel<TOK, STREAM_WAVES, STREAM_STAGES>>(LDS);
     if (e != hipSuccess) return e;
-    q8_stream_kernel<TOK, STREAM_WAVES, STREAM_STAGES><<<dim3((unsigned)((p.m + 31) / 32), (unsigned)slabs), 64 * STREAM_WAVES, LDS, s>>>(p, split);
+    q8_stream_kernel<TOK, STREAM_WAVES, STREAM_STAGES><<<dim3((unsigned)((p.m + 31) / 32), (unsigned)split.slabs), 64 * STREAM_WAVES, LDS, s>>>(p, split);
     return hipGetLastError();
+}
+
+// What a product takes on a tile, us, by constants fitted to the times of 945 products (9 to 8192 tokens, 512 to 36864 rows and
+// columns, operands from memory, each on every tile that suits and in 1 to 16 slabs).  On 668 others the least
+// estimate's choice takes 1.029 times the best one's time in the geometric mean, 1.49 times at most.  A round that does not fill the chip runs with fewer tiles on a
+// compute unit and a higher clock; rounds overlap, so tiles count partly by rounds, partly by their number.  (us, 256 x 256 / 128 x 128 / 128 x 64,
+// whole: 793 tokens, 11776 x 3584 34 / 39 / 46; 609, 12800 x 6144 48 / 38 / 52; 972, 12352 x 4416 47 / 62 / 93.  Whole / best number of
+// slabs: 60 tokens, 9216 x 9216 34 / 20; 300, 9216 x 36864 145 / 100; 128, 5120 x 5120 16 / 18.)
+struct Q8Tile {
+    int bm, bn, resident;                                       // resident: on the chip at a time
+    double step, full, rest;                                    // of a k-step with one tile on a compute unit, on a full chip; outside of them
+};
+constexpr Q8Tile Q8_TILES[] = {{256, 256, RESIDENT, 0.73, 1.08, 8.2}, {128, 128, 2 * RESIDENT, 0.45, 0.78, 1.4},
+                               {128, 64, 2 * RESIDENT, 0.38, 0.60, 0.6}, {128, 32, 2 * RESIDENT, 0.36, 0.53, 0.0}};
+constexpr double BY_NUMBER = 0.4, MEMORY_US = 0.235;            // a MB of operands and result
+constexpr double REDUCE_US = 3.5, SUMS_US = 0.27;               // the launch that adds slabs' sums; a MB of them
+constexpr double SECOND_US = 4.7, SECOND_STEP_US = 0.35;        // a second launch after whole rounds; and for each of its k-steps
+constexpr int SLABS = 16, STEPS_SLAB = 6;                       // most slabs; fewest k-steps of one
+int64_t tiles_of(const Q8Tile& t, int64_t n, int64_t m) { return (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn); }
+double tiles_us(const Q8Tile& t, int64_t count, int steps) {
+    if (count <= RESIDENT) return t.step * steps + t.rest;
+    const double number = (double)count / t.resident, rounds = (double)((count + t.resident - 1) / t.resident);
+    return (BY_NUMBER * number + (1.0 - BY_NUMBER) * rounds) * (t.full * steps + t.rest);
 }
 
 // kernel of a product: stream (bn: tokens), tiles of bm x bn, or neither (the general one); the contraction in `slabs`
@@ -632,49 +701,36 @@ Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
     }
     if (!tile_fits(n, m, K)) return {false, 0, 0, 1, 0, 0, 0};
     const int total = (int)((K + KSTEP - 1) / KSTEP);
-    auto tiles = [&](int bm, int bn, int64_t rows) { return (rows + bm - 1) / bm * ((n + bn - 1) / bn); };
-    // Tile by the time of a k-step of the whole grid, us.  256 x 256 goes by whole rounds of the chip; of the others two are on a
-    // compute unit, and rounds overlap.  (us, 256 x 256 / 128 x 128 / 128 x 64: 777 tokens, 20480 x 5120 105 / 95 / 120; 2048, 5120 x 5120
-    // 50 / 58 / 68; 512, 5120 x 5120 46 / 26 / 25; 256, 9216 x 9216 67 / 41 / 37; 1200, 14336 x 4096 80 / 71 / 92; 8192, 36864 x 9216
-    // 1550 / 2250 / 2930)
-    auto shared = [&](int bn, double one, double two, int64_t rows) {        // one tile on a compute unit, 512 tiles on the chip
-        const int64_t t = tiles(128, bn, rows);
-        const double all = two * (double)t / 512.0;
-        return t <= RESIDENT ? one : all > 0.75 * two ? all : 0.75 * two;
+    const double sums_mb = (double)n * (double)m * 4e-6;
+    const double memory = ((double)m * K * 0.625 + (double)n * K + 2.0 * n * m) * 1e-6 * MEMORY_US;
+    Q8Plan plan = {false, 0, 0, 1, total, total, 0};
+    double best = 0.0;
+    auto consider = [&](double us, const Q8Tile& t, int slabs, int steps, int64_t rows0) {
+        if (plan.bm != 0 && us >= best) return;
+        best = us;
+        plan = {false, t.bm, t.bn, slabs, steps, total, rows0};
     };
-    auto smaller = [&](int64_t rows, int& bn) {                  // the best tile of 128 rows
-        double best = shared(bn = 32, 0.40, 0.50, rows);
-        const double t64 = shared(64, 0.42, 0.67, rows), t128 = shared(128, 0.60, 1.08, rows);
-        if (n > 32 && t64 < best) best = t64, bn = 64;
-        if (n > 64 && t128 < best) best = t128, bn = 128;
-        return best;
-    };
-    Q8Plan plan = {false, 128, 32, 1, total, total, 0};
-    double best = smaller(m, plan.bn);
-    const int64_t t256 = tiles(256, 256, m), rounds = t256 / RESIDENT;
-    if (n > 128 && 1.24 * (double)((t256 + RESIDENT - 1) / RESIDENT) < best) {
-        best = 1.24 * (double)((t256 + RESIDENT - 1) / RESIDENT);
-        plan.bm = plan.bn = 256;
-    }
-    // Or whole rounds of 256 x 256 and the rows that are left on smaller tiles, in a second launch.  (us, one tile / both: 777 tokens, 20480 x 5120, 320
-    // tiles of 256 x 256: 110 / 103; 4096, 5120 x 5120, 320 tiles: 92 / 81; 6000, 9216 x 9216, 864: 333 / 327.  The leftover tiles of the first
-    // in four slabs each, whose 64 MB of sums are written and read once more: 124.)
-    const int64_t rows0 = rounds * RESIDENT / ((n + 255) / 256) * 256;
-    if (n > 128 && rows0 > 0 && rows0 < m) {
-        int bn;
-        const double t = 1.24 * (double)rounds + smaller(m - rows0, bn) + 5.0 / total;
-        if (t < best) return {false, 128, bn, 1, total, total, rows0};
-    }
-    // A slab less than STEPS_WHOLE k-steps long is not worth a second launch, and more than two workgroups a compute unit give nothing
-    // (us, whole / slabs: 128 tokens, 5120 x 5120 16 / 18 with 6; 300, 4096 x 4096 15 / 20 with 2; 60, 9216 x 9216 34 / 20 with 7;
-    // 60, 2560 x 10240 21 / 14 with 12, 20 with 20; 300, 9216 x 36864 145 / 100 with 2)
-    const int64_t t = tiles(plan.bm, plan.bn, m);
-    if (room && total > STEPS_WHOLE) {
-        const int slabs = (int)min(2 * (int64_t)RESIDENT / t, (int64_t)(total + STEPS_SLAB - 1) / STEPS_SLAB);
-        if (slabs > 1) {
-            plan.steps = ((total + slabs - 1) / slabs + 1) / 2 * 2;      // whole pairs of k-steps
-            plan.slabs = (total + plan.steps - 1) / plan.steps;
+    for (const Q8Tile& t : Q8_TILES) {
+        if (t.bn > 32 && t.bn >= 2 * n) continue;                // more than half of it empty
+        const int64_t count = tiles_of(t, n, m);
+        for (int slabs = 1; slabs == 1 || (room && slabs <= SLABS && total / slabs >= STEPS_SLAB && count * slabs <= t.resident); ++slabs) {
+            const int steps = slabs == 1 ? total : ((total + slabs - 1) / slabs + 1) / 2 * 2;        // whole pairs of k-steps
+            const int real = (total + steps - 1) / steps;
+            if (real != slabs) continue;
+            const double us = tiles_us(t, count * slabs, steps) + (slabs > 1 ? REDUCE_US + slabs * sums_mb * SUMS_US : 0.0);
+            consider(sqrt(us * us + memory * memory), t, slabs, steps, 0);
         }
+    }
+    // Whole rounds of 256 x 256 and the rows that are left on tiles of 64 tokens, if these are resident at once, or else of 128.  (us, the best
+    // tile / both: 777 tokens, 20480 x 5120 87 / 74; 3418, 7936 x 13312 236 / 258; 1390, 12800 x 5120 82 / 74; with leftover tiles 64 / 128 tokens wide,
+    // 416 / 208 of them 74 / 75, 852 / 432 1.13 to 1.  The leftover tiles of the first in four slabs each, whose 64 MB of sums are written and
+    // read once more: 21 more than on smaller tiles.)
+    const Q8Tile &large = Q8_TILES[0], &wide = Q8_TILES[1], &narrow = Q8_TILES[2];
+    const int64_t tn = (n + large.bn - 1) / large.bn, rows0 = tiles_of(large, n, m) / large.resident * large.resident / tn * large.bm;
+    if (n > large.bn / 2 && rows0 > 0 && rows0 < m) {
+        const Q8Tile& t = tiles_of(narrow, n, m - rows0) <= narrow.resident ? narrow : wide;
+        const double us = tiles_us(large, rows0 / large.bm * tn, total) + SECOND_US + SECOND_STEP_US * total + tiles_us(t, tiles_of(t, n, m - rows0), total);
+        consider(sqrt(us * us + memory * memory), t, 1, total, rows0);
     }
     return plan;
 }
@@ -727,12 +783,12 @@ hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const ui
         return hipGetLastError();
     }
     float* const part = plan.slabs > 1 ? (float*)room : nullptr;
-    const Q8Split split = {plan.steps, plan.total, part};
+    const Q8Split split = {plan.slabs, plan.steps, plan.total, part};
     hipError_t e;
     if (plan.rows0 > 0) {
         Q8Product first = p;
         first.m = plan.rows0;
-        e = launch_tiles<256, 256, 2>(first, split, 1, s);
+        e = launch_tiles<256, 256, 2>(first, split, s);
         if (e != hipSuccess) return e;
         p.a += plan.rows0 * (p.K / 2);
         p.am += plan.rows0 * (p.K / 8);
@@ -741,11 +797,11 @@ hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const ui
         if (p.add) p.add += plan.rows0;
         p.m -= plan.rows0;
     }
-    if (plan.stream) e = plan.bn == 4 ? launch_stream<4>(p, split, plan.slabs, s) : launch_stream<8>(p, split, plan.slabs, s);
-    else if (plan.bm == 256) e = launch_tiles<256, 256, 2>(p, split, plan.slabs, s);
-    else if (plan.bn == 128) e = launch_tiles<128, 128, 2>(p, split, plan.slabs, s);
-    else if (plan.bn == 64) e = launch_tiles<128, 64, 2>(p, split, plan.slabs, s);
-    else e = launch_tiles<128, 32, 4>(p, split, plan.slabs, s);
+    if (plan.stream) e = plan.bn == 4 ? launch_stream<4>(p, split, s) : launch_stream<8>(p, split, s);
+    else if (plan.bm == 256) e = launch_tiles<256, 256, 2>(p, split, s);
+    else if (plan.bn == 128) e = launch_tiles<128, 128, 2>(p, split, s);
+    else if (plan.bn == 64) e = launch_tiles<128, 64, 2>(p, split, s);
+    else e = launch_tiles<128, 32, 4>(p, split, s);
     if (e != hipSuccess || plan.slabs == 1) return e;
     q8_reduce_kernel<<<grid_of((n * (m / 4) + 255) / 256), 256, 0, s>>>(p, part, plan.slabs);
     return hipGetLastError();

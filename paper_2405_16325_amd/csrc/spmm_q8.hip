@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
 //     1, 3: half of the pair of W after next      0: the next metadata block, which have not to.
 // What bounds it: 52 KB of operands a k-step, which reach a compute unit at about 30 bytes a cycle in all variants tried (a ring of three
 // k-steps with smaller requests, 256 x 192 tiles with two k-steps of look-ahead 13 % slower), at the 1.46 GHz that the power management
-// leaves: 1.05 us a k-step, against 0.70 of products; and 11 us before and after the loop of every tile.
+// leaves: 1.05 us a k-step, against 0.70 of products; and about 11 us before and after the loop of every tile (8192 tokens, 36864 x 9216:
+// 1.50 ms, 3.7 PFLOP/s dense-equivalent, matrix pipes 52 % busy).
 template <int BM, int BN>
 struct Q8Smem {
     static constexpr int A = BM * 128, B = BN * 128, M = BM * 64;         // a pair of W, a k-step of tokens, a block of metadata
@@ -461,7 +462,7 @@ q8_tile_kernel(Q8Product p, int tiles_m, int tiles_n, Q8Split split) {
 }
 
 // ------------------------------------------------------------------------------------------
-// q8_stream_kernel: up to TOK <= 32 tokens, K % 32 == 0: one pass over the packed weight, bound by memory.  A workgroup owns 32 rows
+// q8_stream_kernel: up to TOK (4 or 8) tokens, K % 32 == 0: one pass over the packed weight, bound by memory.  A workgroup owns 32 rows
 // and all tokens; its wavefronts take the stretches of 256 logical k in turn, each through a ring of its own in LDS, without a
 // barrier, and add their sums through LDS at the end, in order.  Loads are of whole 128-byte lines of W: with operands straight to
 // registers, where a load takes 16 bytes from each of 64 places, the address unit is the bound (1 token, 36864 x 9216: 54.6 us).
@@ -648,6 +649,7 @@ hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, hipStream_t s)
 // below it the general kernel's one launch is faster (us, general / copies and tiles: 200 tokens, 2056 x 2056 15.8 / 17; 600, 1000 x 1000
 // 11.8 / 13; 2048, 2056 x 2056 106 / 30)
 constexpr int64_t PAD_WORK = (int64_t)1 << 30;
+// (us, stream / best of the tiles: 4 tokens, 36864 x 9216 34.8 / 49.1, 5120 x 5120 8.4 / 10.6; 8 tokens 40.7 / 49.4, 9.6 / 10.8)
 constexpr int STREAM_WAVES = 4, STREAM_STAGES = 3, STREAM_GROUPS = 1024, STREAM_TOKENS = 8;
 bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && m < ((int64_t)1 << 29); }
 

@@ -18,7 +18,7 @@ pytestmark = pytest.mark.gpu
 
 EPS = 1e-5
 # every way rows are shared out: 8, 16, 32 lanes a row, one wavefront with one or more pieces a lane, several wavefronts, rows
-# that stay in memory (past 32768 elements for the gradient, past 65536 forward); rows that do not fill the last workgroup
+# that stay in memory (past 24576 elements for the gradient, past 32768 forward); rows that do not fill the last workgroup
 SHAPES = [(1, 8), (33, 64), (5, 72), (70, 128), (9, 136), (9, 256), (1, 264), (6, 512), (17, 520), (1, 768), (1000, 1000), (2, 2048),
           (3, 2056), (2100, 2056), (2049, 768), (2, 4104), (5, 9216), (2050, 9216), (3, 20480), (2048, 5120), (2, 36864), (1, 65536),
           (2, 65544), (3, 131080)]

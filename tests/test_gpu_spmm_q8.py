@@ -111,12 +111,7 @@ def test_a_token_of_zeros_and_one_that_is_not_finite(b):
     check(y[rest], q[rest], xs[rest], dev, meta)
 
 
-@pytest.mark.parametrize("b,d_out,d_in", [(1, 36864, 9216), (16, 9216, 36864), (300, 2560, 10240), (2048, 5120, 5120), (777, 20480, 5120),
-                                           (1100, 14080, 4160)])
-def test_layers_at_full_size_against_a_library_product(b, d_out, d_in):
-    """Every element against an fp32 product of the same values; the bound's middle term from the rows' norms, which is what
-    the terms' magnitudes add up to at most."""
-    say(f"spmm_fwd_q8 full size b={b} d_out={d_out} d_in={d_in}")
+def against_a_library_product(b, d_out, d_in, with_add=False):
     gen = torch.Generator(device="cuda")
     gen.manual_seed(inputs.SEED_BASE + b)
     W = (torch.randn(d_out, d_in, generator=gen, device="cuda") * 0.02).to(sl.BF16)
@@ -125,14 +120,41 @@ def test_layers_at_full_size_against_a_library_product(b, d_out, d_in):
     x = torch.randn(b, d_in, generator=gen, device="cuda").to(sl.BF16)
     ones = torch.ones(d_in, dtype=sl.BF16, device="cuda")
     _, _, _, q, xs = sl.slope_rmsnorm_fwd(x, ones, 1e-5, want_y=False, want_q8=True)
-    y = sl.slope_spmm_fwd_q8(q, xs, wq, meta, ws).float()
+    add = torch.randn(b, d_out, generator=gen, device="cuda").to(sl.BF16) if with_add else None
+    y = sl.slope_spmm_fwd_q8(q, xs, wq, meta, ws, add=add).float()
     bits = (mask.unsqueeze(-1) >> torch.arange(8, device="cuda", dtype=torch.uint8)) & 1
     dense = torch.zeros(d_out, d_in, device="cuda")
     dense[bits.view(d_out, d_in).bool()] = (wq.float() * ws[:, None]).view(-1)
     xf = q.float() * xs[:, None]
     want = torch.matmul(xf, dense.t().contiguous())
     terms = xf.norm(dim=1)[:, None] * dense.norm(dim=1)[None]
+    if with_add:
+        want += add.float()
     assert ((y - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -13 * terms).all()
+
+
+# tiles of 128 x 32, 128 x 64, 128 x 128 and 256 x 256; each whole, in slabs of the contraction, and (64 and 128 tokens) for the rows that
+# whole rounds of the largest leave; contractions that end with a k-step and inside one; most with ragged last tiles
+TILES = [(25, 56, 1664), (312, 8, 1216), (36, 488, 2944), (11, 80, 9792), (1273, 1624, 256), (105, 17256, 320), (936, 16856, 2176),
+         (2994, 5936, 1984), (801, 16, 16640), (1179, 40, 12352), (608, 7824, 256), (325, 12352, 320), (1963, 10504, 2944),
+         (2482, 8080, 2752), (2118, 8, 14464), (3060, 16, 13376), (720, 11720, 1408), (667, 12984, 1344), (133, 10544, 11904),
+         (131, 7760, 15296)]
+
+
+@pytest.mark.parametrize("b,d_out,d_in", TILES)
+@pytest.mark.parametrize("with_add", [False, True])
+def test_every_tile_whole_in_slabs_and_for_the_rows_left(b, d_out, d_in, with_add):
+    say(f"spmm_fwd_q8 tiles b={b} d_out={d_out} d_in={d_in} add={with_add}")
+    against_a_library_product(b, d_out, d_in, with_add)
+
+
+@pytest.mark.parametrize("b,d_out,d_in", [(1, 36864, 9216), (16, 9216, 36864), (300, 2560, 10240), (2048, 5120, 5120), (777, 20480, 5120),
+                                           (1100, 14080, 4160)])
+def test_layers_at_full_size_against_a_library_product(b, d_out, d_in):
+    """Every element against an fp32 product of the same values; the bound's middle term from the rows' norms, which is what
+    the terms' magnitudes add up to at most."""
+    say(f"spmm_fwd_q8 full size b={b} d_out={d_out} d_in={d_in}")
+    against_a_library_product(b, d_out, d_in)
 
 
 def test_norm_and_product_agree_with_the_16_bit_path():

@@ -309,6 +309,65 @@ __global__ void __launch_bounds__(bwd_threads(VPT)) rmsnorm_bwd_kernel(NormBwd a
     }
 }
 
+// Both gradients in one launch, where dx is not written over dy.  Workgroups below `dw_groups` make dw, 4 pieces (a line of 64 bytes) and all
+// rows each, added over the lanes and then, in order, over the wavefronts; the others dx, a row a slot.  dy and h are read twice, the
+// second time from the caches.  dw's loads, four rows at a time, bound it (1000 x 1000: 7.5 us).
+template <int LPR>
+__global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_once_kernel(NormBwd a, int wpr, int dw_groups) {
+    __shared__ float part[MAX_WAVES];
+    __shared__ F8 shares[MAX_WAVES][4];
+    const int pieces = a.d / 8;
+    if ((int)blockIdx.x < dw_groups) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 4 + (lane & 3), step = blockDim.x / 4;
+        F8 s;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s.v[k] = 0.0f;
+        if (i < pieces)
+#pragma unroll 4
+            for (int row = threadIdx.x >> 2; row < (int)a.b; row += step) {
+                const size_t at = (size_t)row * a.d + 8 * (size_t)i;
+                const float r = a.rstd[row];
+                const F8 dy = unpack_bf16(*(const u32x4*)(a.dy + at)), h = unpack_bf16(*(const u32x4*)(a.h + at));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s.v[k] += dy.v[k] * (h.v[k] * r);
+            }
+#pragma unroll
+        for (int x = 4; x < 64; x *= 2)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s.v[k] += __shfl_xor(s.v[k], x);
+        if (lane < 4) shares[wave][lane] = s;
+        __syncthreads();
+        if (threadIdx.x >= 4 || i >= pieces) return;
+        for (int w = 1; w < (int)blockDim.x / 64; ++w)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s.v[k] += shares[w][lane].v[k];
+        *(u32x4*)(a.dw + 8 * (size_t)i) = pack_bf16(s);
+        return;
+    }
+    const RowThreads rt = row_threads<LPR>(wpr);
+    const int64_t row = (int64_t)((int)blockIdx.x - dw_groups) * (blockDim.x / rt.threads) + rt.row;
+    const size_t at = (size_t)row * a.d + 8 * (size_t)rt.lane;
+    const bool live = row < a.b && rt.lane < pieces;
+    u32x4 pdy = {0, 0, 0, 0}, ph = pdy, pdh = pdy, pw = pdy;
+    float r = 0.0f;
+    if (live) {
+        pdy = *(const u32x4*)(a.dy + at);
+        ph = *(const u32x4*)(a.h + at);
+        if (a.dh) pdh = *(const u32x4*)(a.dh + at);
+        pw = *(const u32x4*)(a.w + 8 * (size_t)rt.lane);
+        r = a.rstd[row];
+    }
+    const F8 dy = unpack_bf16(pdy), h = unpack_bf16(ph), dh = unpack_bf16(pdh), w = unpack_bf16(pw);
+    float c = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c = fmaf(dy.v[k] * (h.v[k] * r), w.v[k], c);
+    c = row_sum<LPR>(c, wpr, part) / (float)a.d;
+    F8 o;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w.v[k] - h.v[k] * r * c, dh.v[k]);
+    if (live) *(u32x4*)(a.dx + at) = pack_bf16(o);
+}
+
 // Rows too long for registers: dx row by row, reading the row twice, and dw's shares column by column
 __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_wide_kernel(NormBwd a) {
     __shared__ float part[MAX_WAVES];
@@ -402,6 +461,10 @@ RowShape bwd_shape(int64_t b, int64_t d) {
     return row_shape(pieces, pieces <= 2 * 512 ? 2 : pieces <= 3 * 512 ? 3 : pieces <= 4 * 512 ? 4 : 6);
 }
 
+// both gradients in one launch (us in a captured graph, two launches / one: 64 x 768 5.5 / 2.9; 1000 x 1000 9.8 / 7.7; 777 x 5120 14.6 / 12.3;
+// 1024 x 5120 15.5 / 15.9; 1400 x 768 8.5 / 8.4; 2000 x 768 9.1 / 11.0; 1000 x 8192 20.6 / 24.3)
+bool bwd_once(int64_t b, int64_t d) { return bwd_shape(b, d).vpt == 1 && b <= 1024 && b * d <= (int64_t)5 << 20; }
+
 // workgroups of the gradient: as many as are resident together (eight wavefronts on a compute unit), so that each makes one share of
 // dw; for a few rows one, which saves the second launch
 int bwd_groups(int64_t b, int64_t d) {
@@ -441,6 +504,17 @@ hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w
     const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, dw, part};
     const RowShape rs = bwd_shape(b, d);
     const int groups = bwd_groups(b, d);
+    if (bwd_once(b, d) && (dx + b * d <= dy || dy + b * d <= dx)) {
+        const int slots = rs.lpr < 64 ? 512 / rs.lpr : rs.wpr < 8 ? 8 / rs.wpr : 1, threads = rs.lpr < 64 ? 512 : slots * rs.wpr * 64;
+        const int dw_groups = (int)((d / 8 + 3) / 4);
+#define ONCE(LPR) rmsnorm_bwd_once_kernel<LPR><<<dw_groups + (int)((b + slots - 1) / slots), threads, 0, s>>>(a, rs.wpr, dw_groups)
+        if (rs.lpr == 8) ONCE(8);
+        else if (rs.lpr == 16) ONCE(16);
+        else if (rs.lpr == 32) ONCE(32);
+        else ONCE(64);
+#undef ONCE
+        return hipGetLastError();
+    }
     if (rs.vpt == 0) {
         // dw first: dx may be written over dy
         rmsnorm_dw_wide_kernel<<<dim3((unsigned)((d / 8 + 255) / 256), (unsigned)groups), 256, 0, s>>>(a);

@@ -189,6 +189,18 @@ def test_gradient_in_place(b, d, into):
     check_grads(dx, dw, values, r)
 
 
+# both gradients in one launch and, written over dY or of more rows or elements, in two: every number of lanes or wavefronts a row
+@pytest.mark.parametrize("b,d", [(1, 8), (1024, 8), (1025, 8), (1023, 64), (1100, 72), (1024, 136), (1500, 256), (700, 264), (1024, 1032),
+                                 (1030, 768), (100, 1544), (300, 2056), (65, 2568), (600, 3080), (9, 8192), (640, 8192), (641, 8192)])
+@pytest.mark.parametrize("over_dy", [False, True])
+def test_gradient_in_one_launch_and_in_two(b, d, over_dy):
+    say(f"rmsnorm_bwd launches b={b} d={d} over_dy={over_dy}")
+    dy, h, w, rstd, dh, values, r = grad_case(b, d, b % 2 == 0)
+    dx, dw = sl.slope_rmsnorm_bwd(dy, h, w, rstd, dh=dh, out=(dy if over_dy else torch.empty_like(dy), torch.empty_like(w)))
+    torch.cuda.synchronize()
+    check_grads(dx, dw, values, r)
+
+
 def test_gradient_against_differences_of_the_forward():
     """The forward's own fp32 row statistics and 8 significant bits of y bound a difference: steps of a quarter of the values'
     size, so that the second-order term, not the rounding, is what the fp64 function's own difference also has."""

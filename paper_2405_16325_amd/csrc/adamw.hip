@@ -5,7 +5,7 @@
 //
 // Memory bounds both: every element is read and written once, 28 bytes of it with 32-bit states and fp32 master weights, 10
 // with 8-bit states and bf16 weights alone.  157 M elements with masters take 690 us of 32-bit step, 6.3 TB/s, and 55 + 5 of norm,
-// 418 us with 8-bit states, 6.1 TB/s; 510 M with 8-bit states and bf16 weights 930, 5.8 TB/s, where the vector units are as busy.
+// 418 us with 8-bit states, 6.1 TB/s; 531 M with 8-bit states and bf16 weights 930, 5.8 TB/s, where the vector units are as busy.
 // The tensors of a set are cut into chunks of CHUNK elements; a table in device memory (laid out once by adamw_fill_table) names
 // each chunk's tensor, so that one launch covers hundreds of tensors of any sizes evenly and a workgroup finds its work with two
 // scalar loads.
@@ -438,7 +438,7 @@ hipError_t launch_adamw(const void* table, const void* device_table, double lr, 
                         (float)eps, (float)log(beta1), (float)log(beta2), (float)grad_scale, (float)step, control};
     const dim3 grid = grid_of(h->chunks);
     // a set that the last-level cache does not hold goes past it (us, through it / past it: 157 M elements with masters, 32-bit states
-    // and the norm 897 / 771, 8-bit states 473 / 427; 510 M, 8-bit states, bf16 weights 959 / 911 to 947)
+    // and the norm 897 / 771, 8-bit states 473 / 427; 531 M, 8-bit states, bf16 weights 959 / 911 to 947)
     const bool stream = (size_t)h->chunks * CHUNK * (h->state_bits == 8 ? 8 : 16) > LAST_LEVEL_CACHE_BYTES;
     // few chunks: more wavefronts on each, so that all of its loads are under way at once (0.9 M elements with masters,
     // us, 256 / 512: with the norm 17.1 / 15.7; 8-bit states 11.1 / 10.0)

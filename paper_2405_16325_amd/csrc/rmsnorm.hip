@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(bwd_threads(VPT)) rmsnorm_bwd_kernel(NormBwd a
 // Both gradients in one launch, where dx is not written over dy.  Workgroups below `dw_groups` make dw, 4 pieces (a line of 64 bytes) and all
 // rows each, added over the lanes and then, in order, over the wavefronts; the others dx, a row a slot.  dy and h are read twice, the
 // second time from the caches.  dw's loads, four rows at a time, bound it (1000 x 1000: 7.5 us).
-template <int LPR>
+template <int LPR, int VPT>
 __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_once_kernel(NormBwd a, int wpr, int dw_groups) {
     __shared__ float part[MAX_WAVES];
     __shared__ F8 shares[MAX_WAVES][4];
@@ -346,26 +346,37 @@ __global__ void __launch_bounds__(MAX_THREADS) rmsnorm_bwd_once_kernel(NormBwd a
     }
     const RowThreads rt = row_threads<LPR>(wpr);
     const int64_t row = (int64_t)((int)blockIdx.x - dw_groups) * (blockDim.x / rt.threads) + rt.row;
-    const size_t at = (size_t)row * a.d + 8 * (size_t)rt.lane;
-    const bool live = row < a.b && rt.lane < pieces;
-    u32x4 pdy = {0, 0, 0, 0}, ph = pdy, pdh = pdy, pw = pdy;
-    float r = 0.0f;
-    if (live) {
-        pdy = *(const u32x4*)(a.dy + at);
-        ph = *(const u32x4*)(a.h + at);
-        if (a.dh) pdh = *(const u32x4*)(a.dh + at);
-        pw = *(const u32x4*)(a.w + 8 * (size_t)rt.lane);
-        r = a.rstd[row];
-    }
-    const F8 dy = unpack_bf16(pdy), h = unpack_bf16(ph), dh = unpack_bf16(pdh), w = unpack_bf16(pw);
+    const size_t at = (size_t)row * a.d;
+    const float r = row < a.b ? a.rstd[row] : 0.0f;
+    u32x4 pdy[VPT], ph[VPT], pdh[VPT], pw[VPT];
     float c = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) c = fmaf(dy.v[k] * (h.v[k] * r), w.v[k], c);
-    c = row_sum<LPR>(c, wpr, part) / (float)a.d;
-    F8 o;
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        pdy[p] = ph[p] = pdh[p] = pw[p] = (u32x4){0, 0, 0, 0};
+        if (row < a.b && i < pieces) {
+            pdy[p] = *(const u32x4*)(a.dy + at + 8 * (size_t)i);
+            ph[p] = *(const u32x4*)(a.h + at + 8 * (size_t)i);
+            if (a.dh) pdh[p] = *(const u32x4*)(a.dh + at + 8 * (size_t)i);
+            pw[p] = *(const u32x4*)(a.w + 8 * (size_t)i);
+        }
+    }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w.v[k] - h.v[k] * r * c, dh.v[k]);
-    if (live) *(u32x4*)(a.dx + at) = pack_bf16(o);
+    for (int p = 0; p < VPT; ++p) {
+        const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]), w = unpack_bf16(pw[p]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c = fmaf(dy.v[k] * (h.v[k] * r), w.v[k], c);
+    }
+    c = row_sum<LPR>(c, wpr, part) / (float)a.d;
+#pragma unroll
+    for (int p = 0; p < VPT; ++p) {
+        const int i = rt.lane + p * rt.threads;
+        const F8 dy = unpack_bf16(pdy[p]), h = unpack_bf16(ph[p]), dh = unpack_bf16(pdh[p]), w = unpack_bf16(pw[p]);
+        F8 o;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o.v[k] = fmaf(r, dy.v[k] * w.v[k] - h.v[k] * r * c, dh.v[k]);
+        if (row < a.b && i < pieces) *(u32x4*)(a.dx + at + 8 * (size_t)i) = pack_bf16(o);
+    }
 }
 
 // Rows too long for registers: dx row by row, reading the row twice, and dw's shares column by column
@@ -462,8 +473,8 @@ RowShape bwd_shape(int64_t b, int64_t d) {
 }
 
 // both gradients in one launch (us in a captured graph, two launches / one: 64 x 768 5.5 / 2.9; 1000 x 1000 9.8 / 7.7; 777 x 5120 14.6 / 12.3;
-// 1024 x 5120 15.5 / 15.9; 1400 x 768 8.5 / 8.4; 2000 x 768 9.1 / 11.0; 1000 x 8192 20.6 / 24.3)
-bool bwd_once(int64_t b, int64_t d) { return bwd_shape(b, d).vpt == 1 && b <= 1024 && b * d <= (int64_t)5 << 20; }
+// 64 x 9216 9.1 / 4.6; 569 x 9216 18.3 / 18.2; 1024 x 5120 15.5 / 15.9; 1400 x 768 8.5 / 8.4; 2000 x 768 9.1 / 11.0; 1000 x 8192 20.6 / 24.3)
+bool bwd_once(int64_t b, int64_t d) { return d / 8 <= 2 * MAX_THREADS && b <= 1024 && b * d <= (int64_t)5 << 20; }
 
 // workgroups of the gradient: as many as are resident together (eight wavefronts on a compute unit), so that each makes one share of
 // dw; for a few rows one, which saves the second launch
@@ -502,19 +513,21 @@ size_t rmsnorm_bwd_workspace_bytes(int64_t b, int64_t d) { return (size_t)bwd_gr
 hipError_t launch_rmsnorm_bwd(const bf16_t* dy, const bf16_t* h, const bf16_t* w, const float* rstd, const bf16_t* dh, int64_t b,
                               int64_t d, bf16_t* dx, bf16_t* dw, float* part, hipStream_t s) {
     const NormBwd a = {dy, h, w, rstd, dh, b, (int)d, dx, dw, part};
-    const RowShape rs = bwd_shape(b, d);
-    const int groups = bwd_groups(b, d);
     if (bwd_once(b, d) && (dx + b * d <= dy || dy + b * d <= dx)) {
+        const RowShape rs = row_shape(d / 8, d / 8 <= MAX_THREADS ? 1 : 2);
         const int slots = rs.lpr < 64 ? 512 / rs.lpr : rs.wpr < 8 ? 8 / rs.wpr : 1, threads = rs.lpr < 64 ? 512 : slots * rs.wpr * 64;
         const int dw_groups = (int)((d / 8 + 3) / 4);
-#define ONCE(LPR) rmsnorm_bwd_once_kernel<LPR><<<dw_groups + (int)((b + slots - 1) / slots), threads, 0, s>>>(a, rs.wpr, dw_groups)
-        if (rs.lpr == 8) ONCE(8);
-        else if (rs.lpr == 16) ONCE(16);
-        else if (rs.lpr == 32) ONCE(32);
-        else ONCE(64);
+#define ONCE(...) rmsnorm_bwd_once_kernel<__VA_ARGS__><<<dw_groups + (int)((b + slots - 1) / slots), threads, 0, s>>>(a, rs.wpr, dw_groups)
+        if (rs.lpr == 8) ONCE(8, 1);
+        else if (rs.lpr == 16) ONCE(16, 1);
+        else if (rs.lpr == 32) ONCE(32, 1);
+        else if (rs.vpt == 1) ONCE(64, 1);
+        else ONCE(64, 2);
 #undef ONCE
         return hipGetLastError();
     }
+    const RowShape rs = bwd_shape(b, d);
+    const int groups = bwd_groups(b, d);
     if (rs.vpt == 0) {
         // dw first: dx may be written over dy
         rmsnorm_dw_wide_kernel<<<dim3((unsigned)((d / 8 + 255) / 256), (unsigned)groups), 256, 0, s>>>(a);

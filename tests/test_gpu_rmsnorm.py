@@ -191,7 +191,8 @@ def test_gradient_in_place(b, d, into):
 
 # both gradients in one launch and, written over dY or of more rows or elements, in two: every number of lanes or wavefronts a row
 @pytest.mark.parametrize("b,d", [(1, 8), (1024, 8), (1025, 8), (1023, 64), (1100, 72), (1024, 136), (1500, 256), (700, 264), (1024, 1032),
-                                 (1030, 768), (100, 1544), (300, 2056), (65, 2568), (600, 3080), (9, 8192), (640, 8192), (641, 8192)])
+                                 (1030, 768), (100, 1544), (300, 2056), (65, 2568), (600, 3080), (9, 8192), (640, 8192), (641, 8192), (1, 8200), (5, 9216), (569, 9216), (570, 9216),
+                                 (3, 12296), (320, 16384), (2, 16392)])
 @pytest.mark.parametrize("over_dy", [False, True])
 def test_gradient_in_one_launch_and_in_two(b, d, over_dy):
     say(f"rmsnorm_bwd launches b={b} d={d} over_dy={over_dy}")

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(256) q8_generic_kernel(Q8Product p, int64_t ti
 // What bounds it: 52 KB of operands a k-step, which reach a compute unit at about 30 bytes a cycle in all variants tried (a ring of three
 // k-steps with smaller requests, 256 x 192 tiles with two k-steps of look-ahead 13 % slower), at the 1.46 GHz that the power management
 // leaves: 1.05 us a k-step, against 0.70 of products; and about 11 us before and after the loop of every tile (8192 tokens, 36864 x 9216:
-// 1.50 ms, 3.7 PFLOP/s dense-equivalent, matrix pipes 52 % busy).
+// 1.52 ms, 3.7 PFLOP/s dense-equivalent, matrix pipes 52 % busy).
 template <int BM, int BN>
 struct Q8Smem {
     static constexpr int A = BM * 128, B = BN * 128, M = BM * 64;         // a pair of W, a k-step of tokens, a block of metadata

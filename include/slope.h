@@ -405,7 +405,7 @@ typedef struct {
  * slope_adamw_step
  *   control_or_null  as written by slope_grad_norm: c, t and whether the step is left out (nothing is written then) come from
  *            there, so that the host need not wait; NULL: c = grad_scale and t = step >= 1
- *   lr >= 0; 0 <= beta < 1; eps > 0; all finite (SLOPE_ERR_VALUE)
+ *   lr >= 0, finite; 0 <= beta < 1; 2^-126 <= eps <= 2^125, so that 1 / eps is a normal number too (SLOPE_ERR_VALUE)
  */
 size_t slope_adamw_table_bytes(const slope_adamw_tensor* tensors, int64_t count);
 slope_status slope_adamw_table(const slope_adamw_tensor* tensors, int64_t count, int state_bits, void* table, size_t table_bytes);

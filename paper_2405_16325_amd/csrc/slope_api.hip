@@ -554,6 +554,9 @@ slope_status slope_spmm_fwd_q8(const void* Xq, const void* x_scale, int64_t b, c
                                  (float*)workspace_or_null, (hipStream_t)stream));
 }
 
+// the step takes reciprocals of root + eps by an instruction that knows normal numbers only: neither they nor their reciprocals
+// may be subnormal (a root is below 2^77, a bias correction included)
+constexpr float ADAMW_EPS_MIN = 0x1p-126f, ADAMW_EPS_MAX = 0x1p125f;
 // a set's tensors have 32-bit numbers, and so do a tensor's chunks
 constexpr int64_t ADAMW_TENSORS_MAX = (int64_t)1 << 24, ADAMW_ELEMENTS_MAX = (int64_t)1 << 40;
 
@@ -618,7 +621,7 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
     if (e != SLOPE_OK) return e;
     if (misaligned(control_or_null, 16)) return SLOPE_ERR_ALIGN;
     const bool betas = beta1 >= 0.0 && (float)beta1 < 1.0f && beta2 >= 0.0 && (float)beta2 < 1.0f;
-    if (!betas || !(lr >= 0.0 && (float)lr < INFINITY) || !((float)eps > 0.0f && (float)eps < INFINITY)) return SLOPE_ERR_VALUE;
+    if (!betas || !(lr >= 0.0 && (float)lr < INFINITY) || !((float)eps >= ADAMW_EPS_MIN && (float)eps <= ADAMW_EPS_MAX)) return SLOPE_ERR_VALUE;
     // steps are counted in fp32
     if (!control_or_null && (step < 1 || step > (1 << 24) || !(fabs(grad_scale) < INFINITY))) return SLOPE_ERR_VALUE;
     return finish(launch_adamw(table, device_table, lr, beta1, beta2, eps, grad_scale, step, (const float*)control_or_null,

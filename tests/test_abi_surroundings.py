@@ -168,3 +168,11 @@ def test_binding_refuses_what_the_library_cannot_see():
         sl.slope_adamw_plan([g], [g.half()], [g], [g])
     with pytest.raises(ValueError, match="device"):
         sl.slope_adamw_plan(None, [g], [g], [g], masters=[g])
+
+
+@pytest.mark.parametrize("eps", [1e-39, 1e-44, 2.0 ** -126 - 2.0 ** -149, 2.0 ** 125 * (1 + 2.0 ** -23), 3e38])
+def test_an_optimizer_eps_whose_reciprocal_fp32_does_not_hold(eps):
+    """Below the smallest normal number the step's reciprocal is infinite, and an element without a gradient became 0 x infinity;
+    past 2^126 it is subnormal and would be taken for zero."""
+    _, host, _ = table_of(tensor())
+    assert call("slope_adamw_step", STEP, table=host.data_ptr(), eps=eps) == sl.SLOPE_ERR_VALUE

@@ -249,3 +249,20 @@ def test_many_steps_reach_a_minimum_with_either_kind_of_state():
             sl.slope_adamw_step(plan, 1e-2 * (1 - t / 1001), B1, 0.99, EPS, step=t)
         ends[bits] = float((0.5 * curve * w * w).sum())
     assert ends[32] < 1e-2 and ends[8] < max(2 * ends[32], 1e-2), ends
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 2.0 ** 125])
+def test_elements_without_a_gradient_at_the_ends_of_eps(bits, eps):
+    """Zero gradients on zero states: 0 / eps leaves the weights to their decay, p (1 - lr wd) rounded to fp32 and then to bf16."""
+    say(f"adamw bits={bits} eps={eps}")
+    s = Set([300, 4097], bits, True, 32, seed=12)
+    for t in s.grads + s.dm + s.dv:
+        t.view(torch.uint8).zero_()
+    sl.slope_adamw_step(s.plan, LR, B1, B2, eps, step=1)
+    torch.cuda.synchronize()
+    for p, decay, master, param in zip(s.p, s.decay, s.masters, s.params):
+        want = p.astype(np.float64) * (1.0 - LR * decay)
+        assert (np.abs(master.cpu().numpy() - want) <= 2.0 ** -22 * np.abs(want)).all()
+        assert (np.abs(so.bf16_to_f64(sl.bf16_to_host(param)) - want) <= 2.0 ** -8 * 1.01 * np.abs(want)).all()
+    assert all((t.view(torch.uint8) & (0x7F if bits == 8 else 0xFF) == 0).all() for t in s.dm + s.dv)

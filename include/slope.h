@@ -404,7 +404,7 @@ typedef struct {
  *   workspace  slope_grad_norm_workspace_bytes(table) bytes, 256-byte aligned
  * slope_adamw_step
  *   control_or_null  as written by slope_grad_norm: c, t and whether the step is left out (nothing is written then) come from
- *            there, so that the host need not wait; NULL: c = grad_scale and t = step >= 1
+ *            there, so that the host need not wait; NULL: c = grad_scale, finite in fp32, and t = step, 1 to 2^24
  *   lr >= 0, finite; 0 <= beta < 1; 2^-126 <= eps <= 2^125, so that 1 / eps is a normal number too (SLOPE_ERR_VALUE)
  */
 size_t slope_adamw_table_bytes(const slope_adamw_tensor* tensors, int64_t count);

@@ -623,7 +623,7 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
     const bool betas = beta1 >= 0.0 && (float)beta1 < 1.0f && beta2 >= 0.0 && (float)beta2 < 1.0f;
     if (!betas || !(lr >= 0.0 && (float)lr < INFINITY) || !((float)eps >= ADAMW_EPS_MIN && (float)eps <= ADAMW_EPS_MAX)) return SLOPE_ERR_VALUE;
     // steps are counted in fp32
-    if (!control_or_null && (step < 1 || step > (1 << 24) || !(fabs(grad_scale) < INFINITY))) return SLOPE_ERR_VALUE;
+    if (!control_or_null && (step < 1 || step > (1 << 24) || !(fabsf((float)grad_scale) < INFINITY))) return SLOPE_ERR_VALUE;
     return finish(launch_adamw(table, device_table, lr, beta1, beta2, eps, grad_scale, step, (const float*)control_or_null,
                                (hipStream_t)stream));
 }

@@ -176,3 +176,9 @@ def test_an_optimizer_eps_whose_reciprocal_fp32_does_not_hold(eps):
     past 2^126 it is subnormal and would be taken for zero."""
     _, host, _ = table_of(tensor())
     assert call("slope_adamw_step", STEP, table=host.data_ptr(), eps=eps) == sl.SLOPE_ERR_VALUE
+
+
+@pytest.mark.parametrize("scale", [3.5e38, -3.5e38, 1e300])
+def test_a_gradient_scale_that_is_infinite_in_fp32(scale):
+    _, host, _ = table_of(tensor())
+    assert call("slope_adamw_step", STEP, table=host.data_ptr(), scale=scale) == sl.SLOPE_ERR_VALUE

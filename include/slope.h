@@ -438,6 +438,17 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
 slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t r, int with_workspace, int32_t* plan);
 
 /*
+ * slope_spmm_fwd_q8_plan - the same for slope_spmm_fwd_q8.  plan: host int32[7]
+ *   [0] product: 0 streaming kernel (one pass over the packed weight), 1 tile kernel, 2 general kernel
+ *   [1], [2] weight rows and tokens per workgroup
+ *   [3] slabs of the contraction (1 = no split), whose sums a second launch adds
+ *   [4] first weight rows that whole rounds of 256 x 256 tiles take, in a launch before (0 = none)
+ *   [5] columns of the padded copies that the call makes of its operands (0 = none)
+ *   [6] workgroups, of 256 threads, along the first dimension of the product's grid
+ */
+slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int with_workspace, int32_t* plan);
+
+/*
  * slope_tile_order - diagnostics, host only (no GPU call): the workgroup -> tile assignment the
  * MFMA tile kernels use for a grid of tiles_m x tiles_n tiles (the XCD-aware order behind the
  * products of Eq. 1, 4-6).  Workgroup w of the launch computes tile (tm[w], tn[w]); -1 in both

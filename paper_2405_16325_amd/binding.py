@@ -76,6 +76,7 @@ SIGNATURES = {
     "slope_ceiling": (_INT, [_INT, _P, _SZ, _INT, _P, _P]),
     "slope_tile_order": (_I64, [_I64, _I64, _P, _P, _I64]),
     "slope_spmm_fwd_plan": (_INT, [_I64, _I64, _I64, _I64, _INT, _P]),
+    "slope_spmm_fwd_q8_plan": (_INT, [_I64, _I64, _I64, _INT, _P]),
 }
 
 _lib = None
@@ -673,3 +674,11 @@ def slope_spmm_fwd_plan(b: int, d_in: int, d_out: int, r: int = 0, with_workspac
     _check("slope_spmm_fwd_plan", lib().slope_spmm_fwd_plan(b, d_in, d_out, r, int(with_workspace), plan.ctypes.data))
     names = ["product", "rows", "tokens", "slabs", "xl", "xl_chunks"]
     return dict(zip(names, (int(v) for v in plan)))
+
+
+def slope_spmm_fwd_q8_plan(b: int, d_in: int, d_out: int, with_workspace: bool = True):
+    """Kernels slope_spmm_fwd_q8 would launch for a shape (host only): dict of the seven plan fields."""
+    import numpy as np
+    plan = np.zeros(7, dtype=np.int32)
+    _check("slope_spmm_fwd_q8_plan", lib().slope_spmm_fwd_q8_plan(b, d_in, d_out, int(with_workspace), plan.ctypes.data))
+    return dict(zip(["product", "rows", "tokens", "slabs", "rows0", "padded", "groups"], (int(v) for v in plan)))

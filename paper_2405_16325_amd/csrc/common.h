@@ -150,6 +150,7 @@ hipError_t launch_quantize_packed(const bf16_t* vals, int64_t rows, int64_t cols
 size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K);
 hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,
                           int64_t m, int64_t K, const bf16_t* add, bf16_t* y, float* partial_or_null, hipStream_t s);
+void spmm_q8_plan(int64_t n, int64_t m, int64_t K, bool workspace, int32_t* plan);   // the seven fields of slope_spmm_fwd_q8_plan
 int64_t adamw_chunks(const slope_adamw_tensor* tensors, int64_t count);
 size_t adamw_table_bytes(int64_t count, int64_t chunks);
 void adamw_fill_table(const slope_adamw_tensor* tensors, int64_t count, int state_bits, void* table);

@@ -554,6 +554,13 @@ slope_status slope_spmm_fwd_q8(const void* Xq, const void* x_scale, int64_t b, c
                                  (float*)workspace_or_null, (hipStream_t)stream));
 }
 
+slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int with_workspace, int32_t* plan) {
+    if (!plan) return SLOPE_ERR_NULL;
+    if (bad_layer(b, d_out, d_in)) return SLOPE_ERR_SHAPE;
+    spmm_q8_plan(b, d_out, d_in, with_workspace != 0, plan);
+    return SLOPE_OK;
+}
+
 // the step takes reciprocals of root + eps by an instruction that knows normal numbers only: neither they nor their reciprocals
 // may be subnormal (a root is below 2^77, a bias correction included)
 constexpr float ADAMW_EPS_MIN = 0x1p-126f, ADAMW_EPS_MAX = 0x1p125f;

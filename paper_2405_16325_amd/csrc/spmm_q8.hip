@@ -689,6 +689,12 @@ double tiles_us(const Q8Tile& t, int64_t count, int steps) {
 // slabs of `steps` k-steps (stream: stretches)
 // rows0: the first rows, on 256 x 256 tiles in whole rounds of the chip, where the others go to bm x bn
 struct Q8Plan { bool stream; int bm, bn, slabs, steps, total; int64_t rows0; };
+// workgroups along the first dimension of its product's grid (without the whole rounds of rows0)
+int64_t q8_groups(const Q8Plan& p, int64_t n, int64_t m) {
+    if (p.stream) return (m + 31) / 32;
+    if (p.bm == 0) return grid_of((m + 31) / 32 * ((n + 31) / 32)).x;
+    return q8_grid((int)((m - p.rows0 + p.bm - 1) / p.bm), (int)((n + p.bn - 1) / p.bn), p.slabs);
+}
 Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
     if (stream_fits(n, m, K)) {
         Q8Plan plan = {true, 32, n <= 4 ? 4 : 8, 1, 0, (int)((K + 255) / 256), 0};
@@ -759,6 +765,18 @@ size_t spmm_q8_workspace_bytes(int64_t n, int64_t m, int64_t K) {
     const Q8Pad pad = q8_pad(n, m, K);
     const Q8Plan plan = q8_plan(n, m, pad.Kp ? pad.Kp : K, true);
     return pad.a + pad.am + pad.x + (plan.slabs > 1 ? (size_t)plan.slabs * (size_t)n * (size_t)m * 4 : 0);
+}
+
+void spmm_q8_plan(int64_t n, int64_t m, int64_t K, bool workspace, int32_t* plan) {
+    const Q8Pad pad = workspace ? q8_pad(n, m, K) : Q8Pad{0, 0, 0, 0};
+    const Q8Plan p = q8_plan(n, m, pad.Kp ? pad.Kp : K, workspace);
+    plan[0] = p.stream ? 0 : p.bm != 0 ? 1 : 2;
+    plan[1] = p.bm != 0 ? p.bm : 32;
+    plan[2] = p.bm != 0 ? p.bn : 32;
+    plan[3] = p.slabs;
+    plan[4] = (int32_t)p.rows0;
+    plan[5] = (int32_t)pad.Kp;
+    plan[6] = (int32_t)q8_groups(p, n, m);
 }
 
 hipError_t launch_spmm_q8(const uint8_t* x, const float* xs, int64_t n, const uint8_t* a, const uint8_t* am, const float* as,

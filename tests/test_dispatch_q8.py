@@ -1,0 +1,48 @@
+"""Host logic: which kernels slope_spmm_fwd_q8 picks for a shape (slope_spmm_fwd_q8_plan, no GPU needed).  The choices are estimates
+of time over the shape alone; pinned here is that the shapes of the GPU tests reach every kernel in every form."""
+import pytest
+
+from paper_2405_16325_amd import binding as sl
+from tests import test_gpu_spmm_q8 as gpu
+
+STREAM, TILE, GENERAL = range(3)
+KSTEP = 128
+
+
+def form(p):
+    return "rows left" if p["rows0"] else "slabs" if p["slabs"] > 1 else "whole"
+
+
+def test_the_gpu_tests_tiles_are_every_tile_in_every_form():
+    reached = set()
+    for b, d_out, d_in in gpu.TILES:
+        p = sl.slope_spmm_fwd_q8_plan(b, d_in, d_out)
+        assert p["product"] == TILE and p["padded"] == 0, (b, d_out, d_in)
+        reached.add((p["rows"], p["tokens"], form(p), d_in % KSTEP != 0))
+    want = {(rows, tokens, f, tail) for rows, tokens in ((128, 32), (128, 64), (128, 128), (256, 256)) for f in ("whole", "slabs")
+            for tail in (False, True)}
+    want |= {(128, tokens, "rows left", tail) for tokens in (64, 128) for tail in (False, True)}
+    assert reached == want
+
+
+def test_the_gpu_tests_ordinary_shapes_reach_all_kinds():
+    plans = [sl.slope_spmm_fwd_q8_plan(b, d_in, d_out) for b, d_out, d_in in gpu.SHAPES]
+    assert {p["product"] for p in plans} == {STREAM, TILE, GENERAL}
+    assert {p["tokens"] for p in plans if p["product"] == STREAM} == {4, 8}
+    assert any(p["padded"] for p in plans)
+
+
+@pytest.mark.parametrize("b,d_in,d_out", [(1, 9216, 36864), (4, 5120, 5120), (8, 9216, 9216), (777, 5120, 20480), (128, 4096, 512), (33, 1000, 1000)])
+def test_without_a_workspace_nothing_is_split_or_copied(b, d_in, d_out):
+    p = sl.slope_spmm_fwd_q8_plan(b, d_in, d_out, False)
+    assert p["slabs"] == 1 and p["padded"] == 0
+    if sl.slope_workspace_bytes(sl.SLOPE_CALL_SPMM_FWD_Q8, b, d_in, d_out) == 0:
+        assert p == sl.slope_spmm_fwd_q8_plan(b, d_in, d_out)
+
+
+def test_refusals():
+    with pytest.raises(sl.SlopeError):
+        sl.slope_spmm_fwd_q8_plan(0, 64, 64)
+    with pytest.raises(sl.SlopeError):
+        sl.slope_spmm_fwd_q8_plan(1, 64, 12)
+    assert sl.lib().slope_spmm_fwd_q8_plan(1, 64, 64, 1, None) == sl.SLOPE_ERR_NULL

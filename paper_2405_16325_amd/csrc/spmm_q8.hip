@@ -626,9 +626,12 @@ hipError_t launch_quantize_packed(const bf16_t* vals, int64_t rows, int64_t cols
 
 namespace {
 
-// 32-bit offsets inside a tile's rows, and a grid of fewer than 2^32 work items
+// workgroups of 256 along a dimension of a grid, which holds fewer than 2^32 work items
+constexpr int64_t GROUPS_END = (int64_t)1 << 24;
+// 32-bit offsets inside a tile's rows, and tiles whose number, rounded up to a grid, is an int.  (Of the tiles that a plan may take
+// 128 x 32 can be twice as many as are counted here: the plan looks at each one's grid.)
 bool tile_fits(int64_t n, int64_t m, int64_t K) {
-    return K % 64 == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < ((int64_t)1 << 23);
+    return K % 64 == 0 && K < ((int64_t)1 << 23) && (m + 127) / 128 * ((n + 63) / 64) < GROUPS_END / 2;
 }
 
 template <int BM, int BN, int WM, bool TAIL>
@@ -651,7 +654,7 @@ hipError_t launch_tiles(const Q8Product& p, const Q8Split& split, hipStream_t s)
 constexpr int64_t PAD_WORK = (int64_t)1 << 30;
 // (us, stream / best of the tiles: 4 tokens, 36864 x 9216 34.8 / 49.1, 5120 x 5120 8.4 / 10.6; 8 tokens 40.7 / 49.4, 9.6 / 10.8)
 constexpr int STREAM_WAVES = 4, STREAM_STAGES = 3, STREAM_GROUPS = 1024, STREAM_TOKENS = 8;
-bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && m < ((int64_t)1 << 29); }
+bool stream_fits(int64_t n, int64_t m, int64_t K) { return n <= STREAM_TOKENS && K % 32 == 0 && K < ((int64_t)1 << 23) && (m + 31) / 32 < GROUPS_END; }
 
 template <int TOK>
 hipError_t launch_stream(const Q8Product& p, const Q8Split& split, hipStream_t s) {
@@ -715,8 +718,10 @@ Q8Plan q8_plan(int64_t n, int64_t m, int64_t K, bool room) {
     double best = 0.0;
     auto consider = [&](double us, const Q8Tile& t, int slabs, int steps, int64_t rows0) {
         if (plan.bm != 0 && us >= best) return;
+        const Q8Plan p = {false, t.bm, t.bn, slabs, steps, total, rows0};
+        if (q8_groups(p, n, m) >= GROUPS_END) return;
         best = us;
-        plan = {false, t.bm, t.bn, slabs, steps, total, rows0};
+        plan = p;
     };
     for (const Q8Tile& t : Q8_TILES) {
         if (t.bn > 32 && t.bn >= 2 * n) continue;                // more than half of it empty

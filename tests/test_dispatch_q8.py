@@ -46,3 +46,19 @@ def test_refusals():
     with pytest.raises(sl.SlopeError):
         sl.slope_spmm_fwd_q8_plan(1, 64, 12)
     assert sl.lib().slope_spmm_fwd_q8_plan(1, 64, 64, 1, None) == sl.SLOPE_ERR_NULL
+
+
+# A dimension of a grid holds fewer than 2^32 work items, here 2^24 workgroups of 256; a launch beyond that runs a part of them
+# without an error.  Rows: the most that stay below it by the streaming kernel and by 128 x 32 tiles, and what lies around them.
+@pytest.mark.parametrize("b,d_in,d_out", [(b, d_in, m + 8 * off) for b, d_in, m in ((1, 32, 2 ** 29 - 32), (8, 64, 2 ** 29 - 32), (40, 64, 2 ** 30 - 128),
+                                                                              (64, 128, 2 ** 30 - 128), (96, 64, 2 ** 29), (16, 64, 2 ** 30))
+                                          for off in (-2 ** 20, -9, -1, 0, 1, 3, 4, 9, 16, 17)])
+@pytest.mark.parametrize("with_workspace", [False, True])
+def test_no_grid_passes_what_a_launch_holds(b, d_in, d_out, with_workspace):
+    p = sl.slope_spmm_fwd_q8_plan(b, d_in, d_out, with_workspace)
+    assert p["groups"] < 2 ** 24, p
+
+
+def test_the_last_shapes_of_the_streaming_kernel():
+    assert sl.slope_spmm_fwd_q8_plan(1, 32, 2 ** 29 - 32)["product"] == STREAM
+    assert sl.slope_spmm_fwd_q8_plan(1, 32, 2 ** 29 - 24)["product"] != STREAM

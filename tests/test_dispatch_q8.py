@@ -32,6 +32,21 @@ def test_the_gpu_tests_ordinary_shapes_reach_all_kinds():
     assert any(p["padded"] for p in plans)
 
 
+def test_the_gpu_tests_few_tokens_are_in_slabs():
+    plans = [(sl.slope_spmm_fwd_q8_plan(b, d_in, d_out), d_in) for b, d_out, d_in in gpu.STREAM_SLABS]
+    assert all(p["product"] == STREAM and p["slabs"] > 1 for p, _ in plans)
+    assert {(p["tokens"], d_in % 256 != 0) for p, d_in in plans} == {(t, tail) for t in (4, 8) for tail in (False, True)}
+    assert min(p["slabs"] for p, _ in plans) == 2 and max(p["slabs"] for p, _ in plans) >= 8
+    assert any(-(-d_in // 256) % p["slabs"] for p, d_in in plans)                      # a short last slab
+
+
+def test_the_gpu_tests_padded_copies_feed_every_kernel():
+    plans = [sl.slope_spmm_fwd_q8_plan(b, d_in, d_out) for b, d_out, d_in in gpu.PADDED]
+    assert all(p["padded"] for p in plans)
+    assert {(p["rows"], p["tokens"]) for p in plans} == {(32, 4), (32, 8), (128, 32), (128, 64), (128, 128), (256, 256)}
+    assert {form(p) for p in plans} == {"whole", "slabs", "rows left"}
+
+
 @pytest.mark.parametrize("b,d_in,d_out", [(1, 9216, 36864), (4, 5120, 5120), (8, 9216, 9216), (777, 5120, 20480), (128, 4096, 512), (33, 1000, 1000)])
 def test_without_a_workspace_nothing_is_split_or_copied(b, d_in, d_out):
     p = sl.slope_spmm_fwd_q8_plan(b, d_in, d_out, False)

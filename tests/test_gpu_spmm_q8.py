@@ -168,3 +168,38 @@ def test_norm_and_product_agree_with_the_16_bit_path():
     want = sl.slope_spmm_fwd(yn, vals, meta).float()
     got = sl.slope_spmm_fwd_q8(q, s, *(lambda wq, ws: (wq, meta, ws))(*sl.slope_quantize_packed(vals))).float()
     assert float((got - want).norm() / want.norm()) < 2.0 ** -4 / 3 ** 0.5 * 2 ** 0.5
+
+
+# the streaming kernel with its contraction in slabs: 2 to 8 of them, the last shorter; contractions that end with a stretch of 256 and
+# inside one; fewer tokens than the kernel has places for
+STREAM_SLABS = [(1, 5120, 5120), (4, 1032, 8192), (3, 520, 9248), (2, 40, 4128), (8, 264, 16416), (5, 776, 12288), (7, 2056, 4000)]
+
+
+@pytest.mark.parametrize("b,d_out,d_in", STREAM_SLABS)
+@pytest.mark.parametrize("add", ["none", "apart", "in place"])
+def test_few_tokens_in_slabs(b, d_out, d_in, add):
+    say(f"spmm_fwd_q8 few tokens in slabs b={b} d_out={d_out} d_in={d_in} add={add}")
+    _, _, meta, q, xs, dev = make(b, d_out, d_in, seed=b + d_out + d_in)
+    bits = inputs.gaussian_bf16((b, d_out), 1.0, b, 9)
+    term = None if add == "none" else sl.bf16_to_device(bits)
+    args = (dev["q"], dev["xs"], dev["wq"], dev["meta"], dev["ws"])
+    # memory that held something else, of exactly the size asked for
+    ws = torch.full((sl.slope_workspace_bytes(sl.SLOPE_CALL_SPMM_FWD_Q8, b, d_in, d_out),), 0xFF, dtype=torch.uint8, device="cuda")
+    again = sl.slope_spmm_fwd_q8(*args, add=term, workspace=ws)
+    y = sl.slope_spmm_fwd_q8(*args, add=term, out=term if add == "in place" else None)
+    torch.cuda.synchronize()
+    check(y, q, xs, dev, meta, None if term is None else so.bf16_to_f64(bits))
+    assert torch.equal(y, again)
+
+
+# rows that are no multiple of 64, copied into padded ones: for the streaming kernel, every tile, whole, in slabs and with rows left
+PADDED = [(4, 12504, 22416), (7, 6760, 23000), (8, 6496, 20792), (220, 6104, 800), (63, 1568, 10888), (625, 80, 21480), (605, 4728, 376),
+          (597, 5768, 312), (65, 952, 17368), (710, 72, 21016), (772, 6960, 200), (1189, 5136, 176), (1685, 40, 16376),
+          (2018, 32, 16920), (935, 8968, 1368), (1303, 7480, 1192), (936, 16856, 2168), (2482, 8080, 2744)]
+
+
+@pytest.mark.parametrize("b,d_out,d_in", PADDED)
+@pytest.mark.parametrize("with_add", [False, True])
+def test_padded_copies_for_every_kernel(b, d_out, d_in, with_add):
+    say(f"spmm_fwd_q8 padded b={b} d_out={d_out} d_in={d_in} add={with_add}")
+    against_a_library_product(b, d_out, d_in, with_add)

@@ -243,3 +243,68 @@ def test_graph_replays_equal_eager_calls():
         call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (fwd[0], fwd[1], fwd[3].view(torch.uint8), fwd[4], *bwd)))
+
+
+# calls that move more than the last-level cache holds go past it: every number of pieces a lane, the last workgroup's rows and the last
+# pieces of a row incomplete among them.  Compared on the device, in fp64, within the bounds of the small shapes.
+@pytest.mark.parametrize("b,d", [(4200, 8184), (4100, 9216), (2201, 16376), (1701, 20488), (1100, 32768)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_forward_past_the_last_level_cache(b, d, residual):
+    assert b * d * (5 + (4 if residual else 0)) > 256 << 20 or not residual
+    say(f"rmsnorm_fwd past the caches b={b} d={d} residual={residual}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(b + d)
+    if not residual:
+        b = (256 << 20) // (5 * d) + 1
+    x = torch.randn(b, d, generator=gen, device="cuda").to(sl.BF16)
+    res = (2 * torch.randn(b, d, generator=gen, device="cuda")).to(sl.BF16) if residual else None
+    w = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).to(sl.BF16)
+    y, H, rstd, q, scale = sl.slope_rmsnorm_fwd(x, w, EPS, residual=res, want_rstd=True, want_q8=True)
+    h = x if res is None else (x.float() + res.float()).to(sl.BF16)
+    assert H is None if res is None else torch.equal(H, h)
+    for at in range(0, b, 1000):
+        rows = slice(at, at + 1000)
+        want = h[rows].double()
+        r = (want.square().mean(1) + EPS).rsqrt()
+        want = want * r[:, None] * w.double()
+        assert bool(((y[rows].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -16) * want.abs() + 1e-38).all())
+        assert bool(((rstd[rows].double() - r).abs() <= 2.0 ** -16 * r).all())
+        s, got = want.abs().amax(1) / 448, scale[rows].double()
+        assert bool(((got - s).abs() <= 2.0 ** -15 * s).all())
+        off = (q[rows].double() * got[:, None] - want).abs()
+        assert bool((off <= (2.0 ** -4 * want.abs() + 2.0 ** -10 * got[:, None]) * (1 + 2.0 ** -12) + 2.0 ** -14 * want.abs()).all())
+
+
+@pytest.mark.parametrize("b,d", [(4200, 8184), (4100, 9216), (2201, 16376), (1701, 20488), (1401, 24576)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_gradient_past_the_last_level_cache(b, d, residual):
+    if not residual:
+        b = (256 << 20) // (6 * d) + 1
+    assert b * d * (8 if residual else 6) > 256 << 20
+    say(f"rmsnorm_bwd past the caches b={b} d={d} residual={residual}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(b + d + 1)
+    h = (2 * torch.randn(b, d, generator=gen, device="cuda")).to(sl.BF16)
+    dy = (1e-3 * torch.randn(b, d, generator=gen, device="cuda")).to(sl.BF16)
+    dh = (1e-3 * torch.randn(b, d, generator=gen, device="cuda")).to(sl.BF16) if residual else None
+    w = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).to(sl.BF16)
+    rstd = (h.float().square().mean(1) + EPS).rsqrt()
+    dx, dw = sl.slope_rmsnorm_bwd(dy, h, w, rstd, dh=dh)
+    want_dw, terms_dw = torch.zeros(d, dtype=torch.float64, device="cuda"), torch.zeros(d, dtype=torch.float64, device="cuda")
+    for at in range(0, b, 1000):
+        rows = slice(at, at + 1000)
+        r = rstd[rows].double()[:, None]
+        dyv, xh = dy[rows].double(), h[rows].double() * r
+        g = dyv * w.double()
+        want = r * (g - xh * (g * xh).mean(1, keepdim=True))
+        terms = r * (g.abs() + xh.abs() * (g * xh).abs().mean(1, keepdim=True))
+        if residual:
+            want, terms = want + dh[rows].double(), terms + dh[rows].double().abs()
+        assert bool(((dx[rows].double() - want).abs() <= (2.0 ** -8 + 2.0 ** -16) * want.abs() + 2.0 ** -16 * terms).all())
+        want_dw += (dyv * xh).sum(0)
+        terms_dw += (dyv * xh).abs().sum(0)
+    assert bool(((dw.double() - want_dw).abs() <= (2.0 ** -8 + 2.0 ** -16) * want_dw.abs() + 2.0 ** -16 * terms_dw).all())
+    dw2 = torch.empty_like(dw)
+    sl.slope_rmsnorm_bwd(dy, h, w, rstd, dh=dh, out=(dy, dw2))
+    torch.cuda.synchronize()
+    assert torch.equal(dy, dx) and torch.equal(dw, dw2)

@@ -79,12 +79,3 @@ __device__ __forceinline__ u32x2 pack_e4m3(const F8& x) {
     return o;
 }
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ F8 unpack_e4m3(u32x2 p) {
-    F8 o;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)p[i], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)p[i], true);
-        o.v[4 * i] = a[0]; o.v[4 * i + 1] = a[1]; o.v[4 * i + 2] = b[0]; o.v[4 * i + 3] = b[1];
-    }
-    return o;
-}

@@ -320,7 +320,8 @@ slope_status slope_update_sparse(const void* Wnew_vals, const void* Wr_meta, int
  *
  * slope_rmsnorm_fwd - residual addition and root-mean-square norm over the d elements of each of b tokens:
  *     H = bf16(X + residual) (H is X without a residual)    r = 1 / sqrt(mean(H^2) + eps)    y = H r weight
- * The statistics are those of H as it is stored; all sums are fp32.
+ * The statistics are those of H as it is stored; all sums are fp32.  A row whose sum of squares passes fp32 (elements beyond
+ * about 1e19) has r = 0 and y = 0.
  *   X, residual_or_null in bf16[b, d]    weight in bf16[d]
  *   H_or_null     out bf16[b, d]  the summed stream; required with a residual, NULL without; may be X or the residual.
  *                     No other output may overlap an input.
@@ -398,6 +399,8 @@ typedef struct {
  *
  * slope_grad_norm - the global norm of a set's gradients, for clipping and for leaving out steps that are not finite:
  *     norm = inv_scale sqrt(sum grad^2)    c = inv_scale min(1, max_norm / (norm + 1e-6))
+ *   Squares are summed in fp32 within a workgroup, in fp64 over the workgroups: gradients beyond about 1e19, whose v fp32 would
+ *   not hold either, make a norm that is not finite, and squares below fp32's smallest number count as zero.
  *   control  in/out fp32[4], device: {norm, c (0 if norm is not finite), steps taken (incremented if norm is finite), unused};
  *            starts as zeros
  *   inv_scale  1 / loss scale, > 0;  max_norm  > 0, infinity: no clipping

@@ -191,7 +191,8 @@ __device__ __forceinline__ Raw<8, W> to_codes(const Vec<W>& x, uint32_t u, GLOBA
     return o;
 }
 
-// Square roots, exactly rounded: the hardware's is off by one unit at most, and the residuals of its neighbours tell.  (Zeros, infinities
+// Square roots, exactly rounded: the hardware's is off by one unit at most, and the residuals of its neighbours tell (P. W. Markstein,
+// Computation of elementary functions on the IBM RISC System/6000 processor, IBM J. Res. Dev. 34, 1990: the final rounding of a root).  (Zeros, infinities
 // and NaN stay as they are: their residuals are no numbers, or zero.)  Below 2^-96 residuals would vanish: the compiler's form for all then.
 template <int W>
 __device__ __forceinline__ Vec<W> roots(const Vec<W>& x) {

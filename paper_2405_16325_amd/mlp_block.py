@@ -1,4 +1,5 @@
-"""A stack of pre-norm blocks of double-pruned layers, trained with AdamW and served in 8 bits, by the library's calls alone.
+"""A stack of pre-norm blocks of double-pruned layers, trained with AdamW and served in 8 bits, by the library's calls; the
+relu, its gradient and the loss are torch's.
 
     block:  h <- h + W2 norm2(relu(W1 norm1(h)))          W1, W2: packed 2:4 (W^R forward, W^{R,C} backward)
     out  =  norm(h)

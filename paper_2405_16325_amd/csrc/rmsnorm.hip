@@ -6,8 +6,9 @@
 //
 // The statistics are those of the stream as it is stored, rounded: the gradient is taken at that h.  All sums are fp32.
 // Memory bounds both directions (16384 x 9216 with the residual: forward 195 us, 6.2 TB/s, gradient 203, 6.0 TB/s), latency a few hundred
-// rows (777 x 5120, 28 MB from memory to an 8-bit output: 10.4 us, of which 2.8 are what one row takes).  A row is read once and stays in registers: LPR lanes (8 to 64) of a wavefront share a
-// short one, `wpr` wavefronts a longer one; a lane holds VPT pieces of 8 neighbouring elements, so that every load and
+// rows (777 x 5120, 28 MB from memory to an 8-bit output: 10.4 to 11.7 us, of which 2.6 are what one row takes; a row has ten
+// wavefronts here, a compute unit room for three rows, so nine rows take a second turn).  A row is read once and stays in
+// registers: LPR lanes (8 to 64) of a wavefront share a short one, `wpr` wavefronts a longer one; a lane holds VPT pieces of 8 neighbouring elements, so that every load and
 // store of a wavefront covers whole 128-byte lines.
 #include "pipeline.h"
 #include "wave.h"

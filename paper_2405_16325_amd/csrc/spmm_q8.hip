@@ -3,7 +3,8 @@
 //     Y[b, d_out] = bf16( x_scale[b] w_scale[d_out] sum_k X[b, k] W[d_out, k]  (+ add[b, d_out]) ),
 //
 // X in e4m3 with a scale per token (what the norm writes), W packed 2:4 in e4m3 with a scale per row, its metadata as it is.
-// v_smfmac_f32_16x16x128_fp8_fp8 multiplies 16 rows of W by 16 tokens over 128 logical k; lane l holds
+// v_smfmac_f32_16x16x128_fp8_fp8, in the general kernel below (the others take the 32 x 32 x 64 form; in register loops on Gaussian operands 7.3
+// and 5.3 PFLOP/s dense-equivalent), multiplies 16 rows of W by 16 tokens over 128 logical k; lane l holds
 //     of W  row l % 16, packed bytes 16 (l / 16) .. + 15 (logical k 32 (l / 16) ..) and the 4 metadata bytes of that stretch,
 //     of X  token l % 16, k 16 (l / 16) .. + 15 and 64 + that,
 //     of D  token l % 16, rows 4 (l / 16) .. + 3.

@@ -401,7 +401,7 @@ typedef struct {
  *     norm = inv_scale sqrt(sum grad^2)    c = inv_scale min(1, max_norm / (norm + 1e-6))
  *   Squares are summed in fp32 within a workgroup, in fp64 over the workgroups: gradients beyond about 1e19, whose v fp32 would
  *   not hold either, make a norm that is not finite, and squares below fp32's smallest number count as zero.
- *   control  in/out fp32[4], device: {norm, c (0 if norm is not finite), steps taken (incremented if norm is finite), unused};
+ *   control  in/out fp32[4], device: {norm, c (0 if norm is not finite), steps taken (incremented if norm is finite; 2^24 at most), unused};
  *            starts as zeros
  *   inv_scale  1 / loss scale, > 0;  max_norm  > 0, infinity: no clipping
  *   workspace  slope_grad_norm_workspace_bytes(table) bytes, 256-byte aligned

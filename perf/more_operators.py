@@ -1,0 +1,383 @@
+"""The gated feed-forward layer on double-pruned 2:4 weights and activation checkpoints in 8 bits, as measurable cases.
+
+Kinds of a case:
+
+  gated      h = act(x Wg^T) * (x Wu^T) of b tokens; the weight [2 d_ff, d_in] is packed 2:4, gate rows first; optionally with
+             an adapter of rank r over all 2 d_ff columns; keep "bf16" also writes the projections for the backward pass
+  gated_bwd  its elementwise gradient from the kept projections (bf16, or 8-bit codes): the projections' gradients, and h again
+             for the next layer's weight gradient
+  step       forward that keeps the projections in 8 bits, then that gradient from the codes
+  ckpt       an activation to 8 bits and back, as a layer's backward pass reads it
+  wgrad      the packed weight gradient of a layer whose input was kept in 8 bits
+
+8-bit codes are e4m3 with a power of two for each token and 32 columns (bytes: its exponent + 127).  Widths are those of the
+layer sets of `paper_2405_16325_amd/inputs.py` and of the tests' ragged layers, d_ff 8/3 of them where a gate is usual, or
+numbers between them.  With `own` false the same results come from elementary torch operations in 32 bits.
+"""
+import math
+
+import torch
+
+own = False
+
+BF16, F32, F64, F8, U8 = torch.bfloat16, torch.float32, torch.float64, torch.float8_e4m3fn, torch.uint8
+BLOCK = 32
+ACTS = ("silu", "gelu", "relu")
+GELU_A, GELU_B = math.sqrt(2.0 / math.pi), 0.044715
+
+
+# ------------------------------------------------------------------------------------------------------------- the cases
+
+def _gated(name, b, d_ff, d_in, r, act, keep):
+    return {"name": name, "kind": "gated", "b": b, "d_ff": d_ff, "d_in": d_in, "r": r, "act": act, "keep": keep}
+
+
+def _gated_bwd(name, b, d_ff, act, q8):
+    return {"name": name, "kind": "gated_bwd", "b": b, "d_ff": d_ff, "act": act, "q8": q8}
+
+
+def _step(name, b, d_ff, d_in, act):
+    return {"name": name, "kind": "step", "b": b, "d_ff": d_ff, "d_in": d_in, "act": act}
+
+
+def _ckpt(name, b, d):
+    return {"name": name, "kind": "ckpt", "b": b, "d": d}
+
+
+def _wgrad(name, b, d_out, d_in):
+    return {"name": name, "kind": "wgrad", "b": b, "d_out": d_out, "d_in": d_in}
+
+
+def listed():
+    return [
+        # one token through the smallest layer: latency
+        _gated("gated_token_small", 1, 2048, 768, 0, "silu", "none"),
+        # one token through the largest layer: a single pass over the packed weight
+        _gated("gated_token", 1, 24576, 9216, 0, "silu", "none"),
+        # a prompt of odd length through a layer that serves with its adapter
+        _gated("gated_prompt", 777, 13648, 5120, 64, "silu", "none"),
+        # the largest training batch, projections kept as they are
+        _gated("gated_train", 16384, 24576, 9216, 0, "silu", "bf16"),
+        # a micro-batch on widths that are multiples of 8 only
+        _gated("gated_ragged", 1000, 1000, 1000, 0, "gelu", "bf16"),
+        # an ordinary training batch that keeps the projections in 8 bits, and their gradient
+        _step("gated_step_q8", 2048, 6912, 2560, "silu"),
+        # the largest training batch's gradient from 8-bit codes
+        _gated_bwd("gated_bwd_train_q8", 16384, 24576, "silu", True),
+        # a micro-batch of odd length, from bf16
+        _gated_bwd("gated_bwd_small", 333, 2048, "gelu", False),
+        # the input of the largest layer, kept and restored
+        _ckpt("ckpt_train", 16384, 9216),
+        # a micro-batch on a width that is a multiple of 8 only
+        _ckpt("ckpt_ragged", 777, 1000),
+        # the largest layer's weight gradient
+        _wgrad("wgrad_q8_train", 16384, 36864, 9216),
+        # a micro-batch on a ragged layer
+        _wgrad("wgrad_q8_ragged", 700, 4160, 2112),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return lo * (hi / lo) ** rng.random()
+
+
+def _width(rng, lo, hi, quantum):
+    w = int(_log_uniform(rng, lo, hi) / quantum + 0.5) * quantum
+    return max(quantum, min(w, hi // quantum * quantum))
+
+
+def draw(rng):
+    """One more case: kinds, token counts, widths, ranks and activations over the ranges the listed cases span."""
+    kind = rng.choice(["gated", "gated", "gated", "gated_bwd", "step", "ckpt", "wgrad", "wgrad"])
+    q = rng.choices([256, 64, 8], [4, 3, 3])[0]
+    top = {256: 9216, 64: 9216, 8: 2200}[q]
+    b, act = max(1, int(_log_uniform(rng, 1, 16384) + 0.5)), rng.choice(ACTS)
+    if kind == "gated_bwd":
+        d_ff = _width(rng, 64, 24576 if q == 256 else top, q)
+        c = _gated_bwd("", b, d_ff, act, rng.random() < 0.5)
+    elif kind == "ckpt":
+        c = _ckpt("", b, _width(rng, 64, 36864 if q == 256 else top, q))
+        c["b"] = max(1, min(b, 16384 * 9216 // c["d"]))
+    elif kind == "wgrad":
+        d_out, d_in = _width(rng, 128, 36864 if q == 256 else top, q), _width(rng, 128, top, q)
+        c = _wgrad("", b if q >= 64 else min(b, 4096), d_out, d_in)
+    else:
+        d_ff, d_in = _width(rng, 128, 24576 if q == 256 else top, q), _width(rng, 128, top, q)
+        b = b if q >= 64 else min(b, 2048)
+        c = _step("", b, d_ff, d_in, act) if kind == "step" else \
+            _gated("", b, d_ff, d_in, rng.choice([0, 0, 32, 64, 128]), act, rng.choice(["none", "none", "bf16"]))
+    del c["name"]
+    return c
+
+
+# ------------------------------------------------------------------------------------------------------------ the inputs
+
+def _pruned(vals):
+    """Packed 2:4 form of a weight: (values bf16[d_out, d_in/2], index bytes u8[d_out, d_in/8])."""
+    d_out, d_in = vals.shape
+    a = vals.abs().view(d_out, d_in // 4, 4)
+    beats = lambda i, j: a[..., j] > a[..., i] if j > i else a[..., j] >= a[..., i]      # noqa: E731
+    keep = torch.stack([sum(beats(i, j).to(U8) for j in range(4) if j != i) < 2 for i in range(4)], dim=-1)
+    first = keep.to(U8).argmax(-1)
+    last = 3 - keep.flip(-1).to(U8).argmax(-1)
+    at = torch.stack([first, last], dim=-1)
+    kept = torch.gather(vals.view(d_out, d_in // 4, 4), 2, at).reshape(d_out, d_in // 2)
+    nibble = (first | (last << 2)).to(U8).view(d_out, d_in // 8, 2)
+    return kept, (nibble[..., 0] | (nibble[..., 1] << 4)).contiguous()
+
+
+def _power(e):
+    """2^e in 32 bits for whole e from -126 to 127, from its bits: the device's pow is not exact."""
+    return ((e.to(torch.int32) + 127) << 23).view(F32)
+
+
+def _to_codes(x):
+    """x [rows, cols] -> (e4m3 codes [rows, cols], exponent bytes u8[rows, ceil(cols / 32)])."""
+    rows, cols = x.shape
+    blocks = (cols + BLOCK - 1) // BLOCK
+    x = x.float()
+    padded = x if cols == blocks * BLOCK else torch.cat([x, torch.zeros((rows, blocks * BLOCK - cols), device=x.device)], dim=1)
+    padded = padded.view(rows, blocks, BLOCK)
+    amax = padded.abs().amax(2)
+    m, e = torch.frexp(amax)
+    e = (e - 9 + (m > 0.875)).clamp_(min=-126)
+    codes = (padded * _power(-e)[..., None]).to(F8)
+    fine = torch.isfinite(amax)
+    byte = torch.where(fine, e + 127, 255).to(U8)
+    return codes.view(rows, blocks * BLOCK)[:, :cols].contiguous(), byte
+
+
+def _from_codes(codes, byte):
+    """The values, fp32[rows, cols]."""
+    rows, cols = codes.shape
+    e = byte.to(torch.int32).repeat_interleave(BLOCK, dim=1)[:, :cols]
+    return torch.where(e == 255, math.nan, codes.float() * _power(e.clamp(max=254) - 127))
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+
+    def gauss(shape, std, dtype=BF16):
+        return torch.randn(shape, generator=gen, device="cuda", dtype=F32).mul_(std).to(dtype)
+
+    kind, b = case["kind"], case["b"]
+    s = {"kind": kind, "act": case.get("act")}
+    if kind in ("gated", "step"):
+        d_ff, d_in, r = case["d_ff"], case["d_in"], case.get("r", 0)
+        s["x"] = gauss((b, d_in), 1.0)
+        s["vals"], s["meta"] = _pruned(gauss((2 * d_ff, d_in), d_in ** -0.5))
+        s["l"] = gauss((d_in, r), 0.02) if r else None
+        s["r"] = gauss((r, 2 * d_ff), 0.02) if r else None
+        s["keep"] = case.get("keep", "q8")
+        if kind == "step":
+            s["dh"] = gauss((b, d_ff), 1e-3)
+    elif kind == "gated_bwd":
+        s["dh"], gu = gauss((b, case["d_ff"]), 1e-3), gauss((b, 2 * case["d_ff"]), 1.0)
+        s["gu"], s["codes"], s["byte"] = gu, None, None
+        if case["q8"]:                           # a row of 2 d_ff columns is the gate's row and the up projection's
+            s["gu"] = None
+            s["codes"], s["byte"] = _to_codes(gu.view(2 * b, -1))
+    elif kind == "ckpt":
+        # activations behind a norm: columns of different size
+        s["x"] = (gauss((b, case["d"]), 1.0, F32) * torch.exp(gauss((case["d"],), 1.0, F32))).to(BF16)
+    else:
+        d_out, d_in = case["d_out"], case["d_in"]
+        _, s["meta"] = _pruned(gauss((d_out, d_in), 0.02))
+        s["dy"] = gauss((b, d_out), 1e-3)
+        s["codes"], s["byte"] = _to_codes(gauss((b, d_in), 1.0))
+    return s
+
+
+# -------------------------------------------------------------------------------------------------------- the plain forms
+
+def _positions(meta):
+    """Column of each packed value: int64[d_out, d_in/2]."""
+    d_out, bytes_ = meta.shape
+    m = meta.to(torch.int64)
+    idx = torch.stack([m & 3, (m >> 2) & 3, ((m >> 4) & 3) + 4, (m >> 6) + 4], dim=-1)
+    return (idx + 8 * torch.arange(bytes_, device=meta.device)[:, None]).view(d_out, -1)
+
+
+def _plain_act(g, act):
+    """(act(g), act'(g)) in 32 bits."""
+    if act == "relu":
+        on = (g > 0).float()
+        return g * on, on
+    if act == "silu":
+        s = 1.0 / (1.0 + torch.exp(-g))
+        return g * s, s * (1.0 + g * (1.0 - s))
+    s = 1.0 / (1.0 + torch.exp(-2.0 * GELU_A * (g + GELU_B * g * g * g)))
+    return g * s, s + g * s * (1.0 - s) * (2.0 * GELU_A) * (1.0 + 3.0 * GELU_B * g * g)
+
+
+def _plain_projections(s):
+    d_out, half = s["vals"].shape
+    w = torch.zeros((d_out, 2 * half), device="cuda", dtype=F32)
+    w.scatter_(1, _positions(s["meta"]), s["vals"].float())
+    gu = torch.matmul(s["x"].float(), w.t())
+    if s["l"] is not None:
+        gu += torch.matmul(torch.matmul(s["x"].float(), s["l"].float()), s["r"].float())
+    return gu
+
+
+def _plain_bwd(dh, g, u, act):
+    a, d = _plain_act(g, act)
+    dh = dh.float()
+    return {"dgu": torch.cat([dh * u * d, dh * a], dim=1).to(BF16), "h": (a * u).to(BF16)}
+
+
+def _plain(s):
+    kind = s["kind"]
+    if kind in ("gated", "step"):
+        gu = _plain_projections(s)
+        b, d_ff = gu.shape[0], gu.shape[1] // 2
+        g, u = gu[:, :d_ff], gu[:, d_ff:]
+        h = (_plain_act(g, s["act"])[0] * u).to(BF16)
+        if kind == "step":
+            kept = _from_codes(*_to_codes(gu.view(2 * b, d_ff))).view(b, 2 * d_ff)
+            got = _plain_bwd(s["dh"], kept[:, :d_ff], kept[:, d_ff:], s["act"])
+            return {"h": h, "dgu": got["dgu"], "h_again": got["h"]}
+        return {"h": h, "gu": gu.to(BF16)} if s["keep"] == "bf16" else {"h": h}
+    if kind == "gated_bwd":
+        b, d_ff = s["dh"].shape
+        gu = s["gu"].float() if s["gu"] is not None else _from_codes(s["codes"], s["byte"]).view(b, 2 * d_ff)
+        return _plain_bwd(s["dh"], gu[:, :d_ff], gu[:, d_ff:], s["act"])
+    if kind == "ckpt":
+        return _from_codes(*_to_codes(s["x"])).to(BF16)
+    dw = torch.matmul(s["dy"].float().t(), _from_codes(s["codes"], s["byte"]))
+    return torch.gather(dw, 1, _positions(s["meta"])).to(BF16)
+
+
+# -------------------------------------------------------------------------------------------------------------- one pass
+
+def run(state):
+    s, kind = state, state["kind"]
+    if not own:
+        return _plain(s)
+    from paper_2405_16325_amd import binding as sl
+    act = {"silu": sl.SLOPE_ACT_SILU, "gelu": sl.SLOPE_ACT_GELU, "relu": sl.SLOPE_ACT_RELU, None: None}[s["act"]]
+    if kind == "gated":
+        h, gu, _, _ = sl.slope_gated_fwd(s["x"], s["vals"], s["meta"], act, L=s["l"], R=s["r"], want_gu=s["keep"] == "bf16")
+        return {"h": h, "gu": gu} if s["keep"] == "bf16" else {"h": h}
+    if kind == "step":
+        h, _, codes, byte = sl.slope_gated_fwd(s["x"], s["vals"], s["meta"], act, want_q8=True)
+        dgu, again = sl.slope_gated_bwd(s["dh"], act, q8=codes, scale=byte)
+        return {"h": h, "dgu": dgu, "h_again": again}
+    if kind == "gated_bwd":
+        dgu, h = sl.slope_gated_bwd(s["dh"], act, gu=s["gu"], q8=s["codes"], scale=s["byte"])
+        return {"dgu": dgu, "h": h}
+    if kind == "ckpt":
+        return sl.slope_restore_q8(*sl.slope_checkpoint_q8(s["x"]))
+    return sl.slope_wgrad_masked_q8(s["dy"], s["codes"], s["byte"], s["meta"])
+
+
+def _code_bytes(rows, cols):
+    return rows * (cols + (cols + BLOCK - 1) // BLOCK)
+
+
+def work(case):
+    """Each input read once, each output written once.  The 2:4 product executes half of the dense multiply-adds."""
+    kind, b = case["kind"], case["b"]
+    if kind in ("gated", "step"):
+        d_ff, d_in, r = case["d_ff"], case["d_in"], case.get("r", 0)
+        moved = 2 * b * d_in + 2 * d_ff * d_in * 9 // 8 + 2 * b * d_ff + 2 * r * (d_in + 2 * d_ff)
+        flops = 2 * b * d_ff * d_in + 2 * b * r * (d_in + 2 * d_ff) + 8 * b * d_ff
+        if kind == "step":                       # the codes do not have to reach memory
+            return {"bytes": moved + 8 * b * d_ff, "flops": flops + 30 * b * d_ff}
+        return {"bytes": moved + (4 * b * d_ff if case["keep"] == "bf16" else 0), "flops": flops}
+    if kind == "gated_bwd":
+        d_ff = case["d_ff"]
+        return {"bytes": 8 * b * d_ff + (_code_bytes(2 * b, d_ff) if case["q8"] else 4 * b * d_ff), "flops": 16 * b * d_ff}
+    if kind == "ckpt":
+        return {"bytes": 4 * b * case["d"] + 2 * _code_bytes(b, case["d"]), "flops": 6 * b * case["d"]}
+    d_out, d_in = case["d_out"], case["d_in"]
+    return {"bytes": 2 * b * d_out + _code_bytes(b, d_in) + d_out * d_in // 8 + d_out * d_in, "flops": 2 * b * d_out * d_in}
+
+
+# ------------------------------------------------------------------------------------------------- the definition in fp64
+
+def _two_to(e):
+    """2^e in 64 bits, from its bits."""
+    return (e.to(torch.int64) + 1023).bitwise_left_shift(52).view(F64)
+
+
+def _exact_kept(x):
+    """What 8-bit codes of x stand for, by the grid of e4m3 in 64 bits: steps of 1/8 of the power of two below, 2^-9 at least."""
+    rows, cols = x.shape
+    got = torch.empty_like(x)
+    for c in range(0, cols, BLOCK * 64):         # columns by runs of 64 blocks, the last block as wide as it is
+        part = x[:, c:c + BLOCK * 64]
+        tail = part.shape[1] % BLOCK
+        for cut in ((0, part.shape[1] - tail), (part.shape[1] - tail, part.shape[1])):
+            if cut[0] == cut[1]:
+                continue
+            v = part[:, cut[0]:cut[1]].reshape(rows, -1, tail if cut[0] else min(BLOCK, cut[1]))
+            top = v.abs().max(2, keepdim=True).values
+            low = _two_to((torch.frexp(top).exponent - 9).clamp(min=-126))
+            scale = torch.where(top > 448 * low, 2 * low, low)
+            v = v / scale
+            unit = _two_to(torch.frexp(v.abs().clamp(min=2.0 ** -6)).exponent - 4)
+            got[:, c + cut[0]:c + cut[1]] = (torch.round(v / unit) * unit * scale).reshape(rows, -1)
+    return got
+
+
+def _exact_gate(g, u, act, dh=None):
+    """h, and with dh the gradients of g and u."""
+    if act == "relu":
+        a, d = g.clamp(min=0), torch.where(g > 0, 1.0, 0.0).to(F64)
+    elif act == "silu":
+        p = torch.sigmoid(g)
+        a, d = g * p, p + g * p * torch.sigmoid(-g)
+    else:
+        t = torch.tanh(GELU_A * (g + GELU_B * g ** 3))
+        a, d = g * (1 + t) / 2, (1 + t) / 2 + g / 2 * (1 - t ** 2) * GELU_A * (1 + 3 * GELU_B * g ** 2)
+    return a * u if dh is None else (a * u, torch.cat([dh * u * d, dh * a], 1))
+
+
+def exact(case, seed):
+    """The definitions in 64 bits; what passes through 8 bits is rounded to them, results are not rounded."""
+    s, kind, b = prepare(case, seed), case["kind"], case["b"]
+    f = lambda t: t.to(F64)                                                                  # noqa: E731
+    if kind in ("gated", "step"):
+        d_ff, d_in = case["d_ff"], case["d_in"]
+        meta, vals = s["meta"], s["vals"]
+        gu = torch.empty((b, 2 * d_ff), dtype=F64, device="cuda")
+        for half in range(2):
+            w = torch.zeros((d_ff, d_in), dtype=F64, device="cuda")
+            rows = slice(half * d_ff, (half + 1) * d_ff)
+            for slot in range(4):                # value 4 i + slot of a row lies in the group 2 i + slot / 2
+                col = (meta[rows] >> (2 * slot) & 3).long() + 4 * (slot // 2)
+                col += torch.arange(0, d_in, 8, device="cuda")
+                w.scatter_(1, col, f(vals[rows])[:, slot::4])
+            gu[:, rows] = torch.mm(f(s["x"]), w.t().contiguous())
+        if s["l"] is not None:
+            gu += torch.mm(torch.mm(f(s["x"]), f(s["l"])), f(s["r"]))
+        h = _exact_gate(gu[:, :d_ff], gu[:, d_ff:], case["act"])
+        if kind == "step":
+            g, u = _exact_kept(gu[:, :d_ff]), _exact_kept(gu[:, d_ff:])
+            again, dgu = _exact_gate(g, u, case["act"], f(s["dh"]))
+            return {"h": h, "dgu": dgu, "h_again": again}
+        return {"h": h, "gu": gu} if case["keep"] == "bf16" else {"h": h}
+    if kind == "gated_bwd":
+        d_ff = case["d_ff"]
+        if case["q8"]:
+            power = _two_to(s["byte"].long() - 127).repeat_interleave(BLOCK, dim=1)[:, :d_ff]
+            gu = (f(s["codes"]) * power).view(b, 2 * d_ff)
+        else:
+            gu = f(s["gu"])
+        h, dgu = _exact_gate(gu[:, :d_ff], gu[:, d_ff:], case["act"], f(s["dh"]))
+        return {"dgu": dgu, "h": h}
+    if kind == "ckpt":
+        return _exact_kept(f(s["x"]))
+    x = f(s["codes"]) * _two_to(s["byte"].long() - 127).repeat_interleave(BLOCK, dim=1)[:, :case["d_in"]]
+    x, dyt, out = x.t().contiguous(), f(s["dy"]), []
+    for rows in range(0, case["d_out"], 4096):
+        part = torch.mm(x, dyt[:, rows:rows + 4096].contiguous()).t()
+        meta = s["meta"][rows:rows + 4096]
+        kept = torch.empty((part.shape[0], case["d_in"] // 2), dtype=F64, device="cuda")
+        for slot in range(4):
+            col = (meta >> (2 * slot) & 3).long() + 4 * (slot // 2)
+            kept[:, slot::4] = torch.gather(part, 1, col + torch.arange(0, case["d_in"], 8, device="cuda"))
+        out.append(kept)
+    return torch.cat(out)

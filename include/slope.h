@@ -83,7 +83,9 @@ typedef enum {
     SLOPE_CALL_WGRAD_MASKED_T = 9,
     SLOPE_CALL_SPMM_BWD_X_WS = 10,
     SLOPE_CALL_RMSNORM_BWD = 11,       /* d_in: the width d; d_out and r are not looked at */
-    SLOPE_CALL_SPMM_FWD_Q8 = 12        /* r is not looked at                                */
+    SLOPE_CALL_SPMM_FWD_Q8 = 12,       /* r is not looked at                                */
+    SLOPE_CALL_GATED_FWD = 13,         /* d_out: the layer's d_ff                           */
+    SLOPE_CALL_WGRAD_MASKED_Q8 = 14    /* r is not looked at                                */
 } slope_call_id;
 
 /* Bytes of scratch memory a call wants for b tokens, a d_out x d_in layer and adapter rank r (0: none);
@@ -417,6 +419,63 @@ slope_status slope_grad_norm(const void* table, const void* device_table, double
                              void* workspace, size_t workspace_bytes, void* stream);
 slope_status slope_adamw_step(const void* table, const void* device_table, double lr, double beta1, double beta2, double eps,
                               double grad_scale, int64_t step, const void* control_or_null, void* stream);
+
+/*
+ * ---- the gated feed-forward layer, and activations kept in 8 bits ----
+ *
+ * slope_checkpoint_q8 - an activation in 8 bits for the backward pass: e4m3 codes and, for each 32 neighbouring elements of a row (a
+ * row's last block may be shorter), the exponent of a power of two in a byte:
+ *     scale = the smallest power of two, 2^-126 or more, with max |x| <= 448 scale        code = x / scale rounded to nearest even
+ *     byte = log2(scale) + 127; 255: the block holds an infinity or NaN, and all of it reads as NaN
+ * (under the largest scale, 2^120, magnitudes stop at 240 scale: the next one, 2^128, is not a bf16 number).  What a code stands for, code * scale, is a bf16 number (down to bf16's smallest one), so that a restored activation is exact and products
+ * with it lose nothing more.  It is off from x by at most 2^-4 |x|, or 2^-10 scale where |x| < 2^-6 scale.
+ *   X in bf16[rows, d], d % 8 == 0    Q out e4m3[rows, d]    scale out u8[rows, (d + 31) / 32], slope_checkpoint_scale_bytes(rows, d) bytes
+ * slope_restore_q8 - back: X = code * scale, bf16[rows, d].
+ *
+ * slope_wgrad_masked_q8 - slope_wgrad_masked_ws (Eq. 5) for a layer whose input was kept in this form: dW = dY^T X at W^R's kept
+ * positions, X = code * scale.
+ *   dY in bf16[b, d_out]    Xq in e4m3[b, d_in], x_scale in u8[b, (d_in + 31) / 32]    Wr_meta in u8[d_out, d_in/8]
+ *   dW_vals out bf16[d_out, d_in/2]; fp32 accumulation
+ *   workspace  slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) bytes, 256-byte aligned, required
+ */
+#define SLOPE_CHECKPOINT_BLOCK 32
+size_t slope_checkpoint_scale_bytes(int64_t rows, int64_t d);
+slope_status slope_checkpoint_q8(const void* X, int64_t rows, int64_t d, void* Q, void* scale, void* stream);
+slope_status slope_restore_q8(const void* Q, const void* scale, int64_t rows, int64_t d, void* X, void* stream);
+size_t slope_wgrad_masked_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out);
+slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x_scale, int64_t b, const void* Wr_meta, int64_t d_out,
+                                   int64_t d_in, void* dW_vals, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * slope_gated_fwd - both projections of a gated feed-forward layer, the activation and the product, from one packed weight of
+ * 2 d_ff rows, the gate's first (pruned, double-pruned and updated like any other: groups along d_out stay inside a half):
+ *     [g | u] = X (W^R)^T (+ (X L) R)        H = bf16(act(g) u)          g, u in fp32
+ *   X in bf16[b, d_in]    Wr_vals bf16[2 d_ff, d_in/2], Wr_meta u8[2 d_ff, d_in/8]    d_ff % 8 == 0, 2 d_ff <= 2^23
+ *   act   SLOPE_ACT_SILU   g s(g), s the logistic function
+ *         SLOPE_ACT_GELU   g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
+ *         SLOPE_ACT_RELU   max(g, 0)                                     (others: SLOPE_ERR_VALUE)
+ *   L_or_null bf16[d_in, r], R_or_null bf16[r, 2 d_ff], r   as for slope_spmm_fwd
+ *   H out bf16[b, d_ff]
+ *   What the backward pass wants, either or both of (NULL: not kept; fp32 values of g and u rounded once):
+ *     GU_or_null  out bf16[b, 2 d_ff]
+ *     GUq_or_null, GU_scale_or_null  out e4m3[b, 2 d_ff], u8[b, 2, (d_ff + 31) / 32]: slope_checkpoint_q8's form of [2 b, d_ff], a token's
+ *                 gate and then its up projection; both or neither
+ *   workspace_or_null  slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r) bytes (may be 0), 256-byte aligned; required with an adapter
+ *
+ * slope_gated_bwd - its gradient from what was kept, element by element:
+ *     dU = dH act(g)    dG = dH u act'(g)    (relu'(0) = 0)    H = act(g) u
+ * dX and dW of the layer are then those of a layer of 2 d_ff outputs: slope_spmm_bwd_x and slope_wgrad_masked (or _q8) with dGU.
+ *   dH in bf16[b, d_ff]    GU_or_null, or GUq_or_null and GU_scale_or_null, as written above (with GU the others are not looked at)
+ *   dGU out bf16[b, 2 d_ff], may be GU    H_or_null out bf16[b, d_ff]: the layer's output again, for the next layer's weight gradient;
+ *   may be dH
+ */
+typedef enum { SLOPE_ACT_SILU = 0, SLOPE_ACT_GELU = 1, SLOPE_ACT_RELU = 2 } slope_activation;
+size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r);
+slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
+                             const void* L_or_null, const void* R_or_null, int64_t r, void* H, void* GU_or_null, void* GUq_or_null,
+                             void* GU_scale_or_null, void* workspace_or_null, size_t workspace_bytes, void* stream);
+slope_status slope_gated_bwd(const void* dH, const void* GU_or_null, const void* GUq_or_null, const void* GU_scale_or_null, int64_t b,
+                             int64_t d_ff, int act, void* dGU, void* H_or_null, void* stream);
 
 /*
  * slope_spmm_fwd_plan - diagnostics, host only (no GPU call): which kernels slope_spmm_fwd (Eq. 4, 11)

@@ -126,3 +126,63 @@ def adamw(p, g, m, v, coef, lr, beta1, beta2, eps, decay, step):
     p = np.asarray(p, np.float64)
     p = p - lr * decay * p - lr * (m64 / (1 - beta1 ** step)) / (np.sqrt(v64 / (1 - beta2 ** step)) + eps)
     return p, m2, v2
+
+
+# ---- the gated feed-forward layer and activations kept in 8 bits
+CHECKPOINT_BLOCK = 32
+
+
+def checkpoint(x):
+    """(codes u8[rows, d], scale bytes u8[rows, ceil(d / 32)]) of finite or other values; a block with one that is not finite has byte
+    255, and its codes mean nothing."""
+    x = np.asarray(x, dtype=np.float64)
+    rows, d = x.shape
+    blocks = -(-d // CHECKPOINT_BLOCK)
+    codes, bytes_ = np.zeros((rows, d), np.uint8), np.zeros((rows, blocks), np.uint8)
+    for c in range(blocks):
+        part = x[:, c * CHECKPOINT_BLOCK:(c + 1) * CHECKPOINT_BLOCK]
+        top = np.abs(part).max(1)
+        fine = np.isfinite(top)
+        top = np.where(fine, top, 0.0)
+        e = np.full(rows, -126)
+        while (top > MAX * 2.0 ** e).any():                                  # the smallest power of two that holds the block
+            e = np.where(top > MAX * 2.0 ** e, e + 1, e)
+        bytes_[:, c] = np.where(fine, e + 127, 255)
+        part = np.where(fine[:, None], part, 0.0)
+        part = np.where((e == 120)[:, None], np.clip(part, -240 * 2.0 ** 120, 240 * 2.0 ** 120), part)   # 256 would be 2^128
+        codes[:, c * CHECKPOINT_BLOCK:(c + 1) * CHECKPOINT_BLOCK] = e4m3_nearest(part / (2.0 ** e)[:, None])
+    return codes, bytes_
+
+
+def restored(codes, bytes_):
+    scale = np.where(bytes_ == 255, np.nan, 2.0 ** (bytes_.astype(np.float64) - 127))
+    return e4m3_value(codes) * np.repeat(scale, CHECKPOINT_BLOCK, axis=1)[:, :codes.shape[1]]
+
+
+def activation(g, act):
+    """(act(g), act'(g)); act: "silu", "gelu" (tanh form), "relu"."""
+    g = np.asarray(g, np.float64)
+    if act == "relu":
+        return np.maximum(g, 0.0), (g > 0).astype(np.float64)
+    if act == "silu":
+        with np.errstate(over="ignore"):
+            s = 1.0 / (1.0 + np.exp(-g))
+        return g * s, s + g * s * (1.0 - s)
+    c = 2.0 * np.sqrt(2.0 / np.pi)                                          # (1 + tanh z) / 2 = 1 / (1 + exp(-2 z)), which keeps its digits
+    with np.errstate(over="ignore"):
+        s = 1.0 / (1.0 + np.exp(-c * (g + 0.044715 * g ** 3)))
+    return g * s, s + g * s * (1.0 - s) * c * (1.0 + 3 * 0.044715 * g ** 2)
+
+
+def gated(gu, act):
+    """h of the projections [g | u]."""
+    d_ff = gu.shape[1] // 2
+    return activation(gu[:, :d_ff], act)[0] * gu[:, d_ff:]
+
+
+def gated_grad(dh, gu, act):
+    """(dgu, h)"""
+    d_ff = gu.shape[1] // 2
+    u = gu[:, d_ff:]
+    a, d = activation(gu[:, :d_ff], act)
+    return np.concatenate([dh * u * d, dh * a], axis=1), a * u

@@ -26,7 +26,8 @@ SLOPE_STATIC_SCRATCH_BYTES = 72 << 20      # include/slope.h
 # slope_call_id
 (SLOPE_CALL_PRUNE_ROWS, SLOPE_CALL_DOUBLE_PRUNE, SLOPE_CALL_SPMM_FWD, SLOPE_CALL_SPMM_BWD_X, SLOPE_CALL_WGRAD_MASKED,
  SLOPE_CALL_WGRAD_MASKED_WS, SLOPE_CALL_SPMM_BWD_X_ADAPTER, SLOPE_CALL_WGRAD_ADAPTER,
- SLOPE_CALL_WGRAD_MASKED_T, SLOPE_CALL_SPMM_BWD_X_WS, SLOPE_CALL_RMSNORM_BWD, SLOPE_CALL_SPMM_FWD_Q8) = range(1, 13)
+ SLOPE_CALL_WGRAD_MASKED_T, SLOPE_CALL_SPMM_BWD_X_WS, SLOPE_CALL_RMSNORM_BWD, SLOPE_CALL_SPMM_FWD_Q8, SLOPE_CALL_GATED_FWD,
+ SLOPE_CALL_WGRAD_MASKED_Q8) = range(1, 15)
 
 _P, _I64, _INT, _SZ, _DBL = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t, ctypes.c_double
 
@@ -72,6 +73,14 @@ SIGNATURES = {
     "slope_grad_norm_workspace_bytes": (_SZ, [_P]),
     "slope_grad_norm": (_INT, [_P, _P, _DBL, _DBL, _P, _P, _SZ, _P]),
     "slope_adamw_step": (_INT, [_P, _P, _DBL, _DBL, _DBL, _DBL, _DBL, _I64, _P, _P]),
+    "slope_checkpoint_scale_bytes": (_SZ, [_I64, _I64]),
+    "slope_checkpoint_q8": (_INT, [_P, _I64, _I64, _P, _P, _P]),
+    "slope_restore_q8": (_INT, [_P, _P, _I64, _I64, _P, _P]),
+    "slope_wgrad_masked_q8_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "slope_wgrad_masked_q8": (_INT, [_P, _P, _P, _I64, _P, _I64, _I64, _P, _P, _SZ, _P]),
+    "slope_gated_fwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
+    "slope_gated_fwd": (_INT, [_P, _I64, _P, _P, _I64, _I64, _INT, _P, _P, _I64, _P, _P, _P, _P, _P, _SZ, _P]),
+    "slope_gated_bwd": (_INT, [_P, _P, _P, _P, _I64, _I64, _INT, _P, _P, _P]),
     "slope_ceiling_min_bytes": (_SZ, []),
     "slope_ceiling": (_INT, [_INT, _P, _SZ, _INT, _P, _P]),
     "slope_tile_order": (_I64, [_I64, _I64, _P, _P, _I64]),
@@ -627,6 +636,121 @@ def slope_adamw_step(plan: AdamWPlan, lr: float, beta1: float, beta2: float, eps
         _want(control, F32, (4,), "control")
     _check("slope_adamw_step", lib().slope_adamw_step(plan.table, _ptr(plan.device_table), lr, beta1, beta2, eps, grad_scale, step,
                                                       _ptr(control), _stream()))
+
+
+# ---------------------------------------------------------------- the gated feed-forward layer, activations kept in 8 bits
+SLOPE_ACT_SILU, SLOPE_ACT_GELU, SLOPE_ACT_RELU = range(3)
+SLOPE_CHECKPOINT_BLOCK = 32
+
+
+def _blocks(d):
+    return (d + SLOPE_CHECKPOINT_BLOCK - 1) // SLOPE_CHECKPOINT_BLOCK
+
+
+def slope_checkpoint_q8(X: torch.Tensor, out=None):
+    """X bf16[rows, d] in 8 bits for the backward pass: (codes e4m3[rows, d], scale u8[rows, (d + 31) // 32]), a power of two per 32
+    elements of a row.  out: the same two, to write into."""
+    if X is None or X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    rows, d = X.shape
+    _want(X, BF16, (rows, d), "X")
+    if out is None:
+        Q, scale = torch.empty((rows, d), dtype=E4M3, device=X.device), torch.empty((rows, _blocks(d)), dtype=U8, device=X.device)
+    else:
+        Q, scale = _want(out[0], E4M3, (rows, d), "codes"), _want(out[1], U8, (rows, _blocks(d)), "scale")
+    _check("slope_checkpoint_q8", lib().slope_checkpoint_q8(_ptr(X), rows, d, _ptr(Q), _ptr(scale), _stream()))
+    return Q, scale
+
+
+def slope_restore_q8(Q: torch.Tensor, scale: torch.Tensor, out=None):
+    """What slope_checkpoint_q8 kept: bf16[rows, d]."""
+    if Q is None or Q.dim() != 2:
+        raise ValueError("Q must be a matrix")
+    rows, d = Q.shape
+    _want(Q, E4M3, (rows, d), "Q")
+    _want(scale, U8, (rows, _blocks(d)), "scale")
+    X = _want(out, BF16, (rows, d), "out") if out is not None else torch.empty((rows, d), dtype=BF16, device=Q.device)
+    _check("slope_restore_q8", lib().slope_restore_q8(_ptr(Q), _ptr(scale), rows, d, _ptr(X), _stream()))
+    return X
+
+
+def slope_wgrad_masked_q8(dY: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, meta: torch.Tensor, out=None, workspace=None):
+    """slope_wgrad_masked for a layer whose input was kept by slope_checkpoint_q8: dW packed bf16[d_out, d_in/2].
+    workspace: a uint8 device tensor of slope_workspace_bytes(SLOPE_CALL_WGRAD_MASKED_Q8, b, d_in, d_out) bytes, or None (allocated
+    here)."""
+    if Q is None or Q.dim() != 2:
+        raise ValueError("Q must be a matrix")
+    b, d_in = Q.shape
+    if dY is None or dY.dim() != 2:
+        raise ValueError("dY must be a matrix")
+    d_out = dY.shape[1]
+    _want(dY, BF16, (b, d_out), "dY")
+    _want(Q, E4M3, (b, d_in), "Q")
+    _want(scale, U8, (b, _blocks(d_in)), "scale")
+    _want(meta, U8, (d_out, d_in // 8), "meta")
+    G = _want(out, BF16, (d_out, d_in // 2), "out") if out is not None \
+        else torch.empty((d_out, d_in // 2), dtype=BF16, device=dY.device)
+    workspace = _scratch(workspace, int(lib().slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out)), dY.device, "workspace")
+    _check("slope_wgrad_masked_q8", lib().slope_wgrad_masked_q8(_ptr(dY), _ptr(Q), _ptr(scale), b, _ptr(meta), d_out, d_in, _ptr(G),
+                                                                _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
+    return G
+
+
+def slope_gated_fwd(X: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, act: int = SLOPE_ACT_SILU, L=None, R=None,
+                    want_gu: bool = False, want_q8: bool = False, out=None, workspace="auto"):
+    """H = act(g) u, [g | u] = X (W^R)^T [+ (X L) R]: (H bf16[b, d_ff], GU bf16[b, 2 d_ff], codes e4m3[b, 2 d_ff], scale
+    u8[b, 2, (d_ff + 31) // 32]); of what the backward pass wants, what was not asked for is None.  vals, meta: packed W^R of 2 d_ff
+    rows, the gate's first; L bf16[d_in, r], R bf16[r, 2 d_ff].  out: the same four, to write into.
+    workspace: "auto" (allocated here when the call wants one), None (no adapter then, and nothing is split) or a uint8 device tensor of
+    slope_workspace_bytes(SLOPE_CALL_GATED_FWD, b, d_in, d_ff, r) bytes."""
+    b, d_in, rows, r = _fwd_args(X, vals, meta, L, R, None)
+    d_ff = rows // 2
+    if rows != 2 * d_ff:
+        raise ValueError("the weight must have a row of the gate for every row of the up projection")
+    if out is None:
+        H = torch.empty((b, d_ff), dtype=BF16, device=X.device)
+        GU = torch.empty((b, rows), dtype=BF16, device=X.device) if want_gu else None
+        Q = torch.empty((b, rows), dtype=E4M3, device=X.device) if want_q8 else None
+        scale = torch.empty((b, 2, _blocks(d_ff)), dtype=U8, device=X.device) if want_q8 else None
+    else:
+        H, GU, Q, scale = out
+        _want(H, BF16, (b, d_ff), "H")
+        for t, dtype, shape, what in ((GU, BF16, (b, rows), "GU"), (Q, E4M3, (b, rows), "codes"), (scale, U8, (b, 2, _blocks(d_ff)), "scale")):
+            if t is not None:
+                _want(t, dtype, shape, what)
+    if workspace is not None:
+        need = int(lib().slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r))
+        workspace = _scratch(None if isinstance(workspace, str) else workspace, need, X.device, "workspace") if need else None
+    _check("slope_gated_fwd", lib().slope_gated_fwd(_ptr(X), b, _ptr(vals), _ptr(meta), d_ff, d_in, act, _ptr(L), _ptr(R), r, _ptr(H),
+                                                    _ptr(GU), _ptr(Q), _ptr(scale), _ptr(workspace),
+                                                    0 if workspace is None else workspace.numel(), _stream()))
+    return H, GU, Q, scale
+
+
+def slope_gated_bwd(dH: torch.Tensor, act: int = SLOPE_ACT_SILU, gu=None, q8=None, scale=None, want_h: bool = True, out=None):
+    """Gradient of slope_gated_fwd from the projections it kept, gu bf16[b, 2 d_ff] or q8 e4m3[b, 2 d_ff] with its scale:
+    (dGU bf16[b, 2 d_ff], H bf16[b, d_ff] again or None).  out: the same two, to write into; dGU may be gu, H may be dH."""
+    if dH is None or dH.dim() != 2:
+        raise ValueError("dH must be a matrix")
+    b, d_ff = dH.shape
+    _want(dH, BF16, (b, d_ff), "dH")
+    if (gu is None) == (q8 is None):
+        raise ValueError("one of gu and q8 is wanted")
+    if gu is not None:
+        _want(gu, BF16, (b, 2 * d_ff), "gu")
+    else:
+        _want(q8, E4M3, (b, 2 * d_ff), "q8")
+        _want(scale, U8, (b, 2, _blocks(d_ff)), "scale")
+    if out is None:
+        dGU = torch.empty((b, 2 * d_ff), dtype=BF16, device=dH.device)
+        H = torch.empty_like(dH) if want_h else None
+    else:
+        dGU, H = out
+        _want(dGU, BF16, (b, 2 * d_ff), "dGU")
+        if H is not None:
+            _want(H, BF16, (b, d_ff), "H")
+    _check("slope_gated_bwd", lib().slope_gated_bwd(_ptr(dH), _ptr(gu), _ptr(q8), _ptr(scale), b, d_ff, act, _ptr(dGU), _ptr(H), _stream()))
+    return dGU, H
 
 
 (SLOPE_CEILING_SPARSE_MFMA, SLOPE_CEILING_DENSE_MFMA, SLOPE_CEILING_READ, SLOPE_CEILING_COPY,

@@ -161,6 +161,18 @@ hipError_t launch_grad_norm(const void* table, const void* device_table, float i
 hipError_t launch_adamw(const void* table, const void* device_table, double lr, double beta1, double beta2, double eps,
                         double grad_scale, int64_t step, const float* control, hipStream_t s);
 
+// the gated layer and 8-bit checkpoints (spmm.hip, spmm_stream.hip, gated.hip, wgrad_tn.hip)
+struct GateOut;
+hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
+                        int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s);
+hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q, const uint8_t* bytes, int64_t n, int64_t d_ff, int act,
+                            bf16_t* dgu, bf16_t* h, hipStream_t s);
+hipError_t launch_checkpoint_q8(const bf16_t* x, int64_t rows, int64_t d, uint8_t* q, uint8_t* bytes, hipStream_t s);
+hipError_t launch_restore_q8(const uint8_t* q, const uint8_t* bytes, int64_t rows, int64_t d, bf16_t* x, hipStream_t s);
+// dW as launch_wgrad_masked from X in 8-bit blocks; Xt, dYt, tail: required, as for slope_wgrad_masked_ws
+hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
+                                  int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s);
+
 // Launches of any number of workgroups as rows of 2^20: a dimension of a grid holds fewer than 2^32 work items, and a launch
 // beyond that runs a part of them without an error.  A kernel takes flat_block() and leaves when it is past the last.
 constexpr int64_t GRID_ROW = (int64_t)1 << 20;

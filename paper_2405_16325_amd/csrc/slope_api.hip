@@ -5,7 +5,7 @@
 
 #include <atomic>
 
-#include "pipeline.h"
+#include "gated.h"
 
 namespace {
 
@@ -82,6 +82,16 @@ hipError_t skinny_product(const bf16_t* B, int64_t n, int64_t K, const bf16_t* A
     if (K % 64 != 0 || skinny_is_short(n, r, K, a_kmajor))
         return launch_skinny_ragged({B, K, A, a_kmajor ? r : K, a_kmajor, n, r, K, T}, s);
     return launch_skinny_factor(B, n, K, A, a_kmajor, r, T, partial, partial ? dense_tn_plain_partial_bytes(n, r) : 0, s);
+}
+
+// T = X L, rounded to bf16, with room for its sums behind it (adapter_workspace_bytes)
+hipError_t token_factor(const bf16_t* X, int64_t b, int64_t d_in, const bf16_t* L, int64_t r, bf16_t* T, float* sums, hipStream_t s) {
+    if (d_in % 64 == 0 && b <= XL_SMALL_MAX_TOKENS) {
+        const XlSplit x = xl_split(b, d_in, r, (int64_t)(xl_small_scratch_bytes(b, d_in, r) / 4), RESIDENT);
+        const hipError_t e = launch_xl(X, b, d_in, L, r, x, x.slabs > 1 ? sums : nullptr, T, s);
+        return e == hipSuccess && x.slabs > 1 ? launch_xl_reduce(sums, x.slabs, b, r, T, s) : e;
+    }
+    return skinny_product(X, b, d_in, L, true, r, T, b > XL_SMALL_MAX_TOKENS && dense_tn_plain_partial_bytes(b, r) ? sums : nullptr, s);
 }
 
 }  // namespace
@@ -162,6 +172,8 @@ size_t slope_workspace_bytes(int call_id, int64_t b, int64_t d_in, int64_t d_out
         case SLOPE_CALL_WGRAD_ADAPTER: return slope_wgrad_adapter_workspace_bytes(b, d_in, d_out, r);
         case SLOPE_CALL_RMSNORM_BWD: return slope_rmsnorm_bwd_workspace_bytes(b, d_in);
         case SLOPE_CALL_SPMM_FWD_Q8: return slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out);
+        case SLOPE_CALL_GATED_FWD: return slope_gated_fwd_workspace_bytes(b, d_in, d_out, r);
+        case SLOPE_CALL_WGRAD_MASKED_Q8: return slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out);
         default: return 0;      // prune_rows, double_prune, spmm_bwd_x, wgrad_masked need no scratch; unknown ids
     }
 }
@@ -239,16 +251,8 @@ static slope_status spmm_fwd_run(const void* X, int64_t b, const void* Wr_vals, 
                                        (size_t)((uint8_t*)sums - ws), slices != nullptr, s, e))
             return finish(e);
     }
-    if (adapter) {                                            // T = X L, rounded to bf16
-        hipError_t e;
-        if (d_in % 64 == 0 && b <= XL_SMALL_MAX_TOKENS) {
-            const XlSplit x = xl_split(b, d_in, r, (int64_t)(xl_small_scratch_bytes(b, d_in, r) / 4), RESIDENT);
-            e = launch_xl(x_in, b, d_in, l, r, x, x.slabs > 1 ? sums : nullptr, T, s);
-            if (e == hipSuccess && x.slabs > 1) e = launch_xl_reduce(sums, x.slabs, b, r, T, s);
-        } else {
-            e = skinny_product(x_in, b, d_in, l, true, r, T,
-                               b > XL_SMALL_MAX_TOKENS && dense_tn_plain_partial_bytes(b, r) ? sums : nullptr, s);
-        }
+    if (adapter) {
+        const hipError_t e = token_factor(x_in, b, d_in, l, r, T, sums, s);
         if (e != hipSuccess) return finish(e);
     } else {
         T = nullptr;
@@ -633,6 +637,93 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
     if (!control_or_null && (step < 1 || step > (1 << 24) || !(fabsf((float)grad_scale) < INFINITY))) return SLOPE_ERR_VALUE;
     return finish(launch_adamw(table, device_table, lr, beta1, beta2, eps, grad_scale, step, (const float*)control_or_null,
                                (hipStream_t)stream));
+}
+
+// 2 d_ff rows are what slope_double_prune takes
+static bool bad_gated(int64_t b, int64_t d_ff) { return bad_extent(b, 1) || bad_extent(d_ff, 8) || 2 * d_ff > DP_EXTENT_MAX; }
+static bool bad_act(int act) { return act != SLOPE_ACT_SILU && act != SLOPE_ACT_GELU && act != SLOPE_ACT_RELU; }
+// rows of d elements in 8-bit blocks: launches of a workgroup per 256 pieces of eight
+static bool bad_blocks(int64_t rows, int64_t d) { return bad_extent(rows, 1) || bad_extent(d, 8) || !grid_fits(rows * ((d + 31) / 32 * 4) / 256 + 1); }
+
+size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
+    if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
+    return adapter_workspace_bytes(b, d_in, 2 * d_ff, r);
+}
+
+slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
+                             const void* L_or_null, const void* R_or_null, int64_t r, void* H, void* GU_or_null, void* GUq_or_null,
+                             void* GU_scale_or_null, void* workspace_or_null, size_t workspace_bytes, void* stream) {
+    if (!GUq_or_null != !GU_scale_or_null) return SLOPE_ERR_NULL;
+    const slope_status st = spmm_fwd_check(X, b, Wr_vals, Wr_meta, 2 * d_ff, d_in, L_or_null, R_or_null, r, H);
+    if (st != SLOPE_OK) return st;
+    if (bad_gated(b, d_ff)) return SLOPE_ERR_SHAPE;
+    if (bad_act(act)) return SLOPE_ERR_VALUE;
+    if (misaligned(GU_or_null, 16) || misaligned(GUq_or_null, 16) || misaligned(GU_scale_or_null, 16) || misaligned(workspace_or_null, 256))
+        return SLOPE_ERR_ALIGN;
+    const bool adapter = r > 0 && L_or_null && R_or_null;
+    if (!adapter) r = 0;
+    if (adapter && !workspace_or_null) return SLOPE_ERR_NULL;
+    if (workspace_or_null && workspace_bytes < slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r)) return SLOPE_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    uint8_t* const ws = (uint8_t*)workspace_or_null;
+    bf16_t* const T = adapter ? (bf16_t*)ws : nullptr;
+    if (adapter) {
+        float* const sums = (float*)(ws + round256((size_t)b * r * 2) + round256((size_t)d_in * r * 2));
+        const hipError_t e = token_factor((const bf16_t*)X, b, d_in, (const bf16_t*)L_or_null, r, T, sums, s);
+        if (e != hipSuccess) return finish(e);
+    }
+    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null};
+    return finish(launch_gated((const bf16_t*)X, b, (const bf16_t*)Wr_vals, (const uint8_t*)Wr_meta, d_in, T, (const bf16_t*)R_or_null, r,
+                               (bf16_t*)H, gate, s));
+}
+
+slope_status slope_gated_bwd(const void* dH, const void* GU_or_null, const void* GUq_or_null, const void* GU_scale_or_null, int64_t b,
+                             int64_t d_ff, int act, void* dGU, void* H_or_null, void* stream) {
+    if (!dH || !dGU || (!GU_or_null && (!GUq_or_null || !GU_scale_or_null))) return SLOPE_ERR_NULL;
+    if (bad_gated(b, d_ff)) return SLOPE_ERR_SHAPE;
+    if (bad_act(act)) return SLOPE_ERR_VALUE;
+    if (misaligned(dH, 16) || misaligned(GU_or_null, 16) || misaligned(dGU, 16) || misaligned(H_or_null, 16) ||
+        (!GU_or_null && (misaligned(GUq_or_null, 16) || misaligned(GU_scale_or_null, 16))))
+        return SLOPE_ERR_ALIGN;
+    return finish(launch_gated_bwd((const bf16_t*)dH, (const bf16_t*)GU_or_null, (const uint8_t*)GUq_or_null, (const uint8_t*)GU_scale_or_null,
+                                   b, d_ff, act, (bf16_t*)dGU, (bf16_t*)H_or_null, (hipStream_t)stream));
+}
+
+size_t slope_checkpoint_scale_bytes(int64_t rows, int64_t d) {
+    return bad_extent(rows, 1) || bad_extent(d, 8) ? 0 : (size_t)rows * (size_t)((d + SLOPE_CHECKPOINT_BLOCK - 1) / SLOPE_CHECKPOINT_BLOCK);
+}
+
+slope_status slope_checkpoint_q8(const void* X, int64_t rows, int64_t d, void* Q, void* scale, void* stream) {
+    if (!X || !Q || !scale) return SLOPE_ERR_NULL;
+    if (bad_blocks(rows, d)) return SLOPE_ERR_SHAPE;
+    if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(scale, 16)) return SLOPE_ERR_ALIGN;
+    return finish(launch_checkpoint_q8((const bf16_t*)X, rows, d, (uint8_t*)Q, (uint8_t*)scale, (hipStream_t)stream));
+}
+
+slope_status slope_restore_q8(const void* Q, const void* scale, int64_t rows, int64_t d, void* X, void* stream) {
+    if (!Q || !scale || !X) return SLOPE_ERR_NULL;
+    if (bad_blocks(rows, d)) return SLOPE_ERR_SHAPE;
+    if (misaligned(X, 16) || misaligned(Q, 16) || misaligned(scale, 16)) return SLOPE_ERR_ALIGN;
+    return finish(launch_restore_q8((const uint8_t*)Q, (const uint8_t*)scale, rows, d, (bf16_t*)X, (hipStream_t)stream));
+}
+
+size_t slope_wgrad_masked_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out) {
+    return bad_layer(b, d_out, d_in) ? 0 : slope_wgrad_workspace_bytes(b, d_in, d_out);
+}
+
+slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x_scale, int64_t b, const void* Wr_meta, int64_t d_out,
+                                   int64_t d_in, void* dW_vals, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!dY || !Xq || !x_scale || !Wr_meta || !dW_vals || !workspace) return SLOPE_ERR_NULL;
+    if (bad_layer(b, d_out, d_in) || bad_blocks(b, d_in)) return SLOPE_ERR_SHAPE;
+    if (misaligned(dY, 16) || misaligned(Xq, 16) || misaligned(x_scale, 16) || misaligned(Wr_meta, 16) || misaligned(dW_vals, 16) ||
+        misaligned(workspace, 256))
+        return SLOPE_ERR_ALIGN;
+    if (workspace_bytes < slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out)) return SLOPE_ERR_WORKSPACE;
+    uint8_t* const ws = (uint8_t*)workspace;
+    const size_t x_bytes = slope_token_copy_bytes(b, d_in), dy_bytes = slope_token_copy_bytes(b, d_out);
+    float* const tail = slope_wgrad_t_workspace_bytes(b, d_in, d_out) ? (float*)(ws + x_bytes + dy_bytes) : nullptr;
+    return finish(launch_wgrad_masked_q8((const bf16_t*)dY, (const uint8_t*)Xq, (const uint8_t*)x_scale, b, (const uint8_t*)Wr_meta, d_out,
+                                         d_in, (bf16_t*)dW_vals, (bf16_t*)ws, (bf16_t*)(ws + x_bytes), tail, (hipStream_t)stream));
 }
 
 slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t r, int with_workspace, int32_t* plan) {

@@ -40,10 +40,20 @@
 // 59.0 / 59.0, 52.1 / 50.4.)
 #include <type_traits>
 
-#include "pipeline.h"
+#include "gated.h"
 #include "skinny.h"
 
 namespace {
+
+// Column `col` of a k-major factor [k][m], eight of them from a multiple of 8 on; of a gated layer's [k][2 d_ff], by virtual row
+__device__ __forceinline__ size_t factor_pitch(int m) { return (size_t)m; }
+__device__ __forceinline__ size_t factor_pitch(int, const GateOut& gate) { return 2 * (size_t)gate.d_ff; }
+__device__ __forceinline__ bool factor_has(int col, int m) { return col < m; }
+__device__ __forceinline__ size_t factor_offset(int k, int col, int m) { return (size_t)k * m + col; }
+__device__ __forceinline__ bool factor_has(int col, int m, const GateOut& gate) { return col < m && gated_element(col) < gate.d_ff; }
+__device__ __forceinline__ size_t factor_offset(int k, int col, int m, const GateOut& gate) {
+    return (size_t)k * factor_pitch(m, gate) + gated_row(col, gate.d_ff);
+}
 
 template <int BMT> constexpr int FACTOR_PITCH = BMT * 2 + 32;  // pitch % 128 == 32: the four rows of a transposing read fall on distinct banks
 
@@ -58,7 +68,7 @@ template <int BMT> constexpr int FACTOR_PITCH = BMT * 2 + 32;  // pitch % 128 ==
         _Pragma("unroll") for (int u = 0; u < PER; ++u) {                                              \
             const int idx = tid + u * THREADS, k = idx / SEG, col = tile_f0 + 8 * (idx % SEG);         \
             piece[u] = (u32x4){0u, 0u, 0u, 0u};                                                        \
-            if (k < kn && col < m) piece[u] = *(const u32x4*)(A2 + (size_t)(kc + k) * m + col);        \
+            if (k < kn && factor_has(col, m, gate...)) piece[u] = *(const u32x4*)(A2 + factor_offset(kc + k, col, m, gate...)); \
         }                                                                                              \
         __syncthreads();                                      /* the rings are drained / the last chunk is consumed */ \
         _Pragma("unroll") for (int u = 0; u < PER; ++u) {                                              \
@@ -70,8 +80,8 @@ template <int BMT> constexpr int FACTOR_PITCH = BMT * 2 + 32;  // pitch % 128 ==
 // The factor's chunks by the wavefronts that only load, THREADS of them: the first is requested while the others multiply the last k-steps, the
 // next ones while they multiply a chunk.  tid counts from the first of these wavefronts.  (us, from memory, eight wavefronts that stage / four that
 // multiply / four that load: 2132 tokens, 3584 x 512, rank 160 on 256 x 128 23.0 / 23.5 / 22.6; 1239, 2816 x 256, rank 256 on 128 x 128 16.5 / 17.2 / 16.3.)
-template <int BMT, int THREADS>
-__device__ __forceinline__ void stage_factor(const bf16_t* __restrict__ A2, int K2, int m, uint8_t* smem, int tile_f0, int tid) {
+template <int BMT, int THREADS, class... Gate>
+__device__ __forceinline__ void stage_factor(const bf16_t* __restrict__ A2, int K2, int m, uint8_t* smem, int tile_f0, int tid, const Gate&... gate) {
     for (int kc = 0; kc < -K2; kc += 128) {
         const int kn = -K2 - kc < 128 ? -K2 - kc : 128;
         STAGE_CHUNK
@@ -90,11 +100,14 @@ __device__ __forceinline__ void stage_factor(const bf16_t* __restrict__ A2, int 
 //  - epilogue: store_rows. BNT = tokens of the workgroup's tile, tile_t0 its first token; every thread must make the call.
 //  - with a slab buffer (a split over k, see launch_spmm_slabs): the fp32 accumulators go to
 //    partial[token][feature] instead, 16 bytes per lane, and a reduction kernel finishes.
-template <int MF, int NF, int BMT, int BNT, int THREADS, bool STAGED = false>
+//  - Gate: a gated layer's product (K2 > 0 is not one's): store_gated; partial sums lie as [token][m], an element's gate and its up
+//    projection m / 2 apart.
+template <int MF, int NF, int BMT, int BNT, int THREADS, bool STAGED = false, class... Gate>
 __device__ __forceinline__ void extend_and_store(f32x4 (&acc)[MF][NF], int f0, int t0, int m, int n, int l16, int lq,
                                                  const bf16_t* __restrict__ B2, const bf16_t* __restrict__ A2,
                                                  int K2, bf16_t* __restrict__ C, uint8_t* smem, int tile_f0,
-                                                 int tile_t0, float* __restrict__ partial = nullptr) {
+                                                 int tile_t0, float* __restrict__ partial, const Gate&... gate) {
+    constexpr bool GATED = sizeof...(Gate) > 0;
     if (K2 < 0) {
         constexpr int PITCH = FACTOR_PITCH<BMT>;
         const int KR = -K2, tid = (int)threadIdx.x;
@@ -139,7 +152,7 @@ __device__ __forceinline__ void extend_and_store(f32x4 (&acc)[MF][NF], int f0, i
             }
         }
     }
-    if (K2 > 0) {
+    if (!GATED && K2 > 0) {
         // operands of step k0 + 32 are requested before the MFMAs of step k0 are issued
         const bf16_t* a_row[MF];
         const bf16_t* b_row[NF];
@@ -197,12 +210,14 @@ __device__ __forceinline__ void extend_and_store(f32x4 (&acc)[MF][NF], int f0, i
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
                 int col = f0 + i * 16 + lq * 4;               // feature
+                if (GATED) col = gated_element(col) < m / 2 ? gated_element(col) + (i & 1) * (m / 2) : m;
                 if (col < m) *(f32x4*)(partial + (size_t)row * m + col) = acc[i][j];
             }
         }
         return;
     }
-    store_rows<MF, NF, BMT, BNT, THREADS>(acc, f0, t0, m, n, l16, lq, C, smem, tile_f0, tile_t0);
+    if constexpr (GATED) store_gated<MF, NF, BMT, BNT, THREADS>(acc, f0, t0, n, l16, lq, C, smem, tile_f0, tile_t0, gate...);
+    else store_rows<MF, NF, BMT, BNT, THREADS>(acc, f0, t0, m, n, l16, lq, C, smem, tile_f0, tile_t0);
 }
 
 template <int BM, int BN>
@@ -354,8 +369,9 @@ struct SpmmLoads {
     uint8_t* smem;
 
     // loader lanes: 8 lanes per row, chunk rotated by (row / 2) % 8
+    template <class... Gate>
     __device__ __forceinline__ void init(const bf16_t* B, int n, const bf16_t* Av, const uint8_t* Am, int m, int K, int m0, int n0,
-                                         int k_first, int steps, int wave, int lane, uint8_t* lds) {
+                                         int k_first, int steps, int wave, int lane, uint8_t* lds, const Gate&... gate) {
         ksteps = steps;
         loader = wave;
         smem = lds;
@@ -363,7 +379,7 @@ struct SpmmLoads {
 #pragma unroll
         for (int i = 0; i < A_LD; ++i) {
             const int rl = (loader * A_LD + i) * 8 + (lane >> 3);     // row inside the tile
-            a_src[i] = (const uint8_t*)Av + (size_t)wrap_row(m0 + rl, m) * K + (((lane & 7) ^ ((rl >> 1) & 7)) * 16) + (size_t)k_first * 64;
+            a_src[i] = (const uint8_t*)Av + (size_t)weight_row(m0 + rl, m, gate...) * K + (((lane & 7) ^ ((rl >> 1) & 7)) * 16) + (size_t)k_first * 64;
         }
 #pragma unroll
         for (int i = 0; i < B_LD; ++i) {
@@ -374,7 +390,7 @@ struct SpmmLoads {
         for (int p = 0; p < M_ALL; ++p) {
             const int rl = (p * LW + loader) * ML::ROWS;
             const bool has = rl < BM;                         // wave-uniform
-            m_src[p] = Am + (size_t)(has ? wrap_row(m0 + rl + lane / ML::PIECES, m) : 0) * (K / 8) + (size_t)k_first * 8;
+            m_src[p] = Am + (size_t)(has ? weight_row(m0 + rl + lane / ML::PIECES, m, gate...) : 0) * (K / 8) + (size_t)k_first * 8;
             m_dst[p] = has ? S::M_OFF + (p * LW + loader) * 1024 : S::DUMMY;
             m_dst_step[p] = has ? S::M_BLOCK : 0;
         }
@@ -421,14 +437,14 @@ struct SpmmLoads {
     }
 };
 
-template <int BM, int BN, bool TAIL, class Job>
+template <int BM, int BN, bool TAIL, class Job, class... Gate>
 __global__ void __launch_bounds__(SPMM_THREADS) spmm_kernel(const bf16_t* __restrict__ B, int n,
                                                             const bf16_t* __restrict__ Av,
                                                             const uint8_t* __restrict__ Am, int m, int K,
                                                             const bf16_t* __restrict__ B2,
                                                             const bf16_t* __restrict__ A2, int K2,
                                                             bf16_t* __restrict__ C, int tiles_m, int tiles_n,
-                                                            Job job) {
+                                                            Job job, Gate... gate) {
     using S = SpmmSmem<BM, BN>;
     constexpr int MULT = tile_mult(BM, BN, TAIL);                // wavefronts that multiply
     constexpr bool OWN = MULT == 8;                          // all load as well, or LOADERS more do
@@ -472,7 +488,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_kernel(const bf16_t* __rest
     if constexpr (!OWN) {
         if (wave >= MULT) {                                   // (its barriers are those of the others)
             Loads load;
-            load.init(B, n, Av, Am, m, K, m0, n0, k_first, ksteps, wave - MULT, lane, smem);
+            load.init(B, n, Av, Am, m, K, m0, n0, k_first, ksteps, wave - MULT, lane, smem, gate...);
             load.first();
             WAIT_HERE(waitcnt_imm(Loads::A_LD + Loads::B_LD, 15));
             wg_barrier();
@@ -500,12 +516,12 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_kernel(const bf16_t* __rest
                 LAST_STEP(2)
                 step(ks0 + 3, std::integral_constant<int, 3>{});
             }
-            if (K2 < 0 && slab == extension_slab) stage_factor<BM, 64 * LOADERS>(A2, K2, m, smem, m0, t - 64 * MULT);
+            if (K2 < 0 && slab == extension_slab) stage_factor<BM, 64 * LOADERS>(A2, K2, m, smem, m0, t - 64 * MULT, gate...);
             return;
         }
     }
     Loads load;
-    if constexpr (OWN) load.init(B, n, Av, Am, m, K, m0, n0, k_first, ksteps, wave, lane, smem);
+    if constexpr (OWN) load.init(B, n, Av, Am, m, K, m0, n0, k_first, ksteps, wave, lane, smem, gate...);
 
     f32x4 acc[MF][NF];
 #pragma unroll
@@ -603,7 +619,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_kernel(const bf16_t* __rest
     if (!OWN) asm volatile("" : "+v"(te));
     const int we = __builtin_amdgcn_readfirstlane(te >> 6);
     extend_and_store<MF, NF, BM, BN, 64 * MULT, !OWN>(acc, m0 + (we & 1) * MF * 16, n0 + (we >> 1) * NF * 16, m, n, te & 15, te >> 4 & 3, B2, A2,
-                                                slab == extension_slab ? K2 : 0, C, smem, m0, n0, sums);
+                                                slab == extension_slab ? K2 : 0, C, smem, m0, n0, sums, gate...);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -631,13 +647,13 @@ struct SplitSmem {
 constexpr int split_even(int k) { return 2 + ((k & 1) == 0 ? 2 : 0) + ((k & 3) == 1 ? 1 : 0); }
 constexpr int split_odd(int k) { return 2 + ((k & 1) == 0 ? 2 : 0); }
 
-template <bool PREFETCH, bool TAIL>
+template <bool PREFETCH, bool TAIL, class... Gate>
 __global__ void __launch_bounds__(SPMM_THREADS) spmm_split_kernel(const bf16_t* __restrict__ B, int n,
                                                                   const bf16_t* __restrict__ Av,
                                                                   const uint8_t* __restrict__ Am, int m, int K,
                                                                   const bf16_t* __restrict__ B2,
                                                                   const bf16_t* __restrict__ A2, int K2,
-                                                                  bf16_t* __restrict__ C, int tiles_m, int tiles_n) {
+                                                                  bf16_t* __restrict__ C, int tiles_m, int tiles_n, Gate... gate) {
     using S = SplitSmem;
     constexpr int MF = 8, NF = 4;                            // wavefront tile 128 features x 64 tokens
     extern __shared__ __align__(16) uint8_t smem[];
@@ -659,7 +675,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_split_kernel(const bf16_t* 
     for (int q = 0; q < 4; ++q) {
         int rl = ((q >> 1) * 16 + wave * 2 + (q & 1)) * 8 + (lane >> 3);     // row inside the tile
         int sw16 = ((lane & 7) ^ ((rl >> 1) & 7)) * 16;
-        int ra = wrap_row(m0 + rl, m);
+        int ra = weight_row(m0 + rl, m, gate...);
         int rb = wrap_row(n0 + rl, n);
         a_src[q] = (const uint8_t*)Av + (size_t)ra * K + sw16;
         b_src[q] = (const uint8_t*)B + (size_t)rb * K * 2 + sw16;
@@ -668,7 +684,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_split_kernel(const bf16_t* 
     const uint8_t* m_src[2];                                 // 16 rows per wavefront and part
 #pragma unroll
     for (int p = 0; p < 2; ++p)
-        m_src[p] = Am + (size_t)wrap_row(m0 + (p * 8 + wave) * 16 + lane / ML::PIECES, m) * (K / 8);
+        m_src[p] = Am + (size_t)weight_row(m0 + (p * 8 + wave) * 16 + lane / ML::PIECES, m, gate...) * (K / 8);
     const int m_piece = ML::piece(lane) * 16;
 
     // ---- L2 prefetch of the token panel through the scalar cache.  A compute unit holds about 128 vector-memory
@@ -837,7 +853,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_split_kernel(const bf16_t* 
     WAIT_HERE(waitcnt_imm(0, 15));                            // drain the clamped look-ahead loads
     static_assert(S::BN * (S::BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the rings");
     extend_and_store<MF, NF, S::BM, S::BN, SPMM_THREADS>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2, K2, C, smem,
-                                           m0, n0);
+                                           m0, n0, nullptr, gate...);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -890,14 +906,14 @@ constexpr int ring_leave(int u, int pairs, int each, int meta) {
 
 // TAIL: an odd number of k-steps; the values and metadata of the last one are then fetched as the second half of a pair that
 // ends with the row (see spmm_kernel).
-template <int BM, int BN, bool TAIL, class Job>
+template <int BM, int BN, bool TAIL, class Job, class... Gate>
 __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* __restrict__ B, int n,
                                                                  const bf16_t* __restrict__ Av,
                                                                  const uint8_t* __restrict__ Am, int m, int K,
                                                                  const bf16_t* __restrict__ B2,
                                                                  const bf16_t* __restrict__ A2, int K2,
                                                                  bf16_t* __restrict__ C, int tiles_m, int tiles_n,
-                                                                 Job job) {
+                                                                 Job job, Gate... gate) {
     using S = RingSmem<BM, BN>;
     constexpr int META_PAIRS = S::META_PAIRS;
     constexpr int WM = 2, WN = RING_MULT / WM;                // wavefronts over the tile
@@ -953,7 +969,7 @@ __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* _
 #pragma unroll
         for (int i = 0; i < A_LD; ++i) {
             const int rl = (loader * A_LD + i) * 8 + (lane >> 3);
-            a_src[i] = (const uint8_t*)Av + (size_t)wrap_row_near(m0 + rl, m) * K + (((lane & 7) ^ ((rl >> 1) & 7)) * 16) + (size_t)k_first * 64;
+            a_src[i] = (const uint8_t*)Av + (size_t)weight_row_near(m0 + rl, m, gate...) * K + (((lane & 7) ^ ((rl >> 1) & 7)) * 16) + (size_t)k_first * 64;
             load_a(i, 0, smem);
         }
 #pragma unroll
@@ -964,7 +980,7 @@ __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* _
 #pragma unroll
         for (int i = 0; i < M_LD; ++i) {
             const int idx = (loader * M_LD + i) % M_LOADS, rl = (idx * 64 + lane) / META_PAIRS;
-            m_src[i] = Am + (size_t)wrap_row_near(m0 + rl, m) * (K / 8) + (size_t)k_first * 8;
+            m_src[i] = Am + (size_t)weight_row_near(m0 + rl, m, gate...) * (K / 8) + (size_t)k_first * 8;
             m_pair[i] = (lane % META_PAIRS) ^ (rl * META_PAIRS / 16 % META_PAIRS);
             m_dst[i] = S::M_OFF + idx * 1024;
             load_m(i, 0);
@@ -1010,7 +1026,7 @@ __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* _
                 pair(p + 3, std::integral_constant<int, 3>{});
             }
         }
-        if (K2 < 0 && slab == extension_slab) stage_factor<BM, 64 * LOADERS>(A2, K2, m, smem, m0, t - 64 * RING_MULT);
+        if (K2 < 0 && slab == extension_slab) stage_factor<BM, 64 * LOADERS>(A2, K2, m, smem, m0, t - 64 * RING_MULT, gate...);
         return;
     }
 
@@ -1097,7 +1113,7 @@ __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* _
     }
     static_assert(BN * (BM * 2 + 16) <= S::TOTAL && 128 * (BM * 2 + 32) <= S::TOTAL, "the staged output tile and factor fit in the ring");
     extend_and_store<MF, NF, BM, BN, 64 * RING_MULT, true>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2,
-                                                   slab == extension_slab ? K2 : 0, C, smem, m0, n0, sums);
+                                                   slab == extension_slab ? K2 : 0, C, smem, m0, n0, sums, gate...);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1128,14 +1144,15 @@ struct GenSmem {
     static constexpr int TOTAL = G * STAGE > SUMS ? G * STAGE : SUMS;
 };
 
-template <int FORM, int F, int G>
+template <int FORM, int F, int G, class... Gate>
 __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __restrict__ B, int n,
                                                            const bf16_t* __restrict__ Av,
                                                            const uint8_t* __restrict__ Am, int m, int K,
                                                            const bf16_t* __restrict__ B2,
                                                            const bf16_t* __restrict__ A2, int K2,
-                                                           bf16_t* __restrict__ C, int tiles_m) {
+                                                           bf16_t* __restrict__ C, int tiles_m, Gate... gate) {
     using S = GenSmem<F, G>;
+    constexpr bool GATED = sizeof...(Gate) > 0;
     constexpr int MF = F, NF = F, A_LD = F, B_LD = 2 * F;         // 16-byte pieces per lane and pair
     __shared__ __align__(16) uint8_t smem[S::TOTAL];
     const int m0 = (blockIdx.x % tiles_m) * S::BM, n0 = (blockIdx.x / tiles_m) * S::BN;
@@ -1153,7 +1170,7 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
 #pragma unroll
     for (int i = 0; i < A_LD; ++i) {
         const int rl = (t + 256 * i) >> 3;
-        a_src[i] = (const uint8_t*)Av + (size_t)wrap_row(m0 + rl, m) * K + (t & 7) * 16;
+        a_src[i] = (const uint8_t*)Av + (size_t)weight_row(m0 + rl, m, gate...) * K + (t & 7) * 16;
     }
 #pragma unroll
     for (int i = 0; i < B_LD; ++i) {
@@ -1161,7 +1178,7 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
         b_src[i] = B + (size_t)wrap_row(n0 + rl, n) * K + (t & 15) * 8;
     }
     const int mrow = t % S::BM;
-    const uint8_t* const m_src = Am + (size_t)wrap_row(m0 + mrow, m) * (K / 8);
+    const uint8_t* const m_src = Am + (size_t)weight_row(m0 + mrow, m, gate...) * (K / 8);
     f32x4 acc[MF][NF];
 #pragma unroll
     for (int i = 0; i < MF; ++i)
@@ -1245,7 +1262,7 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
     if constexpr (G == 1) {
         static_assert(S::BN * (S::BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the stages");
         extend_and_store<MF, NF, S::BM, S::BN, 256>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2, K2, C,
-                                                    smem, m0, n0);
+                                                    smem, m0, n0, nullptr, gate...);
     } else {
         // adapter extension from global memory, its steps of 32 dealt to the groups (A2 k-contiguous or k-major)
         const int KR = K2 < 0 ? -K2 : K2;
@@ -1256,14 +1273,15 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
                 b2[j].u = *(const u32x4*)(B2 + (size_t)wrap_row(n0 + (wn * NF + j) * 16 + l16, n) * KR + k0 + lq * 8);
 #pragma unroll
             for (int i = 0; i < MF; ++i) {
-                const int row = wrap_row(m0 + (wm * MF + i) * 16 + l16, m);
-                if (K2 > 0) {
+                const int row = weight_row(m0 + (wm * MF + i) * 16 + l16, m, gate...);
+                if (!GATED && K2 > 0) {
                     a2[i].u = *(const u32x4*)(A2 + (size_t)row * KR + k0 + lq * 8);
                 } else {
-                    const bf16_t* p = A2 + (size_t)(k0 + lq * 8) * m + row;
+                    const size_t pitch = factor_pitch(m, gate...);
+                    const bf16_t* p = A2 + (size_t)(k0 + lq * 8) * pitch + row;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        a2[i].u[e] = (uint32_t)p[(size_t)(2 * e) * m] | ((uint32_t)p[(size_t)(2 * e + 1) * m] << 16);
+                        a2[i].u[e] = (uint32_t)p[(size_t)(2 * e) * pitch] | ((uint32_t)p[(size_t)(2 * e + 1) * pitch] << 16);
                 }
             }
 #pragma unroll
@@ -1280,6 +1298,23 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
             for (int j = 0; j < NF; ++j)
                 *(f32x4*)(part + ((group * S::BN + (wn * NF + j) * 16 + l16) * S::SUM_PITCH + (wm * MF + i) * 16 + lq * 4)) = acc[i][j];
         __syncthreads();
+        if constexpr (GATED) {
+            auto sum = [&](int tok, int col) {                // four virtual rows of a token
+                f32x4 v = *(const f32x4*)(part + tok * S::SUM_PITCH + col);
+#pragma unroll
+                for (int q = 1; q < G; ++q) {
+                    const f32x4 x = *(const f32x4*)(part + (q * S::BN + tok) * S::SUM_PITCH + col);
+                    v[0] += x[0]; v[1] += x[1]; v[2] += x[2]; v[3] += x[3];
+                }
+                return v;
+            };
+            static_assert(S::BM == 2 * Q8_BLOCK && S::BM * S::BN / 8 % 64 == 0, "a token of the tile is one block, whole wavefronts have pieces");
+            for (int idx = (int)threadIdx.x; idx < S::BM * S::BN / 8; idx += 256 * G) {
+                const int tok = idx >> 3, e = (idx & 7) * 4, col = (e >> 4) * 32 + (e & 15);
+                finish_gated(sum(tok, col), sum(tok, col + 16), n0 + tok, m0 / 2 + e, n, C, gate...);
+            }
+            return;
+        }
         for (int idx = (int)threadIdx.x; idx < S::BM * S::BN / 4; idx += 256 * G) {
             const int tok = idx / (S::BM / 4), col = (idx % (S::BM / 4)) * 4;
             f32x4 v = *(const f32x4*)(part + tok * S::SUM_PITCH + col);
@@ -1305,16 +1340,16 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
 // were measured too: never better than both this and the tile kernels' rings.
 inline int64_t tiles_of_64(int64_t n, int64_t m) { return ((m + 63) / 64) * ((n + 63) / 64); }
 
-template <int F, int G>
+template <int F, int G, class... Gate>
 hipError_t launch_generic_as(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                             const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s) {
+                             const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Gate&... gate) {
     using S = GenSmem<F, G>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     const int tiles_m = (int)((m + S::BM - 1) / S::BM), tiles_n = (int)((n + S::BN - 1) / S::BN);
-    auto kern = K % 128 == 0 ? spmm_generic_kernel<GEN_WHOLE, F, G>
-                : K % 64 == 0 ? spmm_generic_kernel<GEN_PARTIAL, F, G> : spmm_generic_kernel<GEN_RAGGED, F, G>;
+    auto kern = K % 128 == 0 ? spmm_generic_kernel<GEN_WHOLE, F, G, Gate...>
+                : K % 64 == 0 ? spmm_generic_kernel<GEN_PARTIAL, F, G, Gate...> : spmm_generic_kernel<GEN_RAGGED, F, G, Gate...>;
     kern<<<dim3((unsigned)(tiles_m * tiles_n)), dim3(256 * G), 0, s>>>(B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2,
-                                                                       C, tiles_m);
+                                                                       C, tiles_m, gate...);
     return hipGetLastError();
 }
 
@@ -1767,4 +1802,29 @@ hipError_t launch_spmm(const bf16_t* B, int64_t n, const bf16_t* A_vals, const u
     if (e != hipSuccess || rest == 0) return e;
     // second, so that it finds the packed weight in the last-level cache (777 tokens: the other way round 6 us slower)
     return launch_spmm_stream(B + n * K, rest, A_vals, A_meta, m, K, B2 ? B2 - n * K2 : nullptr, A2, -K2, C + n * m, nullptr, s);
+}
+
+// ------------------------------------------------------------------------------------------
+// The gated product: tokens x [gate; up] with h, and what the backward pass keeps, from the epilogue.
+static hipError_t launch_gated_tiles(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T,
+                                     const bf16_t* R, int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
+    const int64_t m = gated_rows(gate.d_ff);
+    if (spmm_generic_edge(n, m) == 64) return launch_generic_as<2, 4>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
+    return launch_generic_as<4, 1>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
+}
+
+// Tokens by as many as a launch's grid holds (d_ff is at most 2^22: at least 1024 of them, in whole tiles)
+hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
+                        int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
+    const int64_t most = ((int64_t)1 << 21) / ((gated_rows(gate.d_ff) + 63) / 64) * 64 / 256 * 256;
+    const size_t d_ff = (size_t)gate.d_ff, blocks = (d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
+    for (int64_t t = 0; t < n; t += most) {
+        GateOut part = gate;
+        if (part.gu) part.gu += (size_t)t * 2 * d_ff;
+        if (part.q) { part.q += (size_t)t * 2 * d_ff; part.bytes += (size_t)t * 2 * blocks; }
+        const hipError_t e = launch_gated_tiles(B + t * K, n - t < most ? n - t : most, A_vals, A_meta, K, T ? T + t * r : nullptr, R, r,
+                                                H + (size_t)t * d_ff, part, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }

@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "dense.h"
+#include "gated.h"
 
 namespace {
 
@@ -64,6 +65,36 @@ __global__ void __launch_bounds__(256) transpose_pad_kernel(TransposeJob j0, Tra
         if (c0 + c >= j.cols || r0 + r8 >= j.rows_pad) continue;
         const uint32_t* src = (const uint32_t*)&tile[c][r8];
         u32x4 v = {src[0], src[1], src[2], src[3]};
+        __builtin_nontemporal_store(v, (u32x4*)(out + (size_t)(c0 + c) * j.ld + r0 + r8));
+    }
+}
+
+// The same from 8-bit blocks (gated.h): a lane reads eight codes, of one block
+__global__ void __launch_bounds__(256) restore_transposed_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ bytes, TransposeJob j) {
+    __shared__ bf16_t tile[64][TP_ROWS + 2];
+    const int64_t w = flat_block();
+    if (w >= j.tiles) return;
+    bf16_t* __restrict__ out = j.out;
+    const int row_tiles = (j.rows_pad + TP_ROWS - 1) / TP_ROWS, r0 = (int)w % row_tiles * TP_ROWS, c0 = (int)w / row_tiles * 64;
+    const int t = threadIdx.x, blocks = (j.cols + Q8_BLOCK - 1) / Q8_BLOCK;
+#pragma unroll
+    for (int p = 0; p < TP_ROWS / 32; ++p) {
+        const int r = (t >> 3) + 32 * p, c8 = (t & 7) * 8;
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (r0 + r < j.rows && c0 + c8 < j.cols) {
+            const u32x2 codes = __builtin_nontemporal_load((const u32x2*)(q + (size_t)(r0 + r) * j.cols + c0 + c8));
+            v = pack_bf16(unpack_e4m3(codes, scale_of_byte(bytes[(size_t)(r0 + r) * blocks + (c0 + c8) / Q8_BLOCK])));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[c8 + e][r] = (bf16_t)(v[e >> 1] >> (16 * (e & 1)));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < TP_ROWS / 32; ++p) {
+        const int idx = t + 256 * p, c = idx / (TP_ROWS / 8), r8 = (idx % (TP_ROWS / 8)) * 8;
+        if (c0 + c >= j.cols || r0 + r8 >= j.rows_pad) continue;
+        const uint32_t* src = (const uint32_t*)&tile[c][r8];
+        const u32x4 v = {src[0], src[1], src[2], src[3]};
         __builtin_nontemporal_store(v, (u32x4*)(out + (size_t)(c0 + c) * j.ld + r0 + r8));
     }
 }
@@ -1017,6 +1048,9 @@ static int wgrad_copies(int64_t d_in, int64_t d_out, int tile) {
     return best;
 }
 
+// With X token-contiguous anyhow: whether dY's copy costs less than reading it as stored (the estimate above)
+static bool wgrad_copies_dy(int64_t d_in, int64_t d_out) { return 4.0 * (double)d_out / 5.9e6 < 0.032 * 2.0 * (double)d_out * (double)d_in / 1.5e9; }
+
 // Layers that the tiles cannot read as stored.  (Not from copies: us, 500 tokens, 64 x (2^24 + 64), copies and tiles 10580, the kernel
 // with 64-bit addresses 4910.)
 static bool too_wide(int64_t d_in, int64_t d_out) { return d_in >= KMAJOR_EXTENT_MAX || d_out >= KMAJOR_EXTENT_MAX; }
@@ -1043,6 +1077,30 @@ hipError_t launch_wgrad_masked(const bf16_t* dY, const bf16_t* X, int64_t b, con
         case COPY_X | COPY_DY: return launch_dense_tn_split<EPI, false, false>(x, dy, bp / 64, meta, gvals, s, tail_or_null);
         default: return launch_dense_tile<EPI, true, true>(tile, x, dy, bp / 64, meta, gvals, s, tail_or_null);
     }
+}
+
+// The same product from X in 8-bit blocks, restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles
+// get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
+// others, and layers that go elsewhere, X as stored.  Either form of X is in Xt.
+hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
+                                  int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s) {
+    const int64_t bp = (b + 63) / 64 * 64, ld = token_pitch(bp);
+    const bool tiles = !too_wide(d_in, d_out) && !wgrad_in_groups(b, d_in, d_out) && d_in % 32 == 0;
+    if (!tiles || (!tail_or_null && dense_tile_choice(d_in, d_out, bp / 64, gradient_operands(b, d_in, d_out)) != 0)) {
+        const hipError_t e = launch_restore_q8(q, bytes, b, d_in, Xt, s);
+        return e != hipSuccess ? e : launch_wgrad_masked(dY, Xt, b, meta, d_out, d_in, gvals, nullptr, nullptr, tail_or_null, s);
+    }
+    const TransposeJob job = transpose_job(nullptr, b, d_in, bp, ld, Xt);
+    restore_transposed_kernel<<<grid_of(job.tiles), dim3(256), 0, s>>>(q, bytes, job);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const DenseOperand x = {Xt, (int)d_in, (int)ld, (int)bp};
+    constexpr int EPI = EPI_MASKED_PACKED;
+    if (!wgrad_copies_dy(d_in, d_out))
+        return launch_dense_tn_split<EPI, false, true>(x, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, s, tail_or_null);
+    e = launch_transposes(transpose_job(dY, b, d_out, bp, ld, dYt), TransposeJob{}, s);
+    if (e != hipSuccess) return e;
+    return launch_dense_tn_split<EPI, false, false>(x, {dYt, (int)d_out, (int)ld, (int)bp}, bp / 64, meta, gvals, s, tail_or_null);
 }
 
 // C[n, m] = B[n, K] * A[m, K]^T for the skinny products of the adapters (T = X L, dY R^T, and over the tokens dL and

@@ -1,0 +1,381 @@
+"""The gated feed-forward layer and activations kept in 8 bits: HIP path vs the oracle in 64 bits.
+
+Bounds of an element, u = 2^-8 being half a step of bf16:
+  - a projection before it is rounded: fp32 sums of K / 2 products (r more with an adapter) are off by at most (K / 2 + r + 8) 2^-24 of the
+    terms' magnitudes, S; with an adapter X L is rounded to bf16 on the way, u of |X L| |R|.  E is the sum of both.
+  - g and u as they are kept: u of the value, and E; in 8 bits 2^-4 of the value or 2^-10 of the scale, and 1.1 E (the rounding of a
+    value that is E off may go the other way, by no more than that).
+  - h = act(g) u: |act'| <= 1.13, so 1.13 E_g |u| + |act(g)| E_u + E_g E_u; the exponential's argument and result, the reciprocal and two
+    products are off by (|g| + 8) 2^-22 of the value together (gelu: its argument is 1.6 (g + 0.045 g^3)); one rounding, u.
+  - the gradient, from given g and u: the same for du = dh act(g); dg = dh u act'(g), where the terms of act' = s + g s (1 - s) ... may
+    cancel: the relative part is taken of |dh u| (1 + |g|).
+  - the logistic function is 1 / (1 + e^-x), and the reciprocal instruction gives zero for results below fp32's normal numbers: s is off by
+    up to 2^-126, so a by 2^-126 |g| and act' by 2^-126 (1 + 1.6 |g| (1 + 0.135 g^2)).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import slope_oracle as so
+from oracle import surroundings_oracle as oo
+from paper_2405_16325_amd import binding as sl
+from paper_2405_16325_amd import inputs
+from tests.parity_util import check_product
+
+pytestmark = pytest.mark.gpu
+ACTS = {"silu": sl.SLOPE_ACT_SILU, "gelu": sl.SLOPE_ACT_GELU, "relu": sl.SLOPE_ACT_RELU}
+HALF, FLUSH = 2.0 ** -8, 2.0 ** -126
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def codes_of(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+class Layer:
+    """Operands of a gated layer and its projections in 64 bits, with what fp32 sums may be off."""
+
+    def __init__(self, b, d_ff, d_in, r=0, seed=0, std=None):
+        std = std or d_in ** -0.5
+        self.b, self.d_ff, self.d_in = b, d_ff, d_in
+        x = inputs.gaussian_bf16((b, d_in), 1.0, seed, 1)
+        w = inputs.gaussian_bf16((2 * d_ff, d_in), std, seed, 2)
+        self.x = sl.bf16_to_device(x)
+        vals, meta, _ = so.prune_rows_packed(w)
+        self.vals, self.meta = sl.bf16_to_device(vals), torch.from_numpy(meta).cuda()
+        xd, wd = so.bf16_to_f64(x), so.bf16_to_f64(w) * so.prune_rows(w)
+        self.gu = xd @ wd.T
+        self.off = (d_in / 2 + r + 8) * 2.0 ** -24 * (np.abs(xd) @ np.abs(wd).T)
+        self.l = self.r = None
+        if r:
+            lb, rb = inputs.gaussian_bf16((d_in, r), 0.05, seed, 4), inputs.gaussian_bf16((r, 2 * d_ff), 0.2, seed, 5)
+            self.l, self.r = sl.bf16_to_device(lb), sl.bf16_to_device(rb)
+            ld, rd = so.bf16_to_f64(lb), so.bf16_to_f64(rb)
+            t = xd @ ld
+            self.gu = self.gu + t @ rd
+            t_off = HALF * np.abs(t) + (d_in + 8) * 2.0 ** -24 * (np.abs(xd) @ np.abs(ld))
+            self.off = self.off + t_off @ np.abs(rd) + (d_in / 2 + r + 8) * 2.0 ** -24 * (np.abs(t) @ np.abs(rd))
+
+
+def relative(g, act):
+    z = np.abs(g) if act == "silu" else 1.6 * (np.abs(g) + 0.045 * np.abs(g) ** 3)
+    return (z + 8) * 2.0 ** -22
+
+
+def check_h(got, gu, off, act, what):
+    d_ff = got.shape[1]
+    g, u, eg, eu = gu[:, :d_ff], gu[:, d_ff:], off[:, :d_ff], off[:, d_ff:]
+    a = oo.activation(g, act)[0]
+    want = a * u
+    bound = 1.13 * eg * (np.abs(u) + eu) + np.abs(a) * eu + (HALF + relative(g, act)) * np.abs(want) + FLUSH * np.abs(g * u) + 1e-38
+    bad = ~(np.abs(got - want) <= bound * 1.01)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+def check_kept(got, want, off, what):
+    bad = ~(np.abs(got - want) <= HALF * (np.abs(want) + off) + off + 1e-38)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+def check_blocks(codes, bytes_, want, off, what):
+    """codes u8[rows, d], bytes u8[rows, blocks] of values want, which may be `off` off."""
+    got = oo.restored(codes, bytes_)
+    scale = np.repeat(2.0 ** (bytes_.astype(np.float64) - 127), 32, axis=1)[:, :codes.shape[1]]
+    bad = ~(np.abs(got - want) <= np.maximum(2.0 ** -4 * (np.abs(want) + off), 2.0 ** -10 * scale) + 1.1 * off)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+    for c in range(bytes_.shape[1]):                                        # the smallest scale that holds the block
+        part, e = np.abs(want[:, c * 32:(c + 1) * 32]), off[:, c * 32:(c + 1) * 32]
+        s = 2.0 ** (bytes_[:, c].astype(np.float64) - 127)
+        assert ((part - e).max(1) <= 448 * s).all() and (((part + e).max(1) > 224 * s) | (bytes_[:, c] == 1)).all(), (what, c)
+
+
+# one token to many; d_ff a multiple of 256, of 64, of 16, of 8 only, less than a block; contractions of whole quads, pairs, odd steps, parts
+SHAPES = [(1, 8, 8), (1, 256, 128), (1, 64, 1024), (2, 1000, 768), (7, 40, 264), (16, 512, 2048), (17, 136, 704), (31, 2048, 256), (32, 72, 64), (33, 128, 384),
+          (40, 520, 1024), (64, 256, 2304), (100, 1000, 1000), (128, 200, 4096), (129, 1024, 1088), (200, 344, 192), (257, 24, 320),
+          (300, 768, 640), (512, 136, 8), (520, 256, 520), (700, 1032, 448), (1000, 1000, 1000), (1030, 2048, 128), (2100, 320, 256)]
+
+
+@pytest.mark.parametrize("b,d_ff,d_in", SHAPES)
+@pytest.mark.parametrize("act,r", [("silu", 0), ("gelu", 32), ("relu", 160)])
+def test_forward(b, d_ff, d_in, act, r):
+    say(f"gated_fwd b={b} d_ff={d_ff} d_in={d_in} act={act} r={r}")
+    p = Layer(b, d_ff, d_in, r, seed=b + d_ff + d_in)
+    args = dict(act=ACTS[act], L=p.l, R=p.r)
+    h, none_gu, none_q, none_s = sl.slope_gated_fwd(p.x, p.vals, p.meta, **args)
+    assert none_gu is None and none_q is None and none_s is None
+    again = sl.slope_gated_fwd(p.x, p.vals, p.meta, **args)[0]
+    kept, gu, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, want_q8=True, **args)
+    torch.cuda.synchronize()
+    check_h(f64(h), p.gu, p.off, act, "h")
+    check_h(f64(kept), p.gu, p.off, act, "h of the call that keeps")
+    assert torch.equal(h, again)
+    check_kept(f64(gu), p.gu, p.off, "gu")
+    check_blocks(codes_of(q).reshape(2 * b, d_ff), scale.cpu().numpy().reshape(2 * b, -1), p.gu.reshape(2 * b, d_ff),
+                 p.off.reshape(2 * b, d_ff), "codes")
+    if r == 0:
+        alone = sl.slope_gated_fwd(p.x, p.vals, p.meta, act=ACTS[act], workspace=None)[0]
+        check_h(f64(alone), p.gu, p.off, act, "h without scratch")
+
+
+@pytest.mark.parametrize("b,d_ff,d_in,r", [(1, 1000, 768, 32), (20, 264, 448, 0), (70, 72, 1024, 64), (300, 328, 640, 0), (515, 1000, 256, 96), (260, 264, 264, 32)])
+def test_nothing_outside_is_written_and_parts_agree(b, d_ff, d_in, r):
+    say(f"gated_fwd guards b={b} d_ff={d_ff} d_in={d_in} r={r}")
+    p = Layer(b, d_ff, d_in, r, seed=3)
+    pad = 4096
+    blocks = (d_ff + 31) // 32
+    sizes = {"h": (b * d_ff, sl.BF16), "gu": (2 * b * d_ff, sl.BF16), "q": (2 * b * d_ff, torch.uint8), "s": (2 * b * blocks, torch.uint8)}
+    whole = {k: torch.full((n + 2 * pad,), 7, dtype=t, device="cuda") for k, (n, t) in sizes.items()}
+    cut = {k: whole[k][pad:pad + n] for k, (n, _) in sizes.items()}
+    out = (cut["h"].view(b, d_ff), cut["gu"].view(b, 2 * d_ff), cut["q"].view(sl.E4M3).view(b, 2 * d_ff), cut["s"].view(b, 2, blocks))
+    sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, out=out)
+    only = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_gu=True)
+    codes = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_q8=True)
+    torch.cuda.synchronize()
+    for k, (n, _) in sizes.items():
+        assert (whole[k][:pad] == 7).all() and (whole[k][pad + n:] == 7).all(), k
+    assert torch.equal(only[0], out[0]) and torch.equal(only[1], out[1]) and torch.equal(codes[3], out[3])
+    assert torch.equal(codes[2].view(torch.uint8), out[2].view(torch.uint8))
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("b,d_ff", [(1, 8), (3, 40), (5, 256), (333, 1000), (64, 2048), (1025, 72)])
+def test_gradient(b, d_ff, act, q8):
+    say(f"gated_bwd b={b} d_ff={d_ff} act={act} q8={q8}")
+    gu = sl.bf16_to_device(inputs.gaussian_bf16((b, 2 * d_ff), 3.0, b + d_ff, 1))
+    dh = sl.bf16_to_device(inputs.gaussian_bf16((b, d_ff), 1e-3, b + d_ff, 2))
+    if q8:
+        q, scale = sl.slope_checkpoint_q8(gu.view(2 * b, d_ff))
+        v = oo.restored(codes_of(q), scale.cpu().numpy()).reshape(b, 2 * d_ff)
+        dgu, h = sl.slope_gated_bwd(dh, ACTS[act], q8=q.view(b, 2 * d_ff), scale=scale.view(b, 2, -1))
+    else:
+        v = f64(gu)
+        dgu, h = sl.slope_gated_bwd(dh, ACTS[act], gu=gu)
+    torch.cuda.synchronize()
+    check_gradient(f64(dgu), f64(h), f64(dh), v, act)
+
+
+def check_gradient(dgu, h, dh, v, act):
+    d_ff = h.shape[1]
+    g, u = v[:, :d_ff], v[:, d_ff:]
+    check_h(h, v, np.zeros_like(v), act, "h")
+    want = oo.gated_grad(dh, v, act)[0]
+    rel = relative(g, act)
+    flushed = FLUSH * np.abs(dh)
+    bound = HALF * np.abs(want) + 1e-38 + np.concatenate(
+        [rel * np.abs(dh * u) * (1 + np.abs(g)) + flushed * np.abs(u) * (1 + 1.6 * np.abs(g) * (1 + 0.135 * g * g)),
+         rel * np.abs(want[:, d_ff:]) + flushed * np.abs(g)], 1)
+    bad = ~(np.abs(dgu - want) <= bound * 1.01)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), dgu[bad][:4], want[bad][:4])
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+def test_gradient_far_from_zero_and_in_place(act):
+    """Gates from -300 to 300 and beyond, where exponentials leave fp32's range; dGU over GU, H over dH; without H."""
+    say(f"gated_bwd far {act}")
+    b, d_ff = 9, 64
+    g = np.linspace(-300, 300, b * d_ff).reshape(b, d_ff)
+    g[0, :8] = [0.0, -0.0, 1e30, -1e30, 3e38, -3e38, 1e-38, -1e-38]
+    gu = torch.from_numpy(np.concatenate([g, np.ones_like(g)], 1)).to(sl.BF16).cuda()
+    dh = torch.full((b, d_ff), 0.5, dtype=sl.BF16, device="cuda")
+    v = f64(gu)
+    plain = sl.slope_gated_bwd(dh, ACTS[act], gu=gu)
+    alone, none = sl.slope_gated_bwd(dh, ACTS[act], gu=gu, want_h=False)
+    assert none is None and torch.equal(alone, plain[0])
+    d = f64(dh)
+    sl.slope_gated_bwd(dh, ACTS[act], gu=gu, out=(gu, dh))
+    torch.cuda.synchronize()
+    assert torch.equal(gu, plain[0]) and torch.equal(dh, plain[1])
+    with np.errstate(over="ignore", invalid="ignore"):
+        want_h = np.where(v[:, :d_ff] < -80, 0.0, oo.gated(np.clip(v, -80, None), act))
+        d_act = np.where(v[:, :d_ff] < -80, 0.0, np.where(v[:, :d_ff] > 80, 1.0, oo.activation(np.clip(v[:, :d_ff], -80, 80), act)[1]))
+    want_h[0, [2, 4]] = v[0, [2, 4]]                                       # (the cube leaves the range of 64 bits)
+    got_h, got = f64(plain[1]), f64(plain[0])
+    assert (np.abs(got_h - want_h) <= 1.1 * HALF * np.abs(want_h) + 1e-25).all()
+    assert (np.abs(got[:, :d_ff] - d * d_act) <= 1.1 * HALF * d * np.abs(d_act) + 2e-6).all()
+    assert (np.abs(got[:, d_ff:] - d * want_h) <= 1.1 * HALF * np.abs(d * want_h) + 1e-25).all()
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("act", list(ACTS))
+def test_nan_and_infinity_reach_the_results(act, q8):
+    b, d_ff = 4, 96
+    g = torch.ones(b, 2 * d_ff)
+    g[0, 3], g[1, 40], g[2, d_ff + 70] = float("nan"), float("inf"), float("nan")
+    gu = g.to(sl.BF16).cuda()
+    dh = torch.ones(b, d_ff, dtype=sl.BF16, device="cuda")
+    kw = dict(gu=gu)
+    if q8:
+        q, s = sl.slope_checkpoint_q8(gu.view(2 * b, d_ff))
+        kw = dict(q8=q.view(b, 2 * d_ff), scale=s.view(b, 2, -1))
+    dgu, h = sl.slope_gated_bwd(dh, ACTS[act], **kw)
+    touched = torch.zeros(b, d_ff, dtype=torch.bool)
+    for row, col in ((0, 3), (1, 40), (2, 70)):
+        if q8:
+            touched[row, col // 32 * 32:col // 32 * 32 + 32] = True        # the block
+        else:
+            touched[row, col] = True
+    assert (torch.isfinite(h.cpu()) == ~touched).all()
+    assert torch.isfinite(dgu.cpu().view(b, 2, d_ff)[~touched[:, None].expand(b, 2, d_ff)]).all()
+
+
+def test_forward_of_tokens_that_are_not_finite():
+    """A token with a NaN spoils its own row and no other; its blocks read NaN."""
+    p = Layer(40, 136, 256, 0, seed=5)
+    x = p.x.clone()
+    x[7, 100], x[23, 0] = float("nan"), float("inf")
+    h, gu, q, scale = sl.slope_gated_fwd(x, p.vals, p.meta, want_gu=True, want_q8=True)
+    clean = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, want_q8=True)
+    rows = [i for i in range(40) if i not in (7, 23)]
+    assert torch.equal(h[rows], clean[0][rows]) and torch.equal(gu[rows], clean[1][rows]) and torch.equal(scale[rows], clean[3][rows])
+    back = sl.slope_restore_q8(q.view(80, 136), scale.view(80, -1)).view(40, 272)
+    assert not torch.isfinite(h[7]).all()
+    lost = ~torch.isfinite(gu).view(40, 2, 136)
+    for i in (7, 23):
+        assert lost[i].any()
+        for half in range(2):
+            for c in range(5):
+                block = slice(c * 32, min(136, (c + 1) * 32))
+                assert torch.isnan(back.view(40, 2, 136)[i, half, block]).all() == bool(lost[i, half, block].any())
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit blocks of an activation
+@pytest.mark.parametrize("rows,d", [(1, 8), (1, 32), (3, 40), (5, 256), (64, 1000), (333, 2048), (1, 36864), (1025, 72), (2, 8200)])
+def test_checkpoint_is_the_oracles_bit_for_bit(rows, d):
+    say(f"checkpoint_q8 {rows} x {d}")
+    bits = inputs.gaussian_bf16((rows, d), 1.0, rows + d, 1)
+    wide = so.bf16_to_f64(bits) * 2.0 ** np.random.default_rng(d).integers(-60, 60, (rows, d)).clip(-3, 3)
+    x = torch.from_numpy(wide).to(sl.BF16)
+    q, scale = sl.slope_checkpoint_q8(x.cuda())
+    back = sl.slope_restore_q8(q, scale)
+    codes, bytes_ = oo.checkpoint(f64(x))
+    assert (scale.cpu().numpy() == bytes_).all() and (codes_of(q) == codes).all()
+    assert (f64(back) == oo.restored(codes, bytes_)).all()
+
+
+def test_checkpoint_at_the_ends_of_the_range():
+    x = torch.zeros(8, 48, dtype=sl.BF16)
+    x[1, 5] = 2.0 ** -133
+    x[2, 0], x[2, 40] = 3.3895313892515355e38, -2.0 ** -126
+    x[3, 31], x[3, 32] = float("inf"), 1.0
+    x[4, 47] = float("nan")
+    x[5, :] = -0.0
+    x[6, :32] = torch.arange(32) * 14.0                                     # up to 434, ties among them
+    x[7, 0], x[7, 1], x[7, 33] = 448.0 * 2.0 ** -126, 2.0 ** -133, 1.9375 * 2.0 ** 127
+    q, scale = sl.slope_checkpoint_q8(x.cuda())
+    back = f64(sl.slope_restore_q8(q, scale))
+    codes, bytes_ = oo.checkpoint(f64(x))
+    assert (scale.cpu().numpy() == bytes_).all()
+    fine = np.repeat(bytes_ != 255, 32, axis=1)[:, :48]
+    assert (codes_of(q)[fine] == codes[fine]).all()
+    want = oo.restored(codes, bytes_)
+    assert (np.isnan(back) == ~fine).all() and (back[fine] == want[fine]).all()
+
+
+def test_restore_reads_every_code_and_byte():
+    """All 256 codes under all 256 bytes: code * 2^(byte - 127), rounded to bf16 where that is below its range or above it."""
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1)
+    bytes_ = torch.arange(256, dtype=torch.uint8)[:, None].expand(256, 8).contiguous()
+    got = f64(sl.slope_restore_q8(codes.cuda().view(sl.E4M3), bytes_.cuda()))
+    want = oo.restored(codes.numpy(), bytes_.numpy())
+    normal = np.abs(want) >= 2.0 ** -126
+    inside = normal & (np.abs(want) < 3.39e38)
+    assert (got[inside] == want[inside]).all() and (np.isnan(got) == np.isnan(want)).all()
+    small = ~normal & ~np.isnan(want)
+    assert (np.abs(got[small] - want[small]) <= 2.0 ** -134).all()          # half a step of bf16's smallest
+    assert np.isinf(got[np.abs(want) >= 3.4e38]).all()
+
+
+# ------------------------------------------------------------------------------------------- the weight gradient from 8-bit blocks
+@pytest.mark.parametrize("b,d_out,d_in", [(1, 8, 8), (3, 64, 40), (64, 256, 256), (100, 72, 1000), (200, 1000, 264), (333, 512, 2048),
+                                          (700, 1032, 448), (1000, 1000, 1000), (2050, 256, 512), (65, 4160, 96), (130, 2304, 2304), (1536, 4096, 4128)])
+def test_weight_gradient(b, d_out, d_in):
+    say(f"wgrad_masked_q8 b={b} d_out={d_out} d_in={d_in}")
+    t = inputs.layer_inputs(b, d_out, d_in, seed=b + d_out)
+    _, meta, _ = so.prune_rows_packed(t["W"])
+    q, scale = sl.slope_checkpoint_q8(sl.bf16_to_device(t["X"]))
+    dy, m = sl.bf16_to_device(t["dY"]), torch.from_numpy(meta).cuda()
+    x = oo.restored(codes_of(q), scale.cpu().numpy())
+    buf = torch.full((d_out * d_in // 2 + 8192,), 7.0, dtype=sl.BF16, device="cuda")
+    out = buf[4096:4096 + d_out * d_in // 2].view(d_out, d_in // 2)
+    sl.slope_wgrad_masked_q8(dy, q, scale, m, out=out)
+    again = sl.slope_wgrad_masked_q8(dy, q, scale, m)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again) and (buf[:4096] == 7).all() and (buf[4096 + d_out * d_in // 2:] == 7).all()
+    xb = inputs.f32_to_bf16_bits(x.astype(np.float32))                      # exact: codes stand for bf16 numbers
+    assert (so.bf16_to_f64(xb) == x).all()
+    check_product(sl.bf16_to_host(out), so.wgrad_masked(t["dY"], xb, meta), "dW")
+
+
+# ----------------------------------------------------------------------------------------------------------- as they are used
+def test_one_training_step_of_a_layer_against_the_oracle():
+    """Forward that keeps 8 bits, the gradient from the codes, both products of the backward pass, all by the library."""
+    b, d_ff, d_in = 300, 520, 256
+    p = Layer(b, d_ff, d_in, 0, seed=11)
+    vals_t, meta_t, _ = sl.slope_double_prune(p.vals, p.meta)
+    xq, xs = sl.slope_checkpoint_q8(p.x)
+    h, _, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_q8=True)
+    dh_bits = inputs.gaussian_bf16((b, d_ff), 1e-3, 11, 3)
+    dgu, again = sl.slope_gated_bwd(sl.bf16_to_device(dh_bits), q8=q, scale=scale)
+    dx = sl.slope_spmm_bwd_x(dgu, vals_t, meta_t)
+    dw = sl.slope_wgrad_masked_q8(dgu, xq, xs, p.meta)
+    torch.cuda.synchronize()
+    v = oo.restored(codes_of(q).reshape(2 * b, d_ff), scale.cpu().numpy().reshape(2 * b, -1)).reshape(b, 2 * d_ff)
+    check_gradient(f64(dgu), f64(again), so.bf16_to_f64(dh_bits), v, "silu")
+    # the products from the device's own dgu, the weights dense again
+    wb = inputs.gaussian_bf16((2 * d_ff, d_in), d_in ** -0.5, 11, 2)
+    mask = so.prune_rows(wb)
+    dense = so.bf16_to_f64(wb) * so.double_prune(wb, mask)
+    check_product(sl.bf16_to_host(dx), f64(dgu) @ dense, "dX")
+    xr = inputs.f32_to_bf16_bits(oo.restored(codes_of(xq), xs.cpu().numpy()).astype(np.float32))
+    check_product(sl.bf16_to_host(dw), so.wgrad_masked(sl.bf16_to_host(dgu), xr, p.meta.cpu().numpy()), "dW")
+
+
+def test_captured_and_replayed_with_new_inputs_between_eager_calls():
+    """Two graphs of the whole step on one set of buffers each, replayed in turn with eager work between."""
+    b, d_ff, d_in, r = 70, 264, 512, 32
+    runs = []
+    for seed in (1, 2):
+        p = Layer(b, d_ff, d_in, r, seed=seed)
+        ws = torch.empty(max(256, sl.slope_workspace_bytes(sl.SLOPE_CALL_GATED_FWD, b, d_in, d_ff, r)), dtype=torch.uint8, device="cuda")
+        dh = sl.bf16_to_device(inputs.gaussian_bf16((b, d_ff), 1e-3, seed, 3))
+
+        def step(p=p, ws=ws, dh=dh):
+            h, _, q, s = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_q8=True, workspace=ws)
+            xq, xs = sl.slope_checkpoint_q8(p.x)
+            dgu, again = sl.slope_gated_bwd(dh, q8=q, scale=s)
+            return h, dgu, again, sl.slope_wgrad_masked_q8(dgu, xq, xs, p.meta), sl.slope_restore_q8(xq, xs)
+
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step()
+        runs.append((graph, held, p, step))
+    for turn in range(4):
+        for graph, held, p, step in runs:
+            p.x.copy_(torch.randn(p.x.shape, generator=torch.Generator().manual_seed(turn)).to(sl.BF16))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [t.clone() for t in held]
+            for a, e in zip(got, step()):
+                assert torch.equal(a, e)
+
+
+def test_on_another_stream():
+    p = Layer(150, 264, 640, 0, seed=4)
+    want = sl.slope_gated_fwd(p.x, p.vals, p.meta)[0]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = sl.slope_gated_fwd(p.x, p.vals, p.meta)[0]
+    side.synchronize()
+    assert torch.equal(got, want)

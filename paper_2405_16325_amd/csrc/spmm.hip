@@ -1370,47 +1370,47 @@ int tile_grid(int tiles_m, int tiles_n, int64_t n, const SplitJob& job) {
     return ((tiles_m * tiles_n * job.nslabs + XCDS - 1) / XCDS + (xl + XCDS - 1) / XCDS) * XCDS;
 }
 
-template <int BM, int BN, bool TAIL, class Job>
+template <int BM, int BN, bool TAIL, class Job, class... Gate>
 hipError_t launch_tile_as(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                          const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job) {
+                          const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job, const Gate&... gate) {
     using S = SpmmSmem<BM, BN>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     int tiles_m = (int)((m + BM - 1) / BM), tiles_n = (int)((n + BN - 1) / BN);
-    hipError_t e = allow_dynamic_lds<spmm_kernel<BM, BN, TAIL, Job>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<spmm_kernel<BM, BN, TAIL, Job, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
     const int grid = tile_grid<BM, BN>(tiles_m, tiles_n, n, job);
-    spmm_kernel<BM, BN, TAIL, Job><<<dim3((unsigned)grid), dim3(SPMM_THREADS), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n, job);
+    spmm_kernel<BM, BN, TAIL, Job, Gate...><<<dim3((unsigned)grid), dim3(SPMM_THREADS), S::TOTAL, s>>>(
+        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n, job, gate...);
     return hipGetLastError();
 }
 
-template <int BM, int BN, bool TAIL, class Job>
+template <int BM, int BN, bool TAIL, class Job, class... Gate>
 hipError_t launch_ring_as(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                          const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job) {
+                          const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job, const Gate&... gate) {
     using S = RingSmem<BM, BN>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     int tiles_m = (int)((m + BM - 1) / BM), tiles_n = (int)((n + BN - 1) / BN);
-    hipError_t e = allow_dynamic_lds<spmm_ring_kernel<BM, BN, TAIL, Job>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<spmm_ring_kernel<BM, BN, TAIL, Job, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
     const int grid = tile_grid<BM, BN>(tiles_m, tiles_n, n, job);
-    spmm_ring_kernel<BM, BN, TAIL, Job><<<dim3((unsigned)grid), dim3(RING_THREADS), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n, job);
+    spmm_ring_kernel<BM, BN, TAIL, Job, Gate...><<<dim3((unsigned)grid), dim3(RING_THREADS), S::TOTAL, s>>>(
+        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n, job, gate...);
     return hipGetLastError();
 }
 
 // a whole product, or one split over k
-template <int BM, int BN, class Job = WholeJob>
+template <int BM, int BN, class Job = WholeJob, class... Gate>
 hipError_t launch_tile(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                       const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job = {}) {
-    auto launch = K % 256 == 0 ? launch_tile_as<BM, BN, false, Job> : launch_tile_as<BM, BN, true, Job>;
-    return launch(B, n, Av, Am, m, K, B2, A2, K2, C, s, job);
+                       const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job = {}, const Gate&... gate) {
+    auto launch = K % 256 == 0 ? launch_tile_as<BM, BN, false, Job, Gate...> : launch_tile_as<BM, BN, true, Job, Gate...>;
+    return launch(B, n, Av, Am, m, K, B2, A2, K2, C, s, job, gate...);
 }
 
-template <int BM, int BN, class Job = WholeJob>
+template <int BM, int BN, class Job = WholeJob, class... Gate>
 hipError_t launch_ring(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                       const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job = {}) {
-    auto launch = K % 128 == 0 ? launch_ring_as<BM, BN, false, Job> : launch_ring_as<BM, BN, true, Job>;
-    return launch(B, n, Av, Am, m, K, B2, A2, K2, C, s, job);
+                       const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Job& job = {}, const Gate&... gate) {
+    auto launch = K % 128 == 0 ? launch_ring_as<BM, BN, false, Job, Gate...> : launch_ring_as<BM, BN, true, Job, Gate...>;
+    return launch(B, n, Av, Am, m, K, B2, A2, K2, C, s, job, gate...);
 }
 
 // C[idx] = bf16( sum over slabs, in order, of P[s][idx] ), four elements per thread
@@ -1428,16 +1428,16 @@ __global__ void __launch_bounds__(256) slab_reduce_kernel(const f32x4* __restric
     C[idx] = o.u;
 }
 
-template <bool PREFETCH, bool TAIL>
+template <bool PREFETCH, bool TAIL, class... Gate>
 hipError_t launch_split_as(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
                            const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, int tiles_m, int tiles_n, int grid,
-                           hipStream_t s) {
+                           hipStream_t s, const Gate&... gate) {
     using S = SplitSmem;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
-    hipError_t e = allow_dynamic_lds<spmm_split_kernel<PREFETCH, TAIL>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<spmm_split_kernel<PREFETCH, TAIL, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
-    spmm_split_kernel<PREFETCH, TAIL><<<dim3((unsigned)grid), dim3(SPMM_THREADS), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n);
+    spmm_split_kernel<PREFETCH, TAIL, Gate...><<<dim3((unsigned)grid), dim3(SPMM_THREADS), S::TOTAL, s>>>(
+        B, (int)n, Av, Am, (int)m, (int)K, B2, A2, (int)K2, C, tiles_m, tiles_n, gate...);
     return hipGetLastError();
 }
 
@@ -1456,18 +1456,19 @@ inline Leftover leftover_tiles(int tiles_m, int tiles_n, int64_t K) {
     return {(int)(tiles - rem), (int)rem, tiles_m, tiles_n};
 }
 
+template <class... Gate>
 hipError_t launch_split(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                        const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s) {
+                        const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s, const Gate&... gate) {
     using S = SplitSmem;
     int tiles_m = (int)((m + S::BM - 1) / S::BM), tiles_n = (int)((n + S::BN - 1) / S::BN);
     const bool prefetch = wide_grid(tiles_m, tiles_n) && (size_t)n * (size_t)K * 2 > LAST_LEVEL_CACHE_BYTES;
-    auto launch = K % 256 == 0 ? (prefetch ? launch_split_as<true, false> : launch_split_as<false, false>)
-                               : (prefetch ? launch_split_as<true, true> : launch_split_as<false, true>);
+    auto launch = K % 256 == 0 ? (prefetch ? launch_split_as<true, false, Gate...> : launch_split_as<false, false, Gate...>)
+                               : (prefetch ? launch_split_as<true, true, Gate...> : launch_split_as<false, true, Gate...>);
     const Leftover left = leftover_tiles(tiles_m, tiles_n, K);
-    const hipError_t e = launch(B, n, Av, Am, m, K, B2, A2, K2, C, tiles_m, tiles_n, left.count ? left.first : super_grid(tiles_m, tiles_n), s);
+    const hipError_t e = launch(B, n, Av, Am, m, K, B2, A2, K2, C, tiles_m, tiles_n, left.count ? left.first : super_grid(tiles_m, tiles_n), s, gate...);
     if (e != hipSuccess || !left.count) return e;
-    if (left.count > RESIDENT / 4) return launch_tile<256, 128>(B, n, Av, Am, m, K, B2, A2, K2, C, s, left);
-    return launch_ring<128, 128>(B, n, Av, Am, m, K, B2, A2, K2, C, s, left);
+    if (left.count > RESIDENT / 4) return launch_tile<256, 128>(B, n, Av, Am, m, K, B2, A2, K2, C, s, left, gate...);
+    return launch_ring<128, 128>(B, n, Av, Am, m, K, B2, A2, K2, C, s, left, gate...);
 }
 
 }  // namespace
@@ -1595,12 +1596,13 @@ static double launch_us(const TileCost& c, double ksteps, int slabs) {
     return us < c.stream ? c.stream : us;
 }
 
-// the tile of least time and that time
-static double best_tile_us(int64_t n, int64_t m, int64_t K, int& bm, int& bn) {
+// the tile of least time and that time; a gated product's tiles have whole blocks of 32 elements for each wavefront: no 192 rows
+static double best_tile_us(int64_t n, int64_t m, int64_t K, int& bm, int& bn, bool gated = false) {
     bm = bn = 64;
     const double ksteps = (double)K / 64.0;
     double least = one_round_of_64(n, m) ? launch_us(tile_cost(n, m, K, 64, 64), ksteps, 1) : 1e300;
     for (const SpmmTile& t : SPMM_TILES) {
+        if (gated && t.bm == 192) continue;
         const TileCost cost = tile_cost(n, m, K, t.bm, t.bn);
         double us = launch_us(cost, ksteps, 1);
         if (t.bm == 256 && t.bn == 256) {                     // whole rounds, and a round of 128 x 128 or 256 x 128 tiles with its launch
@@ -1743,10 +1745,10 @@ constexpr double FEWEST_BYTES = 2.5e6, FEWEST_BYTES_WITH_ADAPTER = 5e6;
 
 // Tile of the product for n tokens, m sparse rows, contraction K: bm = bn = 0 means the generic kernel, whose whole pairs of
 // k-steps on a round of 64 x 64 tiles count as a tile shape of their own.
-void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn) {
+void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn, bool gated) {
     bm = bn = 0;
     if (!tile_kernel_fits(K)) return;
-    best_tile_us(n, m, K, bm, bn);
+    best_tile_us(n, m, K, bm, bn, gated);
     if (bm != 64) return;
     // (whether a product is split is decided by the estimate as it stands; not up to 64 rows, where half of the taller tile is nothing)
     const double bytes = (double)K * (1.125 * (double)m + 2.0 * (double)n);
@@ -1809,7 +1811,18 @@ hipError_t launch_spmm(const bf16_t* B, int64_t n, const bf16_t* A_vals, const u
 static hipError_t launch_gated_tiles(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T,
                                      const bf16_t* R, int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
     const int64_t m = gated_rows(gate.d_ff);
-    if (spmm_generic_edge(n, m) == 64) return launch_generic_as<2, 4>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
+    int bm, bn;
+    spmm_tile_choice(n, m, K, r != 0, bm, bn, true);
+    switch (bm * 1000 + bn) {
+        case 256256: return launch_split(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
+        case 256192: return launch_tile<256, 192>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 256128: return launch_tile<256, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 128128: return launch_ring<128, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 128096: return launch_ring<128, 96>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 128064: return launch_ring<128, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        default: break;
+    }
+    if (bm == 64 || spmm_generic_edge(n, m) == 64) return launch_generic_as<2, 4>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
     return launch_generic_as<4, 1>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
 }
 

@@ -511,6 +511,14 @@ slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t
 slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int with_workspace, int32_t* plan);
 
 /*
+ * slope_gated_fwd_plan - the same for slope_gated_fwd; kept: whether the call keeps GU or GUq.  plan: host int32[5]
+ *   [0] product, [1], [2] rows of the weight, gate and up projection, and tokens per workgroup, [3] slabs, slices or the tokens of
+ *       the small-batch kernel: as slope_spmm_fwd_plan
+ *   [4] whether the small-batch kernel computes T = X L itself
+ */
+slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept, int with_workspace, int32_t* plan);
+
+/*
  * slope_tile_order - diagnostics, host only (no GPU call): the workgroup -> tile assignment the
  * MFMA tile kernels use for a grid of tiles_m x tiles_n tiles (the XCD-aware order behind the
  * products of Eq. 1, 4-6).  Workgroup w of the launch computes tile (tm[w], tn[w]); -1 in both

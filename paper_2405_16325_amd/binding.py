@@ -86,6 +86,7 @@ SIGNATURES = {
     "slope_tile_order": (_I64, [_I64, _I64, _P, _P, _I64]),
     "slope_spmm_fwd_plan": (_INT, [_I64, _I64, _I64, _I64, _INT, _P]),
     "slope_spmm_fwd_q8_plan": (_INT, [_I64, _I64, _I64, _INT, _P]),
+    "slope_gated_fwd_plan": (_INT, [_I64, _I64, _I64, _I64, _INT, _INT, _P]),
 }
 
 _lib = None
@@ -806,3 +807,11 @@ def slope_spmm_fwd_q8_plan(b: int, d_in: int, d_out: int, with_workspace: bool =
     plan = np.zeros(7, dtype=np.int32)
     _check("slope_spmm_fwd_q8_plan", lib().slope_spmm_fwd_q8_plan(b, d_in, d_out, int(with_workspace), plan.ctypes.data))
     return dict(zip(["product", "rows", "tokens", "slabs", "rows0", "padded", "groups"], (int(v) for v in plan)))
+
+
+def slope_gated_fwd_plan(b: int, d_in: int, d_ff: int, r: int = 0, kept: bool = False, with_workspace: bool = True):
+    """Kernels slope_gated_fwd would launch for a shape (host only): dict of the five plan fields."""
+    import numpy as np
+    plan = np.zeros(5, dtype=np.int32)
+    _check("slope_gated_fwd_plan", lib().slope_gated_fwd_plan(b, d_in, d_ff, r, int(kept), int(with_workspace), plan.ctypes.data))
+    return dict(zip(["product", "rows", "tokens", "slabs", "xl"], (int(v) for v in plan)))

@@ -645,9 +645,18 @@ static bool bad_act(int act) { return act != SLOPE_ACT_SILU && act != SLOPE_ACT_
 // rows of d elements in 8-bit blocks: launches of a workgroup per 256 pieces of eight
 static bool bad_blocks(int64_t rows, int64_t d) { return bad_extent(rows, 1) || bad_extent(d, 8) || !grid_fits(rows * ((d + 31) / 32 * 4) / 256 + 1); }
 
+// Bytes of the call's scratch, and its split over d_in: [ adapter | slabs ], or [ adapter | slices ] for a few tokens of which nothing is
+// kept.  The split does not depend on the adapter, whose T = X L has its launches before the product.
+static size_t gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, SpmmSplit& split) {
+    const int64_t m = gated_rows(d_ff);
+    split = spmm_split(b, m, d_in, 0, spmm_slab_room(b, m, d_in), true);
+    return adapter_workspace_bytes(b, d_in, 2 * d_ff, r) + round256(spmm_split_bytes(split, b, m)) + round256(spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+}
+
 size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
     if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
-    return adapter_workspace_bytes(b, d_in, 2 * d_ff, r);
+    SpmmSplit split;
+    return gated_plan(b, d_in, d_ff, r, split);
 }
 
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
@@ -663,18 +672,55 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     const bool adapter = r > 0 && L_or_null && R_or_null;
     if (!adapter) r = 0;
     if (adapter && !workspace_or_null) return SLOPE_ERR_NULL;
-    if (workspace_or_null && workspace_bytes < slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r)) return SLOPE_ERR_WORKSPACE;
+    SpmmSplit split = {0, 0, 0};
+    if (workspace_or_null && workspace_bytes < gated_plan(b, d_in, d_ff, r, split)) return SLOPE_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
+    const bf16_t *x = (const bf16_t*)X, *wv = (const bf16_t*)Wr_vals, *l = adapter ? (const bf16_t*)L_or_null : nullptr;
+    const bf16_t* const R = adapter ? (const bf16_t*)R_or_null : nullptr;
+    const uint8_t* const wm = (const uint8_t*)Wr_meta;
     uint8_t* const ws = (uint8_t*)workspace_or_null;
-    bf16_t* const T = adapter ? (bf16_t*)ws : nullptr;
+    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null};
+    const bool few = spmm_stream_fits(b, d_in) && !gate.gu && !gate.q;
+    float* const after = (float*)(ws + adapter_workspace_bytes(b, d_in, 2 * d_ff, r));
+    float* const slices = few && ws && spmm_rows_partial_bytes(b, 2 * d_ff, d_in) ? after : nullptr;
+    bf16_t* T = adapter ? (bf16_t*)ws : nullptr;
+    if (few && adapter && gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices != nullptr))
+        return finish(launch_gated_stream(x, b, wv, wm, d_in, nullptr, l, R, r, (bf16_t*)H, nullptr, gate, s));
     if (adapter) {
         float* const sums = (float*)(ws + round256((size_t)b * r * 2) + round256((size_t)d_in * r * 2));
-        const hipError_t e = token_factor((const bf16_t*)X, b, d_in, (const bf16_t*)L_or_null, r, T, sums, s);
+        const hipError_t e = token_factor(x, b, d_in, l, r, T, sums, s);
         if (e != hipSuccess) return finish(e);
     }
-    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null};
-    return finish(launch_gated((const bf16_t*)X, b, (const bf16_t*)Wr_vals, (const uint8_t*)Wr_meta, d_in, T, (const bf16_t*)R_or_null, r,
-                               (bf16_t*)H, gate, s));
+    if (few) return finish(launch_gated_stream(x, b, wv, wm, d_in, T, nullptr, R, r, (bf16_t*)H, slices, gate, s));
+    if (split.slabs) return finish(launch_gated_slabs(x, b, wv, wm, d_in, T, R, r, split, (bf16_t*)H, after, gate, s));
+    return finish(launch_gated(x, b, wv, wm, d_in, T, R, r, (bf16_t*)H, gate, s));
+}
+
+slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept, int with_workspace, int32_t* plan) {
+    if (!plan) return SLOPE_ERR_NULL;
+    if (bad_layer(b, 2 * d_ff, d_in) || bad_gated(b, d_ff) || r < 0) return SLOPE_ERR_SHAPE;
+    if (r > 0 && bad_rank(r)) return SLOPE_ERR_UNSUPPORTED;
+    for (int i = 0; i < 5; ++i) plan[i] = 0;
+    plan[3] = 1;
+    if (spmm_stream_fits(b, d_in) && !kept) {
+        const int slices = spmm_rows_slices(b, 2 * d_ff, d_in, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+        plan[0] = slices > 0 ? 4 : 0;
+        plan[1] = slices > 0 ? 48 : spmm_stream_rows(b, 2 * d_ff, d_in);
+        plan[2] = b <= 16 ? 16 : 32;
+        if (slices > 0) plan[3] = slices;
+        plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+        return SLOPE_OK;
+    }
+    SpmmSplit split = {0, 0, 0};
+    if (with_workspace) gated_plan(b, d_in, d_ff, r, split);
+    const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in, true);
+    int bm, bn;
+    spmm_tile_choice(b - rest, m, d_in, r > 0, bm, bn, true);
+    if (split.slabs) { plan[0] = 1; plan[1] = split.bm; plan[2] = split.bn; plan[3] = split.slabs; }
+    else if (bm == 0) { plan[0] = 3; plan[1] = plan[2] = spmm_generic_edge(b - rest, m); }
+    else { plan[0] = 2; plan[1] = bm; plan[2] = bn; }
+    if (rest) { plan[0] = 5; plan[3] = (int32_t)rest; }
+    return SLOPE_OK;
 }
 
 slope_status slope_gated_bwd(const void* dH, const void* GU_or_null, const void* GUq_or_null, const void* GU_scale_or_null, int64_t b,

@@ -1657,12 +1657,12 @@ constexpr double SPLIT_MIN_US = 13.5;
 // 18 % at most.  us: 166 tokens, 1280 x 27008, rank 32 52 in 8 slabs of 128 x 64, X L 53 chunks; 34 in 9 of 192 x 64, 37 in the 11
 // that are taken; 264 tokens, 2048 x 14272, rank 64 53 in three of 128 x 64 and 38; 330 tokens, 3328 x 13568, rank 64 64 in three of
 // 256 x 128 and 49.)
-SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room) {
+SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room, bool gated) {
     SpmmSplit best = {0, 0, 0};
     if (room.slabs < 2) return best;
     const bool xl = r > 0 && n <= XL_SMALL_MAX_TOKENS;
     int bm, bn;
-    double least = best_tile_us(n, m, K, bm, bn);
+    double least = best_tile_us(n, m, K, bm, bn, gated);
     if (!xl && least < SPLIT_MIN_US) return best;
     // Whole products of 64 k-steps and more take an eighth longer than estimated beside split ones, on weights from HBM: over 44
     // shapes of 129 to 1024 tokens, k of 4096 to 10000, the form chosen takes 0.4 % longer than the best measured one in the
@@ -1700,7 +1700,7 @@ SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom&
         return best;
     }
     consider({128, 64}, true);
-    consider({192, 64}, true);
+    if (!gated) consider({192, 64}, true);
     consider({128, 128}, true);
     if (n > 64 || K >= 7168) consider(tall, false);
     return best;
@@ -1759,15 +1759,15 @@ void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, in
 // Tokens at the end of a batch that a pass of the small-batch kernel over the packed weight (5 TB/s, 6 us for its launch and
 // the drained chip before it) takes for less than the round of tiles that they begin (0: none): up to 32 beyond a multiple
 // of the tile kernels' 256 or 128 (777 tokens, 20480 x 5120: 139 us in two rounds of tiles, 80 + 25 for 768 and 9 tokens).
-int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K) {
+int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K, bool gated) {
     if (n <= 128 || !tile_kernel_fits(K) || one_round_of_64(n, m)) return 0;
     int bm, bn;
-    double least = best_tile_us(n, m, K, bm, bn);
+    double least = best_tile_us(n, m, K, bm, bn, gated);
     int64_t best = 0;
     for (int64_t edge = 256; edge >= 128; edge /= 2) {
         const int64_t rest = n % edge;
         if (rest == 0 || rest > STREAM_MAX_TOKENS || rest == n) continue;
-        const double us = best_tile_us(n - rest, m, K, bm, bn) + 1.125 * (double)m * (double)K / 5e6 + 6.0;
+        const double us = best_tile_us(n - rest, m, K, bm, bn, gated) + 1.125 * (double)m * (double)K / 5e6 + 6.0;
         if (us < 0.95 * least) { least = us / 0.95; best = rest; }
     }
     return best;
@@ -1826,11 +1826,54 @@ static hipError_t launch_gated_tiles(const bf16_t* B, int64_t n, const bf16_t* A
     return launch_generic_as<4, 1>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
 }
 
+// h, and what is kept, of sums P[slabs][n][m] of the two projections, an element's m / 2 apart, added in slab order.  Four elements per lane,
+// eight lanes per block of 32.
+__global__ void __launch_bounds__(256) gated_sum_kernel(const float* __restrict__ P, int slabs, int n, int m, bf16_t* __restrict__ H, GateOut gate) {
+    const uint32_t pieces = ((uint32_t)gate.d_ff + Q8_BLOCK - 1) / Q8_BLOCK * 8, idx = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t tok = idx / pieces;
+    const int e = (int)(idx - tok * pieces) * 4;
+    const bool has = tok < (uint32_t)n && e < gate.d_ff;
+    f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
+    const float* p = P + (has ? (size_t)tok * m + e : 0);
+#pragma unroll 4
+    for (int sl = 0; sl < slabs; ++sl) {
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + m / 2);
+        p += (size_t)n * m;
+        g[0] += a[0]; g[1] += a[1]; g[2] += a[2]; g[3] += a[3];
+        u[0] += b[0]; u[1] += b[1]; u[2] += b[2]; u[3] += b[3];
+    }
+    finish_gated(g, u, (int)tok, e, n, H, gate);
+}
+
+hipError_t launch_gated_sum(const float* P, int slabs, int64_t n, int64_t m, bf16_t* H, const GateOut& gate, hipStream_t s) {
+    const int64_t pieces = n * ((gate.d_ff + Q8_BLOCK - 1) / Q8_BLOCK * 8);          // few tokens: far below 2^32
+    gated_sum_kernel<<<dim3((unsigned)((pieces + 255) / 256)), dim3(256), 0, s>>>(P, slabs, (int)n, (int)m, H, gate);
+    return hipGetLastError();
+}
+
+// Split over the contraction, as launch_spmm_slabs
+hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
+                              int64_t r, const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s) {
+    const int64_t m = gated_rows(gate.d_ff);
+    const int slab_steps = (int)slab_steps_of(K, split.slabs), nslabs = (int)((K / 64 + slab_steps - 1) / slab_steps);
+    const SplitJob job = {nslabs, slab_steps, slabs, nullptr, nullptr, 0, 0, 0};
+    hipError_t e;
+    switch (split.bm * 1000 + split.bn) {
+        case 128064: e = launch_ring<128, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
+        case 256064: e = launch_ring<256, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
+        case 128128: e = launch_ring<128, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
+        default: e = launch_tile<256, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
+    }
+    return e != hipSuccess ? e : launch_gated_sum(slabs, nslabs, n, m, H, gate, s);
+}
+
 // Tokens by as many as a launch's grid holds (d_ff is at most 2^22: at least 1024 of them, in whole tiles)
 hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
                         int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
     const int64_t most = ((int64_t)1 << 21) / ((gated_rows(gate.d_ff) + 63) / 64) * 64 / 256 * 256;
     const size_t d_ff = (size_t)gate.d_ff, blocks = (d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
+    const int64_t rest = gate.gu || gate.q ? 0 : spmm_rest_tokens(n, gated_rows(gate.d_ff), K, true);
+    n -= rest;                                                // the last few: one pass of the small-batch kernel, behind the others
     for (int64_t t = 0; t < n; t += most) {
         GateOut part = gate;
         if (part.gu) part.gu += (size_t)t * 2 * d_ff;
@@ -1839,5 +1882,6 @@ hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const 
                                                 H + (size_t)t * d_ff, part, s);
         if (e != hipSuccess) return e;
     }
-    return hipSuccess;
+    if (rest == 0) return hipSuccess;
+    return launch_gated_stream(B + n * K, rest, A_vals, A_meta, K, T ? T + n * r : nullptr, nullptr, R, r, H + (size_t)n * d_ff, nullptr, gate, s);
 }

@@ -13,7 +13,7 @@
 // fixed order, and rounded to bf16 by xl_reduce_kernel or where T is used (adapter_finish_kernel).
 // (A first version kept the operands in registers and moved them into MFMA order with ds_bpermute;
 // the permutes capped a compute unit near 23 B/ns, against 44 B/ns with the LDS rings.)
-#include "pipeline.h"
+#include "gated.h"
 #include "skinny.h"
 
 namespace {
@@ -38,6 +38,12 @@ __device__ __forceinline__ void stream_xl_part(const StreamXl& xl, int w, const 
                                     xl.Q + (size_t)part * n * xl.r, smem);
 }
 
+// A gated layer's rows here: each 16 of them are eight of the gate and the same eight of the up projection, so that any number of
+// fragments will do (and d_ff, a multiple of 8, leaves no group open).  Virtual row -> row of the weight, of a plain product and of a
+// gated one; the column of a k-major factor that belongs to eight rows from a multiple of 8 on.
+__device__ __forceinline__ int stream_row(int row) { return row; }
+__device__ __forceinline__ int stream_row(int row, const GateOut& gate) { return (row >> 4) * 8 + (row & 7) + (row & 8 ? gate.d_ff : 0); }
+
 union StB { u32x4 u[2]; bf16x16 v; };
 union StA { u32x4 u; bf16x8 v; };
 
@@ -57,15 +63,37 @@ struct StreamLds {
     static constexpr int TOTAL = RING + WAVES * BM * PART_PITCH * 4;
 };
 
+// h of a workgroup's ELEMENTS elements and all tokens from partial sums sum(virtual row, token, w), w < WAVES, added in order
+template <int ELEMENTS, int WAVES, int THREADS, class Sum>
+__device__ __forceinline__ void store_stream_gated(int n, int e0, bf16_t* __restrict__ H, const GateOut& gate, Sum sum) {
+    constexpr int TOKENS = THREADS / ELEMENTS;                // whole groups of ELEMENTS threads
+    const int t = threadIdx.x, o = t % ELEMENTS, row = (o >> 3) * 16 + (o & 7);
+    if (t >= TOKENS * ELEMENTS || e0 + o >= gate.d_ff) return;
+    with_act(gate.act, [&](auto act) {
+        for (int tok = t / ELEMENTS; tok < n; tok += TOKENS) {
+            float g = 0.f, u = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                g += sum(row, tok, w);
+                u += sum(row + 8, tok, w);
+            }
+            union { __bf16 h; bf16_t u; } r;
+            r.h = (__bf16)(act_value<decltype(act)::value>(g) * u);
+            H[(size_t)tok * gate.d_ff + e0 + o] = r.u;
+        }
+    });
+}
+
 // XL: X L in the same launch (StreamXl); else T is given and xl is not looked at
-template <int MF, int WAVES, int NF, bool XL>
+template <int MF, int WAVES, int NF, bool XL, class... Gate>
 __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_t* __restrict__ B, int n,
                                                                    const bf16_t* __restrict__ Av,
                                                                    const uint8_t* __restrict__ Am, int m, int K,
                                                                    const bf16_t* __restrict__ T,
                                                                    const bf16_t* __restrict__ R, int K2,
-                                                                   bf16_t* __restrict__ C, StreamXl xl) {
+                                                                   bf16_t* __restrict__ C, StreamXl xl, Gate... gate) {
     using S = StreamLds<MF, WAVES, NF>;
+    constexpr bool GATED = sizeof...(Gate) > 0;
     extern __shared__ __align__(16) uint8_t smem[];
     static_assert(skinny_lds(WAVES) <= S::RING, "a part of X L fits");
     int block = (int)blockIdx.x;
@@ -95,7 +123,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
         for (int h = 0; h < 2; ++h) {
             int rl = 8 * h + ld_row;
             int row = m0 + 16 * i + rl;
-            row = row < m ? row : m - 1;
+            row = stream_row(row < m ? row : m - 1, gate...);
             a_src[i][h] = (const uint8_t*)Av + (size_t)row * K + ((ld_slot ^ ((rl >> 1) & 7)) * 16);
         }
     const uint8_t* b_src[NF][2];
@@ -111,7 +139,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
     const uint8_t* m_src;
     {
         int row = m0 + (meta_lane ? lane : 0);
-        row = row < m ? row : m - 1;
+        row = stream_row(row < m ? row : m - 1, gate...);
         m_src = Am + (size_t)row * (K / 8);
     }
     auto issue = [&](int stage, int p) {                      // pair p (valid) into ring stage `stage`
@@ -236,7 +264,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
             for (int idx = t; idx < 128 * SEG; idx += WAVES * 64) {
                 int k = idx / SEG, sg = idx % SEG;
                 u32x4 v = {0u, 0u, 0u, 0u};
-                if (k < kn && m0 + 8 * sg < m) v = *(const u32x4*)(R + (size_t)(kc + k) * m + m0 + 8 * sg);
+                if (k < kn && m0 + 8 * sg < m) v = *(const u32x4*)(R + (size_t)(kc + k) * m + stream_row(m0 + 8 * sg, gate...));
                 *(u32x4*)(r_lds + k * RP + sg * 16) = v;
             }
             __syncthreads();
@@ -274,6 +302,12 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
         __syncthreads();
     }
 
+    if constexpr (GATED) {                                    // thread = (element o, token tok)
+        store_stream_gated<S::BM / 2, WAVES, WAVES * 64>(n, m0 / 2, C, gate..., [&](int row, int tok, int w) {
+            return part[(w * S::BM + row) * S::PART_PITCH + tok];
+        });
+        return;
+    }
     // fixed-order sum and store: thread = (feature o, token tok)
     constexpr int TOK_GROUPS = WAVES * 64 / S::BM;            // whole groups of BM threads
     const int o = t % S::BM;
@@ -293,17 +327,17 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
     }
 }
 
-template <int MF, int WAVES, int NF>
+template <int MF, int WAVES, int NF, class... Gate>
 hipError_t launch_stream_lds(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
-                             const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, const StreamXl& xl, hipStream_t s) {
+                             const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, const StreamXl& xl, hipStream_t s, const Gate&... gate) {
     using S = StreamLds<MF, WAVES, NF>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
-    auto kern = xl.L ? spmm_stream_lds_kernel<MF, WAVES, NF, true> : spmm_stream_lds_kernel<MF, WAVES, NF, false>;
-    hipError_t e = xl.L ? allow_dynamic_lds<spmm_stream_lds_kernel<MF, WAVES, NF, true>>(S::TOTAL)
-                        : allow_dynamic_lds<spmm_stream_lds_kernel<MF, WAVES, NF, false>>(S::TOTAL);
+    auto kern = xl.L ? spmm_stream_lds_kernel<MF, WAVES, NF, true, Gate...> : spmm_stream_lds_kernel<MF, WAVES, NF, false, Gate...>;
+    hipError_t e = xl.L ? allow_dynamic_lds<spmm_stream_lds_kernel<MF, WAVES, NF, true, Gate...>>(S::TOTAL)
+                        : allow_dynamic_lds<spmm_stream_lds_kernel<MF, WAVES, NF, false, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
     kern<<<dim3((unsigned)((m + S::BM - 1) / S::BM + xl.groups)), dim3(WAVES * 64), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, xl);
+        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, xl, gate...);
     return hipGetLastError();
 }
 
@@ -401,18 +435,35 @@ __device__ __forceinline__ void rows_main_loop(const uint8_t* const (&a_src)[2],
     WAIT_HERE(waitcnt_imm(0, 15));                            // drain the clamped look-ahead loads
 }
 
+// h from a wavefront's sums: row the lane's first virtual row, lanes of the upper half the up projection's
+template <int NF>
+__device__ __forceinline__ void store_rows_gated(const f32x4 (&acc)[NF], int n, int row, int lq, int l16, int m, bf16_t* __restrict__ H,
+                                                 const GateOut& gate) {
+    with_act(gate.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+            f32x4 h;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = act_value<decltype(act)::value>(acc[j][e]) * __shfl_xor(acc[j][e], 32);
+            const int tok = 16 * j + l16;
+            if (lq < 2 && tok < n && row < m) *(u32x2*)(H + (size_t)tok * gate.d_ff + stream_row(row, gate)) = four_bf16(h);
+        }
+    });
+}
+
 // K % 1024 == 0.  blockIdx.x: block of 48 weight rows; blockIdx.y: slice of slice_pairs pairs of k-steps (a multiple of
 // 8).  partial == nullptr (one slice): C bf16[n][m]; else fp32 sums into partial[slice][n][m].  The adapter term is
 // added by slice 0.
-template <int NF>
+template <int NF, class... Gate>
 __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t* __restrict__ B, int n,
                                                                    const bf16_t* __restrict__ Av,
                                                                    const uint8_t* __restrict__ Am, int m, int K,
                                                                    const bf16_t* __restrict__ T,
                                                                    const bf16_t* __restrict__ R, int K2,
                                                                    bf16_t* __restrict__ C, float* __restrict__ partial,
-                                                                   int slice_pairs) {
+                                                                   int slice_pairs, Gate... gate) {
     using S = RowsLds<NF>;
+    constexpr bool GATED = sizeof...(Gate) > 0;
     extern __shared__ __align__(16) uint8_t smem[];
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -432,7 +483,7 @@ __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int rl = 8 * h + ld_row;
-        const int row = mw + rl < m ? mw + rl : m - 1;
+        const int row = stream_row(mw + rl < m ? mw + rl : m - 1, gate...);
         a_src[h] = (const uint8_t*)Av + (size_t)row * K + ((ld_slot ^ ((rl >> 1) & 7)) * 16);
         m_src[h] = Am + (size_t)row * (K / 8) + ((ld_slot ^ ((rl >> 1) & 7)) * 16);
     }
@@ -475,7 +526,7 @@ __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t
             for (int idx = t; idx < 128 * SEG; idx += ROWS_WAVES * 64) {
                 int k = idx / SEG, sg = idx % SEG;
                 u32x4 v = {0u, 0u, 0u, 0u};
-                if (k < kn && m0 + 8 * sg < m) v = *(const u32x4*)(R + (size_t)(kc + k) * m + m0 + 8 * sg);
+                if (k < kn && m0 + 8 * sg < m) v = *(const u32x4*)(R + (size_t)(kc + k) * m + stream_row(m0 + 8 * sg, gate...));
                 *(u32x4*)(r_lds + k * RP + sg * 16) = v;
             }
             __syncthreads();
@@ -500,11 +551,19 @@ __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t
 
     // lane (l16, lq) holds token 16 j + l16, rows mw + 4 lq .. + 3 (m is a multiple of 8: the four are inside or outside together)
     const int row = mw + 4 * lq;
+    if constexpr (GATED) {
+        if (!partial) {                                       // lanes l and l + 32 have g and u of the same four elements
+            store_rows_gated<NF>(acc, n, row, lq, l16, m, C, gate...);
+            return;
+        }
+    }
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
         const int tok = 16 * j + l16;
         if (tok >= n || row >= m) continue;
-        if (partial) {
+        if (GATED) {
+            *(f32x4*)(partial + ((size_t)blockIdx.y * n + tok) * m + stream_row(row, gate...)) = acc[j];
+        } else if (partial) {
             *(f32x4*)(partial + ((size_t)blockIdx.y * n + tok) * m + row) = acc[j];
         } else {
             union { __bf16 h[4]; u32x2 u; } o;
@@ -738,37 +797,39 @@ size_t spmm_rows_partial_bytes(int64_t n, int64_t m, int64_t K) {
     return slices > 1 ? (size_t)slices * (size_t)n * (size_t)m * 4 : 0;
 }
 
-template <int NF>
+template <int NF, class... Gate>
 static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
                               const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
-                              hipStream_t s) {
+                              hipStream_t s, const Gate&... gate) {
     using S = RowsLds<NF>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
-    hipError_t e = allow_dynamic_lds<spmm_rows_kernel<NF>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<spmm_rows_kernel<NF, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
     const int64_t chunks = K / 1024, per = (chunks + slices - 1) / slices;
-    spmm_rows_kernel<NF><<<dim3((unsigned)((m + ROWS_BM - 1) / ROWS_BM), (unsigned)slices), dim3(ROWS_WAVES * 64), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, slices > 1 ? partial : nullptr, (int)(per * 8));
+    spmm_rows_kernel<NF, Gate...><<<dim3((unsigned)((m + ROWS_BM - 1) / ROWS_BM), (unsigned)slices), dim3(ROWS_WAVES * 64), S::TOTAL, s>>>(
+        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, slices > 1 ? partial : nullptr, (int)(per * 8), gate...);
     if ((e = hipGetLastError()) != hipSuccess || slices == 1) return e;
+    if constexpr (sizeof...(Gate) > 0) return launch_gated_sum(partial, slices, n, m, C, gate..., s);
     const size_t count4 = (size_t)n * (size_t)m / 4;
     rows_sum_kernel<<<dim3((unsigned)((count4 + 255) / 256)), dim3(256), 0, s>>>((const f32x4*)partial, slices, count4, (u32x2*)C);
     return hipGetLastError();
 }
 
+template <class... Gate>
 static hipError_t launch_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t m, int64_t K,
                                 const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
-                                const StreamXl& xl, hipStream_t s) {
+                                const StreamXl& xl, hipStream_t s, const Gate&... gate) {
     if (slices > 0)
-        return n <= 16 ? launch_rows<1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s)
-                       : launch_rows<2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s);
+        return n <= 16 ? launch_rows<1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...)
+                       : launch_rows<2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
     const int rows = spmm_stream_rows(n, m, K);
     if (n <= 16) {
-        if (rows == 32) return launch_stream_lds<2, 8, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s);
-        if (rows == 48) return launch_stream_lds<3, 6, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s);
-        return launch_stream_lds<4, 4, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s);
+        if (rows == 32) return launch_stream_lds<2, 8, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+        if (rows == 48) return launch_stream_lds<3, 6, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+        return launch_stream_lds<4, 4, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
     }
-    if (rows == 48) return launch_stream_lds<3, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s);
-    return launch_stream_lds<2, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s);
+    if (rows == 48) return launch_stream_lds<3, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+    return launch_stream_lds<2, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
 }
 
 // n <= 32, K % 64 == 0, K >= 128; T (bf16[n][K2]) and R (bf16[K2][m]) only when K2 > 0; partial_or_null: scratch of
@@ -844,6 +905,17 @@ bool launch_spmm_stream_adapter(const bf16_t* B, int64_t n, const bf16_t* A_vals
     e = launch_stream(B, n, A_vals, A_meta, m, K, nullptr, nullptr, 0, nullptr, nullptr, 0, xl, s);
     if (e == hipSuccess) e = launch_adapter_finish(P, 1, n, m, Q, xl.slabs, R, r, C, s);
     return true;
+}
+
+// The gated product for n <= 32 tokens, h only: T = X L given (with slices, that is), or L, where every workgroup computes it by itself
+bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced) {
+    return r > 0 && spmm_rows_slices(n, m, K, sliced) == 0 && xl_by_itself(n, m, K, r);
+}
+hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
+                               const bf16_t* R, int64_t r, bf16_t* H, float* partial_or_null, const GateOut& gate, hipStream_t s) {
+    const int64_t m = 2 * (int64_t)gate.d_ff;
+    const StreamXl xl = {L, nullptr, nullptr, (int)r, 0, 0, 0};
+    return launch_stream(B, n, A_vals, A_meta, m, K, T, R, r, H, partial_or_null, spmm_rows_slices(n, m, K, partial_or_null != nullptr), xl, s, gate);
 }
 
 // Scratch for the partial sums of T = X L: slabs of up to four chunks of 64 rows of L as long as there are still

@@ -1,0 +1,94 @@
+"""Which kernels slope_gated_fwd takes (host only, no GPU), and that the shapes of its GPU tests reach all of them."""
+import pytest
+
+from paper_2405_16325_amd import binding as sl
+from tests.test_gpu_gated import LARGE, SHAPES
+
+SMALL_BATCH, SLABS, TILE, GENERAL, ROW_SPLIT, REST = range(6)
+
+
+def plan(b, d_ff, d_in, r=0, **more):
+    return sl.slope_gated_fwd_plan(b, d_in, d_ff, r, **more)
+
+
+def test_regimes():
+    assert plan(1, 2048, 768)["product"] == SMALL_BATCH
+    assert plan(1, 24576, 9216)["product"] == ROW_SPLIT
+    assert plan(1, 24576, 9216, kept=True)["product"] == TILE                # the small-batch kernels keep nothing
+    assert plan(128, 200, 4096)["product"] == SLABS and plan(128, 200, 4096, with_workspace=False)["product"] == TILE
+    assert plan(1000, 1000, 1000) == {"product": GENERAL, "rows": 64, "tokens": 64, "slabs": 1, "xl": 0}
+    p = plan(16384, 24576, 9216)
+    assert (p["product"], p["rows"], p["tokens"]) == (TILE, 256, 256)
+
+
+def test_no_tile_of_192_rows():
+    """A wavefront's rows of a gated tile are whole blocks of 32 elements."""
+    for b in (40, 100, 300, 777, 1000, 2048, 5000):
+        for d_ff in (96, 1000, 2176, 4352, 13648):
+            for d_in in (128, 2112, 4352):
+                assert plan(b, d_ff, d_in)["rows"] in (64, 128, 256)
+
+
+@pytest.mark.parametrize("bad", [dict(b=0), dict(d_ff=12), dict(d_in=4), dict(d_ff=(1 << 22) + 8)])
+def test_refusals(bad):
+    args = dict(b=4, d_ff=64, d_in=64)
+    args.update(bad)
+    with pytest.raises(sl.SlopeError):
+        plan(**args)
+    with pytest.raises(sl.SlopeError):
+        plan(4, 64, 64, 33)
+
+
+def forms():
+    """(product, rows, tokens, split, X L inside, whether the contraction ends inside what the kernel takes at a time)"""
+    found = set()
+    cases = [(b, f, i, r) for b, f, i in SHAPES for r in (0, 32, 160)] + LARGE
+    for b, f, i, r in cases:
+        for kept in (False, True):
+            for ws in (True, False):
+                if not ws and (r or kept):
+                    continue
+                p = plan(b, f, i, r, kept=kept, with_workspace=ws)
+                whole = 256 if p["rows"] == 256 and p["tokens"] != 64 else 128
+                tail = i % whole != 0 if p["product"] != GENERAL else (i % 64 != 0) + (i % 128 != 0)
+                split = p["slabs"] > 1 and p["product"] in (SLABS, ROW_SPLIT)
+                found.add((p["product"], p["rows"], p["tokens"], split, p["xl"], int(tail)))
+    return found
+
+
+def test_the_gpu_tests_reach_every_form():
+    found = forms()
+    for rows in (32, 48, 64):
+        for xl in (0, 1):
+            for tail in (0, 1):
+                assert (SMALL_BATCH, rows, 16, False, xl, tail) in found, (rows, xl, tail)
+    for rows in (32, 48):
+        for xl in (0, 1):
+            assert any((SMALL_BATCH, rows, 32, False, xl, tail) in found for tail in (0, 1)), (rows, xl)
+    for tokens in (16, 32):
+        assert (ROW_SPLIT, 48, tokens, True, 0, 0) in found
+    assert (ROW_SPLIT, 48, 16, False, 0, 0) in found
+    for rows, tokens in ((128, 64), (128, 128), (256, 64), (256, 128)):
+        for tail in (0, 1):
+            assert (SLABS, rows, tokens, True, 0, tail) in found, (rows, tokens, tail)
+    for rows, tokens in ((128, 64), (128, 96), (128, 128), (256, 128), (256, 192), (256, 256)):
+        for tail in (0, 1):
+            assert (TILE, rows, tokens, False, 0, tail) in found, (rows, tokens, tail)
+    assert (TILE, 64, 64, False, 0, 0) in found
+    for edge, tails in ((64, (1, 2)), (128, (1, 2))):
+        for tail in tails:
+            assert (GENERAL, edge, edge, False, 0, tail) in found, (edge, tail)
+    assert {(REST, 128, 128, False, 0, t) for t in (0,)} <= found and any(f[0] == REST and f[1] == 256 for f in found)
+
+
+def test_tiles_left_over_after_whole_rounds():
+    """256 x 256 tiles of a wide grid, more than whole rounds of 256 by up to half a round: 128 x 128 or 256 x 128 ones."""
+    quarter = half = 0
+    for b, f, i, _ in LARGE:
+        p = plan(b, f, i)
+        if (p["product"], p["rows"], p["tokens"]) != (TILE, 256, 256):
+            continue
+        left = (-(-2 * f // 256)) * (-(-b // 256)) % 256
+        quarter |= (0 < left <= 64 and i >= 2048) << (i % 256 != 0)
+        half |= (64 < left <= 128 and i >= 6144) << (i % 256 != 0)
+    assert quarter == 3 and half == 3

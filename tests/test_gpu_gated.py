@@ -39,6 +39,13 @@ def codes_of(t):
     return t.view(torch.uint8).cpu().numpy()
 
 
+def product(a, b):
+    """a b^T in 64 bits; large ones on the device."""
+    if a.shape[0] * b.shape[0] * a.shape[1] < 1e9:
+        return a @ b.T
+    return (torch.from_numpy(a).cuda() @ torch.from_numpy(b.T.copy()).cuda()).cpu().numpy()
+
+
 class Layer:
     """Operands of a gated layer and its projections in 64 bits, with what fp32 sums may be off."""
 
@@ -51,8 +58,8 @@ class Layer:
         vals, meta, _ = so.prune_rows_packed(w)
         self.vals, self.meta = sl.bf16_to_device(vals), torch.from_numpy(meta).cuda()
         xd, wd = so.bf16_to_f64(x), so.bf16_to_f64(w) * so.prune_rows(w)
-        self.gu = xd @ wd.T
-        self.off = (d_in / 2 + r + 8) * 2.0 ** -24 * (np.abs(xd) @ np.abs(wd).T)
+        self.gu = product(xd, wd)
+        self.off = (d_in / 2 + r + 8) * 2.0 ** -24 * product(np.abs(xd), np.abs(wd))
         self.l = self.r = None
         if r:
             lb, rb = inputs.gaussian_bf16((d_in, r), 0.05, seed, 4), inputs.gaussian_bf16((r, 2 * d_ff), 0.2, seed, 5)
@@ -100,11 +107,30 @@ def check_blocks(codes, bytes_, want, off, what):
 SHAPES = [(1, 8, 8), (1, 256, 128), (1, 64, 1024), (2, 1000, 768), (7, 40, 264), (16, 512, 2048), (17, 136, 704), (31, 2048, 256), (32, 72, 64), (33, 128, 384),
           (40, 520, 1024), (64, 256, 2304), (100, 1000, 1000), (128, 200, 4096), (129, 1024, 1088), (200, 344, 192), (257, 24, 320),
           (300, 768, 640), (512, 136, 8), (520, 256, 520), (700, 1032, 448), (1000, 1000, 1000), (1030, 2048, 128), (2100, 320, 256)]
+# what the small ones do not reach: the other numbers of rows of the small-batch kernel, its row-split form with and without slices, every
+# tile and every split, an odd k-step at the end of each, tokens and tiles that are left over (test_dispatch_gated.py)
+LARGE = [(1, 8, 192, 0), (1, 8, 192, 32), (1, 3912, 192, 32), (1, 6872, 128, 32), (1, 7104, 704, 32), (1, 6656, 320, 0), (17, 8, 128, 32), (19, 8, 192, 32),
+         (1, 4056, 128, 0), (1, 4128, 192, 0), (1, 6848, 128, 0), (5, 6656, 320, 32), (17, 4304, 128, 0), (20, 5120, 192, 32), (1, 12288, 1024, 0),
+         (3, 2056, 17408, 0), (16, 2048, 16384, 64), (20, 2048, 16384, 0), (31, 4104, 16384, 32), (9, 12296, 2048, 96),
+         (1, 4272, 128, 32), (17, 4544, 128, 32), (35, 8, 2816, 32), (40, 8, 2624, 0), (4344, 8, 6144, 0), (3546, 8, 8000, 32),
+         (34, 4584, 7424, 0), (33, 4208, 7616, 32), (131, 2880, 5120, 32), (133, 2752, 4672, 0), (5526, 136, 128, 32), (145, 5480, 192, 0),
+         (195, 5568, 128, 32), (198, 6248, 192, 0), (259, 5504, 256, 160), (258, 5576, 128, 0), (654, 5384, 256, 32), (522, 6592, 128, 0),
+         (783, 6696, 256, 0), (770, 6720, 128, 64), (131, 5448, 64, 32), (142, 5504, 8, 0), (1560, 1280, 3584, 32), (1561, 1280, 3712, 0),
+         (1026, 7232, 768, 0), (2054, 3904, 576, 64), (1024, 8320, 2048, 32), (1000, 8312, 2112, 0), (1024, 10752, 6144, 0), (1020, 10752, 6208, 32)]
 
 
 @pytest.mark.parametrize("b,d_ff,d_in", SHAPES)
 @pytest.mark.parametrize("act,r", [("silu", 0), ("gelu", 32), ("relu", 160)])
 def test_forward(b, d_ff, d_in, act, r):
+    check_forward(b, d_ff, d_in, act, r)
+
+
+@pytest.mark.parametrize("b,d_ff,d_in,r", LARGE)
+def test_forward_of_every_kernel(b, d_ff, d_in, r):
+    check_forward(b, d_ff, d_in, "silu", r)
+
+
+def check_forward(b, d_ff, d_in, act, r):
     say(f"gated_fwd b={b} d_ff={d_ff} d_in={d_in} act={act} r={r}")
     p = Layer(b, d_ff, d_in, r, seed=b + d_ff + d_in)
     args = dict(act=ACTS[act], L=p.l, R=p.r)

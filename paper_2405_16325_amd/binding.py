@@ -656,7 +656,7 @@ def slope_checkpoint_q8(X: torch.Tensor, out=None):
     rows, d = X.shape
     _want(X, BF16, (rows, d), "X")
     if out is None:
-        Q, scale = torch.empty((rows, d), dtype=E4M3, device=X.device), torch.empty((rows, _blocks(d)), dtype=U8, device=X.device)
+        Q, scale = torch.empty_like(X, dtype=E4M3), X.new_empty((rows, _blocks(d)), dtype=U8)
     else:
         Q, scale = _want(out[0], E4M3, (rows, d), "codes"), _want(out[1], U8, (rows, _blocks(d)), "scale")
     _check("slope_checkpoint_q8", lib().slope_checkpoint_q8(_ptr(X), rows, d, _ptr(Q), _ptr(scale), _stream()))
@@ -670,7 +670,7 @@ def slope_restore_q8(Q: torch.Tensor, scale: torch.Tensor, out=None):
     rows, d = Q.shape
     _want(Q, E4M3, (rows, d), "Q")
     _want(scale, U8, (rows, _blocks(d)), "scale")
-    X = _want(out, BF16, (rows, d), "out") if out is not None else torch.empty((rows, d), dtype=BF16, device=Q.device)
+    X = _want(out, BF16, (rows, d), "out") if out is not None else torch.empty_like(Q, dtype=BF16)
     _check("slope_restore_q8", lib().slope_restore_q8(_ptr(Q), _ptr(scale), rows, d, _ptr(X), _stream()))
     return X
 
@@ -690,7 +690,7 @@ def slope_wgrad_masked_q8(dY: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor
     _want(scale, U8, (b, _blocks(d_in)), "scale")
     _want(meta, U8, (d_out, d_in // 8), "meta")
     G = _want(out, BF16, (d_out, d_in // 2), "out") if out is not None \
-        else torch.empty((d_out, d_in // 2), dtype=BF16, device=dY.device)
+        else dY.new_empty((d_out, d_in // 2))
     workspace = _scratch(workspace, int(lib().slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out)), dY.device, "workspace")
     _check("slope_wgrad_masked_q8", lib().slope_wgrad_masked_q8(_ptr(dY), _ptr(Q), _ptr(scale), b, _ptr(meta), d_out, d_in, _ptr(G),
                                                                 _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream()))
@@ -709,10 +709,10 @@ def slope_gated_fwd(X: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, act
     if rows != 2 * d_ff:
         raise ValueError("the weight must have a row of the gate for every row of the up projection")
     if out is None:
-        H = torch.empty((b, d_ff), dtype=BF16, device=X.device)
-        GU = torch.empty((b, rows), dtype=BF16, device=X.device) if want_gu else None
-        Q = torch.empty((b, rows), dtype=E4M3, device=X.device) if want_q8 else None
-        scale = torch.empty((b, 2, _blocks(d_ff)), dtype=U8, device=X.device) if want_q8 else None
+        H = X.new_empty((b, d_ff))
+        GU = X.new_empty((b, rows)) if want_gu else None
+        Q = X.new_empty((b, rows), dtype=E4M3) if want_q8 else None
+        scale = X.new_empty((b, 2, _blocks(d_ff)), dtype=U8) if want_q8 else None
     else:
         H, GU, Q, scale = out
         _want(H, BF16, (b, d_ff), "H")
@@ -743,7 +743,7 @@ def slope_gated_bwd(dH: torch.Tensor, act: int = SLOPE_ACT_SILU, gu=None, q8=Non
         _want(q8, E4M3, (b, 2 * d_ff), "q8")
         _want(scale, U8, (b, 2, _blocks(d_ff)), "scale")
     if out is None:
-        dGU = torch.empty((b, 2 * d_ff), dtype=BF16, device=dH.device)
+        dGU = dH.new_empty((b, 2 * d_ff))
         H = torch.empty_like(dH) if want_h else None
     else:
         dGU, H = out

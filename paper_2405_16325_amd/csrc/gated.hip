@@ -11,6 +11,14 @@
 namespace {
 
 constexpr int THREADS = 256;
+// STREAM: a call that moves more than the last-level cache holds, of which the next one would find nothing there
+template <bool STREAM, class T>
+__device__ __forceinline__ T load(const void* p) { return STREAM ? __builtin_nontemporal_load((const T*)p) : *(const T*)p; }
+template <bool STREAM, class T>
+__device__ __forceinline__ void store(void* p, T v) {
+    if (STREAM) __builtin_nontemporal_store(v, (T*)p);
+    else *(T*)p = v;
+}
 
 // Piece `t` after piece c of row `row`, rows of P pieces
 struct Piece { int64_t row; int c; };
@@ -27,97 +35,131 @@ struct GatedBwd {
     int d_ff, act;
 };
 
-template <int ACT, bool Q8>
-__device__ __forceinline__ void gated_bwd_piece(const GatedBwd& j, int64_t row, int c) {
-    const size_t at = (size_t)row * j.d_ff + c * 8, pair = (size_t)row * (2 * (size_t)j.d_ff) + c * 8;
-    F8 g, u;
-    const F8 dh = unpack_bf16(*(const u32x4*)(j.dh + at));
-    if (Q8) {
-        const size_t blocks = ((size_t)j.d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
-        const uint8_t* const byte = j.bytes + (size_t)row * 2 * blocks + c / 4;
-        g = unpack_e4m3(*(const u32x2*)(j.q + pair), scale_of_byte(byte[0]));
-        u = unpack_e4m3(*(const u32x2*)(j.q + pair + j.d_ff), scale_of_byte(byte[blocks]));
-    } else {
-        g = unpack_bf16(*(const u32x4*)(j.gu + pair));
-        u = unpack_bf16(*(const u32x4*)(j.gu + pair + j.d_ff));
-    }
-    F8 dg, du, h;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const ActValue v = act_gradient<ACT>(g.v[i]);
-        dg.v[i] = dh.v[i] * u.v[i] * v.d;
-        du.v[i] = dh.v[i] * v.a;
-        h.v[i] = v.a * u.v[i];
-    }
-    *(u32x4*)(j.dgu + pair) = pack_bf16(dg);
-    *(u32x4*)(j.dgu + pair + j.d_ff) = pack_bf16(du);
-    if (j.h) *(u32x4*)(j.h + at) = pack_bf16(h);
-}
-
-template <bool Q8>
+template <bool Q8, bool STREAM>
 __global__ void __launch_bounds__(THREADS) gated_bwd_kernel(GatedBwd j) {
     const uint32_t P = (uint32_t)j.d_ff / 8;
     const int64_t first = flat_block() * THREADS, row0 = first / P;
     const Piece p = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x, P);
     if (p.row >= j.n) return;
-    with_act(j.act, [&](auto act) { gated_bwd_piece<decltype(act)::value, Q8>(j, p.row, p.c); });
+    const size_t at = (size_t)p.row * j.d_ff + p.c * 8, pair = (size_t)p.row * (2 * (size_t)j.d_ff) + p.c * 8;
+    F8 g, u;
+    const u32x4 dh_bits = load<STREAM, u32x4>(j.dh + at);
+    if (Q8) {
+        const size_t blocks = ((size_t)j.d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
+        const uint8_t* const byte = j.bytes + (size_t)p.row * 2 * blocks + p.c / 4;
+        const uint32_t gb = byte[0], ub = byte[blocks];
+        const u32x2 gq = load<STREAM, u32x2>(j.q + pair), uq = load<STREAM, u32x2>(j.q + pair + j.d_ff);
+        g = unpack_e4m3(gq, scale_of_byte(gb));
+        u = unpack_e4m3(uq, scale_of_byte(ub));
+    } else {
+        const u32x4 gv = load<STREAM, u32x4>(j.gu + pair), uv = load<STREAM, u32x4>(j.gu + pair + j.d_ff);
+        g = unpack_bf16(gv);
+        u = unpack_bf16(uv);
+    }
+    const F8 dh = unpack_bf16(dh_bits);
+    F8 dg, du, h;
+    with_act(j.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const ActValue v = act_gradient<decltype(act)::value>(g.v[i]);
+            dg.v[i] = dh.v[i] * u.v[i] * v.d;
+            du.v[i] = dh.v[i] * v.a;
+            h.v[i] = v.a * u.v[i];
+        }
+    });
+    store<STREAM>(j.dgu + pair, pack_bf16(dg));
+    store<STREAM>(j.dgu + pair + j.d_ff, pack_bf16(du));
+    if (j.h) store<STREAM>(j.h + at, pack_bf16(h));
 }
 
-// rows of P pieces, whole blocks of four: those past the row's end are none
+// rows of P pieces, whole blocks of four: those past the row's end are none.  PER pieces per thread, THREADS apart.
+template <int PER, bool STREAM>
 __global__ void __launch_bounds__(THREADS) checkpoint_kernel(const bf16_t* __restrict__ x, int64_t rows, int d, uint8_t* __restrict__ q,
                                                              uint8_t* __restrict__ bytes) {
     const uint32_t blocks = ((uint32_t)d + Q8_BLOCK - 1) / Q8_BLOCK, P = 4 * blocks;
-    const int64_t first = flat_block() * THREADS, row0 = first / P;
-    const Piece p = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x, P);
-    const bool has = p.row < rows && p.c * 8 < d;
-    const size_t at = (size_t)p.row * d + p.c * 8;
-    u32x4 in = {0u, 0u, 0u, 0u};
-    if (has) in = *(const u32x4*)(x + at);
-    F8 v = unpack_bf16(in);
-    float top = 0.0f;
+    const int64_t first = flat_block() * (THREADS * PER), row0 = first / P;
+    u32x4 in[PER];
+    Piece p[PER];
+    bool has[PER];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max_abs(top, v.v[i]);
-    uint32_t bits = __float_as_uint(top);                     // a block is four neighbouring lanes
-    bits = MaxBits()(bits, dpp<DPP_XOR1>(bits));
-    bits = MaxBits()(bits, dpp<DPP_XOR2>(bits));
-    if (!has) return;
-    const BlockScale s = block_scale(bits);
+    for (int i = 0; i < PER; ++i) {
+        p[i] = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x + i * THREADS, P);
+        has[i] = p[i].row < rows && p[i].c * 8 < d;
+        in[i] = (u32x4){0u, 0u, 0u, 0u};
+        if (has[i]) in[i] = load<STREAM, u32x4>(x + (size_t)p[i].row * d + p[i].c * 8);
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v.v[i] = s.scaled(v.v[i]);
-    *(u32x2*)(q + at) = pack_e4m3(v);
-    if ((p.c & 3) == 0) bytes[(size_t)p.row * blocks + p.c / 4] = (uint8_t)s.byte;
+    for (int i = 0; i < PER; ++i) {
+        F8 v = unpack_bf16(in[i]);
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max_abs(top, v.v[e]);
+        uint32_t bits = __float_as_uint(top);                 // a block is four neighbouring lanes
+        bits = MaxBits()(bits, dpp<DPP_XOR1>(bits));
+        bits = MaxBits()(bits, dpp<DPP_XOR2>(bits));
+        const BlockScale s = block_scale(bits);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.v[e] = s.scaled(v.v[e]);
+        if (has[i]) {
+            store<STREAM>(q + (size_t)p[i].row * d + p[i].c * 8, pack_e4m3(v));
+            if ((p[i].c & 3) == 0) bytes[(size_t)p[i].row * blocks + p[i].c / 4] = (uint8_t)s.byte;
+        }
+    }
 }
 
+template <int PER, bool STREAM>
 __global__ void __launch_bounds__(THREADS) restore_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ bytes, int64_t rows, int d,
                                                           bf16_t* __restrict__ x) {
     const uint32_t P = (uint32_t)d / 8;
-    const int64_t first = flat_block() * THREADS, row0 = first / P;
-    const Piece p = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x, P);
-    if (p.row >= rows) return;
-    const size_t at = (size_t)p.row * d + p.c * 8, blocks = ((size_t)d + Q8_BLOCK - 1) / Q8_BLOCK;
-    *(u32x4*)(x + at) = pack_bf16(unpack_e4m3(*(const u32x2*)(q + at), scale_of_byte(bytes[(size_t)p.row * blocks + p.c / 4])));
+    const int64_t first = flat_block() * (THREADS * PER), row0 = first / P;
+    const size_t blocks = ((size_t)d + Q8_BLOCK - 1) / Q8_BLOCK;
+    u32x2 in[PER];
+    uint32_t byte[PER];
+    Piece p[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        p[i] = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x + i * THREADS, P);
+        if (p[i].row >= rows) continue;
+        in[i] = load<STREAM, u32x2>(q + (size_t)p[i].row * d + p[i].c * 8);
+        byte[i] = bytes[(size_t)p[i].row * blocks + p[i].c / 4];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (p[i].row < rows) store<STREAM>(x + (size_t)p[i].row * d + p[i].c * 8, pack_bf16(unpack_e4m3(in[i], scale_of_byte(byte[i]))));
 }
 
-inline int64_t groups(int64_t pieces) { return (pieces + THREADS - 1) / THREADS; }
+inline dim3 grid_for(int64_t pieces, int per) { return grid_of((pieces + THREADS * per - 1) / (THREADS * per)); }
+inline bool streams(int64_t bytes) { return bytes > (int64_t)LAST_LEVEL_CACHE_BYTES; }
+// Two pieces per thread to and from 8 bits, unless there are few: us, one / two, 777 x 1000 2.7 / 2.9 and 2.5 / 3.0, 2048 x 2560 6.0 / 5.6
+// and 5.95 / 5.8, 16384 x 9216 88 / 78 and 84 / 79 (four: 6.4, 6.6; 77, 81).  The gradient, which has three to five loads a piece, is slower
+// with two (2048 x 6912 from codes 29.0 / 30.6; 16384 x 24576 694 / 711).
+constexpr int64_t PAIRS_FROM = (int64_t)1 << 18;
 
 }  // namespace
 
-// (callers have checked that the pieces' launches fit: ELEMENTS_MAX)
+// (callers have checked that the pieces' launches fit.  16384 x 24576, non-temporal accesses or not: 694 / 698 us from codes, 805 / 844 from bf16)
 hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q, const uint8_t* bytes, int64_t n, int64_t d_ff, int act,
                             bf16_t* dgu, bf16_t* h, hipStream_t s) {
     const GatedBwd j = {dh, gu, q, bytes, dgu, h, n, (int)d_ff, act};
-    const dim3 grid = grid_of(groups(n * (d_ff / 8)));
-    if (gu) gated_bwd_kernel<false><<<grid, dim3(THREADS), 0, s>>>(j);
-    else gated_bwd_kernel<true><<<grid, dim3(THREADS), 0, s>>>(j);
+    const bool stream = streams(n * d_ff * (6 + (h ? 2 : 0) + (gu ? 4 : 2)));
+    auto kern = gu ? (stream ? gated_bwd_kernel<false, true> : gated_bwd_kernel<false, false>)
+                   : (stream ? gated_bwd_kernel<true, true> : gated_bwd_kernel<true, false>);
+    kern<<<grid_for(n * (d_ff / 8), 1), dim3(THREADS), 0, s>>>(j);
     return hipGetLastError();
 }
 
 hipError_t launch_checkpoint_q8(const bf16_t* x, int64_t rows, int64_t d, uint8_t* q, uint8_t* bytes, hipStream_t s) {
-    checkpoint_kernel<<<grid_of(groups(rows * ((d + Q8_BLOCK - 1) / Q8_BLOCK * 4))), dim3(THREADS), 0, s>>>(x, rows, (int)d, q, bytes);
+    const int64_t pieces = rows * ((d + Q8_BLOCK - 1) / Q8_BLOCK * 4);
+    const int per = pieces < PAIRS_FROM ? 1 : 2;
+    auto kern = per == 1 ? checkpoint_kernel<1, false> : streams(3 * rows * d) ? checkpoint_kernel<2, true> : checkpoint_kernel<2, false>;
+    kern<<<grid_for(pieces, per), dim3(THREADS), 0, s>>>(x, rows, (int)d, q, bytes);
     return hipGetLastError();
 }
 
 hipError_t launch_restore_q8(const uint8_t* q, const uint8_t* bytes, int64_t rows, int64_t d, bf16_t* x, hipStream_t s) {
-    restore_kernel<<<grid_of(groups(rows * (d / 8))), dim3(THREADS), 0, s>>>(q, bytes, rows, (int)d, x);
+    const int64_t pieces = rows * (d / 8);
+    const int per = pieces < PAIRS_FROM ? 1 : 2;
+    auto kern = per == 1 ? restore_kernel<1, false> : streams(3 * rows * d) ? restore_kernel<2, true> : restore_kernel<2, false>;
+    kern<<<grid_for(pieces, per), dim3(THREADS), 0, s>>>(q, bytes, rows, (int)d, x);
     return hipGetLastError();
 }

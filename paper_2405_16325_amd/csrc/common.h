@@ -176,6 +176,9 @@ hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q
                             bf16_t* dgu, bf16_t* h, hipStream_t s);
 hipError_t launch_checkpoint_q8(const bf16_t* x, int64_t rows, int64_t d, uint8_t* q, uint8_t* bytes, hipStream_t s);
 hipError_t launch_restore_q8(const uint8_t* q, const uint8_t* bytes, int64_t rows, int64_t d, bf16_t* x, hipStream_t s);
+bool wgrad_q8_in_groups(int64_t b, int64_t d_in, int64_t d_out);
+hipError_t launch_wgrad_groups_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
+                                  int64_t d_in, bf16_t* gvals, hipStream_t s);
 // dW as launch_wgrad_masked from X in 8-bit blocks; Xt, dYt, tail: required, as for slope_wgrad_masked_ws
 hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s);

@@ -11,7 +11,7 @@
 //   D lane l holds column (d_out) l%16 and rows (d_in) 4*(l/16) .. +3 = exactly one group of four
 //   of W^R's row, so the epilogue picks two of a lane's four accumulators with the group's
 //   metadata nibble and stores them as one 4-byte pair of the packed gradient.
-#include "pipeline.h"
+#include "gated.h"
 
 namespace {
 
@@ -167,12 +167,16 @@ struct WgsSmem {
     static constexpr int RING = WGS_GROUPS * 2 * S::STAGE, SUMS = WGS_GROUPS * WGS_EDGE * WGS_SUM_PITCH * 4;
     static constexpr int TOTAL = RING > SUMS ? RING : SUMS;
 };
+// X in 8-bit blocks (gated.h) instead of bf16: restored between the load and the LDS stage
+struct BlocksX { const uint8_t *q, *bytes; };
+template <class... Blocks>
 __global__ void __launch_bounds__(256 * WGS_GROUPS) wgrad_groups_kernel(const bf16_t* __restrict__ dY,
                                                                         const bf16_t* __restrict__ X, int b,
                                                                         const uint8_t* __restrict__ meta, int d_out,
                                                                         int d_in, bf16_t* __restrict__ G, int tiles_m,
-                                                                        int tiles_n) {
+                                                                        int tiles_n, Blocks... blocks) {
     using S = WgSmem<WGS_EDGE, WGS_EDGE>;
+    constexpr bool Q8 = sizeof...(Blocks) > 0;
     __shared__ __align__(16) uint8_t smem[WgsSmem::TOTAL];
     int tm, tn;
     wgrad_tile_of_block(tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
@@ -185,14 +189,25 @@ __global__ void __launch_bounds__(256 * WGS_GROUPS) wgrad_groups_kernel(const bf
     const int row = t >> 3, c = t & 7;
     const bool a_in = i0 + 8 * c < d_in, b_in = o0 + 8 * c < d_out;      // extents are multiples of 8: whole pieces
     uint4 a_reg, b_reg;
+    u32x2 a_codes;
+    uint32_t a_byte;
+    auto load_blocks = [&](bool in, uint32_t tok, const BlocksX& x) {
+        a_codes = (u32x2){0u, 0u};
+        a_byte = 127u;
+        if (!in) return;
+        a_codes = *(const u32x2*)(x.q + (size_t)tok * d_in + i0 + 8 * c);
+        a_byte = x.bytes[(size_t)tok * (((uint32_t)d_in + Q8_BLOCK - 1) / Q8_BLOCK) + (i0 + 8 * c) / Q8_BLOCK];
+    };
     auto load_global = [&](int slab) {
         const uint32_t tok = (uint32_t)slab * WG_KS + row;     // b < 2^31: past the last token, not around it
-        a_reg = tok < (uint32_t)b && a_in ? *(const uint4*)(X + (size_t)tok * d_in + i0 + 8 * c) : make_uint4(0, 0, 0, 0);
+        if constexpr (Q8) load_blocks(tok < (uint32_t)b && a_in, tok, blocks...);
+        else a_reg = tok < (uint32_t)b && a_in ? *(const uint4*)(X + (size_t)tok * d_in + i0 + 8 * c) : make_uint4(0, 0, 0, 0);
         b_reg = tok < (uint32_t)b && b_in ? *(const uint4*)(dY + (size_t)tok * d_out + o0 + 8 * c) : make_uint4(0, 0, 0, 0);
     };
     auto store_lds = [&](int stage) {
         uint8_t* base = ring + stage * S::STAGE;
-        *(uint4*)(base + row * S::PITCH_A + 16 * c) = a_reg;
+        if constexpr (Q8) *(u32x4*)(base + row * S::PITCH_A + 16 * c) = pack_bf16(unpack_e4m3(a_codes, scale_of_byte(a_byte)));
+        else *(uint4*)(base + row * S::PITCH_A + 16 * c) = a_reg;
         *(uint4*)(base + S::A_BYTES + row * S::PITCH_B + 16 * c) = b_reg;
     };
     f32x4 acc[2][2];
@@ -289,7 +304,24 @@ bool wgrad_in_groups(int64_t b, int64_t d_in, int64_t d_out) {
 hipError_t launch_wgrad_groups(const bf16_t* dY, const bf16_t* X, int64_t b, const uint8_t* meta, int64_t d_out, int64_t d_in,
                                bf16_t* gvals, hipStream_t s) {
     const int64_t tm = (d_in + WGS_EDGE - 1) / WGS_EDGE, tn = (d_out + WGS_EDGE - 1) / WGS_EDGE;
-    wgrad_groups_kernel<<<dim3((unsigned)(tm * tn)), dim3(256 * WGS_GROUPS), 0, s>>>(dY, X, (int)b, meta, (int)d_out, (int)d_in, gvals,
-                                                                                     (int)tm, (int)tn);
+    wgrad_groups_kernel<><<<dim3((unsigned)(tm * tn)), dim3(256 * WGS_GROUPS), 0, s>>>(dY, X, (int)b, meta, (int)d_out, (int)d_in, gvals,
+                                                                                       (int)tm, (int)tn);
+    return hipGetLastError();
+}
+
+// From 8-bit blocks the alternative is two launches, X restored by the first (1.5 to 2.5 us more on the card than from bf16, and 3 us of the
+// host's): up to eight trips through one round of tiles, four through two.  us, restored and dense tiles / here: 1000 x 1000, 16 tokens
+// 5.85 / 4.0, 300 8.1 / 6.2, 600 9.9 / 8.2, 1000 11.9 / 11.3, 1500 14.8 / 15.0; 64 x 256, 600 7.9 / 6.9, 1000 8.9 / 9.3; 256 x 4096, 1000 14.3 / 10.7;
+// 2048 x 512, 1000 10.05 / 10.2; two rounds, 1408 x 1408, 16 6.6 / 5.4, 300 8.7 / 8.2, 600 10.35 / 10.8; four, 2048 x 2048, 100 9.0 / 9.2.
+bool wgrad_q8_in_groups(int64_t b, int64_t d_in, int64_t d_out) {
+    const int64_t tiles = ((d_in + WGS_EDGE - 1) / WGS_EDGE) * ((d_out + WGS_EDGE - 1) / WGS_EDGE);
+    constexpr int64_t TRIP = WGS_GROUPS * WG_KS;
+    return tiles <= RESIDENT ? b <= 8 * TRIP : tiles <= 2 * RESIDENT && b <= 4 * TRIP;
+}
+hipError_t launch_wgrad_groups_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
+                                  int64_t d_in, bf16_t* gvals, hipStream_t s) {
+    const int64_t tm = (d_in + WGS_EDGE - 1) / WGS_EDGE, tn = (d_out + WGS_EDGE - 1) / WGS_EDGE;
+    wgrad_groups_kernel<BlocksX><<<dim3((unsigned)(tm * tn)), dim3(256 * WGS_GROUPS), 0, s>>>(
+        dY, nullptr, (int)b, meta, (int)d_out, (int)d_in, gvals, (int)tm, (int)tn, BlocksX{q, bytes});
     return hipGetLastError();
 }

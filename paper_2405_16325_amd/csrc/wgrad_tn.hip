@@ -1079,11 +1079,12 @@ hipError_t launch_wgrad_masked(const bf16_t* dY, const bf16_t* X, int64_t b, con
     }
 }
 
-// The same product from X in 8-bit blocks, restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles
-// get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
+// The same product from X in 8-bit blocks.  Small ones are one launch that restores X on its way (launch_wgrad_groups_q8); else X is restored
+// first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
 // others, and layers that go elsewhere, X as stored.  Either form of X is in Xt.
 hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s) {
+    if (wgrad_q8_in_groups(b, d_in, d_out)) return launch_wgrad_groups_q8(dY, q, bytes, b, meta, d_out, d_in, gvals, s);
     const int64_t bp = (b + 63) / 64 * 64, ld = token_pitch(bp);
     const bool tiles = !too_wide(d_in, d_out) && !wgrad_in_groups(b, d_in, d_out) && d_in % 32 == 0;
     if (!tiles || (!tail_or_null && dense_tile_choice(d_in, d_out, bp / 64, gradient_operands(b, d_in, d_out)) != 0)) {

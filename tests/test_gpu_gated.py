@@ -20,6 +20,7 @@ from oracle import slope_oracle as so
 from oracle import surroundings_oracle as oo
 from paper_2405_16325_amd import binding as sl
 from paper_2405_16325_amd import inputs
+from tests.graph_util import kernels
 from tests.parity_util import check_product
 
 pytestmark = pytest.mark.gpu
@@ -338,6 +339,33 @@ def test_weight_gradient(b, d_out, d_in):
     xb = inputs.f32_to_bf16_bits(x.astype(np.float32))                      # exact: codes stand for bf16 numbers
     assert (so.bf16_to_f64(xb) == x).all()
     check_product(sl.bf16_to_host(out), so.wgrad_masked(t["dY"], xb, meta), "dW")
+
+
+# X restored on the way, as stored, token-contiguous; dY's copy; tiles cut along the tokens; layers whose rows are no multiple of 32
+FORMS = [(1024, 1000, 1000, ["wgrad_groups_kernel"]), (512, 2264, 696, ["wgrad_groups_kernel"]), (513, 2264, 696, ["restore_kernel", "dense_tn_kernel"]),
+         (1025, 1000, 1000, ["restore_kernel", "dense_tn_kernel"]), (2048, 5120, 5120, ["restore_transposed_kernel", "dense_tn_split_kernel"]),
+         (999, 4096, 16384, ["restore_transposed_kernel", "transpose_pad_kernel", "dense_tn_split_kernel"]),
+         (1033, 9216, 9216, ["restore_transposed_kernel", "dense_tn_split_kernel", "dense_tn_split_kernel", "tail_finish_kernel"]),
+         (1024, 4096, 16640, ["restore_transposed_kernel", "transpose_pad_kernel", "dense_tn_split_kernel", "dense_tn_split_kernel", "tail_finish_kernel"])]
+
+
+@pytest.mark.parametrize("b,d_out,d_in,names", FORMS)
+def test_weight_gradient_of_every_form(b, d_out, d_in, names):
+    """Some rows of dW against 64 bits; which kernels ran."""
+    say(f"wgrad_masked_q8 forms b={b} d_out={d_out} d_in={d_in}")
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    x = torch.randn(b, d_in, generator=gen, device="cuda").to(sl.BF16)
+    dy = torch.randn(b, d_out, generator=gen, device="cuda").mul_(1e-3).to(sl.BF16)
+    _, meta, _ = sl.slope_prune_rows(torch.randn(d_out, d_in, generator=gen, device="cuda").to(sl.BF16))
+    q, scale = sl.slope_checkpoint_q8(x)
+    ws = torch.empty(sl.slope_workspace_bytes(sl.SLOPE_CALL_WGRAD_MASKED_Q8, b, d_in, d_out), dtype=torch.uint8, device="cuda")
+    out = torch.zeros(d_out, d_in // 2, dtype=sl.BF16, device="cuda")
+    assert [k[0] for k in kernels(lambda: sl.slope_wgrad_masked_q8(dy, q, scale, meta, out=out, workspace=ws))] == names
+    sl.slope_wgrad_masked_q8(dy, q, scale, meta, out=out, workspace=ws)
+    rows = torch.randperm(d_out, generator=torch.Generator().manual_seed(1))[:96].sort().values.cuda()
+    want = dy[:, rows].double().t().contiguous() @ sl.slope_restore_q8(q, scale).double()
+    mask = torch.from_numpy(so.meta_to_mask(meta[rows].cpu().numpy())).cuda()
+    check_product(sl.bf16_to_host(out[rows]), want[mask].view(len(rows), -1).cpu().numpy(), "dW")
 
 
 # ----------------------------------------------------------------------------------------------------------- as they are used

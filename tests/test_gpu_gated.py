@@ -40,68 +40,109 @@ def codes_of(t):
     return t.view(torch.uint8).cpu().numpy()
 
 
-def product(a, b):
-    """a b^T in 64 bits; large ones on the device."""
-    if a.shape[0] * b.shape[0] * a.shape[1] < 1e9:
-        return a @ b.T
-    return (torch.from_numpy(a).cuda() @ torch.from_numpy(b.T.copy()).cuda()).cpu().numpy()
+def double(t):
+    return t.detach().float().double()
+
+
+def dense_of(vals, meta):
+    """Packed 2:4 -> fp64[rows, cols], on the device."""
+    rows, half = vals.shape
+    m = meta.to(torch.int64)
+    at = torch.stack([m & 3, m >> 2 & 3, (m >> 4 & 3) + 4, (m >> 6) + 4], dim=-1) + 8 * torch.arange(m.shape[1], device="cuda")[:, None]
+    return torch.zeros(rows, 2 * half, dtype=torch.float64, device="cuda").scatter_(1, at.view(rows, half), double(vals))
 
 
 class Layer:
-    """Operands of a gated layer and its projections in 64 bits, with what fp32 sums may be off."""
+    """Operands of a gated layer and its projections in 64 bits, with what fp32 sums may be off (on the device: some are large)."""
 
-    def __init__(self, b, d_ff, d_in, r=0, seed=0, std=None):
-        std = std or d_in ** -0.5
+    def __init__(self, b, d_ff, d_in, r=0, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+
+        def gauss(shape, std):
+            return torch.randn(shape, generator=gen, device="cuda").mul_(std).to(sl.BF16)
+
         self.b, self.d_ff, self.d_in = b, d_ff, d_in
-        x = inputs.gaussian_bf16((b, d_in), 1.0, seed, 1)
-        w = inputs.gaussian_bf16((2 * d_ff, d_in), std, seed, 2)
-        self.x = sl.bf16_to_device(x)
-        vals, meta, _ = so.prune_rows_packed(w)
-        self.vals, self.meta = sl.bf16_to_device(vals), torch.from_numpy(meta).cuda()
-        xd, wd = so.bf16_to_f64(x), so.bf16_to_f64(w) * so.prune_rows(w)
-        self.gu = product(xd, wd)
-        self.off = (d_in / 2 + r + 8) * 2.0 ** -24 * product(np.abs(xd), np.abs(wd))
+        self.x = gauss((b, d_in), 1.0)
+        self.vals, self.meta, _ = sl.slope_prune_rows(gauss((2 * d_ff, d_in), d_in ** -0.5))
+        x, w = double(self.x), dense_of(self.vals, self.meta).t().contiguous()
+        self.gu = x @ w
+        self.off = (d_in / 2 + r + 8) * 2.0 ** -24 * (x.abs() @ w.abs_())
         self.l = self.r = None
         if r:
-            lb, rb = inputs.gaussian_bf16((d_in, r), 0.05, seed, 4), inputs.gaussian_bf16((r, 2 * d_ff), 0.2, seed, 5)
-            self.l, self.r = sl.bf16_to_device(lb), sl.bf16_to_device(rb)
-            ld, rd = so.bf16_to_f64(lb), so.bf16_to_f64(rb)
-            t = xd @ ld
+            self.l, self.r = gauss((d_in, r), 0.05), gauss((r, 2 * d_ff), 0.2)
+            ld, rd = double(self.l), double(self.r)
+            t = x @ ld
             self.gu = self.gu + t @ rd
-            t_off = HALF * np.abs(t) + (d_in + 8) * 2.0 ** -24 * (np.abs(xd) @ np.abs(ld))
-            self.off = self.off + t_off @ np.abs(rd) + (d_in / 2 + r + 8) * 2.0 ** -24 * (np.abs(t) @ np.abs(rd))
+            t_off = HALF * t.abs() + (d_in + 8) * 2.0 ** -24 * (x.abs() @ ld.abs())
+            self.off += t_off @ rd.abs() + (d_in / 2 + r + 8) * 2.0 ** -24 * (t.abs() @ rd.abs())
+
+
+def activation(g, act):
+    """(act(g), act'(g)) in 64 bits, as the oracle has them (test_the_reference_on_the_device)."""
+    if act == "relu":
+        return g.clamp(min=0), (g > 0).double()
+    if act == "silu":
+        s = 1 / (1 + torch.exp(-g))
+        return g * s, s + g * s * (1 - s)
+    c = 2 * (2 / np.pi) ** 0.5
+    s = 1 / (1 + torch.exp(-c * (g + 0.044715 * g ** 3)))
+    return g * s, s + g * s * (1 - s) * c * (1 + 3 * 0.044715 * g ** 2)
+
+
+def restored(codes, bytes_):
+    """Values of 8-bit blocks, fp64."""
+    value = torch.from_numpy(oo.e4m3_value(np.arange(256))).cuda()[codes.view(torch.uint8).long()]
+    return value * scale_of(bytes_, codes.shape[1])
+
+
+def scale_of(bytes_, d):
+    power = torch.from_numpy(np.append(2.0 ** (np.arange(255) - 127.0), np.nan)).cuda()[bytes_.long()]
+    return power.repeat_interleave(32, dim=1)[:, :d]
 
 
 def relative(g, act):
-    z = np.abs(g) if act == "silu" else 1.6 * (np.abs(g) + 0.045 * np.abs(g) ** 3)
+    z = g.abs() if act == "silu" else 1.6 * (g.abs() + 0.045 * g.abs() ** 3)
     return (z + 8) * 2.0 ** -22
+
+
+def within(got, want, bound, what):
+    bad = ~((double(got) - want).abs() <= bound)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4].tolist(), want[bad][:4].tolist())
 
 
 def check_h(got, gu, off, act, what):
     d_ff = got.shape[1]
     g, u, eg, eu = gu[:, :d_ff], gu[:, d_ff:], off[:, :d_ff], off[:, d_ff:]
-    a = oo.activation(g, act)[0]
+    a = activation(g, act)[0]
     want = a * u
-    bound = 1.13 * eg * (np.abs(u) + eu) + np.abs(a) * eu + (HALF + relative(g, act)) * np.abs(want) + FLUSH * np.abs(g * u) + 1e-38
-    bad = ~(np.abs(got - want) <= bound * 1.01)
-    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+    bound = 1.13 * eg * (u.abs() + eu) + a.abs() * eu + (HALF + relative(g, act)) * want.abs() + FLUSH * (g * u).abs() + 1e-38
+    within(got, want, bound * 1.01, what)
 
 
 def check_kept(got, want, off, what):
-    bad = ~(np.abs(got - want) <= HALF * (np.abs(want) + off) + off + 1e-38)
-    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+    within(got, want, HALF * (want.abs() + off) + off + 1e-38, what)
 
 
 def check_blocks(codes, bytes_, want, off, what):
-    """codes u8[rows, d], bytes u8[rows, blocks] of values want, which may be `off` off."""
-    got = oo.restored(codes, bytes_)
-    scale = np.repeat(2.0 ** (bytes_.astype(np.float64) - 127), 32, axis=1)[:, :codes.shape[1]]
-    bad = ~(np.abs(got - want) <= np.maximum(2.0 ** -4 * (np.abs(want) + off), 2.0 ** -10 * scale) + 1.1 * off)
-    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
-    for c in range(bytes_.shape[1]):                                        # the smallest scale that holds the block
-        part, e = np.abs(want[:, c * 32:(c + 1) * 32]), off[:, c * 32:(c + 1) * 32]
-        s = 2.0 ** (bytes_[:, c].astype(np.float64) - 127)
-        assert ((part - e).max(1) <= 448 * s).all() and (((part + e).max(1) > 224 * s) | (bytes_[:, c] == 1)).all(), (what, c)
+    """codes e4m3[rows, d], bytes u8[rows, blocks] of values want, which may be `off` off."""
+    d = codes.shape[1]
+    within(restored(codes, bytes_), want, torch.maximum(2.0 ** -4 * (want.abs() + off), 2.0 ** -10 * scale_of(bytes_, d)) + 1.1 * off, what)
+    pad = (0, bytes_.shape[1] * 32 - d)                                     # the smallest scale that holds the block
+    least = torch.nn.functional.pad((want.abs() - off).clamp(min=0), pad).view(len(codes), -1, 32).amax(2)
+    most = torch.nn.functional.pad(want.abs() + off, pad).view(len(codes), -1, 32).amax(2)
+    s = torch.pow(2.0, bytes_.double() - 127)
+    assert (least <= 448 * s * 1.0001).all() and ((most * 1.0001 > 224 * s) | (bytes_ == 1)).all(), what
+
+
+def test_the_reference_on_the_device():
+    p = Layer(5, 40, 64, 32, seed=1)
+    x, w = f64(p.x), so.bf16_to_f64(so.unpack_2to4(sl.bf16_to_host(p.vals), p.meta.cpu().numpy()))
+    assert np.allclose(p.gu.cpu().numpy(), x @ w.T + x @ f64(p.l) @ f64(p.r), rtol=0, atol=1e-12)
+    for act in ACTS:
+        for mine, theirs in zip(activation(p.gu, act), oo.activation(p.gu.cpu().numpy(), act)):
+            assert np.allclose(mine.cpu().numpy(), theirs, rtol=1e-12, atol=1e-14)
+    q, s = sl.slope_checkpoint_q8(p.x)
+    assert (restored(q, s).cpu().numpy() == oo.restored(codes_of(q), s.cpu().numpy())).all()
 
 
 # one token to many; d_ff a multiple of 256, of 64, of 16, of 8 only, less than a block; contractions of whole quads, pairs, odd steps, parts
@@ -140,15 +181,14 @@ def check_forward(b, d_ff, d_in, act, r):
     again = sl.slope_gated_fwd(p.x, p.vals, p.meta, **args)[0]
     kept, gu, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, want_q8=True, **args)
     torch.cuda.synchronize()
-    check_h(f64(h), p.gu, p.off, act, "h")
-    check_h(f64(kept), p.gu, p.off, act, "h of the call that keeps")
+    check_h(h, p.gu, p.off, act, "h")
+    check_h(kept, p.gu, p.off, act, "h of the call that keeps")
     assert torch.equal(h, again)
-    check_kept(f64(gu), p.gu, p.off, "gu")
-    check_blocks(codes_of(q).reshape(2 * b, d_ff), scale.cpu().numpy().reshape(2 * b, -1), p.gu.reshape(2 * b, d_ff),
-                 p.off.reshape(2 * b, d_ff), "codes")
+    check_kept(gu, p.gu, p.off, "gu")
+    check_blocks(q.view(2 * b, d_ff), scale.view(2 * b, -1), p.gu.view(2 * b, d_ff), p.off.view(2 * b, d_ff), "codes")
     if r == 0:
         alone = sl.slope_gated_fwd(p.x, p.vals, p.meta, act=ACTS[act], workspace=None)[0]
-        check_h(f64(alone), p.gu, p.off, act, "h without scratch")
+        check_h(alone, p.gu, p.off, act, "h without scratch")
 
 
 @pytest.mark.parametrize("b,d_ff,d_in,r", [(1, 1000, 768, 32), (20, 264, 448, 0), (70, 72, 1024, 64), (300, 328, 640, 0), (515, 1000, 256, 96), (260, 264, 264, 32)])
@@ -180,27 +220,25 @@ def test_gradient(b, d_ff, act, q8):
     dh = sl.bf16_to_device(inputs.gaussian_bf16((b, d_ff), 1e-3, b + d_ff, 2))
     if q8:
         q, scale = sl.slope_checkpoint_q8(gu.view(2 * b, d_ff))
-        v = oo.restored(codes_of(q), scale.cpu().numpy()).reshape(b, 2 * d_ff)
+        v = restored(q, scale).view(b, 2 * d_ff)
         dgu, h = sl.slope_gated_bwd(dh, ACTS[act], q8=q.view(b, 2 * d_ff), scale=scale.view(b, 2, -1))
     else:
-        v = f64(gu)
+        v = double(gu)
         dgu, h = sl.slope_gated_bwd(dh, ACTS[act], gu=gu)
     torch.cuda.synchronize()
-    check_gradient(f64(dgu), f64(h), f64(dh), v, act)
+    check_gradient(dgu, h, double(dh), v, act)
 
 
 def check_gradient(dgu, h, dh, v, act):
     d_ff = h.shape[1]
     g, u = v[:, :d_ff], v[:, d_ff:]
-    check_h(h, v, np.zeros_like(v), act, "h")
-    want = oo.gated_grad(dh, v, act)[0]
-    rel = relative(g, act)
-    flushed = FLUSH * np.abs(dh)
-    bound = HALF * np.abs(want) + 1e-38 + np.concatenate(
-        [rel * np.abs(dh * u) * (1 + np.abs(g)) + flushed * np.abs(u) * (1 + 1.6 * np.abs(g) * (1 + 0.135 * g * g)),
-         rel * np.abs(want[:, d_ff:]) + flushed * np.abs(g)], 1)
-    bad = ~(np.abs(dgu - want) <= bound * 1.01)
-    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), dgu[bad][:4], want[bad][:4])
+    check_h(h, v, torch.zeros_like(v), act, "h")
+    a, d = activation(g, act)
+    want = torch.cat([dh * u * d, dh * a], 1)
+    rel, flushed = relative(g, act), FLUSH * dh.abs()
+    bound = HALF * want.abs() + 1e-38 + torch.cat([rel * (dh * u).abs() * (1 + g.abs()) + flushed * u.abs() * (1 + 1.6 * g.abs() * (1 + 0.135 * g * g)),
+                                                   rel * (dh * a).abs() + flushed * g.abs()], 1)
+    within(dgu, want, bound * 1.01, "dgu")
 
 
 @pytest.mark.parametrize("act", list(ACTS))
@@ -381,12 +419,9 @@ def test_one_training_step_of_a_layer_against_the_oracle():
     dx = sl.slope_spmm_bwd_x(dgu, vals_t, meta_t)
     dw = sl.slope_wgrad_masked_q8(dgu, xq, xs, p.meta)
     torch.cuda.synchronize()
-    v = oo.restored(codes_of(q).reshape(2 * b, d_ff), scale.cpu().numpy().reshape(2 * b, -1)).reshape(b, 2 * d_ff)
-    check_gradient(f64(dgu), f64(again), so.bf16_to_f64(dh_bits), v, "silu")
+    check_gradient(dgu, again, double(sl.bf16_to_device(dh_bits)), restored(q.view(2 * b, d_ff), scale.view(2 * b, -1)).view(b, 2 * d_ff), "silu")
     # the products from the device's own dgu, the weights dense again
-    wb = inputs.gaussian_bf16((2 * d_ff, d_in), d_in ** -0.5, 11, 2)
-    mask = so.prune_rows(wb)
-    dense = so.bf16_to_f64(wb) * so.double_prune(wb, mask)
+    dense = so.bf16_to_f64(so.unpack_2to4(sl.bf16_to_host(vals_t), meta_t.cpu().numpy())).T
     check_product(sl.bf16_to_host(dx), f64(dgu) @ dense, "dX")
     xr = inputs.f32_to_bf16_bits(oo.restored(codes_of(xq), xs.cpu().numpy()).astype(np.float32))
     check_product(sl.bf16_to_host(dw), so.wgrad_masked(sl.bf16_to_host(dgu), xr, p.meta.cpu().numpy()), "dW")

@@ -167,6 +167,7 @@ struct GateOut;
 hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
                               int64_t r, const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s);
 hipError_t launch_gated_sum(const float* P, int slabs, int64_t n, int64_t m, bf16_t* H, const GateOut& gate, hipStream_t s);
+bool gated_rows_of_64(int64_t n, int64_t m, int64_t K, int slices);
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced);
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
                                const bf16_t* R, int64_t r, bf16_t* H, float* partial_or_null, const GateOut& gate, hipStream_t s);

@@ -705,7 +705,7 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
     if (spmm_stream_fits(b, d_in) && !kept) {
         const int slices = spmm_rows_slices(b, 2 * d_ff, d_in, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
         plan[0] = slices > 0 ? 4 : 0;
-        plan[1] = slices > 0 ? 48 : spmm_stream_rows(b, 2 * d_ff, d_in);
+        plan[1] = slices > 0 ? (gated_rows_of_64(b, 2 * d_ff, d_in, slices) ? 64 : 48) : spmm_stream_rows(b, 2 * d_ff, d_in);
         plan[2] = b <= 16 ? 16 : 32;
         if (slices > 0) plan[3] = slices;
         plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));

@@ -362,24 +362,24 @@ hipError_t launch_stream_lds(const bf16_t* B, int64_t n, const bf16_t* Av, const
 // 36864 x 9216 at 16 tokens, rank-128 adapters: 91 -> 78 us; 9216 x 36864: 107 -> 85 us; without adapters 67 and 72 us
 // (5.7 and 5.3 TB/s of packed weight).
 constexpr int ROWS_WAVES = 3, ROWS_DEPTH = 3, ROWS_BM = 16 * ROWS_WAVES;
-template <int NF>
+template <int NF, int WAVES = ROWS_WAVES>
 struct RowsLds {
     static constexpr int A_STAGE = 2048;                      // 16 rows x 128 B: both steps of a pair
     static constexpr int M_SLOT = 2048;                       // 16 rows x 128 B: the metadata of 8 pairs
     static constexpr int WAVE_BYTES = ROWS_DEPTH * A_STAGE + 2 * M_SLOT;
     static constexpr int X_OPS = 4 * NF;                      // 1 KiB loads per pair: 2 steps x NF fragments x 2 halves
     static constexpr int X_STAGE = X_OPS * 1024;
-    static constexpr int TOTAL = ROWS_WAVES * WAVE_BYTES + ROWS_DEPTH * X_STAGE;
+    static constexpr int BM = 16 * WAVES, TOTAL = WAVES * WAVE_BYTES + ROWS_DEPTH * X_STAGE;
 };
 
 // The main loop of one wavefront.  XW = how many of the pair's X_OPS token loads this wavefront issues, so that the
 // number of its loads per pair, 2 + XW, is a constant the s_waitcnt immediates can be built from.
-template <int NF, int XW>
+template <int NF, int WAVES, int XW>
 __device__ __forceinline__ void rows_main_loop(const uint8_t* const (&a_src)[2], const uint8_t* const (&m_src)[2],
                                                const uint8_t* const (&b_src)[NF][2], int wave, uint8_t* mine,
                                                uint8_t* xring, int pair0, int npairs, int l16, int lq,
                                                f32x4 (&acc)[NF]) {
-    using S = RowsLds<NF>;
+    using S = RowsLds<NF, WAVES>;
     constexpr int L = 2 + XW;                                 // loads per pair (the metadata loads come on top, every 8th pair)
     const int sw = (l16 >> 1) & 7;
     // pair q of this slice (late ones clamped to the last, so that every call issues its L loads) into stage q % DEPTH
@@ -391,7 +391,7 @@ __device__ __forceinline__ void rows_main_loop(const uint8_t* const (&a_src)[2],
         uint8_t* xs = xring + (q % ROWS_DEPTH) * S::X_STAGE;
 #pragma unroll
         for (int x = 0; x < S::X_OPS; ++x)                    // load x = (step e, fragment j, half h), dealt in turn
-            if (x % ROWS_WAVES == wave) {
+            if (x % WAVES == wave) {
                 const int e = x / (2 * NF), j = (x / 2) % NF, h = x & 1;
                 dma16(b_src[j][h] + ((size_t)2 * p + e) * 128, xs + x * 1024);
             }
@@ -454,26 +454,26 @@ __device__ __forceinline__ void store_rows_gated(const f32x4 (&acc)[NF], int n, 
 // K % 1024 == 0.  blockIdx.x: block of 48 weight rows; blockIdx.y: slice of slice_pairs pairs of k-steps (a multiple of
 // 8).  partial == nullptr (one slice): C bf16[n][m]; else fp32 sums into partial[slice][n][m].  The adapter term is
 // added by slice 0.
-template <int NF, class... Gate>
-__global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t* __restrict__ B, int n,
+template <int NF, int WAVES, class... Gate>
+__global__ void __launch_bounds__(WAVES * 64) spmm_rows_kernel(const bf16_t* __restrict__ B, int n,
                                                                    const bf16_t* __restrict__ Av,
                                                                    const uint8_t* __restrict__ Am, int m, int K,
                                                                    const bf16_t* __restrict__ T,
                                                                    const bf16_t* __restrict__ R, int K2,
                                                                    bf16_t* __restrict__ C, float* __restrict__ partial,
                                                                    int slice_pairs, Gate... gate) {
-    using S = RowsLds<NF>;
+    using S = RowsLds<NF, WAVES>;
     constexpr bool GATED = sizeof...(Gate) > 0;
     extern __shared__ __align__(16) uint8_t smem[];
     const int t = threadIdx.x, lane = t & 63;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int l16 = lane & 15, lq = lane >> 4;
-    const int m0 = blockIdx.x * ROWS_BM, mw = m0 + 16 * wave;   // the workgroup's and the wavefront's first row
+    const int m0 = blockIdx.x * S::BM, mw = m0 + 16 * wave;   // the workgroup's and the wavefront's first row
     const int kpairs = K / 128;
     const int pair0 = blockIdx.y * slice_pairs;
     const int npairs = kpairs - pair0 < slice_pairs ? kpairs - pair0 : slice_pairs;   // > 0 by the launch's grid
     uint8_t* const mine = smem + wave * S::WAVE_BYTES;
-    uint8_t* const xring = smem + ROWS_WAVES * S::WAVE_BYTES;
+    uint8_t* const xring = smem + WAVES * S::WAVE_BYTES;
 
     // loader lanes: 8 lanes per row, the 16-byte pieces of a line rotated by (row / 2) % 8; rows and tokens past
     // the end are read from the last one and never stored
@@ -499,11 +499,16 @@ __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t
     f32x4 acc[NF];
 #pragma unroll
     for (int j = 0; j < NF; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    // the token loads of a pair go to the wavefronts in turn: wavefront w issues those with x % 3 == w
-    constexpr int XW0 = (S::X_OPS + 2) / 3, XW1 = (S::X_OPS + 1) / 3, XW2 = S::X_OPS / 3;
-    if (wave == 0) rows_main_loop<NF, XW0>(a_src, m_src, b_src, 0, mine, xring, pair0, npairs, l16, lq, acc);
-    else if (wave == 1) rows_main_loop<NF, XW1>(a_src, m_src, b_src, 1, mine, xring, pair0, npairs, l16, lq, acc);
-    else rows_main_loop<NF, XW2>(a_src, m_src, b_src, 2, mine, xring, pair0, npairs, l16, lq, acc);
+    // the token loads of a pair go to the wavefronts in turn: wavefront w issues those with x % WAVES == w
+    if constexpr (S::X_OPS % WAVES == 0) {
+        rows_main_loop<NF, WAVES, S::X_OPS / WAVES>(a_src, m_src, b_src, wave, mine, xring, pair0, npairs, l16, lq, acc);
+    } else {
+        static_assert(WAVES == 3, "each wavefront its own number of loads");
+        constexpr int XW0 = (S::X_OPS + 2) / 3, XW1 = (S::X_OPS + 1) / 3, XW2 = S::X_OPS / 3;
+        if (wave == 0) rows_main_loop<NF, WAVES, XW0>(a_src, m_src, b_src, 0, mine, xring, pair0, npairs, l16, lq, acc);
+        else if (wave == 1) rows_main_loop<NF, WAVES, XW1>(a_src, m_src, b_src, 1, mine, xring, pair0, npairs, l16, lq, acc);
+        else rows_main_loop<NF, WAVES, XW2>(a_src, m_src, b_src, 2, mine, xring, pair0, npairs, l16, lq, acc);
+    }
     __syncthreads();                                          // the rings are free
 
     // Adapter term T R on dense MFMA, as in the kernel above: chunks of 128 of the rank, T and the workgroup's
@@ -511,19 +516,19 @@ __global__ void __launch_bounds__(ROWS_WAVES * 64) spmm_rows_kernel(const bf16_t
     // owns the fragments of its 16 rows and adds them to its accumulators.
     if (K2 > 0 && blockIdx.y == 0) {
         constexpr int TP = 128 * 2 + 16, RP = 160;            // bytes per staged row of T and of R's tile
-        constexpr int SEG = ROWS_BM / 8;                      // 16-byte segments per row of R's tile
+        constexpr int SEG = S::BM / 8;                        // 16-byte segments per row of R's tile
         static_assert(16 * NF * TP + 128 * RP <= S::TOTAL, "adapter operands fit in the rings");
         uint8_t* const t_lds = smem;                          // [16 NF tokens][TP]
         uint8_t* const r_lds = smem + 16 * NF * TP;           // [128 k][RP]
         for (int kc = 0; kc < K2; kc += 128) {
             const int kn = K2 - kc < 128 ? K2 - kc : 128;     // a multiple of 32
-            for (int idx = t; idx < 16 * NF * 16; idx += ROWS_WAVES * 64) {
+            for (int idx = t; idx < 16 * NF * 16; idx += WAVES * 64) {
                 int tok = idx >> 4, pc = idx & 15;
                 u32x4 v = {0u, 0u, 0u, 0u};
                 if (tok < n && pc * 8 < kn) v = *(const u32x4*)(T + (size_t)tok * K2 + kc + pc * 8);
                 *(u32x4*)(t_lds + tok * TP + pc * 16) = v;
             }
-            for (int idx = t; idx < 128 * SEG; idx += ROWS_WAVES * 64) {
+            for (int idx = t; idx < 128 * SEG; idx += WAVES * 64) {
                 int k = idx / SEG, sg = idx % SEG;
                 u32x4 v = {0u, 0u, 0u, 0u};
                 if (k < kn && m0 + 8 * sg < m) v = *(const u32x4*)(R + (size_t)(kc + k) * m + stream_row(m0 + 8 * sg, gate...));
@@ -797,16 +802,16 @@ size_t spmm_rows_partial_bytes(int64_t n, int64_t m, int64_t K) {
     return slices > 1 ? (size_t)slices * (size_t)n * (size_t)m * 4 : 0;
 }
 
-template <int NF, class... Gate>
+template <int NF, int WAVES, class... Gate>
 static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
                               const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
                               hipStream_t s, const Gate&... gate) {
-    using S = RowsLds<NF>;
+    using S = RowsLds<NF, WAVES>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
-    hipError_t e = allow_dynamic_lds<spmm_rows_kernel<NF, Gate...>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<spmm_rows_kernel<NF, WAVES, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
     const int64_t chunks = K / 1024, per = (chunks + slices - 1) / slices;
-    spmm_rows_kernel<NF, Gate...><<<dim3((unsigned)((m + ROWS_BM - 1) / ROWS_BM), (unsigned)slices), dim3(ROWS_WAVES * 64), S::TOTAL, s>>>(
+    spmm_rows_kernel<NF, WAVES, Gate...><<<dim3((unsigned)((m + S::BM - 1) / S::BM), (unsigned)slices), dim3(WAVES * 64), S::TOTAL, s>>>(
         B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, slices > 1 ? partial : nullptr, (int)(per * 8), gate...);
     if ((e = hipGetLastError()) != hipSuccess || slices == 1) return e;
     if constexpr (sizeof...(Gate) > 0) return launch_gated_sum(partial, slices, n, m, C, gate..., s);
@@ -815,13 +820,33 @@ static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, cons
     return hipGetLastError();
 }
 
+// Gated layers on the row-split kernel take four wavefronts, 64 rows a workgroup, where that saves a thin last round: three workgroups are
+// resident either way.  A workgroup pulls 12.5 bytes per ns, or its share of 4.9 TB/s with many beside it, 5.3 in whole rounds.  us, 48 / 64 rows:
+// one token, 49152 x 9216 110.8 / 95.1, 40960 x 5120 57.5 / 52.4, 16 tokens, 27296 x 5120 41.3 / 37.8; but 36864 x 9216 73.5 / 80.9, 24576 x 9216
+// 54.0 / 56.4, 55296 x 10240 130 / 134.
+bool gated_rows_of_64(int64_t n, int64_t m, int64_t K, int slices) {
+    if (n > 16 || slices != 1) return false;
+    auto us = [&](int64_t rows) {
+        constexpr int64_t AT_ONCE = 3 * RESIDENT;
+        const double kb = 1.125e-3 * (double)rows * (double)K;
+        const int64_t blocks = (m + rows - 1) / rows, rest = blocks % AT_ONCE;
+        const double share = rest ? 4.9e3 / (double)rest : 1.0;
+        return (double)(blocks / AT_ONCE) * kb * AT_ONCE / 5.3e3 + (rest ? kb / (share < 12.5 ? share : 12.5) : 0.0);
+    };
+    return us(64) < 0.97 * us(48);
+}
+
 template <class... Gate>
 static hipError_t launch_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t m, int64_t K,
                                 const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
                                 const StreamXl& xl, hipStream_t s, const Gate&... gate) {
     if (slices > 0)
-        return n <= 16 ? launch_rows<1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...)
-                       : launch_rows<2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
+    {
+        if constexpr (sizeof...(Gate) > 0)
+            if (gated_rows_of_64(n, m, K, slices)) return launch_rows<1, 4>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
+        return n <= 16 ? launch_rows<1, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...)
+                       : launch_rows<2, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
+    }
     const int rows = spmm_stream_rows(n, m, K);
     if (n <= 16) {
         if (rows == 32) return launch_stream_lds<2, 8, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);

@@ -21,6 +21,12 @@ def test_regimes():
     assert (p["product"], p["rows"], p["tokens"]) == (TILE, 256, 256)
 
 
+def test_workgroups_of_64_rows_where_they_save_a_thin_round():
+    for d_ff, d_in, rows in ((24576, 9216, 64), (20480, 5120, 64), (18432, 9216, 48), (12288, 9216, 48), (27648, 10240, 48)):
+        assert plan(1, d_ff, d_in)["rows"] == rows, (d_ff, d_in)
+    assert plan(1, 2048, 16384) == {"product": ROW_SPLIT, "rows": 48, "tokens": 16, "slabs": 8, "xl": 0}
+
+
 def test_no_tile_of_192_rows():
     """A wavefront's rows of a gated tile are whole blocks of 32 elements."""
     for b in (40, 100, 300, 777, 1000, 2048, 5000):
@@ -67,7 +73,7 @@ def test_the_gpu_tests_reach_every_form():
             assert any((SMALL_BATCH, rows, 32, False, xl, tail) in found for tail in (0, 1)), (rows, xl)
     for tokens in (16, 32):
         assert (ROW_SPLIT, 48, tokens, True, 0, 0) in found
-    assert (ROW_SPLIT, 48, 16, False, 0, 0) in found
+    assert (ROW_SPLIT, 48, 16, False, 0, 0) in found and (ROW_SPLIT, 64, 16, False, 0, 0) in found
     for rows, tokens in ((128, 64), (128, 128), (256, 64), (256, 128)):
         for tail in (0, 1):
             assert (SLABS, rows, tokens, True, 0, tail) in found, (rows, tokens, tail)

@@ -702,7 +702,7 @@ def slope_gated_fwd(X: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, act
     """H = act(g) u, [g | u] = X (W^R)^T [+ (X L) R]: (H bf16[b, d_ff], GU bf16[b, 2 d_ff], codes e4m3[b, 2 d_ff], scale
     u8[b, 2, (d_ff + 31) // 32]); of what the backward pass wants, what was not asked for is None.  vals, meta: packed W^R of 2 d_ff
     rows, the gate's first; L bf16[d_in, r], R bf16[r, 2 d_ff].  out: the same four, to write into.
-    workspace: "auto" (allocated here when the call wants one), None (no adapter then, and nothing is split) or a uint8 device tensor of
+    workspace: "auto" (allocated here when the call wants one), None (no adapter then, nothing is split or padded) or a uint8 device tensor of
     slope_workspace_bytes(SLOPE_CALL_GATED_FWD, b, d_in, d_ff, r) bytes."""
     b, d_in, rows, r = _fwd_args(X, vals, meta, L, R, None)
     d_ff = rows // 2
@@ -810,8 +810,8 @@ def slope_spmm_fwd_q8_plan(b: int, d_in: int, d_out: int, with_workspace: bool =
 
 
 def slope_gated_fwd_plan(b: int, d_in: int, d_ff: int, r: int = 0, kept: bool = False, with_workspace: bool = True):
-    """Kernels slope_gated_fwd would launch for a shape (host only): dict of the five plan fields."""
+    """Kernels slope_gated_fwd would launch for a shape (host only): dict of the six plan fields."""
     import numpy as np
-    plan = np.zeros(5, dtype=np.int32)
+    plan = np.zeros(6, dtype=np.int32)
     _check("slope_gated_fwd_plan", lib().slope_gated_fwd_plan(b, d_in, d_ff, r, int(kept), int(with_workspace), plan.ctypes.data))
-    return dict(zip(["product", "rows", "tokens", "slabs", "xl"], (int(v) for v in plan)))
+    return dict(zip(["product", "rows", "tokens", "slabs", "xl", "padded"], (int(v) for v in plan)))

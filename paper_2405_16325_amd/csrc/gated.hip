@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;      // (of a workgroup, in pieces: one to two per thread)
 // STREAM: a call that moves more than the last-level cache holds, of which the next one would find nothing there
 template <bool STREAM, class T>
 __device__ __forceinline__ T load(const void* p) { return STREAM ? __builtin_nontemporal_load((const T*)p) : *(const T*)p; }
@@ -135,7 +135,46 @@ inline bool streams(int64_t bytes) { return bytes > (int64_t)LAST_LEVEL_CACHE_BY
 // with two (2048 x 6912 from codes 29.0 / 30.6; 16384 x 24576 694 / 711).
 constexpr int64_t PAIRS_FROM = (int64_t)1 << 18;
 
+// Rows of P = Kp / 8 pieces of eight of the contraction: first the tokens' (16 bytes each), then the packed weight's (8 bytes, and a byte of
+// metadata).  Past K: zeros, under metadata that names positions 0 and 1, a legal pair.
+struct PadJob {
+    const bf16_t *x, *vals;
+    const uint8_t* meta;
+    bf16_t *xp, *vp;
+    uint8_t* mp;
+    int64_t n, rows;
+    int K, Kp;
+};
+__global__ void __launch_bounds__(THREADS) pad_kernel(PadJob j) {
+    const uint32_t P = (uint32_t)j.Kp / 8, have = (uint32_t)j.K / 8;
+    const int64_t first = flat_block() * THREADS, row0 = first / P;
+    const Piece p = piece_after(row0, (uint32_t)(first - row0 * P), threadIdx.x, P);
+    const bool in = (uint32_t)p.c < have;
+    if (p.row < j.n) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (in) v = *(const u32x4*)(j.x + (size_t)p.row * j.K + p.c * 8);
+        *(u32x4*)(j.xp + (size_t)p.row * j.Kp + p.c * 8) = v;
+        return;
+    }
+    const int64_t row = p.row - j.n;
+    if (row >= j.rows) return;
+    u32x2 v = {0u, 0u};
+    uint8_t byte = 0x44;
+    if (in) {
+        v = *(const u32x2*)((const uint8_t*)j.vals + (size_t)row * j.K + p.c * 8);
+        byte = j.meta[(size_t)row * have + p.c];
+    }
+    *(u32x2*)((uint8_t*)j.vp + (size_t)row * j.Kp + p.c * 8) = v;
+    j.mp[(size_t)row * P + p.c] = byte;
+}
+
 }  // namespace
+
+hipError_t launch_pad_operands(const bf16_t* x, int64_t n, const bf16_t* vals, const uint8_t* meta, int64_t rows, int64_t K, int64_t Kp,
+                               bf16_t* xp, bf16_t* vp, uint8_t* mp, hipStream_t s) {
+    pad_kernel<<<grid_for((n + rows) * (Kp / 8), 1), dim3(THREADS), 0, s>>>({x, vals, meta, xp, vp, mp, n, rows, (int)K, (int)Kp});
+    return hipGetLastError();
+}
 
 // (callers have checked that the pieces' launches fit.  16384 x 24576, non-temporal accesses or not: 694 / 698 us from codes, 805 / 844 from bf16)
 hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q, const uint8_t* bytes, int64_t n, int64_t d_ff, int act,

@@ -645,18 +645,30 @@ static bool bad_act(int act) { return act != SLOPE_ACT_SILU && act != SLOPE_ACT_
 // rows of d elements in 8-bit blocks: launches of a workgroup per 256 pieces of eight
 static bool bad_blocks(int64_t rows, int64_t d) { return bad_extent(rows, 1) || bad_extent(d, 8) || !grid_fits(rows * ((d + 31) / 32 * 4) / 256 + 1); }
 
-// Bytes of the call's scratch, and its split over d_in: [ adapter | slabs ], or [ adapter | slices ] for a few tokens of which nothing is
-// kept.  The split does not depend on the adapter, whose T = X L has its launches before the product.
-static size_t gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, SpmmSplit& split) {
+// The call's scratch, in bytes: [ adapter | padded copies of X, values, metadata | slabs, or slices for a few tokens of which nothing is
+// kept ], and its split over the contraction.  The split does not depend on the adapter, whose T = X L has its launches before the product.
+struct GatedPlan {
+    SpmmSplit split;
+    int64_t padded, K;                                        // columns of the copies (0: none); the contraction's
+    size_t x_at, vals_at, meta_at, sums_at, total;
+};
+static GatedPlan gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
+    GatedPlan p;
     const int64_t m = gated_rows(d_ff);
-    split = spmm_split(b, m, d_in, 0, spmm_slab_room(b, m, d_in), true);
-    return adapter_workspace_bytes(b, d_in, 2 * d_ff, r) + round256(spmm_split_bytes(split, b, m)) + round256(spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+    p.padded = gated_padded(b, d_ff, d_in);
+    p.K = p.padded ? p.padded : d_in;
+    p.split = spmm_split(b, m, p.K, 0, spmm_slab_room(b, m, p.K), true);
+    p.x_at = adapter_workspace_bytes(b, d_in, 2 * d_ff, r);
+    p.vals_at = p.x_at + (p.padded ? round256((size_t)b * p.K * 2) : 0);
+    p.meta_at = p.vals_at + (p.padded ? round256((size_t)2 * d_ff * p.K) : 0);
+    p.sums_at = p.meta_at + (p.padded ? round256((size_t)2 * d_ff * (p.K / 8)) : 0);
+    p.total = p.sums_at + round256(spmm_split_bytes(p.split, b, m)) + round256(spmm_rows_partial_bytes(b, 2 * d_ff, p.K));
+    return p;
 }
 
 size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
     if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
-    SpmmSplit split;
-    return gated_plan(b, d_in, d_ff, r, split);
+    return gated_plan(b, d_in, d_ff, r).total;
 }
 
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
@@ -672,16 +684,19 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     const bool adapter = r > 0 && L_or_null && R_or_null;
     if (!adapter) r = 0;
     if (adapter && !workspace_or_null) return SLOPE_ERR_NULL;
-    SpmmSplit split = {0, 0, 0};
-    if (workspace_or_null && workspace_bytes < gated_plan(b, d_in, d_ff, r, split)) return SLOPE_ERR_WORKSPACE;
+    GatedPlan plan = {};
+    if (workspace_or_null) {
+        plan = gated_plan(b, d_in, d_ff, r);
+        if (workspace_bytes < plan.total) return SLOPE_ERR_WORKSPACE;
+    }
     hipStream_t s = (hipStream_t)stream;
     const bf16_t *x = (const bf16_t*)X, *wv = (const bf16_t*)Wr_vals, *l = adapter ? (const bf16_t*)L_or_null : nullptr;
     const bf16_t* const R = adapter ? (const bf16_t*)R_or_null : nullptr;
-    const uint8_t* const wm = (const uint8_t*)Wr_meta;
+    const uint8_t* wm = (const uint8_t*)Wr_meta;
     uint8_t* const ws = (uint8_t*)workspace_or_null;
     const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null};
     const bool few = spmm_stream_fits(b, d_in) && !gate.gu && !gate.q;
-    float* const after = (float*)(ws + adapter_workspace_bytes(b, d_in, 2 * d_ff, r));
+    float* const after = (float*)(ws + plan.sums_at);
     float* const slices = few && ws && spmm_rows_partial_bytes(b, 2 * d_ff, d_in) ? after : nullptr;
     bf16_t* T = adapter ? (bf16_t*)ws : nullptr;
     if (few && adapter && gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices != nullptr))
@@ -692,7 +707,17 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
         if (e != hipSuccess) return finish(e);
     }
     if (few) return finish(launch_gated_stream(x, b, wv, wm, d_in, T, nullptr, R, r, (bf16_t*)H, slices, gate, s));
-    if (split.slabs) return finish(launch_gated_slabs(x, b, wv, wm, d_in, T, R, r, split, (bf16_t*)H, after, gate, s));
+    if (plan.padded) {
+        bf16_t *xp = (bf16_t*)(ws + plan.x_at), *vp = (bf16_t*)(ws + plan.vals_at);
+        uint8_t* const mp = ws + plan.meta_at;
+        const hipError_t e = launch_pad_operands(x, b, wv, wm, 2 * d_ff, d_in, plan.padded, xp, vp, mp, s);
+        if (e != hipSuccess) return finish(e);
+        x = xp;
+        wv = vp;
+        wm = mp;
+        d_in = plan.padded;
+    }
+    if (plan.split.slabs) return finish(launch_gated_slabs(x, b, wv, wm, d_in, T, R, r, plan.split, (bf16_t*)H, after, gate, s));
     return finish(launch_gated(x, b, wv, wm, d_in, T, R, r, (bf16_t*)H, gate, s));
 }
 
@@ -700,7 +725,7 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
     if (!plan) return SLOPE_ERR_NULL;
     if (bad_layer(b, 2 * d_ff, d_in) || bad_gated(b, d_ff) || r < 0) return SLOPE_ERR_SHAPE;
     if (r > 0 && bad_rank(r)) return SLOPE_ERR_UNSUPPORTED;
-    for (int i = 0; i < 5; ++i) plan[i] = 0;
+    for (int i = 0; i < 6; ++i) plan[i] = 0;
     plan[3] = 1;
     if (spmm_stream_fits(b, d_in) && !kept) {
         const int slices = spmm_rows_slices(b, 2 * d_ff, d_in, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
@@ -712,7 +737,12 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
         return SLOPE_OK;
     }
     SpmmSplit split = {0, 0, 0};
-    if (with_workspace) gated_plan(b, d_in, d_ff, r, split);
+    if (with_workspace) {
+        const GatedPlan p = gated_plan(b, d_in, d_ff, r);
+        split = p.split;
+        plan[5] = (int32_t)p.padded;
+        d_in = p.K;
+    }
     const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in, true);
     int bm, bn;
     spmm_tile_choice(b - rest, m, d_in, r > 0, bm, bn, true);

@@ -1826,6 +1826,21 @@ static hipError_t launch_gated_tiles(const bf16_t* B, int64_t n, const bf16_t* A
     return launch_generic_as<4, 1>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
 }
 
+// Columns of padded copies that a gated call makes of its operands, 0: none.  The tile kernels want whole k-steps; other contractions are the
+// general kernel's, which takes (us) about 3 + 0.0072 K a round of its 64 x 64 tiles, and 3 + 0.0215 K, more than a round in proportion, on 128 x 128;
+// copies take 3 us and their bytes at 4 TB/s.  us, general kernel / tiles on whole k-steps, without the copies: 1000 tokens, 2000 x 1000 18.0 /
+// 7.9, 2048, 4112 x 2056 85.7 / 38.7, 1000, 1040 x 2200 32.9 / 12.1; 300, 2000 x 1000 9.5 / 7.3, which stays.
+int64_t gated_padded(int64_t n, int64_t d_ff, int64_t K) {
+    if (K % 64 == 0 || K < 128 || n <= STREAM_MAX_TOKENS || n > ((int64_t)1 << 20)) return 0;
+    const int64_t m = gated_rows(d_ff), Kp = (K + 63) / 64 * 64;
+    const double tiles = (double)(((m + 127) / 128) * ((n + 127) / 128)) / (1.2 * RESIDENT);
+    const double general = spmm_generic_edge(n, m) == 64 ? (double)((tiles_of_64(n, m) + RESIDENT - 1) / RESIDENT) * (3.0 + 0.0072 * (double)K)
+                                                         : (3.0 + 0.0215 * (double)K) * (tiles > 1.0 ? tiles : 1.0);
+    int bm, bn;
+    const double padded = best_tile_us(n, m, Kp, bm, bn, true) + 3.0 + 2.0 * (double)Kp * (2.0 * (double)n + 1.125 * (double)m) / 4e6;
+    return padded < 0.85 * general ? Kp : 0;                  // (for a launch more, 3 us of the host's)
+}
+
 // h, and what is kept, of sums P[slabs][n][m] of the two projections, an element's m / 2 apart, added in slab order.  Four elements per lane,
 // eight lanes per block of 32.
 __global__ void __launch_bounds__(256) gated_sum_kernel(const float* __restrict__ P, int slabs, int n, int m, bf16_t* __restrict__ H, GateOut gate) {

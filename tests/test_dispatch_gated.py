@@ -16,7 +16,9 @@ def test_regimes():
     assert plan(1, 24576, 9216)["product"] == ROW_SPLIT
     assert plan(1, 24576, 9216, kept=True)["product"] == TILE                # the small-batch kernels keep nothing
     assert plan(128, 200, 4096)["product"] == SLABS and plan(128, 200, 4096, with_workspace=False)["product"] == TILE
-    assert plan(1000, 1000, 1000) == {"product": GENERAL, "rows": 64, "tokens": 64, "slabs": 1, "xl": 0}
+    assert plan(300, 1000, 1000) == {"product": GENERAL, "rows": 64, "tokens": 64, "slabs": 1, "xl": 0, "padded": 0}
+    p = plan(1000, 1000, 1000)
+    assert (p["product"], p["padded"]) == (TILE, 1024) and plan(1000, 1000, 1000, with_workspace=False)["product"] == GENERAL
     p = plan(16384, 24576, 9216)
     assert (p["product"], p["rows"], p["tokens"]) == (TILE, 256, 256)
 
@@ -24,7 +26,7 @@ def test_regimes():
 def test_workgroups_of_64_rows_where_they_save_a_thin_round():
     for d_ff, d_in, rows in ((24576, 9216, 64), (20480, 5120, 64), (18432, 9216, 48), (12288, 9216, 48), (27648, 10240, 48)):
         assert plan(1, d_ff, d_in)["rows"] == rows, (d_ff, d_in)
-    assert plan(1, 2048, 16384) == {"product": ROW_SPLIT, "rows": 48, "tokens": 16, "slabs": 8, "xl": 0}
+    assert plan(1, 2048, 16384) == {"product": ROW_SPLIT, "rows": 48, "tokens": 16, "slabs": 8, "xl": 0, "padded": 0}
 
 
 def test_no_tile_of_192_rows():
@@ -56,7 +58,8 @@ def forms():
                     continue
                 p = plan(b, f, i, r, kept=kept, with_workspace=ws)
                 whole = 256 if p["rows"] == 256 and p["tokens"] != 64 else 128
-                tail = i % whole != 0 if p["product"] != GENERAL else (i % 64 != 0) + (i % 128 != 0)
+                k = p["padded"] or i
+                tail = k % whole != 0 if p["product"] != GENERAL else (i % 64 != 0) + (i % 128 != 0)
                 split = p["slabs"] > 1 and p["product"] in (SLABS, ROW_SPLIT)
                 found.add((p["product"], p["rows"], p["tokens"], split, p["xl"], int(tail)))
     return found
@@ -85,6 +88,16 @@ def test_the_gpu_tests_reach_every_form():
         for tail in tails:
             assert (GENERAL, edge, edge, False, 0, tail) in found, (edge, tail)
     assert {(REST, 128, 128, False, 0, t) for t in (0,)} <= found and any(f[0] == REST and f[1] == 256 for f in found)
+
+
+def test_the_gpu_tests_reach_padded_copies():
+    found = set()
+    for b, f, i, r in [(b, f, i, r) for b, f, i in SHAPES for r in (0, 32, 160)] + LARGE:
+        p = plan(b, f, i, r)
+        if p["padded"]:
+            assert p["padded"] % 64 == 0 and 0 < p["padded"] - i < 64
+            found.add((p["product"], r > 0))
+    assert {(TILE, False), (TILE, True), (SLABS, False), (SLABS, True)} <= found
 
 
 def test_tiles_left_over_after_whole_rounds():

@@ -153,7 +153,7 @@ SHAPES = [(1, 8, 8), (1, 256, 128), (1, 64, 1024), (2, 1000, 768), (7, 40, 264),
 # tile and every split, an odd k-step at the end of each, tokens and tiles that are left over (test_dispatch_gated.py)
 LARGE = [(1, 8, 192, 0), (1, 8, 192, 32), (1, 3912, 192, 32), (1, 6872, 128, 32), (1, 7104, 704, 32), (1, 6656, 320, 0), (17, 8, 128, 32), (19, 8, 192, 32),
          (1, 4056, 128, 0), (1, 4128, 192, 0), (1, 6848, 128, 0), (5, 6656, 320, 32), (17, 4304, 128, 0), (20, 5120, 192, 32), (1, 12288, 1024, 0),
-         (3, 2056, 17408, 0), (2, 24576, 1024, 0), (13, 20488, 1024, 32), (16, 2048, 16384, 64), (20, 2048, 16384, 0), (31, 4104, 16384, 32), (9, 12296, 2048, 96),
+         (3, 2056, 17408, 0), (2, 24576, 1024, 0), (13, 20488, 1024, 32), (300, 2056, 2056, 0), (1000, 520, 2200, 32), (2048, 264, 520, 0), (200, 8, 4104, 0), (400, 520, 8200, 32), (1999, 1000, 1096, 64), (16, 2048, 16384, 64), (20, 2048, 16384, 0), (31, 4104, 16384, 32), (9, 12296, 2048, 96),
          (1, 4272, 128, 32), (17, 4544, 128, 32), (35, 8, 2816, 32), (40, 8, 2624, 0), (4344, 8, 6144, 0), (3546, 8, 8000, 32),
          (34, 4584, 7424, 0), (33, 4208, 7616, 32), (131, 2880, 5120, 32), (133, 2752, 4672, 0), (5526, 136, 128, 32), (145, 5480, 192, 0),
          (195, 5568, 128, 32), (198, 6248, 192, 0), (259, 5504, 256, 160), (258, 5576, 128, 0), (654, 5384, 256, 32), (522, 6592, 128, 0),

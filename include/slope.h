@@ -460,7 +460,8 @@ slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x
  *     GU_or_null  out bf16[b, 2 d_ff]
  *     GUq_or_null, GU_scale_or_null  out e4m3[b, 2 d_ff], u8[b, 2, (d_ff + 31) / 32]: slope_checkpoint_q8's form of [2 b, d_ff], a token's
  *                 gate and then its up projection; both or neither
- *   workspace_or_null  slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r) bytes (may be 0), 256-byte aligned; required with an adapter.
+ *   workspace_or_null  slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, kept) bytes (may be 0), 256-byte aligned; kept: 0 where only H is
+ *                 wanted, 8 or 16 (slope_workspace_bytes answers for these) where anything is kept.  Required with an adapter.
  *                 Lets the call split the contraction, and copy operands whose d_in is no multiple of 64 into padded ones where that pays
  *
  * slope_gated_bwd - its gradient from what was kept, element by element:
@@ -471,7 +472,7 @@ slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x
  *   may be dH
  */
 typedef enum { SLOPE_ACT_SILU = 0, SLOPE_ACT_GELU = 1, SLOPE_ACT_RELU = 2 } slope_activation;
-size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r);
+size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept);
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
                              const void* L_or_null, const void* R_or_null, int64_t r, void* H, void* GU_or_null, void* GUq_or_null,
                              void* GU_scale_or_null, void* workspace_or_null, size_t workspace_bytes, void* stream);
@@ -512,7 +513,8 @@ slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t
 slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int with_workspace, int32_t* plan);
 
 /*
- * slope_gated_fwd_plan - the same for slope_gated_fwd; kept: whether the call keeps GU or GUq.  plan: host int32[6]
+ * slope_gated_fwd_plan - the same for slope_gated_fwd; kept: 0, 16 where the call keeps GU, 8 where it
+ * keeps GUq.  plan: host int32[6]
  *   [0] product, [1], [2] rows of the weight, gate and up projection, and tokens per workgroup, [3] slabs, slices or the tokens of
  *       the small-batch kernel: as slope_spmm_fwd_plan
  *   [4] whether the small-batch kernel computes T = X L itself

@@ -78,7 +78,7 @@ SIGNATURES = {
     "slope_restore_q8": (_INT, [_P, _P, _I64, _I64, _P, _P]),
     "slope_wgrad_masked_q8_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
     "slope_wgrad_masked_q8": (_INT, [_P, _P, _P, _I64, _P, _I64, _I64, _P, _P, _SZ, _P]),
-    "slope_gated_fwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
+    "slope_gated_fwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _INT]),
     "slope_gated_fwd": (_INT, [_P, _I64, _P, _P, _I64, _I64, _INT, _P, _P, _I64, _P, _P, _P, _P, _P, _SZ, _P]),
     "slope_gated_bwd": (_INT, [_P, _P, _P, _P, _I64, _I64, _INT, _P, _P, _P]),
     "slope_ceiling_min_bytes": (_SZ, []),
@@ -720,7 +720,7 @@ def slope_gated_fwd(X: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, act
             if t is not None:
                 _want(t, dtype, shape, what)
     if workspace is not None:
-        need = int(lib().slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r))
+        need = int(lib().slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, 0 if GU is None and Q is None else 8))
         workspace = _scratch(None if isinstance(workspace, str) else workspace, need, X.device, "workspace") if need else None
     _check("slope_gated_fwd", lib().slope_gated_fwd(_ptr(X), b, _ptr(vals), _ptr(meta), d_ff, d_in, act, _ptr(L), _ptr(R), r, _ptr(H),
                                                     _ptr(GU), _ptr(Q), _ptr(scale), _ptr(workspace),
@@ -809,9 +809,9 @@ def slope_spmm_fwd_q8_plan(b: int, d_in: int, d_out: int, with_workspace: bool =
     return dict(zip(["product", "rows", "tokens", "slabs", "rows0", "padded", "groups"], (int(v) for v in plan)))
 
 
-def slope_gated_fwd_plan(b: int, d_in: int, d_ff: int, r: int = 0, kept: bool = False, with_workspace: bool = True):
-    """Kernels slope_gated_fwd would launch for a shape (host only): dict of the six plan fields."""
+def slope_gated_fwd_plan(b: int, d_in: int, d_ff: int, r: int = 0, kept: int = 0, with_workspace: bool = True):
+    """Kernels slope_gated_fwd would launch for a shape (host only): dict of the six plan fields.  kept: 0, 16 (GU) or 8 (codes)."""
     import numpy as np
     plan = np.zeros(6, dtype=np.int32)
-    _check("slope_gated_fwd_plan", lib().slope_gated_fwd_plan(b, d_in, d_ff, r, int(kept), int(with_workspace), plan.ctypes.data))
+    _check("slope_gated_fwd_plan", lib().slope_gated_fwd_plan(b, d_in, d_ff, r, kept, int(with_workspace), plan.ctypes.data))
     return dict(zip(["product", "rows", "tokens", "slabs", "xl", "padded"], (int(v) for v in plan)))

@@ -35,9 +35,9 @@ hipError_t launch_spmm(const bf16_t* B, int64_t n, const bf16_t* A_vals, const u
                        int64_t K, const bf16_t* B2, const bf16_t* A2, int64_t K2, bf16_t* C, hipStream_t s);
 // the choices behind it (pure functions of the shape): tile of the tile kernels (0 x 0 = the generic kernel),
 // weight rows per workgroup of the small-batch kernel, chunks of 64 rows of L per slab that the scratch of X L is sized by
-void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn, bool gated = false);
+void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn, bool blocks = false);
 int spmm_generic_edge(int64_t n, int64_t m);                 // edge of the generic kernel's tile
-int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K, bool gated = false);   // the last tokens, which the small-batch kernel takes (adapters: K2 <= 0)
+int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K);   // the last tokens, which the small-batch kernel takes (adapters: K2 <= 0)
 int spmm_stream_rows(int64_t n, int64_t m, int64_t K);
 int xl_subs(int64_t n, int64_t d_in, int64_t r);
 // T = X L for few tokens (n <= XL_SMALL_MAX_TOKENS, d_in % 64 == 0) from L as stored, split over d_in: `slabs` slabs of
@@ -67,7 +67,7 @@ struct SpmmSplit { int bm, bn, slabs; };
 inline size_t spmm_split_bytes(const SpmmSplit& split, int64_t n, int64_t m) { return (size_t)split.slabs * (size_t)n * (size_t)m * 4; }
 struct SlabRoom { int slabs; bool optional, long_weight; };
 SlabRoom spmm_slab_room(int64_t n, int64_t m, int64_t K);
-SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room, bool gated = false);
+SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room);
 bool slab_xl_split(int64_t n, int64_t m, int64_t K, int64_t r, const SpmmSplit& split, XlSplit& x);
 hipError_t launch_spmm_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t m,
                              int64_t K, const SlabAdapter& ad, const SpmmSplit& split, bf16_t* C, float* slabs, hipStream_t s);
@@ -173,7 +173,8 @@ hipError_t launch_gated_sum(const float* P, int slabs, int64_t n, int64_t m, bf1
 bool gated_rows_of_64(int64_t n, int64_t m, int64_t K, int slices);
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced);
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
-                               const bf16_t* R, int64_t r, bf16_t* H, float* partial_or_null, const GateOut& gate, hipStream_t s);
+                               const bf16_t* R, int64_t r, bf16_t* H, float* sums_or_null, const GateOut& gate, hipStream_t s);
+size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, bool keeps);
 hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
                         int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s);
 hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q, const uint8_t* bytes, int64_t n, int64_t d_ff, int act,

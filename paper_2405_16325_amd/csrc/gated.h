@@ -16,6 +16,8 @@ struct GateOut {
     int d_ff, act;
     bf16_t* gu;                                               // bf16[n][2 d_ff], or null
     uint8_t *q, *bytes;                                       // e4m3[2 n][d_ff] with a scale byte per 32 of a row, or null
+    float* sums;                                              // small-batch kernels: [n][2 d_ff] instead of h, or null
+    __host__ __device__ bool keeps() const { return gu || q; }
 };
 constexpr int GATE_GROUP = 16;
 inline int64_t gated_rows(int64_t d_ff) { return (d_ff + GATE_GROUP - 1) / GATE_GROUP * (2 * GATE_GROUP); }
@@ -161,7 +163,7 @@ __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int
 template <int MF, int NF, int BMT, int BNT, int THREADS>
 __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, int t0, int n, int l16, int lq, bf16_t* __restrict__ H,
                                             uint8_t* smem, int tile_f0, int tile_t0, const GateOut& gate) {
-    static_assert(MF % 4 == 0, "whole blocks of 32 elements in a wavefront's rows");
+    static_assert(MF % 2 == 0, "pairs of fragments");
     constexpr int HALF = BMT / 2;                             // elements of h in the tile
     const int tile_e0 = tile_f0 / 2, e0 = f0 / 2, d_ff = gate.d_ff;
     const int le = e0 - tile_e0 + lq * 4, lt = t0 - tile_t0 + l16;        // the lane's first element and token inside the tile
@@ -212,7 +214,7 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
             if (e < d_ff) *(u32x4*)(gate.gu + (size_t)tok * (2 * (size_t)d_ff) + half * d_ff + e) = v;
         });
     }
-    if (gate.q) {
+    if constexpr (MF % 4 == 0) if (gate.q) {                  // whole blocks in a wavefront's rows: no other tile is given codes to write
         const size_t blocks = ((size_t)d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
         __syncthreads();
 #pragma unroll

@@ -172,7 +172,7 @@ size_t slope_workspace_bytes(int call_id, int64_t b, int64_t d_in, int64_t d_out
         case SLOPE_CALL_WGRAD_ADAPTER: return slope_wgrad_adapter_workspace_bytes(b, d_in, d_out, r);
         case SLOPE_CALL_RMSNORM_BWD: return slope_rmsnorm_bwd_workspace_bytes(b, d_in);
         case SLOPE_CALL_SPMM_FWD_Q8: return slope_spmm_fwd_q8_workspace_bytes(b, d_in, d_out);
-        case SLOPE_CALL_GATED_FWD: return slope_gated_fwd_workspace_bytes(b, d_in, d_out, r);
+        case SLOPE_CALL_GATED_FWD: return slope_gated_fwd_workspace_bytes(b, d_in, d_out, r, 8);
         case SLOPE_CALL_WGRAD_MASKED_Q8: return slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out);
         default: return 0;      // prune_rows, double_prune, spmm_bwd_x, wgrad_masked need no scratch; unknown ids
     }
@@ -645,30 +645,30 @@ static bool bad_act(int act) { return act != SLOPE_ACT_SILU && act != SLOPE_ACT_
 // rows of d elements in 8-bit blocks: launches of a workgroup per 256 pieces of eight
 static bool bad_blocks(int64_t rows, int64_t d) { return bad_extent(rows, 1) || bad_extent(d, 8) || !grid_fits(rows * ((d + 31) / 32 * 4) / 256 + 1); }
 
-// The call's scratch, in bytes: [ adapter | padded copies of X, values, metadata | slabs, or slices for a few tokens of which nothing is
-// kept ], and its split over the contraction.  The split does not depend on the adapter, whose T = X L has its launches before the product.
+// The call's scratch, in bytes: [ adapter | padded copies of X, values, metadata | sums of slabs, or of the small-batch
+// kernels ], and its split over the contraction.  The split does not depend on the adapter, whose T = X L has its launches before the product.
 struct GatedPlan {
     SpmmSplit split;
     int64_t padded, K;                                        // columns of the copies (0: none); the contraction's
     size_t x_at, vals_at, meta_at, sums_at, total;
 };
-static GatedPlan gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
+static GatedPlan gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, bool keeps) {
     GatedPlan p;
     const int64_t m = gated_rows(d_ff);
     p.padded = gated_padded(b, d_ff, d_in);
     p.K = p.padded ? p.padded : d_in;
-    p.split = spmm_split(b, m, p.K, 0, spmm_slab_room(b, m, p.K), true);
+    p.split = spmm_split(b, m, p.K, 0, spmm_slab_room(b, m, p.K));
     p.x_at = adapter_workspace_bytes(b, d_in, 2 * d_ff, r);
     p.vals_at = p.x_at + (p.padded ? round256((size_t)b * p.K * 2) : 0);
     p.meta_at = p.vals_at + (p.padded ? round256((size_t)2 * d_ff * p.K) : 0);
     p.sums_at = p.meta_at + (p.padded ? round256((size_t)2 * d_ff * (p.K / 8)) : 0);
-    p.total = p.sums_at + round256(spmm_split_bytes(p.split, b, m)) + round256(spmm_rows_partial_bytes(b, 2 * d_ff, p.K));
+    p.total = p.sums_at + round256(spmm_split_bytes(p.split, b, m)) + round256(gated_stream_bytes(b, d_ff, p.K, keeps));
     return p;
 }
 
-size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r) {
+size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept) {
     if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
-    return gated_plan(b, d_in, d_ff, r).total;
+    return gated_plan(b, d_in, d_ff, r, kept != 0).total;
 }
 
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
@@ -686,7 +686,7 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     if (adapter && !workspace_or_null) return SLOPE_ERR_NULL;
     GatedPlan plan = {};
     if (workspace_or_null) {
-        plan = gated_plan(b, d_in, d_ff, r);
+        plan = gated_plan(b, d_in, d_ff, r, GU_or_null || GUq_or_null);
         if (workspace_bytes < plan.total) return SLOPE_ERR_WORKSPACE;
     }
     hipStream_t s = (hipStream_t)stream;
@@ -694,19 +694,19 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     const bf16_t* const R = adapter ? (const bf16_t*)R_or_null : nullptr;
     const uint8_t* wm = (const uint8_t*)Wr_meta;
     uint8_t* const ws = (uint8_t*)workspace_or_null;
-    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null};
-    const bool few = spmm_stream_fits(b, d_in) && !gate.gu && !gate.q;
-    float* const after = (float*)(ws + plan.sums_at);
-    float* const slices = few && ws && spmm_rows_partial_bytes(b, 2 * d_ff, d_in) ? after : nullptr;
+    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null, nullptr};
+    const bool few = spmm_stream_fits(b, d_in) && (ws || !gate.keeps());
+    // (none without a workspace, nor where the call needs no sums)
+    float* const after = plan.total > plan.sums_at ? (float*)(ws + plan.sums_at) : nullptr;
     bf16_t* T = adapter ? (bf16_t*)ws : nullptr;
-    if (few && adapter && gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices != nullptr))
-        return finish(launch_gated_stream(x, b, wv, wm, d_in, nullptr, l, R, r, (bf16_t*)H, nullptr, gate, s));
+    if (few && adapter && gated_stream_takes_l(b, 2 * d_ff, d_in, r, after != nullptr))
+        return finish(launch_gated_stream(x, b, wv, wm, d_in, nullptr, l, R, r, (bf16_t*)H, after, gate, s));
     if (adapter) {
         float* const sums = (float*)(ws + round256((size_t)b * r * 2) + round256((size_t)d_in * r * 2));
         const hipError_t e = token_factor(x, b, d_in, l, r, T, sums, s);
         if (e != hipSuccess) return finish(e);
     }
-    if (few) return finish(launch_gated_stream(x, b, wv, wm, d_in, T, nullptr, R, r, (bf16_t*)H, slices, gate, s));
+    if (few) return finish(launch_gated_stream(x, b, wv, wm, d_in, T, nullptr, R, r, (bf16_t*)H, after, gate, s));
     if (plan.padded) {
         bf16_t *xp = (bf16_t*)(ws + plan.x_at), *vp = (bf16_t*)(ws + plan.vals_at);
         uint8_t* const mp = ws + plan.meta_at;
@@ -725,27 +725,28 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
     if (!plan) return SLOPE_ERR_NULL;
     if (bad_layer(b, 2 * d_ff, d_in) || bad_gated(b, d_ff) || r < 0) return SLOPE_ERR_SHAPE;
     if (r > 0 && bad_rank(r)) return SLOPE_ERR_UNSUPPORTED;
+    if (kept != 0 && kept != 8 && kept != 16) return SLOPE_ERR_VALUE;
     for (int i = 0; i < 6; ++i) plan[i] = 0;
     plan[3] = 1;
-    if (spmm_stream_fits(b, d_in) && !kept) {
-        const int slices = spmm_rows_slices(b, 2 * d_ff, d_in, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+    if (spmm_stream_fits(b, d_in) && (with_workspace || !kept)) {
+        const int slices = spmm_rows_slices(b, 2 * d_ff, d_in, with_workspace != 0);
         plan[0] = slices > 0 ? 4 : 0;
         plan[1] = slices > 0 ? (gated_rows_of_64(b, 2 * d_ff, d_in, slices) ? 64 : 48) : spmm_stream_rows(b, 2 * d_ff, d_in);
         plan[2] = b <= 16 ? 16 : 32;
         if (slices > 0) plan[3] = slices;
-        plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, with_workspace && spmm_rows_partial_bytes(b, 2 * d_ff, d_in));
+        plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices > 1);
         return SLOPE_OK;
     }
     SpmmSplit split = {0, 0, 0};
     if (with_workspace) {
-        const GatedPlan p = gated_plan(b, d_in, d_ff, r);
+        const GatedPlan p = gated_plan(b, d_in, d_ff, r, kept != 0);
         split = p.split;
         plan[5] = (int32_t)p.padded;
         d_in = p.K;
     }
-    const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in, true);
+    const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in);
     int bm, bn;
-    spmm_tile_choice(b - rest, m, d_in, r > 0, bm, bn, true);
+    spmm_tile_choice(b - rest, m, d_in, r > 0, bm, bn, kept == 8);
     if (split.slabs) { plan[0] = 1; plan[1] = split.bm; plan[2] = split.bn; plan[3] = split.slabs; }
     else if (bm == 0) { plan[0] = 3; plan[1] = plan[2] = spmm_generic_edge(b - rest, m); }
     else { plan[0] = 2; plan[1] = bm; plan[2] = bn; }

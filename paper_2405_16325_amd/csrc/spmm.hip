@@ -1596,13 +1596,14 @@ static double launch_us(const TileCost& c, double ksteps, int slabs) {
     return us < c.stream ? c.stream : us;
 }
 
-// the tile of least time and that time; a gated product's tiles have whole blocks of 32 elements for each wavefront: no 192 rows
-static double best_tile_us(int64_t n, int64_t m, int64_t K, int& bm, int& bn, bool gated = false) {
+// the tile of least time and that time; blocks: of a gated product that writes 8-bit
+// codes, whose tiles have whole blocks of 32 elements for each wavefront, not 192 rows
+static double best_tile_us(int64_t n, int64_t m, int64_t K, int& bm, int& bn, bool blocks = false) {
     bm = bn = 64;
     const double ksteps = (double)K / 64.0;
     double least = one_round_of_64(n, m) ? launch_us(tile_cost(n, m, K, 64, 64), ksteps, 1) : 1e300;
     for (const SpmmTile& t : SPMM_TILES) {
-        if (gated && t.bm == 192) continue;
+        if (blocks && t.bm == 192) continue;
         const TileCost cost = tile_cost(n, m, K, t.bm, t.bn);
         double us = launch_us(cost, ksteps, 1);
         if (t.bm == 256 && t.bn == 256) {                     // whole rounds, and a round of 128 x 128 or 256 x 128 tiles with its launch
@@ -1657,12 +1658,12 @@ constexpr double SPLIT_MIN_US = 13.5;
 // 18 % at most.  us: 166 tokens, 1280 x 27008, rank 32 52 in 8 slabs of 128 x 64, X L 53 chunks; 34 in 9 of 192 x 64, 37 in the 11
 // that are taken; 264 tokens, 2048 x 14272, rank 64 53 in three of 128 x 64 and 38; 330 tokens, 3328 x 13568, rank 64 64 in three of
 // 256 x 128 and 49.)
-SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room, bool gated) {
+SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom& room) {
     SpmmSplit best = {0, 0, 0};
     if (room.slabs < 2) return best;
     const bool xl = r > 0 && n <= XL_SMALL_MAX_TOKENS;
     int bm, bn;
-    double least = best_tile_us(n, m, K, bm, bn, gated);
+    double least = best_tile_us(n, m, K, bm, bn);
     if (!xl && least < SPLIT_MIN_US) return best;
     // Whole products of 64 k-steps and more take an eighth longer than estimated beside split ones, on weights from HBM: over 44
     // shapes of 129 to 1024 tokens, k of 4096 to 10000, the form chosen takes 0.4 % longer than the best measured one in the
@@ -1700,7 +1701,7 @@ SpmmSplit spmm_split(int64_t n, int64_t m, int64_t K, int64_t r, const SlabRoom&
         return best;
     }
     consider({128, 64}, true);
-    if (!gated) consider({192, 64}, true);
+    consider({192, 64}, true);
     consider({128, 128}, true);
     if (n > 64 || K >= 7168) consider(tall, false);
     return best;
@@ -1745,10 +1746,10 @@ constexpr double FEWEST_BYTES = 2.5e6, FEWEST_BYTES_WITH_ADAPTER = 5e6;
 
 // Tile of the product for n tokens, m sparse rows, contraction K: bm = bn = 0 means the generic kernel, whose whole pairs of
 // k-steps on a round of 64 x 64 tiles count as a tile shape of their own.
-void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn, bool gated) {
+void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, int& bn, bool blocks) {
     bm = bn = 0;
     if (!tile_kernel_fits(K)) return;
-    best_tile_us(n, m, K, bm, bn, gated);
+    best_tile_us(n, m, K, bm, bn, blocks);
     if (bm != 64) return;
     // (whether a product is split is decided by the estimate as it stands; not up to 64 rows, where half of the taller tile is nothing)
     const double bytes = (double)K * (1.125 * (double)m + 2.0 * (double)n);
@@ -1759,15 +1760,15 @@ void spmm_tile_choice(int64_t n, int64_t m, int64_t K, bool adapter, int& bm, in
 // Tokens at the end of a batch that a pass of the small-batch kernel over the packed weight (5 TB/s, 6 us for its launch and
 // the drained chip before it) takes for less than the round of tiles that they begin (0: none): up to 32 beyond a multiple
 // of the tile kernels' 256 or 128 (777 tokens, 20480 x 5120: 139 us in two rounds of tiles, 80 + 25 for 768 and 9 tokens).
-int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K, bool gated) {
+int64_t spmm_rest_tokens(int64_t n, int64_t m, int64_t K) {
     if (n <= 128 || !tile_kernel_fits(K) || one_round_of_64(n, m)) return 0;
     int bm, bn;
-    double least = best_tile_us(n, m, K, bm, bn, gated);
+    double least = best_tile_us(n, m, K, bm, bn);
     int64_t best = 0;
     for (int64_t edge = 256; edge >= 128; edge /= 2) {
         const int64_t rest = n % edge;
         if (rest == 0 || rest > STREAM_MAX_TOKENS || rest == n) continue;
-        const double us = best_tile_us(n - rest, m, K, bm, bn, gated) + 1.125 * (double)m * (double)K / 5e6 + 6.0;
+        const double us = best_tile_us(n - rest, m, K, bm, bn) + 1.125 * (double)m * (double)K / 5e6 + 6.0;
         if (us < 0.95 * least) { least = us / 0.95; best = rest; }
     }
     return best;
@@ -1812,8 +1813,13 @@ static hipError_t launch_gated_tiles(const bf16_t* B, int64_t n, const bf16_t* A
                                      const bf16_t* R, int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
     const int64_t m = gated_rows(gate.d_ff);
     int bm, bn;
-    spmm_tile_choice(n, m, K, r != 0, bm, bn, true);
+    spmm_tile_choice(n, m, K, r != 0, bm, bn, gate.q != nullptr);
     switch (bm * 1000 + bn) {
+        case 192256: return launch_tile<192, 256>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 192192: return launch_tile<192, 192>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 192128: return launch_tile<192, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 192096: return launch_ring<192, 96>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
+        case 192064: return launch_ring<192, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
         case 256256: return launch_split(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, gate);
         case 256192: return launch_tile<256, 192>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
         case 256128: return launch_tile<256, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, H, s, WholeJob{}, gate);
@@ -1837,7 +1843,7 @@ int64_t gated_padded(int64_t n, int64_t d_ff, int64_t K) {
     const double general = spmm_generic_edge(n, m) == 64 ? (double)((tiles_of_64(n, m) + RESIDENT - 1) / RESIDENT) * (3.0 + 0.0072 * (double)K)
                                                          : (3.0 + 0.0215 * (double)K) * (tiles > 1.0 ? tiles : 1.0);
     int bm, bn;
-    const double padded = best_tile_us(n, m, Kp, bm, bn, true) + 3.0 + 2.0 * (double)Kp * (2.0 * (double)n + 1.125 * (double)m) / 4e6;
+    const double padded = best_tile_us(n, m, Kp, bm, bn) + 3.0 + 2.0 * (double)Kp * (2.0 * (double)n + 1.125 * (double)m) / 4e6;
     return padded < 0.85 * general ? Kp : 0;                  // (for a launch more, 3 us of the host's)
 }
 
@@ -1875,6 +1881,7 @@ hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, 
     hipError_t e;
     switch (split.bm * 1000 + split.bn) {
         case 128064: e = launch_ring<128, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
+        case 192064: e = launch_ring<192, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
         case 256064: e = launch_ring<256, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
         case 128128: e = launch_ring<128, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
         default: e = launch_tile<256, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
@@ -1887,7 +1894,7 @@ hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const 
                         int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
     const int64_t most = ((int64_t)1 << 21) / ((gated_rows(gate.d_ff) + 63) / 64) * 64 / 256 * 256;
     const size_t d_ff = (size_t)gate.d_ff, blocks = (d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
-    const int64_t rest = gate.gu || gate.q ? 0 : spmm_rest_tokens(n, gated_rows(gate.d_ff), K, true);
+    const int64_t rest = gate.keeps() ? 0 : spmm_rest_tokens(n, gated_rows(gate.d_ff), K);
     n -= rest;                                                // the last few: one pass of the small-batch kernel, behind the others
     for (int64_t t = 0; t < n; t += most) {
         GateOut part = gate;

@@ -69,6 +69,20 @@ __device__ __forceinline__ void store_stream_gated(int n, int e0, bf16_t* __rest
     constexpr int TOKENS = THREADS / ELEMENTS;                // whole groups of ELEMENTS threads
     const int t = threadIdx.x, o = t % ELEMENTS, row = (o >> 3) * 16 + (o & 7);
     if (t >= TOKENS * ELEMENTS || e0 + o >= gate.d_ff) return;
+    if (gate.sums) {                                          // uniform
+        for (int tok = t / ELEMENTS; tok < n; tok += TOKENS) {
+            float g = 0.f, u = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                g += sum(row, tok, w);
+                u += sum(row + 8, tok, w);
+            }
+            float* const at = gate.sums + (size_t)tok * (2 * (size_t)gate.d_ff) + e0 + o;
+            at[0] = g;
+            at[gate.d_ff] = u;
+        }
+        return;
+    }
     with_act(gate.act, [&](auto act) {
         for (int tok = t / ELEMENTS; tok < n; tok += TOKENS) {
             float g = 0.f, u = 0.f;
@@ -812,9 +826,9 @@ static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, cons
     if (e != hipSuccess) return e;
     const int64_t chunks = K / 1024, per = (chunks + slices - 1) / slices;
     spmm_rows_kernel<NF, WAVES, Gate...><<<dim3((unsigned)((m + S::BM - 1) / S::BM), (unsigned)slices), dim3(WAVES * 64), S::TOTAL, s>>>(
-        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, slices > 1 ? partial : nullptr, (int)(per * 8), gate...);
+        B, (int)n, Av, Am, (int)m, (int)K, T, R, (int)K2, C, slices > 1 || sizeof...(Gate) > 0 ? partial : nullptr, (int)(per * 8), gate...);
     if ((e = hipGetLastError()) != hipSuccess || slices == 1) return e;
-    if constexpr (sizeof...(Gate) > 0) return launch_gated_sum(partial, slices, n, m, C, gate..., s);
+    if constexpr (sizeof...(Gate) > 0) return e;              // (launch_gated_stream adds the slices)
     const size_t count4 = (size_t)n * (size_t)m / 4;
     rows_sum_kernel<<<dim3((unsigned)((count4 + 255) / 256)), dim3(256), 0, s>>>((const f32x4*)partial, slices, count4, (u32x2*)C);
     return hipGetLastError();
@@ -932,15 +946,26 @@ bool launch_spmm_stream_adapter(const bf16_t* B, int64_t n, const bf16_t* A_vals
     return true;
 }
 
-// The gated product for n <= 32 tokens, h only: T = X L given (with slices, that is), or L, where every workgroup computes it by itself
+// The gated product for n <= 32 tokens: T = X L given, or L, where every workgroup computes it by itself.  sums_or_null: scratch of
+// gated_stream_bytes; without it no slices, and nothing is kept.  Where something is, the kernels leave sums, and gated_sum_kernel does the
+// rest, since a workgroup's elements are no whole blocks (us, 10 tokens, 1024 x 7424, in 8 bits, tiles / so: 24.7 / 11.8).
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced) {
     return r > 0 && spmm_rows_slices(n, m, K, sliced) == 0 && xl_by_itself(n, m, K, r);
 }
+size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, bool keeps) {
+    if (!spmm_stream_fits(n, K)) return 0;
+    const int slices = spmm_rows_slices(n, 2 * d_ff, K, true);
+    return slices > 1 || keeps ? (size_t)(slices > 1 ? slices : 1) * (size_t)n * (size_t)(2 * d_ff) * 4 : 0;
+}
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
-                               const bf16_t* R, int64_t r, bf16_t* H, float* partial_or_null, const GateOut& gate, hipStream_t s) {
+                               const bf16_t* R, int64_t r, bf16_t* H, float* sums_or_null, const GateOut& gate, hipStream_t s) {
     const int64_t m = 2 * (int64_t)gate.d_ff;
-    const StreamXl xl = {L, nullptr, nullptr, (int)r, 0, 0, 0};
-    return launch_stream(B, n, A_vals, A_meta, m, K, T, R, r, H, partial_or_null, spmm_rows_slices(n, m, K, partial_or_null != nullptr), xl, s, gate);
+    const int slices = spmm_rows_slices(n, m, K, sums_or_null != nullptr);
+    const bool leave = gate.keeps() || slices > 1;            // sums, not h
+    GateOut out = gate;
+    out.sums = leave ? sums_or_null : nullptr;
+    const hipError_t e = launch_stream(B, n, A_vals, A_meta, m, K, T, R, r, H, out.sums, slices, StreamXl{L, nullptr, nullptr, (int)r, 0, 0, 0}, s, out);
+    return e != hipSuccess || !leave ? e : launch_gated_sum(out.sums, slices > 1 ? slices : 1, n, m, H, gate, s);
 }
 
 // Scratch for the partial sums of T = X L: slabs of up to four chunks of 64 rows of L as long as there are still

@@ -71,11 +71,14 @@ def test_size_queries():
         assert lib.slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) == lib.slope_workspace_bytes(sl.SLOPE_CALL_WGRAD_MASKED_Q8, b, d_in, d_out, 0)
         assert lib.slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) >= 2 * b * d_in
     for b, d_in, d_ff, r in ((1, 768, 2048, 0), (777, 5120, 13648, 64), (64, 9216, 24576, 128)):
-        need = lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r)
+        need = lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, 8)
         assert need == lib.slope_workspace_bytes(sl.SLOPE_CALL_GATED_FWD, b, d_in, d_ff, r) and need >= 2 * b * r
-        assert call("slope_gated_fwd", FWD, b=b, d_in=d_in, d_ff=d_ff, r=64, ws_bytes=lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, 64) - 1) \
-            == sl.SLOPE_ERR_WORKSPACE
-    assert lib.slope_gated_fwd_workspace_bytes(0, 64, 64, 0) == 0 and lib.slope_gated_fwd_workspace_bytes(4, 64, 12, 0) == 0
+        assert need == lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, 16) >= lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, 0)
+        for kept, none in ((8, {}), (0, dict(gu=None, q=None, scale=None))):
+            short = lib.slope_gated_fwd_workspace_bytes(b, d_in, d_ff, 64, kept) - 1
+            assert call("slope_gated_fwd", FWD, b=b, d_in=d_in, d_ff=d_ff, r=64, ws_bytes=short, **none) == sl.SLOPE_ERR_WORKSPACE
+    assert lib.slope_gated_fwd_workspace_bytes(1, 768, 2048, 0, 0) == 0                  # nothing to allocate for the smallest calls
+    assert lib.slope_gated_fwd_workspace_bytes(0, 64, 64, 0, 0) == 0 and lib.slope_gated_fwd_workspace_bytes(4, 64, 12, 0, 0) == 0
 
 
 def test_the_binding_refuses_what_is_not_a_device_matrix():

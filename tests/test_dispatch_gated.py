@@ -14,7 +14,8 @@ def plan(b, d_ff, d_in, r=0, **more):
 def test_regimes():
     assert plan(1, 2048, 768)["product"] == SMALL_BATCH
     assert plan(1, 24576, 9216)["product"] == ROW_SPLIT
-    assert plan(1, 24576, 9216, kept=True)["product"] == TILE                # the small-batch kernels keep nothing
+    assert plan(1, 24576, 9216, kept=8)["product"] == ROW_SPLIT
+    assert plan(1, 24576, 9216, kept=8, with_workspace=False)["product"] == TILE         # the small-batch kernels leave sums of what is kept
     assert plan(128, 200, 4096)["product"] == SLABS and plan(128, 200, 4096, with_workspace=False)["product"] == TILE
     assert plan(300, 1000, 1000) == {"product": GENERAL, "rows": 64, "tokens": 64, "slabs": 1, "xl": 0, "padded": 0}
     p = plan(1000, 1000, 1000)
@@ -29,12 +30,16 @@ def test_workgroups_of_64_rows_where_they_save_a_thin_round():
     assert plan(1, 2048, 16384) == {"product": ROW_SPLIT, "rows": 48, "tokens": 16, "slabs": 8, "xl": 0, "padded": 0}
 
 
-def test_no_tile_of_192_rows():
-    """A wavefront's rows of a gated tile are whole blocks of 32 elements."""
-    for b in (40, 100, 300, 777, 1000, 2048, 5000):
-        for d_ff in (96, 1000, 2176, 4352, 13648):
-            for d_in in (128, 2112, 4352):
-                assert plan(b, d_ff, d_in)["rows"] in (64, 128, 256)
+def test_codes_from_no_tile_of_192_rows():
+    """A wavefront's rows of a tile that writes 8-bit blocks are whole blocks of 32 elements."""
+    tall = set()
+    for b in (40, 100, 128, 300, 777, 1000, 2048, 5000):
+        for d_ff in (96, 1000, 2176, 4352, 13648, 24576):
+            for d_in in (128, 2112, 2560, 4352):
+                p = plan(b, d_ff, d_in, kept=8)
+                assert p["rows"] in (64, 128, 256) or p["product"] == SLABS
+                tall.add(plan(b, d_ff, d_in, kept=16)["rows"])
+    assert 192 in tall
 
 
 @pytest.mark.parametrize("bad", [dict(b=0), dict(d_ff=12), dict(d_in=4), dict(d_ff=(1 << 22) + 8)])
@@ -52,16 +57,18 @@ def forms():
     found = set()
     cases = [(b, f, i, r) for b, f, i in SHAPES for r in (0, 32, 160)] + LARGE
     for b, f, i, r in cases:
-        for kept in (False, True):
+        for kept in (0, 8, 16):
             for ws in (True, False):
                 if not ws and (r or kept):
                     continue
                 p = plan(b, f, i, r, kept=kept, with_workspace=ws)
-                whole = 256 if p["rows"] == 256 and p["tokens"] != 64 else 128
+                whole = 256 if p["rows"] * p["tokens"] >= 192 * 128 else 128
                 k = p["padded"] or i
                 tail = k % whole != 0 if p["product"] != GENERAL else (i % 64 != 0) + (i % 128 != 0)
                 split = p["slabs"] > 1 and p["product"] in (SLABS, ROW_SPLIT)
                 found.add((p["product"], p["rows"], p["tokens"], split, p["xl"], int(tail)))
+                if p["product"] in (SMALL_BATCH, ROW_SPLIT):
+                    found.add((p["product"], p["rows"], p["tokens"], split, "kept" if kept else "h"))
     return found
 
 
@@ -76,18 +83,22 @@ def test_the_gpu_tests_reach_every_form():
             assert any((SMALL_BATCH, rows, 32, False, xl, tail) in found for tail in (0, 1)), (rows, xl)
     for tokens in (16, 32):
         assert (ROW_SPLIT, 48, tokens, True, 0, 0) in found
+        for rows in (32, 48):
+            assert (SMALL_BATCH, rows, tokens, False, "kept") in found
+        assert (ROW_SPLIT, 48, tokens, True, "kept") in found
+    assert (SMALL_BATCH, 64, 16, False, "kept") in found and (ROW_SPLIT, 48, 16, False, "kept") in found and (ROW_SPLIT, 64, 16, False, "kept") in found
     assert (ROW_SPLIT, 48, 16, False, 0, 0) in found and (ROW_SPLIT, 64, 16, False, 0, 0) in found
-    for rows, tokens in ((128, 64), (128, 128), (256, 64), (256, 128)):
+    for rows, tokens in ((128, 64), (128, 128), (192, 64), (256, 64), (256, 128)):
         for tail in (0, 1):
             assert (SLABS, rows, tokens, True, 0, tail) in found, (rows, tokens, tail)
-    for rows, tokens in ((128, 64), (128, 96), (128, 128), (256, 128), (256, 192), (256, 256)):
+    for rows, tokens in ((128, 64), (128, 96), (128, 128), (192, 64), (192, 96), (192, 128), (192, 192), (192, 256), (256, 128), (256, 192), (256, 256)):
         for tail in (0, 1):
             assert (TILE, rows, tokens, False, 0, tail) in found, (rows, tokens, tail)
     assert (TILE, 64, 64, False, 0, 0) in found
     for edge, tails in ((64, (1, 2)), (128, (1, 2))):
         for tail in tails:
             assert (GENERAL, edge, edge, False, 0, tail) in found, (edge, tail)
-    assert {(REST, 128, 128, False, 0, t) for t in (0,)} <= found and any(f[0] == REST and f[1] == 256 for f in found)
+    assert (REST, 256, 256, False, 0, 0) in found and (REST, 256, 256, False, 0, 1) in found
 
 
 def test_the_gpu_tests_reach_padded_copies():

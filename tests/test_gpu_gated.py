@@ -151,7 +151,8 @@ SHAPES = [(1, 8, 8), (1, 256, 128), (1, 64, 1024), (2, 1000, 768), (7, 40, 264),
           (300, 768, 640), (512, 136, 8), (520, 256, 520), (700, 1032, 448), (1000, 1000, 1000), (1030, 2048, 128), (2100, 320, 256)]
 # what the small ones do not reach: the other numbers of rows of the small-batch kernel, its row-split form with and without slices, every
 # tile and every split, an odd k-step at the end of each, tokens and tiles that are left over (test_dispatch_gated.py)
-LARGE = [(1, 8, 192, 0), (1, 8, 192, 32), (1, 3912, 192, 32), (1, 6872, 128, 32), (1, 7104, 704, 32), (1, 6656, 320, 0), (17, 8, 128, 32), (19, 8, 192, 32),
+LARGE = [(1568, 5056, 768, 32), (785, 9984, 832, 0), (35, 2600, 10048, 0), (65, 1688, 15360, 32), (130, 1040, 12096, 0), (98, 8504, 192, 0), (131, 8368, 192, 32), (197, 8200, 256, 64), (199, 8224, 128, 0),
+         (385, 11080, 256, 0), (386, 10936, 128, 32), (1, 8, 192, 0), (1, 8, 192, 32), (1, 3912, 192, 32), (1, 6872, 128, 32), (1, 7104, 704, 32), (1, 6656, 320, 0), (17, 8, 128, 32), (19, 8, 192, 32),
          (1, 4056, 128, 0), (1, 4128, 192, 0), (1, 6848, 128, 0), (5, 6656, 320, 32), (17, 4304, 128, 0), (20, 5120, 192, 32), (1, 12288, 1024, 0),
          (3, 2056, 17408, 0), (2, 24576, 1024, 0), (13, 20488, 1024, 32), (300, 2056, 2056, 0), (1000, 520, 2200, 32), (2048, 264, 520, 0), (200, 8, 4104, 0), (400, 520, 8200, 32), (1999, 1000, 1096, 64), (16, 2048, 16384, 64), (20, 2048, 16384, 0), (31, 4104, 16384, 32), (9, 12296, 2048, 96),
          (1, 4272, 128, 32), (17, 4544, 128, 32), (35, 8, 2816, 32), (40, 8, 2624, 0), (4344, 8, 6144, 0), (3546, 8, 8000, 32),
@@ -180,7 +181,10 @@ def check_forward(b, d_ff, d_in, act, r):
     assert none_gu is None and none_q is None and none_s is None
     again = sl.slope_gated_fwd(p.x, p.vals, p.meta, **args)[0]
     kept, gu, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, want_q8=True, **args)
+    wide, gu_only, _, _ = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, **args)
     torch.cuda.synchronize()
+    check_h(wide, p.gu, p.off, act, "h of the call that keeps bf16")
+    check_kept(gu_only, p.gu, p.off, "gu without codes")
     check_h(h, p.gu, p.off, act, "h")
     check_h(kept, p.gu, p.off, act, "h of the call that keeps")
     assert torch.equal(h, again)
@@ -189,6 +193,10 @@ def check_forward(b, d_ff, d_in, act, r):
     if r == 0:
         alone = sl.slope_gated_fwd(p.x, p.vals, p.meta, act=ACTS[act], workspace=None)[0]
         check_h(alone, p.gu, p.off, act, "h without scratch")
+        if b <= 32:                                                         # kept by the tile kernels then
+            _, gu, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, act=ACTS[act], want_gu=True, want_q8=True, workspace=None)
+            check_kept(gu, p.gu, p.off, "gu without scratch")
+            check_blocks(q.view(2 * b, d_ff), scale.view(2 * b, -1), p.gu.view(2 * b, d_ff), p.off.view(2 * b, d_ff), "codes without scratch")
 
 
 @pytest.mark.parametrize("b,d_ff,d_in,r", [(1, 1000, 768, 32), (20, 264, 448, 0), (70, 72, 1024, 64), (300, 328, 640, 0), (515, 1000, 256, 96), (260, 264, 264, 32)])
@@ -207,7 +215,9 @@ def test_nothing_outside_is_written_and_parts_agree(b, d_ff, d_in, r):
     torch.cuda.synchronize()
     for k, (n, _) in sizes.items():
         assert (whole[k][:pad] == 7).all() and (whole[k][pad + n:] == 7).all(), k
-    assert torch.equal(only[0], out[0]) and torch.equal(only[1], out[1]) and torch.equal(codes[3], out[3])
+    assert torch.equal(codes[0], out[0]) and torch.equal(codes[3], out[3])
+    check_h(only[0], p.gu, p.off, "silu", "h")
+    check_kept(only[1], p.gu, p.off, "gu")
     assert torch.equal(codes[2].view(torch.uint8), out[2].view(torch.uint8))
 
 

@@ -158,17 +158,36 @@ __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int
     }
 }
 
+// The largest of the four quarters of 16 lanes, lane by lane: rows of the register exchanged without an LDS round trip
+__device__ __forceinline__ uint32_t quarters_max(uint32_t v) {
+    const auto far = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = MaxBits()(far[0], far[1]);
+    const auto near = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return MaxBits()(near[0], near[1]);
+}
+// Everybody's LDS accesses are done; stores to memory go on.
+__device__ __forceinline__ void lds_barrier() {
+    WAIT_HERE(waitcnt_imm(63, 0));
+    wg_barrier();
+}
+
 // A tile's results, BMT virtual rows (BMT / 2 elements) x BNT tokens, by THREADS threads: like store_rows through LDS, since whole rows
-// of a tile leave in whole lines.  h first, then the projections as they are kept.  All threads make the call.
+// of a tile leave in whole lines.  h and the codes together, then bf16 projections.  All threads make the call.
+// What is kept is for the backward pass, long after, and passes the caches by, but for codes that fit a quarter of the last-level one beside
+// others' (us, 16384 tokens, 18432 x 2560, bf16 924 -> 875, codes 931 -> 901; 2048, 13824 x 2560, bf16 111 -> 107, codes 107 -> 105 but, with the
+// gradient right behind, 128.5 -> 131).  The tiles of a round end together, so that their results are a burst at the memory's rate, 5 us for the
+// projections of 256 tiles of 256 x 256 in bf16; codes are half of it and as long again in conversions (16384, 4096 x 768: h 86, with bf16
+// 106, with codes 107).
 template <int MF, int NF, int BMT, int BNT, int THREADS>
 __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, int t0, int n, int l16, int lq, bf16_t* __restrict__ H,
                                             uint8_t* smem, int tile_f0, int tile_t0, const GateOut& gate) {
     static_assert(MF % 2 == 0, "pairs of fragments");
     constexpr int HALF = BMT / 2;                             // elements of h in the tile
+    constexpr int CODES = BNT * (BMT + 16);                   // where the codes are staged, behind h
     const int tile_e0 = tile_f0 / 2, e0 = f0 / 2, d_ff = gate.d_ff;
     const int le = e0 - tile_e0 + lq * 4, lt = t0 - tile_t0 + l16;        // the lane's first element and token inside the tile
-    // rows of BYTES bytes per token in LDS -> rows of the result, which starts at out + tok * pitch + offset(byte) bytes
-    auto leave = [&](auto bytes, auto to) {
+    // rows of BYTES bytes per token at `from` in LDS, piece by piece of 16 bytes, to to(token, piece, its bytes)
+    auto leave = [&](auto bytes, const uint8_t* from, auto to) {
         constexpr int BYTES = decltype(bytes)::value, CP = BYTES + 16, PPR = BYTES / 16, PIECES = BNT * PPR;
         constexpr int PER_THREAD = (PIECES + THREADS - 1) / THREADS;
         constexpr bool EVEN = PIECES % THREADS == 0;
@@ -176,7 +195,7 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
 #pragma unroll
         for (int u = 0; u < PER_THREAD; ++u) {
             const int idx = (int)threadIdx.x + u * THREADS;
-            if (EVEN || idx < PIECES) piece[u] = *(const u32x4*)(smem + (idx / PPR) * CP + (idx % PPR) * 16);
+            if (EVEN || idx < PIECES) piece[u] = *(const u32x4*)(from + (idx / PPR) * CP + (idx % PPR) * 16);
         }
 #pragma unroll
         for (int u = 0; u < PER_THREAD; ++u) {
@@ -196,27 +215,8 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                 *(u32x2*)(smem + (lt + j * 16) * (BMT + 16) + (le + i * 16) * 2) = four_bf16(h);
             }
     });
-    __syncthreads();
-    leave(std::integral_constant<int, BMT>{}, [&](int tok, int p, const u32x4& v) {
-        const int e = tile_e0 + p * 8;
-        if (e < d_ff) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
-    });
-    if (gate.gu) {                                            // uniform
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < NF; ++j)
-#pragma unroll
-            for (int i = 0; i < MF; ++i)
-                *(u32x2*)(smem + (lt + j * 16) * (2 * BMT + 16) + ((i & 1) * HALF + le + (i >> 1) * 16) * 2) = four_bf16(acc[i][j]);
-        __syncthreads();
-        leave(std::integral_constant<int, 2 * BMT>{}, [&](int tok, int p, const u32x4& v) {
-            const int half = p * 8 / HALF, e = tile_e0 + p * 8 % HALF;
-            if (e < d_ff) *(u32x4*)(gate.gu + (size_t)tok * (2 * (size_t)d_ff) + half * d_ff + e) = v;
-        });
-    }
+    const size_t blocks = ((size_t)d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
     if constexpr (MF % 4 == 0) if (gate.q) {                  // whole blocks in a wavefront's rows: no other tile is given codes to write
-        const size_t blocks = ((size_t)d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
-        __syncthreads();
 #pragma unroll
         for (int j = 0; j < NF; ++j)
 #pragma unroll
@@ -227,22 +227,40 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                     const int e = e0 + c * 32;                // the block's first element
                     uint32_t top = e + lq * 4 < d_ff ? top_of(a) : 0u;
                     if (e + 16 + lq * 4 < d_ff) top = MaxBits()(top, top_of(b));
-                    top = MaxBits()(top, (uint32_t)__shfl_xor((int)top, 16));
-                    top = MaxBits()(top, (uint32_t)__shfl_xor((int)top, 32));
-                    const BlockScale s = block_scale(top);
-                    uint8_t* const at = smem + (lt + j * 16) * (BMT + 16) + half * HALF + le + c * 32;
+                    const BlockScale s = block_scale(quarters_max(top));
+                    uint8_t* const at = smem + CODES + (lt + j * 16) * (BMT + 16) + half * HALF + le + c * 32;
                     *(uint32_t*)at = four_codes(a, s);
                     *(uint32_t*)(at + 16) = four_codes(b, s);
                     const int tok = t0 + j * 16 + l16;
                     if (lq == 0 && tok < n && e < d_ff) gate.bytes[((size_t)tok * 2 + half) * blocks + e / Q8_BLOCK] = (uint8_t)s.byte;
                 }
-        __syncthreads();
-        leave(std::integral_constant<int, BMT>{}, [&](int tok, int p, const u32x4& v) {
+    }
+    lds_barrier();
+    leave(std::integral_constant<int, BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
+        const int e = tile_e0 + p * 8;
+        if (e < d_ff) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
+    });
+    const bool large = (size_t)n * d_ff > LAST_LEVEL_CACHE_BYTES / 8;
+    if constexpr (MF % 4 == 0) if (gate.q)
+        leave(std::integral_constant<int, BMT>{}, smem + CODES, [&](int tok, int p, const u32x4& v) {
             const int half = p * 16 / HALF, e = tile_e0 + p * 16 % HALF;
             uint8_t* const to = gate.q + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e;
             // d_ff is a multiple of 8: a row's codes may start 8 bytes off, and its last piece may be half a one
-            if (e + 8 < d_ff) *(u32x4_a8*)to = v;
+            if (e + 8 < d_ff && large) __builtin_nontemporal_store((u32x4_a8)v, (u32x4_a8*)to);
+            else if (e + 8 < d_ff) *(u32x4_a8*)to = v;
             else if (e < d_ff) *(u32x2*)to = (u32x2){v[0], v[1]};
+        });
+    if (gate.gu) {                                            // uniform
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
+#pragma unroll
+            for (int i = 0; i < MF; ++i)
+                *(u32x2*)(smem + (lt + j * 16) * (2 * BMT + 16) + ((i & 1) * HALF + le + (i >> 1) * 16) * 2) = four_bf16(acc[i][j]);
+        lds_barrier();
+        leave(std::integral_constant<int, 2 * BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
+            const int half = p * 8 / HALF, e = tile_e0 + p * 8 % HALF;
+            if (e < d_ff) __builtin_nontemporal_store(v, (u32x4*)(gate.gu + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e));
         });
     }
 }

@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_kernel(const bf16_t* __rest
     }
     if (OWN) WAIT_HERE(waitcnt_imm(0, 15));  // drain the clamped look-ahead loads
 
-    static_assert(BN * (BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the rings");
+    static_assert(BN * (BM * 2 + 16 * (1 + sizeof...(Gate))) <= S::TOTAL, "the staged output tile fits in the rings");
     int te = threadIdx.x;                                    // (the lane's coordinates again rather than kept across the loop)
     if (!OWN) asm volatile("" : "+v"(te));
     const int we = __builtin_amdgcn_readfirstlane(te >> 6);
@@ -851,7 +851,7 @@ __global__ void __launch_bounds__(SPMM_THREADS) spmm_split_kernel(const bf16_t* 
     for (int r = 0; r < 2 * PF_ROWS; ++r) asm volatile("" ::"s"(pf[r]));
 #undef PF_ISSUE
     WAIT_HERE(waitcnt_imm(0, 15));                            // drain the clamped look-ahead loads
-    static_assert(S::BN * (S::BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the rings");
+    static_assert(S::BN * (S::BM * 2 + 16 * (1 + sizeof...(Gate))) <= S::TOTAL, "the staged output tile fits in the rings");
     extend_and_store<MF, NF, S::BM, S::BN, SPMM_THREADS>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2, K2, C, smem,
                                            m0, n0, nullptr, gate...);
 }
@@ -1111,7 +1111,7 @@ __global__ void __launch_bounds__(RING_THREADS) spmm_ring_kernel(const bf16_t* _
             pair(p + 3, std::integral_constant<int, 3>{});
         }
     }
-    static_assert(BN * (BM * 2 + 16) <= S::TOTAL && 128 * (BM * 2 + 32) <= S::TOTAL, "the staged output tile and factor fit in the ring");
+    static_assert(BN * (BM * 2 + 16 * (1 + sizeof...(Gate))) <= S::TOTAL && 128 * (BM * 2 + 32) <= S::TOTAL, "the staged output tile and factor fit in the ring");
     extend_and_store<MF, NF, BM, BN, 64 * RING_MULT, true>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2,
                                                    slab == extension_slab ? K2 : 0, C, smem, m0, n0, sums, gate...);
 }
@@ -1260,7 +1260,7 @@ __global__ void __launch_bounds__(256 * G) spmm_generic_kernel(const bf16_t* __r
     }
     __syncthreads();                                          // the stages are free
     if constexpr (G == 1) {
-        static_assert(S::BN * (S::BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the stages");
+        static_assert(S::BN * (S::BM * 2 + 16 * (1 + sizeof...(Gate))) <= S::TOTAL, "the staged output tile fits in the stages");
         extend_and_store<MF, NF, S::BM, S::BN, 256>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, m, n, l16, lq, B2, A2, K2, C,
                                                     smem, m0, n0, nullptr, gate...);
     } else {

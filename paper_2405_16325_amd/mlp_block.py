@@ -1,15 +1,18 @@
-"""A stack of pre-norm blocks of double-pruned layers, trained with AdamW and served in 8 bits, by the library's calls; the
-relu, its gradient and the loss are torch's.
+"""Stacks of pre-norm blocks of double-pruned layers, trained with AdamW and served, by the library's calls; the loss, and the
+first stack's relu with its gradient, are torch's.
 
     block:  h <- h + W2 norm2(relu(W1 norm1(h)))          W1, W2: packed 2:4 (W^R forward, W^{R,C} backward)
+    gated block:  h <- h + W2 (act(g) u),  [g | u] = W1 norm1(h)
     out  =  norm(h)
 
 Training: every norm adds the stream's last contribution itself (slope_rmsnorm_fwd with a residual) and its gradient carries the
 stream's along (slope_rmsnorm_bwd with dh); the packed gradients go to AdamW as they are, with fp32 masters and 32- or 8-bit
 states; slope_update_sparse brings the transposed copies in line.  The host waits for nothing in a step.
 Serving: the norms write 8 bits with a scale per token, the products read them, the second one adds the stream.
+The gated stack keeps 8-bit codes of what its layers' gradients want, the input and the projections (33/32 bytes an element); the layer's
+output is made again from them (slope_gated_bwd).  It serves in bf16, activation and product inside the first product.
 
-`python -m paper_2405_16325_amd.mlp_block` trains a small one on a random teacher and compares the two paths.
+`python -m paper_2405_16325_amd.mlp_block` trains a small one of each on a random teacher and compares the paths.
 """
 from __future__ import annotations
 
@@ -47,6 +50,30 @@ class SparseLayer:
         return sl.slope_spmm_fwd_q8(q, scale, self.q[0], self.meta, self.q[1], add=add)
 
 
+class GatedLayer(SparseLayer):
+    """act(g) u of the projections g, u of one weight of 2 d_ff rows, the gate's first."""
+
+    def __init__(self, d_ff, d_in, generator, act=sl.SLOPE_ACT_SILU):
+        super().__init__(2 * d_ff, d_in, generator)
+        self.act = act
+
+    def forward(self, x):
+        """(output, what backward wants)"""
+        h, _, codes, scale = sl.slope_gated_fwd(x, self.vals, self.meta, self.act, want_q8=True)
+        return h, (sl.slope_checkpoint_q8(x), codes, scale)
+
+    def output(self, dh, saved):
+        """(gradient of the projections, the output again)"""
+        return sl.slope_gated_bwd(dh, self.act, q8=saved[1], scale=saved[2])
+
+    def backward(self, dgu, saved):
+        sl.slope_wgrad_masked_q8(dgu, *saved[0], self.meta, out=self.grad)
+        return sl.slope_spmm_bwd_x(dgu, self.vals_t, self.meta_t)
+
+    def serve(self, x):
+        return sl.slope_gated_fwd(x, self.vals, self.meta, self.act)[0]
+
+
 class Norm:
     def __init__(self, d):
         self.w, self.master = torch.ones(d, dtype=BF16, device="cuda"), torch.ones(d, device="cuda")
@@ -69,10 +96,10 @@ class PrenormMLP:
     def __init__(self, d, hidden, blocks, state_bits=8, weight_decay=0.0, seed=0):
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
-        self.blocks = [(Norm(d), SparseLayer(hidden, d, gen), Norm(hidden), SparseLayer(d, hidden, gen)) for _ in range(blocks)]
+        self.blocks = [self.block(d, hidden, gen) for _ in range(blocks)]
         self.out = Norm(d)
-        self.layers = [x for b in self.blocks for x in (b[1], b[3])]
-        norms = [x for b in self.blocks for x in (b[0], b[2])] + [self.out]
+        self.layers = [x for b in self.blocks for x in b if isinstance(x, SparseLayer)]
+        norms = [x for b in self.blocks for x in b if isinstance(x, Norm)] + [self.out]
         parts = self.layers + norms
         params = [x.vals for x in self.layers] + [x.w for x in norms]
         scales = (None, None)
@@ -86,6 +113,9 @@ class PrenormMLP:
                                         m_scales=scales[0], v_scales=scales[1],
                                         weight_decay=[weight_decay] * len(self.layers) + [0.0] * len(norms))
         self.control = torch.zeros(4, device="cuda")
+
+    def block(self, d, hidden, gen):
+        return Norm(d), SparseLayer(hidden, d, gen), Norm(hidden), SparseLayer(d, hidden, gen)
 
     def forward(self, x):
         """x bf16[b, d] -> (out, what backward wants)"""
@@ -124,6 +154,41 @@ class PrenormMLP:
         return sl.slope_rmsnorm_fwd(h, self.out.w, EPS)[0]
 
 
+class PrenormGatedMLP(PrenormMLP):
+    def __init__(self, d, hidden, blocks, act=sl.SLOPE_ACT_SILU, **kw):
+        self.act = act
+        super().__init__(d, hidden, blocks, **kw)
+
+    def block(self, d, hidden, gen):
+        return Norm(d), GatedLayer(hidden, d, gen, self.act), SparseLayer(d, hidden, gen)
+
+    def forward(self, x):
+        saved, part, h = [], x, None
+        for norm, gated, down in self.blocks:
+            y, h, s = norm.forward(part, residual=h)
+            a, kept = gated.forward(y)
+            part = down.forward(a)
+            saved.append((s, kept))
+        out, _, s = self.out.forward(part, residual=h)
+        return out, (saved, s)
+
+    def backward(self, dout, kept):
+        saved, s = kept
+        dh = self.out.backward(dout, s)
+        for (norm, gated, down), (s, codes) in zip(reversed(self.blocks), reversed(saved)):
+            dgu, a = gated.output(sl.slope_spmm_bwd_x(dh, down.vals_t, down.meta_t), codes)
+            sl.slope_wgrad_masked(dh, a, down.meta, out=down.grad)
+            dh = norm.backward(gated.backward(dgu, codes), s, dh=dh)
+        return dh
+
+    def serve(self, x):
+        part, h = x, None
+        for norm, gated, down in self.blocks:
+            y, h, _ = norm.forward(part, residual=h)
+            part = down.forward(gated.serve(y))
+        return self.out.forward(part, residual=h)[0]
+
+
 def train(model, d, steps=150, b=512, lr=3e-3, loss_scale=1024.0, seed=1):
     """Mean squared errors, first and last, against a random smooth teacher."""
     gen = torch.Generator(device="cuda")
@@ -149,6 +214,11 @@ def main():
         out, served = model.forward(x)[0].float(), model.serve(x).float()
         print("%2d-bit states: loss %.3f -> %.3f; 8-bit serving differs by %.3f of the output's norm; %d steps taken"
               % (bits, first, last, float((out - served).norm() / out.norm()), int(model.control[2])))
+    model = PrenormGatedMLP(256, 512, 2)
+    first, last = train(model, 256)
+    x = torch.randn(1, 256, device="cuda").to(BF16)
+    same = torch.equal(model.forward(x)[0], model.serve(x))
+    print("gated, activations kept in 8 bits: loss %.3f -> %.3f; one token served as in training: %s" % (first, last, same))
 
 
 if __name__ == "__main__":

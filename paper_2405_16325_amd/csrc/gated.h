@@ -99,6 +99,19 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float
     const int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
 }
+// eight codes -> eight bf16 numbers, exactly: one instruction for two of them, which takes the scale's exponent
+__device__ __forceinline__ u32x4 restored_bf16(u32x2 codes, uint32_t byte) {
+    const float scale = __uint_as_float(byte << 23);
+    union { __attribute__((ext_vector_type(2))) __bf16 h[4]; u32x4 u; } o;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        o.h[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, false);
+        o.h[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[i], scale, true);
+    }
+    return o.u;
+}
+// an activation in this form, as an operand of the weight gradient
+struct BlocksX { const uint8_t *q, *bytes; };
 // eight codes -> the values they stand for
 __device__ __forceinline__ F8 unpack_e4m3(u32x2 codes, float scale) {
     F8 o;

@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(THREADS) restore_kernel(const uint8_t* __restr
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if (p[i].row < rows) store<STREAM>(x + (size_t)p[i].row * d + p[i].c * 8, pack_bf16(unpack_e4m3(in[i], scale_of_byte(byte[i]))));
+        if (p[i].row < rows) store<STREAM>(x + (size_t)p[i].row * d + p[i].c * 8, restored_bf16(in[i], byte[i]));
 }
 
 inline dim3 grid_for(int64_t pieces, int per) { return grid_of((pieces + THREADS * per - 1) / (THREADS * per)); }

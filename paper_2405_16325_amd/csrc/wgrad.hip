@@ -167,8 +167,7 @@ struct WgsSmem {
     static constexpr int RING = WGS_GROUPS * 2 * S::STAGE, SUMS = WGS_GROUPS * WGS_EDGE * WGS_SUM_PITCH * 4;
     static constexpr int TOTAL = RING > SUMS ? RING : SUMS;
 };
-// X in 8-bit blocks (gated.h) instead of bf16: restored between the load and the LDS stage
-struct BlocksX { const uint8_t *q, *bytes; };
+// Blocks: X in 8-bit blocks (BlocksX) instead of bf16, restored between the load and the LDS stage
 template <class... Blocks>
 __global__ void __launch_bounds__(256 * WGS_GROUPS) wgrad_groups_kernel(const bf16_t* __restrict__ dY,
                                                                         const bf16_t* __restrict__ X, int b,
@@ -206,7 +205,7 @@ __global__ void __launch_bounds__(256 * WGS_GROUPS) wgrad_groups_kernel(const bf
     };
     auto store_lds = [&](int stage) {
         uint8_t* base = ring + stage * S::STAGE;
-        if constexpr (Q8) *(u32x4*)(base + row * S::PITCH_A + 16 * c) = pack_bf16(unpack_e4m3(a_codes, scale_of_byte(a_byte)));
+        if constexpr (Q8) *(u32x4*)(base + row * S::PITCH_A + 16 * c) = restored_bf16(a_codes, a_byte);
         else *(uint4*)(base + row * S::PITCH_A + 16 * c) = a_reg;
         *(uint4*)(base + S::A_BYTES + row * S::PITCH_B + 16 * c) = b_reg;
     };

@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(256) restore_transposed_kernel(const uint8_t* 
         u32x4 v = {0u, 0u, 0u, 0u};
         if (r0 + r < j.rows && c0 + c8 < j.cols) {
             const u32x2 codes = __builtin_nontemporal_load((const u32x2*)(q + (size_t)(r0 + r) * j.cols + c0 + c8));
-            v = pack_bf16(unpack_e4m3(codes, scale_of_byte(bytes[(size_t)(r0 + r) * blocks + (c0 + c8) / Q8_BLOCK])));
+            v = restored_bf16(codes, bytes[(size_t)(r0 + r) * blocks + (c0 + c8) / Q8_BLOCK]);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) tile[c8 + e][r] = (bf16_t)(v[e >> 1] >> (16 * (e & 1)));
@@ -241,15 +241,95 @@ __device__ __forceinline__ void store_sums(const f32x4 (&acc)[MF][NF], int m, in
     }
 }
 
+// The loading wavefronts where A, k-major, comes in 8-bit blocks: `wave` of TN_LOADERS, each with the loads of EACH of eight, as they would be of
+// bf16 (DenseLoader).  Codes go through registers, restored on their way to the same places in LDS, AHEAD k-steps after their request (three where the
+// ring has room for seven: 2398 tokens, 448 x 1488 17.1 us, 15.5 so); B's loads are as ever.  All loads complete in order, and a k-step's codes are
+// requested after its rows of B, so that when its codes are there B's rows are.  For that every wavefront requests codes in every k-step (columns past the last are the
+// last eight, for rows that are not stored).
+template <int BM, int BN, int NS, bool BKM, int WROWS, int PRE>
+__device__ __forceinline__ void load_and_restore(const DenseOperand& At, const DenseOperand& Bt, const BlocksX& x, int ksteps, int k_begin, int k_end,
+                                                 int m0, int n0, int wave, int lane, uint8_t* smem) {
+    using S = TnSmem<BM, BN, NS>;
+    constexpr int MULT = tn_mult(BM, BN), EACH = 8 / TN_LOADERS, LD_A = BM / 64, LD_B = BN / 64, LAST = (NS - 1) * S::STAGE;
+    constexpr int AHEAD = NS - 1;
+    DenseLoader<BKM, true, BN, WROWS> lb[EACH];
+#pragma unroll
+    for (int v = 0; v < EACH; ++v) lb[v].init(Bt, n0, 0, wave + v * TN_LOADERS, lane, 0, ksteps, smem);
+    auto load_b = [&](int ks, int at, int from) {             // the loads of the eight from `from` on
+#pragma unroll
+        for (int v = 0; v < EACH; ++v)
+            if (v * TN_LOADERS >= from)
+#pragma unroll
+                for (int i = 0; i < LD_B; ++i) lb[v].load(ks, i, smem, at + S::A_BYTES, wave + v * TN_LOADERS);
+    };
+    // A k-step of 64 tokens is read through buffer descriptors of its own, offsets inside it being the same in every step; zeros past the
+    // last token, which stand for zeros.
+    struct Codes { u32x2 q[EACH][LD_A]; uint32_t byte[EACH][LD_A]; };
+    const uint32_t rows = (uint32_t)At.rows, blocks = (rows + Q8_BLOCK - 1) / Q8_BLOCK;
+    uint32_t q_at[EACH][LD_A], byte_at[EACH][LD_A];
+#pragma unroll
+    for (int v = 0; v < EACH; ++v) {
+        const int w = wave + v * TN_LOADERS;
+        const uint32_t tok = 8 * w + (lane >> 3);
+#pragma unroll
+        for (int i = 0; i < LD_A; ++i) {
+            const uint32_t c = m0 + 64 * i + 8 * ((lane & 7) ^ ((((lane >> 4) & 1) | ((w & 1) << 1)) * 2)), col = c < rows ? c : rows - 8;
+            q_at[v][i] = tok * rows + col;
+            byte_at[v][i] = tok * blocks + col / Q8_BLOCK;
+        }
+    }
+    auto fetch = [&](Codes& c, int ks) {
+        const uint32_t left = (uint32_t)At.k - (uint32_t)ks * 64, tokens = left < 64 ? left : 64;
+        const auto q = __builtin_amdgcn_make_buffer_rsrc((void*)(x.q + (size_t)(uint32_t)ks * 64 * rows), 0, (int)(tokens * rows), 0x00020000);
+        const auto b = __builtin_amdgcn_make_buffer_rsrc((void*)(x.bytes + (size_t)(uint32_t)ks * 64 * blocks), 0, (int)(tokens * blocks), 0x00020000);
+#pragma unroll
+        for (int v = 0; v < EACH; ++v)
+#pragma unroll
+            for (int i = 0; i < LD_A; ++i) {
+                c.q[v][i] = __builtin_amdgcn_raw_buffer_load_b64(q, (int)q_at[v][i], 0, 0);
+                c.byte[v][i] = __builtin_amdgcn_raw_buffer_load_b8(b, (int)byte_at[v][i], 0, 0);
+            }
+    };
+    auto restore = [&](const Codes& c, int at) {
+#pragma unroll
+        for (int v = 0; v < EACH; ++v)
+#pragma unroll
+            for (int i = 0; i < LD_A; ++i)
+                *(u32x4*)(smem + at + (i * 8 + wave + v * TN_LOADERS) * 1024 + lane * 16) = restored_bf16(c.q[v][i], c.byte[v][i]);
+    };
+    Codes codes[AHEAD];
+#pragma unroll
+    for (int p = 0; p < NS - 1; ++p)
+        if (k_begin + p < k_end) {
+            load_b(k_begin + p, p * S::STAGE, p < PRE ? MULT : 0);
+            fetch(codes[p], k_begin + p);
+        }
+    int at = 0;
+    for (int ks0 = k_begin; ks0 < k_end; ks0 += AHEAD)
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int ks = ks0 + u;
+            if (ks >= k_end) break;
+            restore(codes[u], at);
+            WAIT_HERE(waitcnt_imm(63, 0));
+            wg_barrier();                                     // step ks is there, and everybody has read the one before it
+            if (ks + NS - 1 < k_end) load_b(ks + NS - 1, at == 0 ? LAST : at - S::STAGE, 0);
+            if (ks + AHEAD < k_end) fetch(codes[u], ks + AHEAD);
+            at = at == LAST ? 0 : at + S::STAGE;
+        }
+}
+
 // acc = the tile at (m0, n0) of D[i, j] = sum_k At[i, k] * Bt[j, k] over the k-steps [k_begin, k_end), of ksteps k-steps of 64 in
 // all (the look-ahead past a slab's end reads real, unused data).  AKM, BKM: the operand is k-major.
 // NS = ring depth: loads run NS - 1 k-steps ahead.  Two stages are all that fits beside a 256 x 256
 // tile; small tiles (memory-bound skinny products) take a deeper ring to cover the HBM latency.
 // Every thread of the workgroup must make the call; wavefront w holds the fragments at rows w % 2 * BM / 2, columns w / 2 * WROWS.
 // False: a wavefront that has only loaded, and is done.
-template <int BM, int BN, int NS, bool AKM, bool BKM>
+// Blocks: At.p is null, and A comes in 8-bit blocks (BlocksX).
+template <int BM, int BN, int NS, bool AKM, bool BKM, class... Blocks>
 __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const DenseOperand& Bt, int ksteps, int k_begin, int k_end, int m0,
-                                              int n0, uint8_t* smem, f32x4 (&acc)[BM / 32][BN / (8 * tn_mult(BM, BN))]) {
+                                              int n0, uint8_t* smem, f32x4 (&acc)[BM / 32][BN / (8 * tn_mult(BM, BN))], const Blocks&... x) {
+    constexpr bool Q8 = sizeof...(Blocks) > 0;
     using S = TnSmem<BM, BN, NS>;
     constexpr int MULT = tn_mult(BM, BN), WROWS = BN / (MULT / 2);
     constexpr int MF = BM / 32, NF = WROWS / 16;             // 16 x 16 fragments per wavefront (2 x 4 or 2 x 2 waves)
@@ -265,6 +345,11 @@ __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const Dens
     constexpr int PRE = NS - 1 < 3 ? NS - 1 : 3;              // (what `behind` is asked for knows)
     static_assert(PRE <= NS - 1, "the steps that are shared out are among those loaded before the loop, so that each is loaded once");
     constexpr int LAST = (NS - 1) * S::STAGE;
+    static_assert(!Q8 || (LOADERS && AKM && NS >= 3), "restored by wavefronts that only load, into a stage that nobody reads");
+    if constexpr (Q8) if (wave >= MULT) {
+        load_and_restore<BM, BN, NS, BKM, WROWS, PRE>(At, Bt, x..., ksteps, k_begin, k_end, m0, n0, wave - MULT, lane, smem);
+        return false;
+    }
     if (LOADERS && wave >= MULT) {
         constexpr int EACH = 8 / TN_LOADERS;                  // a loader has the loads of so many of the eight
         // loads behind step k_begin + s, those of the NS - 2 steps after it
@@ -318,8 +403,9 @@ __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const Dens
     opa.init(At, m0, (wave & 1) * (BM / 2), wave, lane, 0, ksteps, smem);
     opb.init(Bt, n0, (wave >> 1) * WROWS, wave, lane, 0, ksteps, smem);
     auto issue = [&](int ks, int at) {                       // k-step ks (clamped) into the stage at byte `at`
+        if constexpr (!Q8)
 #pragma unroll
-        for (int i = 0; i < LD_A; ++i) opa.load(ks, i, smem, at, wave);
+            for (int i = 0; i < LD_A; ++i) opa.load(ks, i, smem, at, wave);
 #pragma unroll
         for (int i = 0; i < LD_B; ++i) opb.load(ks, i, smem, at + S::A_BYTES, wave);
     };
@@ -337,7 +423,7 @@ __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const Dens
 #pragma unroll
         for (int p = 0; p < PRE; ++p)
             if (k_begin + p < k_end) issue(k_begin + p, p * S::STAGE);
-        if (k_begin + PRE - 1 < k_end) WAIT_HERE(waitcnt_imm((PRE - 1) * (LD_A + LD_B), 15));
+        if (k_begin + PRE - 1 < k_end) WAIT_HERE(waitcnt_imm((PRE - 1) * ((Q8 ? 0 : LD_A) + LD_B), 15));
         else WAIT_HERE(waitcnt_imm(0, 15));
     } else {
 #pragma unroll
@@ -477,9 +563,9 @@ __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const Dens
 // D[i, j] = sum_k At[i, k] * Bt[j, k] over ksteps k-steps of 64;  At: m rows, Bt: n rows.
 //   EPI_MASKED_PACKED: out = packed gradient [n][m/2] selected by meta (u8[n][m/8])
 //   EPI_PLAIN        : out = bf16 [n][m]  (row j, four consecutive i per lane)
-template <int BM, int BN, int EPI, int NS, bool AKM, bool BKM>
+template <int BM, int BN, int EPI, int NS, bool AKM, bool BKM, class... Blocks>
 __global__ void __launch_bounds__(tn_threads(BM, BN)) dense_tn_kernel(DenseOperand At, DenseOperand Bt, int ksteps, const uint8_t* __restrict__ meta,
-                                                              bf16_t* __restrict__ out, int tiles_m, int tiles_n) {
+                                                              bf16_t* __restrict__ out, int tiles_m, int tiles_n, Blocks... x) {
     using S = TnSmem<BM, BN, NS>;
     constexpr int MULT = tn_mult(BM, BN), MF = BM / 32, NF = BN / (8 * MULT);
     extern __shared__ __align__(16) uint8_t smem[];
@@ -490,7 +576,7 @@ __global__ void __launch_bounds__(tn_threads(BM, BN)) dense_tn_kernel(DenseOpera
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), mw = m0 + (wave & 1) * (BM / 2), nw = n0 + (wave >> 1) * (BN / (MULT / 2));
     const int m = At.rows, n = Bt.rows;
     f32x4 acc[MF][NF];
-    if (!dense_tn_sums<BM, BN, NS, AKM, BKM>(At, Bt, ksteps, 0, ksteps, m0, n0, smem, acc)) return;
+    if (!dense_tn_sums<BM, BN, NS, AKM, BKM>(At, Bt, ksteps, 0, ksteps, m0, n0, smem, acc, x...)) return;
     if constexpr (EPI == EPI_PLAIN) {
         static_assert(BN * (BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the ring");
         store_rows<MF, NF, BM, BN, 64 * MULT>(acc, mw, nw, m, n, l16, lq, out, smem, m0, n0);
@@ -816,15 +902,16 @@ __global__ void __launch_bounds__(TN_THREADS) tail_finish_kernel(const f32x4* __
     }
 }
 
-template <int BM, int BN, int EPI, int NS, bool AKM, bool BKM>
-hipError_t launch_dense_tn(const DenseOperand& A, const DenseOperand& B, int64_t ksteps, const uint8_t* meta, bf16_t* out, hipStream_t s) {
+template <int BM, int BN, int EPI, int NS, bool AKM, bool BKM, class... Blocks>
+hipError_t launch_dense_tn(const DenseOperand& A, const DenseOperand& B, int64_t ksteps, const uint8_t* meta, bf16_t* out, hipStream_t s,
+                           const Blocks&... x) {
     using S = TnSmem<BM, BN, NS>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     const int tiles_m = (A.rows + BM - 1) / BM, tiles_n = (B.rows + BN - 1) / BN;
-    hipError_t e = allow_dynamic_lds<dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM>>(S::TOTAL);
+    hipError_t e = allow_dynamic_lds<dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM, Blocks...>>(S::TOTAL);
     if (e != hipSuccess) return e;
-    dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM><<<dim3((unsigned)super_grid(tiles_m, tiles_n)), dim3(tn_threads(BM, BN)), S::TOTAL, s>>>(
-        A, B, (int)ksteps, meta, out, tiles_m, tiles_n);
+    dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM, Blocks...><<<dim3((unsigned)super_grid(tiles_m, tiles_n)), dim3(tn_threads(BM, BN)), S::TOTAL, s>>>(
+        A, B, (int)ksteps, meta, out, tiles_m, tiles_n, x...);
     return hipGetLastError();
 }
 
@@ -1005,6 +1092,23 @@ static hipError_t launch_dense_tile(int tile, const DenseOperand& A, const Dense
     }
 }
 
+// Tiles whose loading wavefronts restore X on its way to LDS.  They take up to 18 % longer than from bf16, a launch that restores it first
+// 2 us and its bytes, and 3 us of the host's.  us, from bf16 / restored first / so: 128 x 128, 2048 tokens, 2048 x 2048 23.9 / 28.1 / 27.3, 300 8.0
+// / 10.4 / 8.9; 64 x 128, 912, 1024 x 2048 9.6 / 12.9 / 11.2; 64 x 64, 1025, 1000 x 1000 9.6 / 12.1 / 10.3, 2398, 448 x 1488 14.2 / 21.6 / 15.5, 5000, 768 x
+// 768 26.1 / 31.9 / 31.1, 16384, 1024 x 1024 83.9 / 92.0 / 99.8; on 256 x 128 8192, 2560 x 2560 119 / 128 / 139.
+static bool restores_on_the_way(int tile, int64_t b, int64_t d_in, int64_t d_out) {
+    return tn_loaders(DENSE_TILES[tile].bm, DENSE_TILES[tile].bn) != 0 && 0.2 * dense_tile_us(tile, d_in, d_out, (b + 63) / 64) < 4.0 + 3.0 * (double)b * (double)d_in / 4.5e6;
+}
+static hipError_t launch_dense_tile_q8(int tile, const DenseOperand& A, const DenseOperand& B, int64_t ksteps, const uint8_t* meta, bf16_t* out,
+                                       const BlocksX& x, hipStream_t s) {
+    constexpr int EPI = EPI_MASKED_PACKED;
+    if (tile == 3) return launch_dense_tn<256, 128, EPI, 3, true, true>(A, B, ksteps, meta, out, s, x);
+    if (tile == 4) return launch_dense_tn<192, 128, EPI, 4, true, true>(A, B, ksteps, meta, out, s, x);
+    if (tile == 5) return launch_dense_tn<128, 128, EPI, 4, true, true>(A, B, ksteps, meta, out, s, x);
+    if (tile == 6) return launch_dense_tn<64, 128, EPI, 6, true, true>(A, B, ksteps, meta, out, s, x);
+    return launch_dense_tn<64, 64, EPI, 8, true, true>(A, B, ksteps, meta, out, s, x);
+}
+
 // Scratch bytes of launch_wgrad_masked_t's tail pass, 0 where it does not cut: where the estimate above takes whole tiles, of
 // this or another shape (1153 tokens, 5120 x 4096: 78 us cut, 58 on 256 x 192; 1640, 19840 x 1000: 89 cut, 80 whole), and where a rule of fewest rounds x
 // rows among four of the tiles would not cut, which is as much scratch as this call ever asks for: programs keep buffers.
@@ -1079,15 +1183,18 @@ hipError_t launch_wgrad_masked(const bf16_t* dY, const bf16_t* X, int64_t b, con
     }
 }
 
-// The same product from X in 8-bit blocks.  Small ones are one launch that restores X on its way (launch_wgrad_groups_q8); else X is restored
-// first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
+// The same product from X in 8-bit blocks.  Small ones are one launch that restores X on its way (launch_wgrad_groups_q8, restores_on_the_way); else X
+// is restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
 // others, and layers that go elsewhere, X as stored.  Either form of X is in Xt.
 hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s) {
     if (wgrad_q8_in_groups(b, d_in, d_out)) return launch_wgrad_groups_q8(dY, q, bytes, b, meta, d_out, d_in, gvals, s);
     const int64_t bp = (b + 63) / 64 * 64, ld = token_pitch(bp);
-    const bool tiles = !too_wide(d_in, d_out) && !wgrad_in_groups(b, d_in, d_out) && d_in % 32 == 0;
-    if (!tiles || (!tail_or_null && dense_tile_choice(d_in, d_out, bp / 64, gradient_operands(b, d_in, d_out)) != 0)) {
+    const bool tiles = !too_wide(d_in, d_out) && !wgrad_in_groups(b, d_in, d_out);
+    const int tile = tail_or_null ? 0 : dense_tile_choice(d_in, d_out, bp / 64, gradient_operands(b, d_in, d_out));
+    if (tiles && restores_on_the_way(tile, b, d_in, d_out))
+        return launch_dense_tile_q8(tile, {nullptr, (int)d_in, (int)d_in, (int)b}, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, {q, bytes}, s);
+    if (!tiles || tile != 0 || d_in % 32 != 0) {
         const hipError_t e = launch_restore_q8(q, bytes, b, d_in, Xt, s);
         return e != hipSuccess ? e : launch_wgrad_masked(dY, Xt, b, meta, d_out, d_in, gvals, nullptr, nullptr, tail_or_null, s);
     }

@@ -389,12 +389,16 @@ def test_weight_gradient(b, d_out, d_in):
     check_product(sl.bf16_to_host(out), so.wgrad_masked(t["dY"], xb, meta), "dW")
 
 
-# X restored on the way, as stored, token-contiguous; dY's copy; tiles cut along the tokens; layers whose rows are no multiple of 32
-FORMS = [(1024, 1000, 1000, ["wgrad_groups_kernel"]), (512, 2264, 696, ["wgrad_groups_kernel"]), (513, 2264, 696, ["restore_kernel", "dense_tn_kernel"]),
-         (1025, 1000, 1000, ["restore_kernel", "dense_tn_kernel"]), (2048, 5120, 5120, ["restore_transposed_kernel", "dense_tn_split_kernel"]),
-         (999, 4096, 16384, ["restore_transposed_kernel", "transpose_pad_kernel", "dense_tn_split_kernel"]),
-         (1033, 9216, 9216, ["restore_transposed_kernel", "dense_tn_split_kernel", "dense_tn_split_kernel", "tail_finish_kernel"]),
-         (1024, 4096, 16640, ["restore_transposed_kernel", "transpose_pad_kernel", "dense_tn_split_kernel", "dense_tn_split_kernel", "tail_finish_kernel"])]
+# X restored on the way by groups of wavefronts, by those of a tile that load; first, as stored, token-contiguous; dY's copy; tiles cut along the
+# tokens; layers whose rows are no multiple of 32
+FORMS = [(1024, 1000, 1000, ["wgrad_groups"]), (512, 2264, 696, ["wgrad_groups"]), (513, 2264, 696, ["dense_tn 64 128"]), (912, 1024, 2048, ["dense_tn 64 128"]),
+         (1025, 1000, 1000, ["dense_tn 64 64"]), (1500, 200, 2200, ["dense_tn 64 64"]), (300, 2048, 2048, ["dense_tn 128 128"]), (1100, 1032, 1992, ["dense_tn 128 128"]),
+         (65, 2048, 2040, ["dense_tn 128 128"]), (33, 4160, 1032, ["dense_tn 192 128"]), (130, 2560, 2568, ["dense_tn 256 128"]), (16384, 1024, 1024, ["restore", "dense_tn 64 64"]), (2047, 2040, 2056, ["dense_tn 192 128"]),
+         (700, 4160, 2112, ["restore", "dense_tn 192 192"]), (8192, 2560, 2568, ["restore", "dense_tn 256 128"]),
+         (2048, 5120, 5120, ["restore_transposed", "dense_tn_split"]),
+         (999, 4096, 16384, ["restore_transposed", "transpose_pad", "dense_tn_split"]),
+         (1033, 9216, 9216, ["restore_transposed", "dense_tn_split", "dense_tn_split", "tail_finish"]),
+         (1024, 4096, 16640, ["restore_transposed", "transpose_pad", "dense_tn_split", "dense_tn_split", "tail_finish"])]
 
 
 @pytest.mark.parametrize("b,d_out,d_in,names", FORMS)
@@ -408,7 +412,8 @@ def test_weight_gradient_of_every_form(b, d_out, d_in, names):
     q, scale = sl.slope_checkpoint_q8(x)
     ws = torch.empty(sl.slope_workspace_bytes(sl.SLOPE_CALL_WGRAD_MASKED_Q8, b, d_in, d_out), dtype=torch.uint8, device="cuda")
     out = torch.zeros(d_out, d_in // 2, dtype=sl.BF16, device="cuda")
-    assert [k[0] for k in kernels(lambda: sl.slope_wgrad_masked_q8(dy, q, scale, meta, out=out, workspace=ws))] == names
+    ran = kernels(lambda: sl.slope_wgrad_masked_q8(dy, q, scale, meta, out=out, workspace=ws))
+    assert [k.replace("_kernel", "") + (" %d %d" % n[:2] if k == "dense_tn_kernel" else "") for k, n in ran] == names
     sl.slope_wgrad_masked_q8(dy, q, scale, meta, out=out, workspace=ws)
     rows = torch.randperm(d_out, generator=torch.Generator().manual_seed(1))[:96].sort().values.cuda()
     want = dy[:, rows].double().t().contiguous() @ sl.slope_restore_q8(q, scale).double()

@@ -436,7 +436,8 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
  * positions, X = code * scale.
  *   dY in bf16[b, d_out]    Xq in e4m3[b, d_in], x_scale in u8[b, (d_in + 31) / 32]    Wr_meta in u8[d_out, d_in/8]
  *   dW_vals out bf16[d_out, d_in/2]; fp32 accumulation
- *   workspace  slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) bytes, 256-byte aligned, required
+ *   workspace_or_null  slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) bytes, 256-byte aligned; NULL where that is 0, as for layers
+ *              of up to some thousand rows, for which X is restored on its way into the product
  */
 #define SLOPE_CHECKPOINT_BLOCK 32
 size_t slope_checkpoint_scale_bytes(int64_t rows, int64_t d);
@@ -444,7 +445,7 @@ slope_status slope_checkpoint_q8(const void* X, int64_t rows, int64_t d, void* Q
 slope_status slope_restore_q8(const void* Q, const void* scale, int64_t rows, int64_t d, void* X, void* stream);
 size_t slope_wgrad_masked_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out);
 slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x_scale, int64_t b, const void* Wr_meta, int64_t d_out,
-                                   int64_t d_in, void* dW_vals, void* workspace, size_t workspace_bytes, void* stream);
+                                   int64_t d_in, void* dW_vals, void* workspace_or_null, size_t workspace_bytes, void* stream);
 
 /*
  * slope_gated_fwd - both projections of a gated feed-forward layer, the activation and the product, from one packed weight of

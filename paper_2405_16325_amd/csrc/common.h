@@ -184,7 +184,9 @@ hipError_t launch_restore_q8(const uint8_t* q, const uint8_t* bytes, int64_t row
 bool wgrad_q8_in_groups(int64_t b, int64_t d_in, int64_t d_out);
 hipError_t launch_wgrad_groups_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, hipStream_t s);
-// dW as launch_wgrad_masked from X in 8-bit blocks; Xt, dYt, tail: required, as for slope_wgrad_masked_ws
+// dW as launch_wgrad_masked from X in 8-bit blocks; Xt, dYt, tail: the bytes of wgrad_q8_room
+struct Q8Room { size_t x, dy, tail; };
+Q8Room wgrad_q8_room(int64_t b, int64_t d_in, int64_t d_out);
 hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s);
 

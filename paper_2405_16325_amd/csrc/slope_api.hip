@@ -785,22 +785,26 @@ slope_status slope_restore_q8(const void* Q, const void* scale, int64_t rows, in
 }
 
 size_t slope_wgrad_masked_q8_workspace_bytes(int64_t b, int64_t d_in, int64_t d_out) {
-    return bad_layer(b, d_out, d_in) ? 0 : slope_wgrad_workspace_bytes(b, d_in, d_out);
+    if (bad_layer(b, d_out, d_in)) return 0;
+    const Q8Room room = wgrad_q8_room(b, d_in, d_out);
+    return round256(room.x) + round256(room.dy) + room.tail;
 }
 
 slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x_scale, int64_t b, const void* Wr_meta, int64_t d_out,
-                                   int64_t d_in, void* dW_vals, void* workspace, size_t workspace_bytes, void* stream) {
-    if (!dY || !Xq || !x_scale || !Wr_meta || !dW_vals || !workspace) return SLOPE_ERR_NULL;
+                                   int64_t d_in, void* dW_vals, void* workspace_or_null, size_t workspace_bytes, void* stream) {
+    if (!dY || !Xq || !x_scale || !Wr_meta || !dW_vals) return SLOPE_ERR_NULL;
     if (bad_layer(b, d_out, d_in) || bad_blocks(b, d_in)) return SLOPE_ERR_SHAPE;
     if (misaligned(dY, 16) || misaligned(Xq, 16) || misaligned(x_scale, 16) || misaligned(Wr_meta, 16) || misaligned(dW_vals, 16) ||
-        misaligned(workspace, 256))
+        misaligned(workspace_or_null, 256))
         return SLOPE_ERR_ALIGN;
-    if (workspace_bytes < slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out)) return SLOPE_ERR_WORKSPACE;
-    uint8_t* const ws = (uint8_t*)workspace;
-    const size_t x_bytes = slope_token_copy_bytes(b, d_in), dy_bytes = slope_token_copy_bytes(b, d_out);
-    float* const tail = slope_wgrad_t_workspace_bytes(b, d_in, d_out) ? (float*)(ws + x_bytes + dy_bytes) : nullptr;
+    const Q8Room room = wgrad_q8_room(b, d_in, d_out);
+    const size_t x_bytes = round256(room.x), dy_bytes = round256(room.dy), need = x_bytes + dy_bytes + room.tail;
+    if (need && !workspace_or_null) return SLOPE_ERR_NULL;
+    if (workspace_bytes < need) return SLOPE_ERR_WORKSPACE;
+    uint8_t* const ws = (uint8_t*)workspace_or_null;
     return finish(launch_wgrad_masked_q8((const bf16_t*)dY, (const uint8_t*)Xq, (const uint8_t*)x_scale, b, (const uint8_t*)Wr_meta, d_out,
-                                         d_in, (bf16_t*)dW_vals, (bf16_t*)ws, (bf16_t*)(ws + x_bytes), tail, (hipStream_t)stream));
+                                         d_in, (bf16_t*)dW_vals, (bf16_t*)ws, (bf16_t*)(ws + x_bytes),
+                                         room.tail ? (float*)(ws + x_bytes + dy_bytes) : nullptr, (hipStream_t)stream));
 }
 
 slope_status slope_spmm_fwd_plan(int64_t b, int64_t d_in, int64_t d_out, int64_t r, int with_workspace, int32_t* plan) {

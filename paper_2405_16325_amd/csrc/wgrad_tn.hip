@@ -1183,18 +1183,36 @@ hipError_t launch_wgrad_masked(const bf16_t* dY, const bf16_t* X, int64_t b, con
     }
 }
 
+// How the gradient of a layer with X in 8-bit blocks runs: X restored on the way by groups of wavefronts or by those of a tile that load, or first,
+// token-contiguous (with a copy of dY) or as stored.
+struct Q8Form { bool groups, direct, transposed, copy_dy; int tile; };
+static Q8Form q8_form(int64_t b, int64_t d_in, int64_t d_out) {
+    Q8Form f = {wgrad_q8_in_groups(b, d_in, d_out), false, false, false, 0};
+    if (f.groups || too_wide(d_in, d_out) || wgrad_in_groups(b, d_in, d_out)) return f;
+    f.tile = wgrad_tail_bytes(b, d_in, d_out) && wgrad_tn_fits(d_in) ? 0 : dense_tile_choice(d_in, d_out, (b + 63) / 64, gradient_operands(b, d_in, d_out));
+    f.direct = restores_on_the_way(f.tile, b, d_in, d_out);
+    f.transposed = f.tile == 0 && d_in % 32 == 0;
+    f.copy_dy = f.transposed && wgrad_copies_dy(d_in, d_out);
+    return f;
+}
+Q8Room wgrad_q8_room(int64_t b, int64_t d_in, int64_t d_out) {
+    const Q8Form f = q8_form(b, d_in, d_out);
+    if (f.groups || f.direct) return {0, 0, 0};
+    return {token_copy_bytes(b, d_in), f.copy_dy ? token_copy_bytes(b, d_out) : 0, wgrad_tn_fits(d_in) ? wgrad_tail_bytes(b, d_in, d_out) : 0};
+}
+
 // The same product from X in 8-bit blocks.  Small ones are one launch that restores X on its way (launch_wgrad_groups_q8, restores_on_the_way); else X
-// is restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and which is written as fast as the other, and dY's copy where that pays then; all
-// others, and layers that go elsewhere, X as stored.  Either form of X is in Xt.
+// is restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and
+// which is written as fast as the other, and dY's copy where that pays then; all others, and layers that go elsewhere, X as stored.  Either form of
+// X is in Xt.
 hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint8_t* bytes, int64_t b, const uint8_t* meta, int64_t d_out,
                                   int64_t d_in, bf16_t* gvals, bf16_t* Xt, bf16_t* dYt, float* tail_or_null, hipStream_t s) {
-    if (wgrad_q8_in_groups(b, d_in, d_out)) return launch_wgrad_groups_q8(dY, q, bytes, b, meta, d_out, d_in, gvals, s);
+    const Q8Form form = q8_form(b, d_in, d_out);
     const int64_t bp = (b + 63) / 64 * 64, ld = token_pitch(bp);
-    const bool tiles = !too_wide(d_in, d_out) && !wgrad_in_groups(b, d_in, d_out);
-    const int tile = tail_or_null ? 0 : dense_tile_choice(d_in, d_out, bp / 64, gradient_operands(b, d_in, d_out));
-    if (tiles && restores_on_the_way(tile, b, d_in, d_out))
-        return launch_dense_tile_q8(tile, {nullptr, (int)d_in, (int)d_in, (int)b}, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, {q, bytes}, s);
-    if (!tiles || tile != 0 || d_in % 32 != 0) {
+    if (form.groups) return launch_wgrad_groups_q8(dY, q, bytes, b, meta, d_out, d_in, gvals, s);
+    if (form.direct)
+        return launch_dense_tile_q8(form.tile, {nullptr, (int)d_in, (int)d_in, (int)b}, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, {q, bytes}, s);
+    if (!form.transposed) {
         const hipError_t e = launch_restore_q8(q, bytes, b, d_in, Xt, s);
         return e != hipSuccess ? e : launch_wgrad_masked(dY, Xt, b, meta, d_out, d_in, gvals, nullptr, nullptr, tail_or_null, s);
     }
@@ -1204,7 +1222,7 @@ hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint
     if (e != hipSuccess) return e;
     const DenseOperand x = {Xt, (int)d_in, (int)ld, (int)bp};
     constexpr int EPI = EPI_MASKED_PACKED;
-    if (!wgrad_copies_dy(d_in, d_out))
+    if (!form.copy_dy)
         return launch_dense_tn_split<EPI, false, true>(x, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, s, tail_or_null);
     e = launch_transposes(transpose_job(dY, b, d_out, bp, ld, dYt), TransposeJob{}, s);
     if (e != hipSuccess) return e;

@@ -423,12 +423,16 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
 /*
  * ---- the gated feed-forward layer, and activations kept in 8 bits ----
  *
+ * No output may overlap an input or another output but where that is said.  Workspaces hold nothing from one call to the next: calls
+ * that run one behind the other may share one, captured ones too.
+ *
  * slope_checkpoint_q8 - an activation in 8 bits for the backward pass: e4m3 codes and, for each 32 neighbouring elements of a row (a
  * row's last block may be shorter), the exponent of a power of two in a byte:
  *     scale = the smallest power of two, 2^-126 or more, with max |x| <= 448 scale        code = x / scale rounded to nearest even
  *     byte = log2(scale) + 127; 255: the block holds an infinity or NaN, and all of it reads as NaN
- * (under the largest scale, 2^120, magnitudes stop at 240 scale: the next one, 2^128, is not a bf16 number).  What a code stands for, code * scale, is a bf16 number (down to bf16's smallest one), so that a restored activation is exact and products
- * with it lose nothing more.  It is off from x by at most 2^-4 |x|, or 2^-10 scale where |x| < 2^-6 scale.
+ * (under the largest scale, 2^120, magnitudes stop at 240 scale: the next one, 2^128, is not a bf16 number).  What a code stands
+ * for, code * scale, is a bf16 number (down to bf16's smallest one), so that a restored activation is exact and products with it
+ * lose nothing more.  It is off from x by at most 2^-4 |x|, or 2^-10 scale where |x| < 2^-6 scale.
  *   X in bf16[rows, d], d % 8 == 0    Q out e4m3[rows, d]    scale out u8[rows, (d + 31) / 32], slope_checkpoint_scale_bytes(rows, d) bytes
  * slope_restore_q8 - back: X = code * scale, bf16[rows, d].
  *

@@ -675,9 +675,9 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
                              const void* L_or_null, const void* R_or_null, int64_t r, void* H, void* GU_or_null, void* GUq_or_null,
                              void* GU_scale_or_null, void* workspace_or_null, size_t workspace_bytes, void* stream) {
     if (!GUq_or_null != !GU_scale_or_null) return SLOPE_ERR_NULL;
-    const slope_status st = spmm_fwd_check(X, b, Wr_vals, Wr_meta, 2 * d_ff, d_in, L_or_null, R_or_null, r, H);
+    const bool shape = !bad_gated(b, d_ff);
+    const slope_status st = spmm_fwd_check(X, b, Wr_vals, Wr_meta, shape ? 2 * d_ff : 0, d_in, L_or_null, R_or_null, r, H);
     if (st != SLOPE_OK) return st;
-    if (bad_gated(b, d_ff)) return SLOPE_ERR_SHAPE;
     if (bad_act(act)) return SLOPE_ERR_VALUE;
     if (misaligned(GU_or_null, 16) || misaligned(GUq_or_null, 16) || misaligned(GU_scale_or_null, 16) || misaligned(workspace_or_null, 256))
         return SLOPE_ERR_ALIGN;
@@ -723,7 +723,7 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
 
 slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept, int with_workspace, int32_t* plan) {
     if (!plan) return SLOPE_ERR_NULL;
-    if (bad_layer(b, 2 * d_ff, d_in) || bad_gated(b, d_ff) || r < 0) return SLOPE_ERR_SHAPE;
+    if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return SLOPE_ERR_SHAPE;
     if (r > 0 && bad_rank(r)) return SLOPE_ERR_UNSUPPORTED;
     if (kept != 0 && kept != 8 && kept != 16) return SLOPE_ERR_VALUE;
     for (int i = 0; i < 6; ++i) plan[i] = 0;
@@ -757,7 +757,7 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
 slope_status slope_gated_bwd(const void* dH, const void* GU_or_null, const void* GUq_or_null, const void* GU_scale_or_null, int64_t b,
                              int64_t d_ff, int act, void* dGU, void* H_or_null, void* stream) {
     if (!dH || !dGU || (!GU_or_null && (!GUq_or_null || !GU_scale_or_null))) return SLOPE_ERR_NULL;
-    if (bad_gated(b, d_ff)) return SLOPE_ERR_SHAPE;
+    if (bad_gated(b, d_ff) || bad_blocks(b, d_ff)) return SLOPE_ERR_SHAPE;
     if (bad_act(act)) return SLOPE_ERR_VALUE;
     if (misaligned(dH, 16) || misaligned(GU_or_null, 16) || misaligned(dGU, 16) || misaligned(H_or_null, 16) ||
         (!GU_or_null && (misaligned(GUq_or_null, 16) || misaligned(GU_scale_or_null, 16))))

@@ -854,8 +854,7 @@ template <class... Gate>
 static hipError_t launch_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t m, int64_t K,
                                 const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
                                 const StreamXl& xl, hipStream_t s, const Gate&... gate) {
-    if (slices > 0)
-    {
+    if (slices > 0) {
         if constexpr (sizeof...(Gate) > 0)
             if (gated_rows_of_64(n, m, K, slices)) return launch_rows<1, 4>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
         return n <= 16 ? launch_rows<1, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...)

@@ -31,7 +31,7 @@ WGRAD = dict(dy=P, q=P, scale=P, b=700, meta=P, d_out=4160, d_in=2112, dw=P, ws=
     (dict(x=None), NULL), (dict(vals=None), NULL), (dict(meta=None), NULL), (dict(h=None), NULL), (dict(q=None), NULL),
     (dict(scale=None), NULL), (dict(l=None), NULL), (dict(r_=None), NULL), (dict(ws=None), NULL),
     (dict(b=0), SHAPE), (dict(b=1 << 31), SHAPE), (dict(d_ff=0), SHAPE), (dict(d_ff=-8), SHAPE), (dict(d_ff=12), SHAPE),
-    (dict(d_ff=(1 << 22) + 8), SHAPE), (dict(d_in=4), SHAPE), (dict(d_in=1 << 31), SHAPE), (dict(r=-32), SHAPE),
+    (dict(d_ff=(1 << 22) + 8), SHAPE), (dict(d_ff=(1 << 62) + 64), SHAPE), (dict(d_in=4), SHAPE), (dict(d_in=1 << 31), SHAPE), (dict(r=-32), SHAPE),
     (dict(r=33), sl.SLOPE_ERR_UNSUPPORTED), (dict(r=544), sl.SLOPE_ERR_UNSUPPORTED), (dict(act=3), VALUE), (dict(act=-1), VALUE),
     (dict(x=ODD), ALIGN), (dict(h=ODD), ALIGN), (dict(gu=ODD), ALIGN), (dict(q=ODD), ALIGN), (dict(scale=ODD), ALIGN),
     (dict(ws=ODD16), ALIGN), (dict(ws_bytes=0), sl.SLOPE_ERR_WORKSPACE)])
@@ -41,7 +41,7 @@ def test_forward_refusals(changed, status):
 
 @pytest.mark.parametrize("changed,status", [
     (dict(dh=None), NULL), (dict(dgu=None), NULL), (dict(gu=None, q=None), NULL), (dict(gu=None, scale=None), NULL), (dict(b=0), SHAPE),
-    (dict(d_ff=12), SHAPE), (dict(d_ff=(1 << 22) + 8), SHAPE), (dict(act=7), VALUE), (dict(dh=ODD), ALIGN), (dict(gu=ODD), ALIGN),
+    (dict(d_ff=12), SHAPE), (dict(d_ff=(1 << 22) + 8), SHAPE), (dict(b=(1 << 31) - 1, d_ff=1 << 22), SHAPE), (dict(act=7), VALUE), (dict(dh=ODD), ALIGN), (dict(gu=ODD), ALIGN),
     (dict(gu=None, q=ODD), ALIGN), (dict(h=ODD), ALIGN), (dict(dgu=ODD), ALIGN)])
 def test_gradient_refusals(changed, status):
     assert call("slope_gated_bwd", BWD, **changed) == status

@@ -475,6 +475,72 @@ def test_captured_and_replayed_with_new_inputs_between_eager_calls():
                 assert torch.equal(a, e)
 
 
+# ------------------------------------------------------------------------------------------------- offsets that pass 32 bits
+def far_rows(b):
+    """Rows at both ends and on both sides of the middle ones."""
+    return torch.cat([torch.arange(0, 40), torch.arange(b // 2 - 20, b // 2 + 20), torch.arange(b - 40, b)]).cuda()
+
+
+def test_checkpoints_and_gradient_of_more_than_two_to_the_32_elements():
+    say("more than 2^32 elements")
+    rows, d = 560_008, 8200                                                 # 4.6e9
+    x = torch.randn(4099, d, device="cuda").to(sl.BF16).repeat(rows // 4099 + 1, 1)[:rows].contiguous()
+    q, scale = sl.slope_checkpoint_q8(x)
+    back = sl.slope_restore_q8(q, scale)
+    at = far_rows(rows)
+    q1, s1 = sl.slope_checkpoint_q8(x[at].contiguous())
+    assert torch.equal(codes(q)[at], codes(q1)) and torch.equal(scale[at], s1) and torch.equal(back[at], sl.slope_restore_q8(q1, s1))
+    del back
+    b, d_ff = rows // 2, d                                                  # the rows as a gate and an up projection each
+    dh = torch.randn(4099, d_ff, device="cuda").to(sl.BF16).repeat(b // 4099 + 1, 1)[:b].contiguous()
+    at = far_rows(b)
+    pairs = lambda t: t.view(b, -1)[at].contiguous()                        # noqa: E731
+    dgu, h = sl.slope_gated_bwd(dh, gu=x.view(b, 2 * d_ff))
+    dgu1, h1 = sl.slope_gated_bwd(dh[at].contiguous(), gu=pairs(x))
+    assert torch.equal(dgu[at], dgu1) and torch.equal(h[at], h1)
+    del dgu, h
+    dgu, h = sl.slope_gated_bwd(dh, q8=q.view(b, 2 * d_ff), scale=scale.view(b, 2, -1))
+    dgu1, h1 = sl.slope_gated_bwd(dh[at].contiguous(), q8=codes(q).view(b, -1)[at].contiguous().view(q.dtype).view(len(at), 2 * d_ff),
+                                  scale=pairs(scale).view(len(at), 2, -1))
+    assert torch.equal(dgu[at], dgu1) and torch.equal(h[at], h1)
+
+
+def codes(q):
+    return q.view(torch.uint8)
+
+
+@pytest.mark.parametrize("b,d_out,d_in", [(1_060_001, 64, 4160), (1_060_001, 72, 4104), (40, 64, (1 << 24) + 64)])
+def test_weight_gradient_of_long_batches_and_wide_layers(b, d_out, d_in):
+    """More than 2^32 codes, restored on the way by wavefronts that load, and a layer wider than the tiles take: as from X restored first."""
+    say(f"wgrad_masked_q8 b={b} d_out={d_out} d_in={d_in}")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    part = min(b, 4099)
+    x = torch.randn(part, d_in, generator=gen, device="cuda").to(sl.BF16)
+    q, scale = (t.repeat(b // part + 1, 1)[:b].contiguous() for t in map(codes, sl.slope_checkpoint_q8(x)))
+    dy = torch.randn(b, d_out, generator=gen, device="cuda").mul_(1e-3).to(sl.BF16)
+    _, meta, _ = sl.slope_prune_rows(torch.randn(d_out, d_in, generator=gen, device="cuda").to(sl.BF16))
+    got = sl.slope_wgrad_masked_q8(dy, q.view(torch.float8_e4m3fn), scale, meta)
+    want = sl.slope_wgrad_masked(dy, sl.slope_restore_q8(q.view(torch.float8_e4m3fn), scale), meta)
+    if d_in > 1 << 20:                                                      # (then the same kernel)
+        assert torch.equal(got, want)
+    else:
+        check_product(sl.bf16_to_host(got), f64(want), "dW")
+
+
+def test_forward_of_more_than_two_to_the_32_elements():
+    say("gated_fwd of long batches")
+    b, d_ff, d_in = 1_060_001, 2048, 128                                    # kept projections: 4.3e9
+    p = Layer(3, d_ff, d_in, 0, seed=5)
+    p.x = torch.randn(b, d_in, device="cuda").to(sl.BF16)
+    h, gu, q, scale = sl.slope_gated_fwd(p.x, p.vals, p.meta, want_gu=True, want_q8=True)
+    at = far_rows(b)
+    x, w = double(p.x[at]), dense_of(p.vals, p.meta).t().contiguous()
+    want, off = x @ w, (d_in / 2 + 8) * 2.0 ** -24 * (x.abs() @ w.abs())
+    check_h(h[at], want, off, "silu", "h")
+    check_kept(gu[at], want, off, "gu")
+    check_blocks(codes(q)[at].view(-1, d_ff), scale[at].view(2 * len(at), -1), want.view(-1, d_ff), off.view(-1, d_ff), "codes")
+
+
 def test_on_another_stream():
     p = Layer(150, 264, 640, 0, seed=4)
     want = sl.slope_gated_fwd(p.x, p.vals, p.meta)[0]

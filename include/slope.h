@@ -521,7 +521,8 @@ slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int 
  * slope_gated_fwd_plan - the same for slope_gated_fwd; kept: 0, 16 where the call keeps GU, 8 where it
  * keeps GUq.  plan: host int32[6]
  *   [0] product, [1], [2] rows of the weight, gate and up projection, and tokens per workgroup, [3] slabs, slices or the tokens of
- *       the small-batch kernel: as slope_spmm_fwd_plan
+ *       the small-batch kernel: as slope_spmm_fwd_plan; or [0] 6, tiles of that size for the last rows and, in a launch before,
+ *       256 x 256 ones for the first [3], which are whole rounds of them
  *   [4] whether the small-batch kernel computes T = X L itself
  *   [5] columns of the padded copies that the call makes of its operands (0 = none)
  */

@@ -13,7 +13,7 @@
 #include "wave.h"
 
 struct GateOut {
-    int d_ff, act;
+    int d_ff, count, act;                                     // elements of a row, those of the launch (a part starts at a multiple of 128)
     bf16_t* gu;                                               // bf16[n][2 d_ff], or null
     uint8_t *q, *bytes;                                       // e4m3[2 n][d_ff] with a scale byte per 32 of a row, or null
     float* sums;                                              // small-batch kernels: [n][2 d_ff] instead of h, or null
@@ -26,16 +26,16 @@ inline int64_t gated_rows(int64_t d_ff) { return (d_ff + GATE_GROUP - 1) / GATE_
 __device__ __forceinline__ int gated_element(int row) { return (row >> 5) * GATE_GROUP + (row & (GATE_GROUP - 1)); }
 __device__ __forceinline__ int gated_half(int row) { return row >> 4 & 1; }
 // row of the weight that is read for a virtual row; d_ff is a multiple of 8, so a group may have eight rows too many: the eight before
-__device__ __forceinline__ int gated_row(int row, int d_ff) {
+__device__ __forceinline__ int gated_row(int row, const GateOut& gate) {
     const int e = gated_element(row);
-    return (e < d_ff ? e : e - 8) + (gated_half(row) ? d_ff : 0);
+    return (e < gate.count ? e : e - 8) + (gated_half(row) ? gate.d_ff : 0);
 }
 
 // The weight's row for row `row` of a tile, of a plain product (no gate) and of a gated one
 __device__ __forceinline__ int weight_row(int row, int m) { return wrap_row(row, m); }
-__device__ __forceinline__ int weight_row(int row, int m, const GateOut& gate) { return gated_row(wrap_row(row, m), gate.d_ff); }
+__device__ __forceinline__ int weight_row(int row, int m, const GateOut& gate) { return gated_row(wrap_row(row, m), gate); }
 __device__ __forceinline__ int weight_row_near(int row, int m) { return wrap_row_near(row, m); }
-__device__ __forceinline__ int weight_row_near(int row, int m, const GateOut& gate) { return gated_row(wrap_row_near(row, m), gate.d_ff); }
+__device__ __forceinline__ int weight_row_near(int row, int m, const GateOut& gate) { return gated_row(wrap_row_near(row, m), gate); }
 
 // ---- activations.  sigmoid by the hardware's exponential and reciprocal (each within 1 ulp; the exponent's rounding adds |x| 2^-24):
 // results are rounded to bf16 or multiplied by what was.
@@ -125,7 +125,7 @@ __device__ __forceinline__ F8 unpack_e4m3(u32x2 codes, float scale) {
 }
 
 // ---- results.  Four elements e .. e + 3 of token `tok` from their sums; eight neighbouring lanes have a block of 32 of a token (all of
-// them make the call, elements from d_ff on being none).
+// them make the call, elements from the launch's last on being none).
 __device__ __forceinline__ uint32_t four_codes(const f32x4& v, const BlockScale& s) {
     return pack_e4m3x4(s.scaled(v[0]), s.scaled(v[1]), s.scaled(v[2]), s.scaled(v[3]));
 }
@@ -142,7 +142,7 @@ __device__ __forceinline__ uint32_t top_of(const f32x4& v) {
     return __float_as_uint(top);
 }
 __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int tok, int e, int n, bf16_t* __restrict__ H, const GateOut& gate) {
-    const bool has = tok < n && e < gate.d_ff;
+    const bool has = tok < n && e < gate.count;
     const size_t at = (size_t)tok * gate.d_ff + e;
     f32x4 h;
     with_act(gate.act, [&](auto act) {
@@ -156,8 +156,8 @@ __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int
         *(u32x2*)(row + gate.d_ff) = four_bf16(u);
     }
     if (gate.q) {
-        const BlockScale sg = block_scale(lanes_reduce<8>(e < gate.d_ff ? top_of(g) : 0u, MaxBits()));
-        const BlockScale su = block_scale(lanes_reduce<8>(e < gate.d_ff ? top_of(u) : 0u, MaxBits()));
+        const BlockScale sg = block_scale(lanes_reduce<8>(e < gate.count ? top_of(g) : 0u, MaxBits()));
+        const BlockScale su = block_scale(lanes_reduce<8>(e < gate.count ? top_of(u) : 0u, MaxBits()));
         if (!has) return;
         uint8_t* const row = gate.q + (size_t)tok * (2 * (size_t)gate.d_ff) + e;
         *(uint32_t*)row = four_codes(g, sg);
@@ -197,7 +197,7 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
     static_assert(MF % 2 == 0, "pairs of fragments");
     constexpr int HALF = BMT / 2;                             // elements of h in the tile
     constexpr int CODES = BNT * (BMT + 16);                   // where the codes are staged, behind h
-    const int tile_e0 = tile_f0 / 2, e0 = f0 / 2, d_ff = gate.d_ff;
+    const int tile_e0 = tile_f0 / 2, e0 = f0 / 2, d_ff = gate.d_ff, count = gate.count;
     const int le = e0 - tile_e0 + lq * 4, lt = t0 - tile_t0 + l16;        // the lane's first element and token inside the tile
     // rows of BYTES bytes per token at `from` in LDS, piece by piece of 16 bytes, to to(token, piece, its bytes)
     auto leave = [&](auto bytes, const uint8_t* from, auto to) {
@@ -238,20 +238,20 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                 for (int half = 0; half < 2; ++half) {
                     const f32x4 &a = acc[4 * c + half][j], &b = acc[4 * c + 2 + half][j];
                     const int e = e0 + c * 32;                // the block's first element
-                    uint32_t top = e + lq * 4 < d_ff ? top_of(a) : 0u;
-                    if (e + 16 + lq * 4 < d_ff) top = MaxBits()(top, top_of(b));
+                    uint32_t top = e + lq * 4 < count ? top_of(a) : 0u;
+                    if (e + 16 + lq * 4 < count) top = MaxBits()(top, top_of(b));
                     const BlockScale s = block_scale(quarters_max(top));
                     uint8_t* const at = smem + CODES + (lt + j * 16) * (BMT + 16) + half * HALF + le + c * 32;
                     *(uint32_t*)at = four_codes(a, s);
                     *(uint32_t*)(at + 16) = four_codes(b, s);
                     const int tok = t0 + j * 16 + l16;
-                    if (lq == 0 && tok < n && e < d_ff) gate.bytes[((size_t)tok * 2 + half) * blocks + e / Q8_BLOCK] = (uint8_t)s.byte;
+                    if (lq == 0 && tok < n && e < count) gate.bytes[((size_t)tok * 2 + half) * blocks + e / Q8_BLOCK] = (uint8_t)s.byte;
                 }
     }
     lds_barrier();
     leave(std::integral_constant<int, BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
         const int e = tile_e0 + p * 8;
-        if (e < d_ff) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
+        if (e < count) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
     });
     const bool large = (size_t)n * d_ff > LAST_LEVEL_CACHE_BYTES / 8;
     if constexpr (MF % 4 == 0) if (gate.q)
@@ -259,9 +259,9 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
             const int half = p * 16 / HALF, e = tile_e0 + p * 16 % HALF;
             uint8_t* const to = gate.q + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e;
             // d_ff is a multiple of 8: a row's codes may start 8 bytes off, and its last piece may be half a one
-            if (e + 8 < d_ff && large) __builtin_nontemporal_store((u32x4_a8)v, (u32x4_a8*)to);
-            else if (e + 8 < d_ff) *(u32x4_a8*)to = v;
-            else if (e < d_ff) *(u32x2*)to = (u32x2){v[0], v[1]};
+            if (e + 8 < count && large) __builtin_nontemporal_store((u32x4_a8)v, (u32x4_a8*)to);
+            else if (e + 8 < count) *(u32x4_a8*)to = v;
+            else if (e < count) *(u32x2*)to = (u32x2){v[0], v[1]};
         });
     if (gate.gu) {                                            // uniform
         lds_barrier();
@@ -273,7 +273,7 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
         lds_barrier();
         leave(std::integral_constant<int, 2 * BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
             const int half = p * 8 / HALF, e = tile_e0 + p * 8 % HALF;
-            if (e < d_ff) __builtin_nontemporal_store(v, (u32x4*)(gate.gu + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e));
+            if (e < count) __builtin_nontemporal_store(v, (u32x4*)(gate.gu + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e));
         });
     }
 }

@@ -694,7 +694,7 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     const bf16_t* const R = adapter ? (const bf16_t*)R_or_null : nullptr;
     const uint8_t* wm = (const uint8_t*)Wr_meta;
     uint8_t* const ws = (uint8_t*)workspace_or_null;
-    const GateOut gate = {(int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null, nullptr};
+    const GateOut gate = {(int)d_ff, (int)d_ff, act, (bf16_t*)GU_or_null, (uint8_t*)GUq_or_null, (uint8_t*)GU_scale_or_null, nullptr};
     const bool few = spmm_stream_fits(b, d_in) && (ws || !gate.keeps());
     // (none without a workspace, nor where the call needs no sums)
     float* const after = plan.total > plan.sums_at ? (float*)(ws + plan.sums_at) : nullptr;
@@ -751,6 +751,13 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
     else if (bm == 0) { plan[0] = 3; plan[1] = plan[2] = spmm_generic_edge(b - rest, m); }
     else { plan[0] = 2; plan[1] = bm; plan[2] = bn; }
     if (rest) { plan[0] = 5; plan[3] = (int32_t)rest; }
+    else if (const int64_t first = split.slabs ? 0 : gated_first_rows(b, m, d_in, kept == 8)) {
+        spmm_tile_choice(b, m - first, d_in, r > 0, bm, bn, kept == 8);
+        plan[0] = 6;
+        plan[1] = bm ? bm : spmm_generic_edge(b, m - first);
+        plan[2] = bm ? bn : plan[1];
+        plan[3] = (int32_t)first;
+    }
     return SLOPE_OK;
 }
 

@@ -4,7 +4,7 @@ import pytest
 from paper_2405_16325_amd import binding as sl
 from tests.test_gpu_gated import LARGE, SHAPES
 
-SMALL_BATCH, SLABS, TILE, GENERAL, ROW_SPLIT, REST = range(6)
+SMALL_BATCH, SLABS, TILE, GENERAL, ROW_SPLIT, REST, TWO_TILES = range(7)
 
 
 def plan(b, d_ff, d_in, r=0, **more):
@@ -109,6 +109,23 @@ def test_the_gpu_tests_reach_padded_copies():
             assert p["padded"] % 64 == 0 and 0 < p["padded"] - i < 64
             found.add((p["product"], r > 0))
     assert {(TILE, False), (TILE, True), (SLABS, False), (SLABS, True)} <= found
+
+
+def test_whole_rounds_of_the_largest_tiles_and_others_behind():
+    p = plan(512, 24576, 9216)
+    assert p == {"product": TWO_TILES, "rows": 256, "tokens": 128, "slabs": 32768, "xl": 0, "padded": 0}
+    assert plan(2048, 6912, 2560)["product"] == TILE
+    found = set()
+    for b, f, i, r in LARGE:
+        for kept in (0, 8, 16):
+            p = plan(b, f, i, r, kept=kept)
+            if p["product"] == TWO_TILES:
+                assert p["slabs"] % 256 == 0 and 0 < p["slabs"] < 2 * f
+                columns, rows = -(-b // 256), p["slabs"] // 256
+                assert columns * rows <= 256 * -(-columns * rows // 256) < columns * (rows + 1)      # as many as whole rounds have
+                found |= {(p["rows"], kept), ("adapter", r > 0), ("block", f % 32 == 0), ("padded", p["padded"] > 0)}
+    assert {(rows, kept) for rows in (64, 128) for kept in (0, 8, 16)} <= found and (256, 0) in found
+    assert {(what, yes) for what in ("adapter", "block", "padded") for yes in (False, True)} <= found
 
 
 def test_tiles_left_over_after_whole_rounds():

@@ -159,7 +159,8 @@ LARGE = [(1568, 5056, 768, 32), (785, 9984, 832, 0), (35, 2600, 10048, 0), (65, 
          (34, 4584, 7424, 0), (33, 4208, 7616, 32), (131, 2880, 5120, 32), (133, 2752, 4672, 0), (5526, 136, 128, 32), (145, 5480, 192, 0),
          (195, 5568, 128, 32), (198, 6248, 192, 0), (259, 5504, 256, 160), (258, 5576, 128, 0), (654, 5384, 256, 32), (522, 6592, 128, 0),
          (783, 6696, 256, 0), (770, 6720, 128, 64), (131, 5448, 64, 32), (142, 5504, 8, 0), (1560, 1280, 3584, 32), (1561, 1280, 3712, 0),
-         (1026, 7232, 768, 0), (2054, 3904, 576, 64), (1024, 8320, 2048, 32), (1000, 8312, 2112, 0), (1024, 10752, 6144, 0), (1020, 10752, 6208, 32)]
+         (1026, 7232, 768, 0), (2054, 3904, 576, 64), (1024, 8320, 2048, 32), (1000, 8312, 2112, 0), (1024, 10752, 6144, 0), (1020, 10752, 6208, 32),
+         (962, 8200, 640, 32), (423, 16520, 664, 0), (435, 17696, 768, 32), (11211, 680, 768, 0), (608, 16568, 1264, 32), (8235, 968, 2048, 32), (8287, 976, 2112, 0)]
 
 
 @pytest.mark.parametrize("b,d_ff,d_in", SHAPES)

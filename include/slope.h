@@ -440,8 +440,8 @@ slope_status slope_adamw_step(const void* table, const void* device_table, doubl
  * positions, X = code * scale.
  *   dY in bf16[b, d_out]    Xq in e4m3[b, d_in], x_scale in u8[b, (d_in + 31) / 32]    Wr_meta in u8[d_out, d_in/8]
  *   dW_vals out bf16[d_out, d_in/2]; fp32 accumulation
- *   workspace_or_null  slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) bytes, 256-byte aligned; NULL where that is 0, as for layers
- *              of up to some thousand rows, for which X is restored on its way into the product
+ *   workspace_or_null  slope_wgrad_masked_q8_workspace_bytes(b, d_in, d_out) bytes, 256-byte aligned; NULL where that is 0, as for
+ *              most layers of up to some hundred rows and columns or tokens, for which X is restored on its way into the product
  */
 #define SLOPE_CHECKPOINT_BLOCK 32
 size_t slope_checkpoint_scale_bytes(int64_t rows, int64_t d);

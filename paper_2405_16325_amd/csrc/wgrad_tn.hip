@@ -126,7 +126,7 @@ constexpr int TN_LOADERS = 4;
 constexpr int tn_loaders(int bm, int bn) { return bm * bn <= 256 * 128 ? TN_LOADERS : 0; }
 constexpr int tn_mult(int bm, int bn) { return tn_loaders(bm, bn) ? 4 : 8; }
 constexpr int tn_threads(int bm, int bn) { return 64 * (tn_mult(bm, bn) + tn_loaders(bm, bn)); }
-enum { EPI_MASKED_PACKED = 0, EPI_PLAIN = 1 };
+enum { EPI_MASKED_PACKED = 0, EPI_PLAIN = 1, EPI_MASKED_SUMS = 2 };
 
 // Metadata of the 32 Q columns of W^R from c (a multiple of 32) of rows o, o + 16, .. of N, by dwords; columns outside the matrix: any.  The
 // dwords of rows that are not a multiple of 32 columns may lie at any byte, and the last of such a row, which ends inside it, is read by
@@ -222,6 +222,28 @@ __device__ __forceinline__ void store_masked_packed(const f32x4 (&acc)[MF][NF], 
         const int idx = (int)threadIdx.x + u * THREADS;
         const int o = tile_o0 + idx / PPR, col = tile_c0 + (idx % PPR) * 16;
         if ((EVEN || idx < PIECES) && o < n && col + 8 == m) *(u32x2*)(out + (size_t)o * gpitch + (col >> 1)) = (u32x2){piece[u][0], piece[u][1]};
+    }
+}
+
+// The pairs that W^R keeps, as fp32 sums[n][m / 2] for a later reduction: two of a lane's four accumulators, eight bytes.
+template <int MF, int NF>
+__device__ __forceinline__ void store_masked_sums(const f32x4 (&acc)[MF][NF], int m, int n, int c0, int o0, int l16, int lq,
+                                                  const uint8_t* __restrict__ meta, float* __restrict__ sums) {
+    constexpr int WM = MF * 16;
+    uint32_t mw[NF][WM / 32];
+    load_meta(meta, o0 + l16, c0, m, n, mw);
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+        const int o = o0 + j * 16 + l16;
+        if (o >= n) continue;
+        float* const row = sums + (size_t)o * (m / 2);
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+            const int gl = i * 4 + lq, col = c0 + gl * 4;
+            const uint32_t nib = (mw[j][i >> 1] >> (4 * (gl & 7))) & 0xFu, a = nib & 3u, c = nib >> 2;
+            const f32x4 v = acc[i][j];
+            if (col < m) *(f32x2*)(row + col / 2) = (f32x2){a == 0 ? v[0] : (a == 1 ? v[1] : v[2]), c == 1 ? v[1] : (c == 2 ? v[2] : v[3])};
+        }
     }
 }
 
@@ -563,6 +585,11 @@ __device__ __forceinline__ bool dense_tn_sums(const DenseOperand& At, const Dens
 // D[i, j] = sum_k At[i, k] * Bt[j, k] over ksteps k-steps of 64;  At: m rows, Bt: n rows.
 //   EPI_MASKED_PACKED: out = packed gradient [n][m/2] selected by meta (u8[n][m/8])
 //   EPI_PLAIN        : out = bf16 [n][m]  (row j, four consecutive i per lane)
+//   EPI_MASKED_SUMS  : of a slab of the contraction (BlockSlabs), fp32 [slab][n][m/2].  Workgroups go to the XCDs in equal runs, slab after slab: those
+//                      that read the same tokens share a cache, and no XCD has more of them than another (a tile's order of its own in
+//                      each slab left some with a fifth more, and a round of 252 took the time of two)
+struct BlockSlabs : BlocksX { int slabs, steps; float* sums; };
+__host__ __device__ __forceinline__ const BlockSlabs& slabs_of(const BlockSlabs& x) { return x; }
 template <int BM, int BN, int EPI, int NS, bool AKM, bool BKM, class... Blocks>
 __global__ void __launch_bounds__(tn_threads(BM, BN)) dense_tn_kernel(DenseOperand At, DenseOperand Bt, int ksteps, const uint8_t* __restrict__ meta,
                                                               bf16_t* __restrict__ out, int tiles_m, int tiles_n, Blocks... x) {
@@ -570,12 +597,27 @@ __global__ void __launch_bounds__(tn_threads(BM, BN)) dense_tn_kernel(DenseOpera
     constexpr int MULT = tn_mult(BM, BN), MF = BM / 32, NF = BN / (8 * MULT);
     extern __shared__ __align__(16) uint8_t smem[];
     fetch_arguments(At.p, At.rows, At.ld, At.k, Bt.p, Bt.rows, Bt.ld, Bt.k, ksteps, meta, out, tiles_m, tiles_n);
-    int tm, tn;
-    if (!tile_of_block(tiles_m, tiles_n, tm, tn)) return;
+    int tm, tn, slab = 0;
+    if constexpr (EPI == EPI_MASKED_SUMS) {
+        const int tiles = tiles_m * tiles_n, all = tiles * slabs_of(x...).slabs, run = (all + XCDS - 1) / XCDS;
+        const int w = (int)blockIdx.x % XCDS * run + (int)blockIdx.x / XCDS;
+        if (w >= all) return;
+        slab = w / tiles;
+        tn = (w - slab * tiles) / tiles_m;
+        tm = w - slab * tiles - tn * tiles_m;
+    } else if (!tile_of_block(tiles_m, tiles_n, tm, tn)) {
+        return;
+    }
     const int m0 = tm * BM, n0 = tn * BN, lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), mw = m0 + (wave & 1) * (BM / 2), nw = n0 + (wave >> 1) * (BN / (MULT / 2));
     const int m = At.rows, n = Bt.rows;
     f32x4 acc[MF][NF];
+    if constexpr (EPI == EPI_MASKED_SUMS) {
+        const int first = slab * slabs_of(x...).steps;
+        if (!dense_tn_sums<BM, BN, NS, AKM, BKM>(At, Bt, ksteps, first, min(first + slabs_of(x...).steps, ksteps), m0, n0, smem, acc, x...)) return;
+        store_masked_sums<MF, NF>(acc, m, n, mw, nw, l16, lq, meta, slabs_of(x...).sums + (size_t)slab * n * (m / 2));
+        return;
+    }
     if (!dense_tn_sums<BM, BN, NS, AKM, BKM>(At, Bt, ksteps, 0, ksteps, m0, n0, smem, acc, x...)) return;
     if constexpr (EPI == EPI_PLAIN) {
         static_assert(BN * (BM * 2 + 16) <= S::TOTAL, "the staged output tile fits in the ring");
@@ -908,9 +950,12 @@ hipError_t launch_dense_tn(const DenseOperand& A, const DenseOperand& B, int64_t
     using S = TnSmem<BM, BN, NS>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     const int tiles_m = (A.rows + BM - 1) / BM, tiles_n = (B.rows + BN - 1) / BN;
+    int grid;
+    if constexpr (EPI == EPI_MASKED_SUMS) grid = (tiles_m * tiles_n * slabs_of(x...).slabs + XCDS - 1) / XCDS * XCDS;
+    else grid = super_grid(tiles_m, tiles_n);
     hipError_t e = allow_dynamic_lds<dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM, Blocks...>>(S::TOTAL);
     if (e != hipSuccess) return e;
-    dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM, Blocks...><<<dim3((unsigned)super_grid(tiles_m, tiles_n)), dim3(tn_threads(BM, BN)), S::TOTAL, s>>>(
+    dense_tn_kernel<BM, BN, EPI, NS, AKM, BKM, Blocks...><<<dim3((unsigned)grid), dim3(tn_threads(BM, BN)), S::TOTAL, s>>>(
         A, B, (int)ksteps, meta, out, tiles_m, tiles_n, x...);
     return hipGetLastError();
 }
@@ -1092,16 +1137,20 @@ static hipError_t launch_dense_tile(int tile, const DenseOperand& A, const Dense
     }
 }
 
-// Tiles whose loading wavefronts restore X on its way to LDS.  They take up to 18 % longer than from bf16, a launch that restores it first
-// 2 us and its bytes, and 3 us of the host's.  us, from bf16 / restored first / so: 128 x 128, 2048 tokens, 2048 x 2048 23.9 / 28.1 / 27.3, 300 8.0
-// / 10.4 / 8.9; 64 x 128, 912, 1024 x 2048 9.6 / 12.9 / 11.2; 64 x 64, 1025, 1000 x 1000 9.6 / 12.1 / 10.3, 2398, 448 x 1488 14.2 / 21.6 / 15.5, 5000, 768 x
-// 768 26.1 / 31.9 / 31.1, 16384, 1024 x 1024 83.9 / 92.0 / 99.8; on 256 x 128 8192, 2560 x 2560 119 / 128 / 139.
-static bool restores_on_the_way(int tile, int64_t b, int64_t d_in, int64_t d_out) {
-    return tn_loaders(DENSE_TILES[tile].bm, DENSE_TILES[tile].bn) != 0 && 0.2 * dense_tile_us(tile, d_in, d_out, (b + 63) / 64) < 4.0 + 3.0 * (double)b * (double)d_in / 4.5e6;
+// Tiles whose loading wavefronts restore X on its way to LDS, whole or in `slabs` of the tokens, whose sums a second launch adds: rounds as
+// above, with constants fitted to 2300 products of 600 to 27000 tokens (within 7 %; the form that the estimate chooses among these takes 0.4 % longer
+// than the best one in the mean), and 1 us more for a launch of the host's.  us, restored first or whole / in slabs: 16384 tokens, 256 x 256 58.8 / 14.7, 2304 x 768
+// 147 / 85, 1024 x 1024 96 / 55; 5000, 768 x 768 29.1 / 20.6; 4096, 2040 x 280 24.0 / 19.0; 65536, 1024 x 1024 350 / 162.
+static double q8_tile_us(int c, int64_t m, int64_t n, int64_t ksteps, int64_t slabs) {
+    const int bm = DENSE_TILES[c].bm, bn = DENSE_TILES[c].bn;
+    const int64_t steps = (ksteps + slabs - 1) / slabs, tiles = ((m + bm - 1) / bm) * ((n + bn - 1) / bn) * slabs, rounds = (tiles + RESIDENT - 1) / RESIDENT;
+    const double step = (bm == bn && bm == 64 ? 1.23 : 1.13) * 128.0 * (double)(bm + bn) / 53e3, busy = (double)tiles / (double)(rounds * RESIDENT);
+    const double us = (double)rounds * (1.5 + 9.5 * (double)(bm * bn) / 65536.0 + (double)steps * step * (1.0 - 0.12 * (1.0 - busy)));
+    return slabs == 1 ? us : us + 4.0 + 1.0 + 0.09 * (double)slabs + 4.0 * (double)slabs * (double)m * (double)n / 4.7e6;
 }
+template <int EPI, class Blocks>
 static hipError_t launch_dense_tile_q8(int tile, const DenseOperand& A, const DenseOperand& B, int64_t ksteps, const uint8_t* meta, bf16_t* out,
-                                       const BlocksX& x, hipStream_t s) {
-    constexpr int EPI = EPI_MASKED_PACKED;
+                                       const Blocks& x, hipStream_t s) {
     if (tile == 3) return launch_dense_tn<256, 128, EPI, 3, true, true>(A, B, ksteps, meta, out, s, x);
     if (tile == 4) return launch_dense_tn<192, 128, EPI, 4, true, true>(A, B, ksteps, meta, out, s, x);
     if (tile == 5) return launch_dense_tn<128, 128, EPI, 4, true, true>(A, B, ksteps, meta, out, s, x);
@@ -1183,25 +1232,42 @@ hipError_t launch_wgrad_masked(const bf16_t* dY, const bf16_t* X, int64_t b, con
     }
 }
 
-// How the gradient of a layer with X in 8-bit blocks runs: X restored on the way by groups of wavefronts or by those of a tile that load, or first,
-// token-contiguous (with a copy of dY) or as stored.
-struct Q8Form { bool groups, direct, transposed, copy_dy; int tile; };
+// How the gradient of a layer with X in 8-bit blocks runs: X restored on the way by groups of wavefronts or by those of a tile that load, whole or in
+// slabs of `steps` k-steps, or first, token-contiguous (with a copy of dY) or as stored.
+struct Q8Form { bool groups, direct, transposed, copy_dy; int tile, slabs, steps; };
 static Q8Form q8_form(int64_t b, int64_t d_in, int64_t d_out) {
-    Q8Form f = {wgrad_q8_in_groups(b, d_in, d_out), false, false, false, 0};
+    Q8Form f = {wgrad_q8_in_groups(b, d_in, d_out), false, false, false, 0, 1, 0};
     if (f.groups || too_wide(d_in, d_out) || wgrad_in_groups(b, d_in, d_out)) return f;
     f.tile = wgrad_tail_bytes(b, d_in, d_out) && wgrad_tn_fits(d_in) ? 0 : dense_tile_choice(d_in, d_out, (b + 63) / 64, gradient_operands(b, d_in, d_out));
-    f.direct = restores_on_the_way(f.tile, b, d_in, d_out);
+    const int64_t ksteps = (b + 63) / 64;
+    // restored first: 2 us and its bytes
+    double least = dense_tile_us(f.tile, d_in, d_out, ksteps) + 2.0 + 3.0 * (double)b * (double)d_in / 4.5e6;
+    for (int c = 3; c < (int)(sizeof(DENSE_TILES) / sizeof(DENSE_TILES[0])); ++c) {
+        const int64_t tiles = ((d_in + DENSE_TILES[c].bm - 1) / DENSE_TILES[c].bm) * ((d_out + DENSE_TILES[c].bn - 1) / DENSE_TILES[c].bn);
+        for (int64_t fill = RESIDENT; fill >= 0; fill -= RESIDENT / 2) {
+            int64_t slabs = fill / tiles;
+            if (slabs > ksteps / 4) slabs = ksteps / 4;
+            if (slabs < 1) slabs = 1;
+            const double us = q8_tile_us(c, d_in, d_out, ksteps, slabs);
+            if (us >= least) continue;
+            least = us;
+            f.direct = true;
+            f.tile = c;
+            f.steps = (int)((ksteps + slabs - 1) / slabs);
+            f.slabs = (int)((ksteps + f.steps - 1) / f.steps);
+        }
+    }
     f.transposed = f.tile == 0 && d_in % 32 == 0;
     f.copy_dy = f.transposed && wgrad_copies_dy(d_in, d_out);
     return f;
 }
 Q8Room wgrad_q8_room(int64_t b, int64_t d_in, int64_t d_out) {
     const Q8Form f = q8_form(b, d_in, d_out);
-    if (f.groups || f.direct) return {0, 0, 0};
+    if (f.groups || f.direct) return {0, 0, f.slabs > 1 ? (size_t)f.slabs * (size_t)d_out * (size_t)d_in * 2 : 0};
     return {token_copy_bytes(b, d_in), f.copy_dy ? token_copy_bytes(b, d_out) : 0, wgrad_tn_fits(d_in) ? wgrad_tail_bytes(b, d_in, d_out) : 0};
 }
 
-// The same product from X in 8-bit blocks.  Small ones are one launch that restores X on its way (launch_wgrad_groups_q8, restores_on_the_way); else X
+// The same product from X in 8-bit blocks.  Small layers are products that restore X on its way (launch_wgrad_groups_q8, q8_tile_us); else X
 // is restored first: exactly, what a code stands for being a bf16 number.  The 256 x 256 tiles get the token-contiguous form, which they prefer and
 // which is written as fast as the other, and dY's copy where that pays then; all others, and layers that go elsewhere, X as stored.  Either form of
 // X is in Xt.
@@ -1210,8 +1276,15 @@ hipError_t launch_wgrad_masked_q8(const bf16_t* dY, const uint8_t* q, const uint
     const Q8Form form = q8_form(b, d_in, d_out);
     const int64_t bp = (b + 63) / 64 * 64, ld = token_pitch(bp);
     if (form.groups) return launch_wgrad_groups_q8(dY, q, bytes, b, meta, d_out, d_in, gvals, s);
-    if (form.direct)
-        return launch_dense_tile_q8(form.tile, {nullptr, (int)d_in, (int)d_in, (int)b}, {dY, (int)d_out, (int)d_out, (int)b}, bp / 64, meta, gvals, {q, bytes}, s);
+    if (form.direct) {
+        const DenseOperand x = {nullptr, (int)d_in, (int)d_in, (int)b}, dy = {dY, (int)d_out, (int)d_out, (int)b};
+        if (form.slabs == 1) return launch_dense_tile_q8<EPI_MASKED_PACKED>(form.tile, x, dy, bp / 64, meta, gvals, BlocksX{q, bytes}, s);
+        const hipError_t e = launch_dense_tile_q8<EPI_MASKED_SUMS>(form.tile, x, dy, bp / 64, meta, nullptr, BlockSlabs{{q, bytes}, form.slabs, form.steps, tail_or_null}, s);
+        if (e != hipSuccess) return e;
+        const int64_t count4 = d_out * (d_in / 8);
+        skinny_sum_kernel<<<dim3((unsigned)((count4 + 255) / 256)), dim3(256), 0, s>>>({(const f32x4*)tail_or_null, form.slabs, count4, (u32x2*)gvals}, {});
+        return hipGetLastError();
+    }
     if (!form.transposed) {
         const hipError_t e = launch_restore_q8(q, bytes, b, d_in, Xt, s);
         return e != hipSuccess ? e : launch_wgrad_masked(dY, Xt, b, meta, d_out, d_in, gvals, nullptr, nullptr, tail_or_null, s);

@@ -394,8 +394,11 @@ def test_weight_gradient(b, d_out, d_in):
 # tokens; layers whose rows are no multiple of 32
 FORMS = [(1024, 1000, 1000, ["wgrad_groups"]), (512, 2264, 696, ["wgrad_groups"]), (513, 2264, 696, ["dense_tn 64 128"]), (912, 1024, 2048, ["dense_tn 64 128"]),
          (1025, 1000, 1000, ["dense_tn 64 64"]), (1500, 200, 2200, ["dense_tn 64 64"]), (300, 2048, 2048, ["dense_tn 128 128"]), (1100, 1032, 1992, ["dense_tn 128 128"]),
-         (65, 2048, 2040, ["dense_tn 128 128"]), (33, 4160, 1032, ["dense_tn 192 128"]), (130, 2560, 2568, ["dense_tn 256 128"]), (16384, 1024, 1024, ["restore", "dense_tn 64 64"]), (2047, 2040, 2056, ["dense_tn 192 128"]),
+         (65, 2048, 2040, ["dense_tn 128 128"]), (33, 4160, 1032, ["dense_tn 192 128"]), (130, 2560, 2568, ["dense_tn 256 128"]), (16384, 1024, 1024, ["dense_tn 256 128", "skinny_sum"]), (2047, 2040, 2056, ["dense_tn 192 128"]),
          (700, 4160, 2112, ["restore", "dense_tn 192 192"]), (8192, 2560, 2568, ["restore", "dense_tn 256 128"]),
+         (4053, 3008, 392, ["dense_tn 256 128", "skinny_sum"]), (4854, 2704, 144, ["dense_tn 192 128", "skinny_sum"]), (3591, 136, 2112, ["dense_tn 128 128", "skinny_sum"]),
+         (2068, 2736, 72, ["dense_tn 64 128", "skinny_sum"]), (1421, 64, 64, ["dense_tn 64 64", "skinny_sum"]), (16384, 256, 256, ["dense_tn 64 64", "skinny_sum"]),
+         (1155, 3752, 2352, ["restore", "dense_tn 256 192"]),
          (2048, 5120, 5120, ["restore_transposed", "dense_tn_split"]),
          (999, 4096, 16384, ["restore_transposed", "transpose_pad", "dense_tn_split"]),
          (1033, 9216, 9216, ["restore_transposed", "dense_tn_split", "dense_tn_split", "tail_finish"]),

@@ -399,6 +399,7 @@ FORMS = [(1024, 1000, 1000, ["wgrad_groups"]), (512, 2264, 696, ["wgrad_groups"]
          (4053, 3008, 392, ["dense_tn 256 128", "skinny_sum"]), (4854, 2704, 144, ["dense_tn 192 128", "skinny_sum"]), (3591, 136, 2112, ["dense_tn 128 128", "skinny_sum"]),
          (2068, 2736, 72, ["dense_tn 64 128", "skinny_sum"]), (1421, 64, 64, ["dense_tn 64 64", "skinny_sum"]), (16384, 256, 256, ["dense_tn 64 64", "skinny_sum"]),
          (1155, 3752, 2352, ["restore", "dense_tn 256 192"]),
+         (16384, 4096, 768, ["restore_transposed", "dense_tn_split", "tail_finish"]), (18181, 3280, 1184, ["restore_transposed", "dense_tn_split", "tail_finish"]),
          (2048, 5120, 5120, ["restore_transposed", "dense_tn_split"]),
          (999, 4096, 16384, ["restore_transposed", "transpose_pad", "dense_tn_split"]),
          (1033, 9216, 9216, ["restore_transposed", "dense_tn_split", "dense_tn_split", "tail_finish"]),

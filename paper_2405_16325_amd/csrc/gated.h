@@ -80,24 +80,46 @@ __device__ __forceinline__ void with_act(int act, F f) {
 // for is a bf16 number: under the largest scale, 2^120, values stop at 240, since 256 would be 2^128.
 constexpr int Q8_BLOCK = 32;
 struct BlockScale {
-    float inv;
     uint32_t byte;
-    __device__ __forceinline__ float scaled(float v) const {
+    __device__ __forceinline__ float inverse() const { return __uint_as_float((byte == 255u ? 0u : 254u - byte) << 23); }
+    __device__ __forceinline__ float clamped(float v) const {
         const float most = byte == 247u ? 240.0f : Q8_MAX;
-        return __builtin_amdgcn_fmed3f(v * inv, -most, most);
+        return __builtin_amdgcn_fmed3f(v * inverse(), -most, most);
     }
 };
 __device__ __forceinline__ BlockScale block_scale(uint32_t top) {             // bits of the largest magnitude
     const int e = (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u);
-    const uint32_t byte = top >= 0x7F800000u ? 255u : (uint32_t)(e > 1 ? e : 1);
-    return {__uint_as_float((byte == 255u ? 0u : 254u - byte) << 23), byte};
+    return {top >= 0x7F800000u ? 255u : (uint32_t)(e > 1 ? e : 1)};
 }
-__device__ __forceinline__ float scale_of_byte(uint32_t byte) {
-    return __uint_as_float(byte == 255u ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);   // (0, which is never written: 2^-127)
+// Bits of the largest magnitude, NaN above all: one instruction for two values
+template <int N>
+__device__ __forceinline__ uint32_t top_of(const float (&v)[N]) {
+    float top = __builtin_elementwise_maximum(__builtin_fabsf(v[0]), __builtin_fabsf(v[1]));
+#pragma unroll
+    for (int e = 2; e < N; e += 2) top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(top, __builtin_fabsf(v[e])), __builtin_fabsf(v[e + 1]));
+    return __float_as_uint(top) & 0x7FFFFFFFu;
 }
-__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
-    const int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
+// Codes of N values, four to a word.  The conversion divides by the scale itself; with magnitudes of 448 scale at most it needs no clamp.  Blocks of the
+// largest scale, and those that read as NaN, which no lane of a wavefront has as a rule, take the long way.
+template <int N>
+__device__ __forceinline__ void block_codes(const float (&v)[N], const BlockScale& s, uint32_t (&o)[N / 4]) {
+    if (__any(s.byte >= 247u)) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const int p = __builtin_amdgcn_cvt_pk_fp8_f32(s.clamped(v[4 * i]), s.clamped(v[4 * i + 1]), 0, false);
+            o[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(s.clamped(v[4 * i + 2]), s.clamped(v[4 * i + 3]), p, true);
+        }
+        return;
+    }
+    const float scale = __uint_as_float(s.byte << 23);
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        s16x2 p = {0, 0};
+        p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[4 * i], v[4 * i + 1], scale, false);
+        p = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(p, v[4 * i + 2], v[4 * i + 3], scale, true);
+        o[i] = __builtin_bit_cast(uint32_t, p);
+    }
 }
 // eight codes -> eight bf16 numbers, exactly: one instruction for two of them, which takes the scale's exponent
 __device__ __forceinline__ u32x4 restored_bf16(u32x2 codes, uint32_t byte) {
@@ -112,34 +134,14 @@ __device__ __forceinline__ u32x4 restored_bf16(u32x2 codes, uint32_t byte) {
 }
 // an activation in this form, as an operand of the weight gradient
 struct BlocksX { const uint8_t *q, *bytes; };
-// eight codes -> the values they stand for
-__device__ __forceinline__ F8 unpack_e4m3(u32x2 codes, float scale) {
-    F8 o;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], true);
-        o.v[4 * i] = lo[0] * scale; o.v[4 * i + 1] = lo[1] * scale;
-        o.v[4 * i + 2] = hi[0] * scale; o.v[4 * i + 3] = hi[1] * scale;
-    }
-    return o;
-}
 
 // ---- results.  Four elements e .. e + 3 of token `tok` from their sums; eight neighbouring lanes have a block of 32 of a token (all of
 // them make the call, elements from the launch's last on being none).
-__device__ __forceinline__ uint32_t four_codes(const f32x4& v, const BlockScale& s) {
-    return pack_e4m3x4(s.scaled(v[0]), s.scaled(v[1]), s.scaled(v[2]), s.scaled(v[3]));
-}
 __device__ __forceinline__ u32x2 four_bf16(const f32x4& v) {
     union { __bf16 h[4]; u32x2 u; } o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o.h[e] = (__bf16)v[e];
     return o.u;
-}
-__device__ __forceinline__ uint32_t top_of(const f32x4& v) {
-    float top = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = max_abs(top, v[e]);
-    return __float_as_uint(top);
 }
 __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int tok, int e, int n, bf16_t* __restrict__ H, const GateOut& gate) {
     const bool has = tok < n && e < gate.count;
@@ -156,12 +158,16 @@ __device__ __forceinline__ void finish_gated(const f32x4& g, const f32x4& u, int
         *(u32x2*)(row + gate.d_ff) = four_bf16(u);
     }
     if (gate.q) {
-        const BlockScale sg = block_scale(lanes_reduce<8>(e < gate.count ? top_of(g) : 0u, MaxBits()));
-        const BlockScale su = block_scale(lanes_reduce<8>(e < gate.count ? top_of(u) : 0u, MaxBits()));
+        const float gv[4] = {g[0], g[1], g[2], g[3]}, uv[4] = {u[0], u[1], u[2], u[3]};
+        const BlockScale sg = block_scale(lanes_reduce<8>(e < gate.count ? top_of(gv) : 0u, MaxBits()));
+        const BlockScale su = block_scale(lanes_reduce<8>(e < gate.count ? top_of(uv) : 0u, MaxBits()));
+        uint32_t gq[1], uq[1];
+        block_codes(gv, sg, gq);
+        block_codes(uv, su, uq);
         if (!has) return;
         uint8_t* const row = gate.q + (size_t)tok * (2 * (size_t)gate.d_ff) + e;
-        *(uint32_t*)row = four_codes(g, sg);
-        *(uint32_t*)(row + gate.d_ff) = four_codes(u, su);
+        *(uint32_t*)row = gq[0];
+        *(uint32_t*)(row + gate.d_ff) = uq[0];
         if ((e & (Q8_BLOCK - 1)) == 0) {
             const size_t blocks = ((size_t)gate.d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
             uint8_t* const byte = gate.bytes + (size_t)tok * 2 * blocks + e / Q8_BLOCK;
@@ -238,12 +244,16 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                 for (int half = 0; half < 2; ++half) {
                     const f32x4 &a = acc[4 * c + half][j], &b = acc[4 * c + 2 + half][j];
                     const int e = e0 + c * 32;                // the block's first element
-                    uint32_t top = e + lq * 4 < count ? top_of(a) : 0u;
-                    if (e + 16 + lq * 4 < count) top = MaxBits()(top, top_of(b));
-                    const BlockScale s = block_scale(quarters_max(top));
+                    float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+                    if (tile_e0 + HALF > count)               // uniform: elements past the last are none
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) v[x] = e + x / 4 * 16 + lq * 4 < count ? v[x] : 0.0f;
+                    const BlockScale s = block_scale(quarters_max(top_of(v)));
+                    uint32_t codes[2];
+                    block_codes(v, s, codes);
                     uint8_t* const at = smem + CODES + (lt + j * 16) * (BMT + 16) + half * HALF + le + c * 32;
-                    *(uint32_t*)at = four_codes(a, s);
-                    *(uint32_t*)(at + 16) = four_codes(b, s);
+                    *(uint32_t*)at = codes[0];
+                    *(uint32_t*)(at + 16) = codes[1];
                     const int tok = t0 + j * 16 + l16;
                     if (lq == 0 && tok < n && e < count) gate.bytes[((size_t)tok * 2 + half) * blocks + e / Q8_BLOCK] = (uint8_t)s.byte;
                 }

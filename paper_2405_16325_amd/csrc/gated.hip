@@ -49,8 +49,8 @@ __global__ void __launch_bounds__(THREADS) gated_bwd_kernel(GatedBwd j) {
         const uint8_t* const byte = j.bytes + (size_t)p.row * 2 * blocks + p.c / 4;
         const uint32_t gb = byte[0], ub = byte[blocks];
         const u32x2 gq = load<STREAM, u32x2>(j.q + pair), uq = load<STREAM, u32x2>(j.q + pair + j.d_ff);
-        g = unpack_e4m3(gq, scale_of_byte(gb));
-        u = unpack_e4m3(uq, scale_of_byte(ub));
+        g = unpack_bf16(restored_bf16(gq, gb));
+        u = unpack_bf16(restored_bf16(uq, ub));
     } else {
         const u32x4 gv = load<STREAM, u32x4>(j.gu + pair), uv = load<STREAM, u32x4>(j.gu + pair + j.d_ff);
         g = unpack_bf16(gv);
@@ -90,18 +90,15 @@ __global__ void __launch_bounds__(THREADS) checkpoint_kernel(const bf16_t* __res
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        F8 v = unpack_bf16(in[i]);
-        float top = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = max_abs(top, v.v[e]);
-        uint32_t bits = __float_as_uint(top);                 // a block is four neighbouring lanes
+        const F8 v = unpack_bf16(in[i]);
+        uint32_t bits = top_of(v.v);                          // a block is four neighbouring lanes
         bits = MaxBits()(bits, dpp<DPP_XOR1>(bits));
         bits = MaxBits()(bits, dpp<DPP_XOR2>(bits));
         const BlockScale s = block_scale(bits);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v.v[e] = s.scaled(v.v[e]);
+        uint32_t codes[2];
+        block_codes(v.v, s, codes);
         if (has[i]) {
-            store<STREAM>(q + (size_t)p[i].row * d + p[i].c * 8, pack_e4m3(v));
+            store<STREAM>(q + (size_t)p[i].row * d + p[i].c * 8, (u32x2){codes[0], codes[1]});
             if ((p[i].c & 3) == 0) bytes[(size_t)p[i].row * blocks + p[i].c / 4] = (uint8_t)s.byte;
         }
     }

@@ -556,3 +556,68 @@ def test_on_another_stream():
         got = sl.slope_gated_fwd(p.x, p.vals, p.meta)[0]
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_two_graphs_share_a_workspace():
+    """Calls of two layers, each captured, with one workspace: its contents are a call's own."""
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    runs = []
+    for b, d_ff, d_in, r, seed in ((128, 200, 4096, 32, 1), (1000, 520, 1000, 0, 2), (4053, 1504, 392, 0, 3)):
+        p = Layer(b, d_ff, d_in, r, seed=seed)
+        dgu = sl.bf16_to_device(inputs.gaussian_bf16((b, 2 * d_ff), 1e-3, seed, 3))
+        xq, xs = sl.slope_checkpoint_q8(p.x)
+
+        def step(p=p, dgu=dgu, xq=xq, xs=xs):
+            h, _, q, s = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_q8=True, workspace=ws)
+            return h, codes(q), s, sl.slope_wgrad_masked_q8(dgu, xq, xs, p.meta, workspace=ws)
+
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step()
+        runs.append((graph, held, want, step))                              # (step holds the operands, which the graph reads)
+    for turn in range(3):
+        for graph, held, want, _ in runs:
+            ws.fill_(255)                                                   # NaN, were it read
+            graph.replay()
+            for a, e in zip(held, want):
+                assert torch.equal(a, e)
+
+
+def test_two_streams_at_once():
+    p = Layer(515, 1000, 256, 96, seed=6)
+    want = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_gu=True)[:2]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for turn in range(8):
+        with torch.cuda.stream(streams[turn % 2]):
+            got.append(sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_gu=True)[:2])
+    torch.cuda.synchronize()
+    for h, gu in got:
+        assert torch.equal(h, want[0]) and torch.equal(gu, want[1])
+
+
+def test_the_binding_refuses_wrong_types_shapes_and_strides():
+    b, d_ff, d_in = 8, 64, 128
+    p = Layer(b, d_ff, d_in, 32, seed=7)
+    h, gu, q, s = sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, want_gu=True, want_q8=True)
+    xq, xs = sl.slope_checkpoint_q8(p.x)
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    wide = torch.zeros(b, 2 * d_in, dtype=sl.BF16, device="cuda")
+    bad = [lambda: sl.slope_gated_fwd(wide[:, :d_in], p.vals, p.meta), lambda: sl.slope_gated_fwd(p.x.float(), p.vals, p.meta),
+           lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta[:-1]), lambda: sl.slope_gated_fwd(p.x, p.vals[:-1], p.meta[:-1]),
+           lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l), lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r[:, :d_ff]),
+           lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, workspace=small), lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, out=(gu, None, None, None)),
+           lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, out=(h, h, None, None)), lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, out=(h, None, q, s[:, :1])),
+           lambda: sl.slope_gated_bwd(h, gu=gu, q8=q, scale=s), lambda: sl.slope_gated_bwd(h, gu=h), lambda: sl.slope_gated_bwd(h, q8=q), lambda: sl.slope_gated_bwd(h, q8=gu, scale=s),
+           lambda: sl.slope_checkpoint_q8(p.x.t()), lambda: sl.slope_restore_q8(xq, xs[:, :1]), lambda: sl.slope_restore_q8(codes(xq), xs),
+           lambda: sl.slope_wgrad_masked_q8(gu, xq, xs[:-1], p.meta), lambda: sl.slope_wgrad_masked_q8(gu[:-1], xq, xs, p.meta),
+           lambda: sl.slope_wgrad_masked_q8(gu, p.x, xs, p.meta), lambda: sl.slope_wgrad_masked_q8(gu, xq, xs, p.meta[:, :-1])]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, act=3), lambda: sl.slope_gated_bwd(h, act=-1, gu=gu),
+                 lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, L=p.l, R=p.r, workspace=None), lambda: sl.slope_gated_fwd(p.x, p.vals, p.meta, out=(h, None, q, None))):
+        with pytest.raises(sl.SlopeError):
+            call()

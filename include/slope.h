@@ -523,7 +523,7 @@ slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int 
  *   [0] product, [1], [2] rows of the weight, gate and up projection, and tokens per workgroup, [3] slabs, slices or the tokens of
  *       the small-batch kernel: as slope_spmm_fwd_plan; or [0] 6, tiles of that size for the last rows and, in a launch before,
  *       256 x 256 ones for the first [3], which are whole rounds of them
- *   [4] whether the small-batch kernel computes T = X L itself
+ *   [4] T = X L: 1 computed by the small-batch kernel's workgroups, 2 by others beside the product's, 0 before it (or no adapter)
  *   [5] columns of the padded copies that the call makes of its operands (0 = none)
  */
 slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept, int with_workspace, int32_t* plan);

@@ -168,14 +168,20 @@ int64_t gated_first_rows(int64_t n, int64_t m, int64_t K, bool blocks);
 hipError_t launch_pad_operands(const bf16_t* x, int64_t n, const bf16_t* vals, const uint8_t* meta, int64_t rows, int64_t K, int64_t Kp,
                                bf16_t* xp, bf16_t* vp, uint8_t* mp, hipStream_t s);
 // (m of the split and of the sums: gated_rows(d_ff), or 2 d_ff for the small-batch kernels' slices)
-hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
-                              int64_t r, const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s);
+hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const SlabAdapter& ad,
+                              const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s);
 hipError_t launch_gated_sum(const float* P, int slabs, int64_t n, int64_t m, bf16_t* H, const GateOut& gate, hipStream_t s);
 bool gated_rows_of_64(int64_t n, int64_t m, int64_t K, int slices);
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced);
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
                                const bf16_t* R, int64_t r, bf16_t* H, float* sums_or_null, const GateOut& gate, hipStream_t s);
-size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, bool keeps);
+size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, int64_t r, bool keeps);
+bool gated_stream_beside(int64_t n, int64_t m, int64_t K, int64_t r);
+hipError_t launch_gated_stream_beside(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* L,
+                                      const bf16_t* R, int64_t r, bf16_t* H, float* Q, float* sums, const GateOut& gate, hipStream_t s);
+// as launch_adapter_finish, P[slices][n][2 half]
+hipError_t launch_gated_adapter_finish(const float* P, int slices, int64_t n, int64_t half, const float* Q, int q_slabs, const bf16_t* R, int64_t r,
+                                       bf16_t* H, const GateOut& gate, hipStream_t s);
 hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
                         int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s);
 hipError_t launch_gated_bwd(const bf16_t* dh, const bf16_t* gu, const uint8_t* q, const uint8_t* bytes, int64_t n, int64_t d_ff, int act,

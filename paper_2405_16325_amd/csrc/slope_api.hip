@@ -646,29 +646,35 @@ static bool bad_act(int act) { return act != SLOPE_ACT_SILU && act != SLOPE_ACT_
 static bool bad_blocks(int64_t rows, int64_t d) { return bad_extent(rows, 1) || bad_extent(d, 8) || !grid_fits(rows * ((d + 31) / 32 * 4) / 256 + 1); }
 
 // The call's scratch, in bytes: [ adapter | padded copies of X, values, metadata | sums of slabs, or of the small-batch
-// kernels ], and its split over the contraction.  The split does not depend on the adapter, whose T = X L has its launches before the product.
+// kernels ], and its split over the contraction, beside whose slabs X L is computed (x) where that is given and nothing is kept; else T = X L has
+// its launches before the product.
 struct GatedPlan {
     SpmmSplit split;
+    bool beside;
+    XlSplit x;
     int64_t padded, K;                                        // columns of the copies (0: none); the contraction's
     size_t x_at, vals_at, meta_at, sums_at, total;
 };
 static GatedPlan gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, bool keeps) {
-    GatedPlan p;
+    GatedPlan p = {};
     const int64_t m = gated_rows(d_ff);
     p.padded = gated_padded(b, d_ff, d_in);
     p.K = p.padded ? p.padded : d_in;
-    p.split = spmm_split(b, m, p.K, 0, spmm_slab_room(b, m, p.K));
+    const int64_t xl = keeps || p.padded ? 0 : r;
+    p.split = spmm_split(b, m, p.K, xl, spmm_slab_room(b, m, p.K));
+    p.beside = p.split.slabs && xl > 0 && b <= XL_SMALL_MAX_TOKENS && slab_xl_split(b, m, p.K, r, p.split, p.x);
     p.x_at = adapter_workspace_bytes(b, d_in, 2 * d_ff, r);
     p.vals_at = p.x_at + (p.padded ? round256((size_t)b * p.K * 2) : 0);
     p.meta_at = p.vals_at + (p.padded ? round256((size_t)2 * d_ff * p.K) : 0);
     p.sums_at = p.meta_at + (p.padded ? round256((size_t)2 * d_ff * (p.K / 8)) : 0);
-    p.total = p.sums_at + round256(spmm_split_bytes(p.split, b, m)) + round256(gated_stream_bytes(b, d_ff, p.K, keeps));
+    p.total = p.sums_at + round256(spmm_split_bytes(p.split, b, m)) + round256(gated_stream_bytes(b, d_ff, p.K, r, keeps));
     return p;
 }
 
 size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept) {
     if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
-    return gated_plan(b, d_in, d_ff, r, kept != 0).total;
+    const size_t h = gated_plan(b, d_in, d_ff, r, false).total, all = kept ? gated_plan(b, d_in, d_ff, r, true).total : 0;
+    return h > all ? h : all;                                 // (room for what is kept is room for h alone)
 }
 
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,
@@ -701,8 +707,11 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
     bf16_t* T = adapter ? (bf16_t*)ws : nullptr;
     if (few && adapter && gated_stream_takes_l(b, 2 * d_ff, d_in, r, after != nullptr))
         return finish(launch_gated_stream(x, b, wv, wm, d_in, nullptr, l, R, r, (bf16_t*)H, after, gate, s));
+    float* const sums = adapter ? (float*)(ws + round256((size_t)b * r * 2) + round256((size_t)d_in * r * 2)) : nullptr;
+    if (few && adapter && !gate.keeps() && gated_stream_beside(b, 2 * d_ff, d_in, r))
+        return finish(launch_gated_stream_beside(x, b, wv, wm, d_in, l, R, r, (bf16_t*)H, sums, after, gate, s));
+    if (plan.beside) return finish(launch_gated_slabs(x, b, wv, wm, d_in, {nullptr, sums, l, R, r, plan.x}, plan.split, (bf16_t*)H, after, gate, s));
     if (adapter) {
-        float* const sums = (float*)(ws + round256((size_t)b * r * 2) + round256((size_t)d_in * r * 2));
         const hipError_t e = token_factor(x, b, d_in, l, r, T, sums, s);
         if (e != hipSuccess) return finish(e);
     }
@@ -717,7 +726,7 @@ slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, cons
         wm = mp;
         d_in = plan.padded;
     }
-    if (plan.split.slabs) return finish(launch_gated_slabs(x, b, wv, wm, d_in, T, R, r, plan.split, (bf16_t*)H, after, gate, s));
+    if (plan.split.slabs) return finish(launch_gated_slabs(x, b, wv, wm, d_in, {T, sums, l, R, r, {0, 0, 0}}, plan.split, (bf16_t*)H, after, gate, s));
     return finish(launch_gated(x, b, wv, wm, d_in, T, R, r, (bf16_t*)H, gate, s));
 }
 
@@ -734,13 +743,14 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
         plan[1] = slices > 0 ? (gated_rows_of_64(b, 2 * d_ff, d_in, slices) ? 64 : 48) : spmm_stream_rows(b, 2 * d_ff, d_in);
         plan[2] = b <= 16 ? 16 : 32;
         if (slices > 0) plan[3] = slices;
-        plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices > 1);
+        plan[4] = gated_stream_takes_l(b, 2 * d_ff, d_in, r, slices > 1) ? 1 : !kept && gated_stream_beside(b, 2 * d_ff, d_in, r) ? 2 : 0;
         return SLOPE_OK;
     }
     SpmmSplit split = {0, 0, 0};
     if (with_workspace) {
         const GatedPlan p = gated_plan(b, d_in, d_ff, r, kept != 0);
         split = p.split;
+        if (p.beside) plan[4] = 2;
         plan[5] = (int32_t)p.padded;
         d_in = p.K;
     }

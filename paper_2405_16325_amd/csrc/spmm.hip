@@ -1902,11 +1902,13 @@ hipError_t launch_gated_sum(const float* P, int slabs, int64_t n, int64_t m, bf1
 }
 
 // Split over the contraction, as launch_spmm_slabs
-hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
-                              int64_t r, const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s) {
+hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const SlabAdapter& ad,
+                              const SpmmSplit& split, bf16_t* H, float* slabs, const GateOut& gate, hipStream_t s) {
     const int64_t m = gated_rows(gate.d_ff);
     const int slab_steps = (int)slab_steps_of(K, split.slabs), nslabs = (int)((K / 64 + slab_steps - 1) / slab_steps);
-    const SplitJob job = {nslabs, slab_steps, slabs, nullptr, nullptr, 0, 0, 0};
+    const SplitJob job = {nslabs, slab_steps, slabs, ad.T ? nullptr : ad.L, ad.Q, (int)ad.r, ad.x.k_per, ad.x.slabs};
+    const bf16_t *T = ad.T, *R = ad.T ? ad.R : nullptr;
+    const int64_t r = ad.T ? ad.r : 0;
     hipError_t e;
     switch (split.bm * 1000 + split.bn) {
         case 128064: e = launch_ring<128, 64>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
@@ -1915,7 +1917,9 @@ hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, 
         case 128128: e = launch_ring<128, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
         default: e = launch_tile<256, 128>(B, n, A_vals, A_meta, m, K, T, R, -r, nullptr, s, job, gate); break;
     }
-    return e != hipSuccess ? e : launch_gated_sum(slabs, nslabs, n, m, H, gate, s);
+    if (e != hipSuccess) return e;
+    if (ad.r && !ad.T) return launch_gated_adapter_finish(slabs, nslabs, n, m / 2, ad.Q, ad.x.slabs, ad.R, ad.r, H, gate, s);
+    return launch_gated_sum(slabs, nslabs, n, m, H, gate, s);
 }
 
 // Tokens by as many as a launch's grid holds (d_ff is at most 2^22: at least 1024 of them, in whole tiles)

@@ -648,10 +648,31 @@ __device__ __forceinline__ u32x4 t_piece(const float* __restrict__ Q, int slabs,
 // X L before the product and its reduction, took 12.7).  The sliced small-batch kernel gains nothing from it (72 + 8.6 us
 // against 72 + 5.3 + 5.2), nor any small-batch kernel from adding up the sums of T itself (65.8 -> 75.9 us for one token).  It is the second
 // kernel of a small-batch product too where X L runs beside that (xl_beside).
+// Gate: a gated layer's, C its h; features in the small-batch kernels' order (stream_row), P[slice][n][2 half] with the two projections of an
+// element `half` apart.  A lane and the one 32 further have g and u of the same four elements.
 constexpr int AF_TOK = 32, AF_FEAT = 64;
+struct GateSums { GateOut gate; int half; };
+__device__ __forceinline__ int finish_column(int feat) { return feat; }
+__device__ __forceinline__ int finish_column(int feat, const GateSums& g) { return stream_row(feat, g.gate); }
+__device__ __forceinline__ size_t sums_offset(size_t row, int feat, int m) { return row * m + feat; }
+__device__ __forceinline__ size_t sums_offset(size_t row, int feat, int, const GateSums& g) {
+    return row * (2 * (size_t)g.half) + (feat >> 4) * 8 + (feat & 7) + (feat & 8 ? g.half : 0);
+}
+__device__ __forceinline__ void store_finished(const f32x4& v, bool has, int tok, int feat, int m, bf16_t* __restrict__ C) {
+    if (has) *(u32x2*)(C + (size_t)tok * m + feat) = four_bf16(v);
+}
+__device__ __forceinline__ void store_finished(const f32x4& v, bool has, int tok, int feat, int, bf16_t* __restrict__ H, const GateSums& g) {
+    with_act(g.gate.act, [&](auto act) {
+        f32x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = act_value<decltype(act)::value>(v[e]) * __shfl_xor(v[e], 32);
+        if (has && (feat & 8) == 0) *(u32x2*)(H + (size_t)tok * g.gate.d_ff + stream_row(feat, g.gate)) = four_bf16(h);
+    });
+}
+template <class... Gate>
 __global__ void __launch_bounds__(256) adapter_finish_kernel(const float* __restrict__ P, int slices, int n, int m,
                                                              const float* __restrict__ Q, int q_slabs,
-                                                             const bf16_t* __restrict__ R, int r, bf16_t* __restrict__ C) {
+                                                             const bf16_t* __restrict__ R, int r, bf16_t* __restrict__ C, Gate... gate) {
     constexpr int TP = 128 * 2 + 16, RP = 160;                // bytes per staged row of T and of R's tile
     __shared__ __align__(16) uint8_t smem[AF_TOK * TP + 128 * RP];
     uint8_t* const t_lds = smem;
@@ -668,7 +689,7 @@ __global__ void __launch_bounds__(256) adapter_finish_kernel(const float* __rest
         for (int sl = 0; sl < AHEAD; ++sl) {
             const int tok = t0 + 16 * j + l16;
             p[j][sl] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (tok < n && feat < m && sl < slices) p[j][sl] = *(const f32x4*)(P + ((size_t)sl * n + tok) * m + feat);
+            if (tok < n && feat < m && sl < slices) p[j][sl] = *(const f32x4*)(P + sums_offset((size_t)sl * n + tok, feat, m, gate...));
         }
     f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     for (int kc = 0; kc < r; kc += 128) {
@@ -679,7 +700,7 @@ __global__ void __launch_bounds__(256) adapter_finish_kernel(const float* __rest
         for (int u = 0; u < 4; ++u) {
             const int idx = t + 256 * u, k = idx >> 3, sg = idx & 7;
             rv[u] = (u32x4){0u, 0u, 0u, 0u};
-            if (k < kn && f0 + 8 * sg < m) rv[u] = *(const u32x4*)(R + (size_t)(kc + k) * m + f0 + 8 * sg);
+            if (k < kn && f0 + 8 * sg < m) rv[u] = *(const u32x4*)(R + (size_t)(kc + k) * m + finish_column(f0 + 8 * sg, gate...));
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -711,19 +732,20 @@ __global__ void __launch_bounds__(256) adapter_finish_kernel(const float* __rest
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int tok = t0 + 16 * j + l16;
-        if (tok >= n || feat >= m) continue;
+        const bool has = tok < n && feat < m;
+        if (sizeof...(Gate) == 0 && !has) continue;
         f32x4 v = p[j][0];
 #pragma unroll
         for (int sl = 1; sl < AHEAD; ++sl) { v[0] += p[j][sl][0]; v[1] += p[j][sl][1]; v[2] += p[j][sl][2]; v[3] += p[j][sl][3]; }
 #pragma unroll 4
         for (int sl = AHEAD; sl < slices; ++sl) {
-            const f32x4 w = *(const f32x4*)(P + ((size_t)sl * n + tok) * m + feat);
+            if (!has) break;
+            const f32x4 w = *(const f32x4*)(P + sums_offset((size_t)sl * n + tok, feat, m, gate...));
             v[0] += w[0]; v[1] += w[1]; v[2] += w[2]; v[3] += w[3];
         }
-        union { __bf16 h[4]; u32x2 u; } o;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o.h[e] = (__bf16)(v[e] + acc[j][e]);
-        *(u32x2*)(C + (size_t)tok * m + feat) = o.u;
+        for (int e = 0; e < 4; ++e) v[e] += acc[j][e];
+        store_finished(v, has, tok, feat, m, C, gate...);
     }
 }
 
@@ -951,10 +973,30 @@ bool launch_spmm_stream_adapter(const bf16_t* B, int64_t n, const bf16_t* A_vals
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced) {
     return r > 0 && spmm_rows_slices(n, m, K, sliced) == 0 && xl_by_itself(n, m, K, r);
 }
-size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, bool keeps) {
+// Beside the product, as xl_beside says, where nothing is kept: sums of both, and adapter_finish_kernel (us, 13824 x 2560, X L before / so: one token, rank
+// 32 21.5 / 17.9, rank 128 22.8 / 18.7; 8, 22.4 / 18.4 and 23.6 / 19.3).
+static bool gated_beside(int64_t n, int64_t m, int64_t K, int64_t r, StreamXl& xl) {
+    return r > 0 && spmm_rows_slices(n, m, K, true) == 0 && !xl_by_itself(n, m, K, r) &&
+           xl_beside(n, m, K, r, (int64_t)(xl_small_scratch_bytes(n, K, r) / 4), xl);
+}
+bool gated_stream_beside(int64_t n, int64_t m, int64_t K, int64_t r) {
+    StreamXl xl;
+    return gated_beside(n, m, K, r, xl);
+}
+size_t gated_stream_bytes(int64_t n, int64_t d_ff, int64_t K, int64_t r, bool keeps) {
     if (!spmm_stream_fits(n, K)) return 0;
     const int slices = spmm_rows_slices(n, 2 * d_ff, K, true);
-    return slices > 1 || keeps ? (size_t)(slices > 1 ? slices : 1) * (size_t)n * (size_t)(2 * d_ff) * 4 : 0;
+    return slices > 1 || keeps || gated_stream_beside(n, 2 * d_ff, K, r) ? (size_t)(slices > 1 ? slices : 1) * (size_t)n * (size_t)(2 * d_ff) * 4 : 0;
+}
+hipError_t launch_gated_stream_beside(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* L,
+                                      const bf16_t* R, int64_t r, bf16_t* H, float* Q, float* sums, const GateOut& gate, hipStream_t s) {
+    const int64_t m = 2 * (int64_t)gate.d_ff;
+    StreamXl xl = {L, Q, nullptr, (int)r, 0, 0, 0};
+    if (!gated_beside(n, m, K, r, xl)) return hipErrorInvalidValue;
+    GateOut out = gate;
+    out.sums = sums;
+    const hipError_t e = launch_stream(B, n, A_vals, A_meta, m, K, nullptr, nullptr, 0, H, nullptr, 0, xl, s, out);
+    return e != hipSuccess ? e : launch_gated_adapter_finish(sums, 1, n, gate.d_ff, Q, xl.slabs, R, r, H, gate, s);
 }
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
                                const bf16_t* R, int64_t r, bf16_t* H, float* sums_or_null, const GateOut& gate, hipStream_t s) {
@@ -1012,7 +1054,14 @@ hipError_t launch_xl_reduce(const float* Q, int slabs, int64_t n, int64_t r, bf1
 
 hipError_t launch_adapter_finish(const float* P, int slices, int64_t n, int64_t m, const float* Q, int q_slabs,
                                  const bf16_t* R, int64_t r, bf16_t* C, hipStream_t s) {
-    adapter_finish_kernel<<<dim3((unsigned)((m + 63) / 64), (unsigned)((n + 31) / 32)), dim3(256), 0, s>>>(
+    adapter_finish_kernel<><<<dim3((unsigned)((m + 63) / 64), (unsigned)((n + 31) / 32)), dim3(256), 0, s>>>(
         P, slices, (int)n, (int)m, Q, q_slabs, R, (int)r, C);
+    return hipGetLastError();
+}
+hipError_t launch_gated_adapter_finish(const float* P, int slices, int64_t n, int64_t half, const float* Q, int q_slabs, const bf16_t* R, int64_t r,
+                                       bf16_t* H, const GateOut& gate, hipStream_t s) {
+    const int64_t m = 2 * (int64_t)gate.d_ff;
+    adapter_finish_kernel<><<<dim3((unsigned)((m + 63) / 64), (unsigned)((n + 31) / 32)), dim3(256), 0, s>>>(
+        P, slices, (int)n, (int)m, Q, q_slabs, R, (int)r, H, GateSums{gate, (int)half});
     return hipGetLastError();
 }

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2405_16325_amd import binding as sl
-from tests.test_gpu_gated import LARGE, SHAPES
+from tests.test_gpu_gated import BESIDE, LARGE, SHAPES
 
 SMALL_BATCH, SLABS, TILE, GENERAL, ROW_SPLIT, REST, TWO_TILES = range(7)
 
@@ -109,6 +109,20 @@ def test_the_gpu_tests_reach_padded_copies():
             assert p["padded"] % 64 == 0 and 0 < p["padded"] - i < 64
             found.add((p["product"], r > 0))
     assert {(TILE, False), (TILE, True), (SLABS, False), (SLABS, True)} <= found
+
+
+def test_the_adapter_beside_the_product():
+    """Where only h is wanted; what is kept needs the projections before they are finished."""
+    found = set()
+    for b, f, i, r in BESIDE:
+        p = plan(b, f, i, r)
+        found.add((p["product"], p["rows"], p["tokens"], f % 16 != 0))
+        assert p["xl"] == 2, (b, f, i, r)
+        assert plan(b, f, i, r, kept=8)["xl"] != 2 and plan(b, f, i, r, kept=16)["xl"] != 2 and plan(b, f, i, 0)["xl"] == 0
+    for rows, tokens in ((32, 16), (48, 16), (64, 16), (32, 32), (48, 32)):
+        assert {(SMALL_BATCH, rows, tokens, odd) for odd in (False, True)} & found, (rows, tokens)
+    assert {(SLABS, rows, tokens) for rows, tokens in ((128, 64), (128, 128), (192, 64), (256, 64), (256, 128))} <= {k[:3] for k in found}
+    assert {k[3] for k in found if k[0] == SLABS} == {k[3] for k in found if k[0] == SMALL_BATCH} == {False, True}
 
 
 def test_whole_rounds_of_the_largest_tiles_and_others_behind():

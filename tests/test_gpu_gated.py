@@ -163,6 +163,18 @@ LARGE = [(1568, 5056, 768, 32), (785, 9984, 832, 0), (35, 2600, 10048, 0), (65, 
          (962, 8200, 640, 32), (423, 16520, 664, 0), (435, 17696, 768, 32), (11211, 680, 768, 0), (608, 16568, 1264, 32), (8235, 968, 2048, 32), (8287, 976, 2112, 0)]
 
 
+# X L beside the product and the adapter added with the sums (test_dispatch_gated.py)
+BESIDE = [(1, 8, 1088, 96), (9, 40, 1152, 96), (16, 520, 2048, 32), (17, 6992, 1152, 64), (18, 6792, 1152, 96), (1, 4600, 1216, 64), (3, 4944, 1280, 128),
+          (18, 5680, 1408, 32), (17, 4664, 1856, 32), (2, 15936, 1728, 32), (3, 6424, 2176, 128), (33, 16, 1920, 64), (37, 8, 1856, 128), (100, 200, 4096, 160), (321, 16, 12224, 160),
+          (400, 8, 9088, 160), (436, 72, 7936, 192), (33, 2592, 10304, 96), (37, 1720, 15680, 192), (485, 112, 15168, 192), (137, 808, 15232, 192)]
+
+
+@pytest.mark.parametrize("b,d_ff,d_in,r", BESIDE)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_forward_with_the_adapter_beside(b, d_ff, d_in, r, act):
+    check_forward(b, d_ff, d_in, act, r)
+
+
 @pytest.mark.parametrize("b,d_ff,d_in", SHAPES)
 @pytest.mark.parametrize("act,r", [("silu", 0), ("gelu", 32), ("relu", 160)])
 def test_forward(b, d_ff, d_in, act, r):

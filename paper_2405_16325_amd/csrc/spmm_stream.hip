@@ -44,6 +44,11 @@ __device__ __forceinline__ void stream_xl_part(const StreamXl& xl, int w, const 
 __device__ __forceinline__ int stream_row(int row) { return row; }
 __device__ __forceinline__ int stream_row(int row, const GateOut& gate) { return (row >> 4) * 8 + (row & 7) + (row & 8 ? gate.d_ff : 0); }
 
+// A gated layer's calls of up to eight tokens load the first eight rows of a token fragment only; what lies in the others' place reaches sums that
+// nobody reads.  (TBD)
+struct GateFew : GateOut {};
+template <class... Gate> constexpr int TOKEN_HALVES = (std::is_same_v<Gate, GateFew> || ...) ? 1 : 2;
+
 union StB { u32x4 u[2]; bf16x16 v; };
 union StA { u32x4 u; bf16x8 v; };
 
@@ -52,12 +57,12 @@ union StA { u32x4 u; bf16x8 v; };
 // two (up to 32 tokens, 4 wavefronts).  Ring stage of one wavefront:
 //     A: MF fragments x (16 rows x 128 B: both steps of the pair) | B: 2 steps x NF x (16 tokens x 128 B)
 //     | metadata: 16 MF rows x 16 B
-template <int MF, int WAVES, int NF>
+template <int MF, int WAVES, int NF, int HALVES = 2>
 struct StreamLds {
     static constexpr int BM = 16 * MF;
     static constexpr int A_BYTES = MF * 2048, B_BYTES = 2 * NF * 2048, M_BYTES = MF * 256;
     static constexpr int STAGE = A_BYTES + B_BYTES + M_BYTES;
-    static constexpr int OPS = 2 * MF + 4 * NF + 1;           // loads per wavefront and pair
+    static constexpr int OPS = 2 * MF + 2 * HALVES * NF + 1;  // loads per wavefront and pair
     static constexpr int RING = WAVES * 2 * STAGE;
     static constexpr int PART_PITCH = 16 * NF + 1;
     static constexpr int TOTAL = RING + WAVES * BM * PART_PITCH * 4;
@@ -106,7 +111,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
                                                                    const bf16_t* __restrict__ T,
                                                                    const bf16_t* __restrict__ R, int K2,
                                                                    bf16_t* __restrict__ C, StreamXl xl, Gate... gate) {
-    using S = StreamLds<MF, WAVES, NF>;
+    using S = StreamLds<MF, WAVES, NF, TOKEN_HALVES<Gate...>>;
     constexpr bool GATED = sizeof...(Gate) > 0;
     extern __shared__ __align__(16) uint8_t smem[];
     static_assert(skinny_lds(WAVES) <= S::RING, "a part of X L fits");
@@ -171,7 +176,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
 #pragma unroll
             for (int j = 0; j < NF; ++j) {
                 dma16(b_src[j][0] + (s0 + e) * 128, st + S::A_BYTES + (e * NF + j) * 2048);
-                dma16(b_src[j][1] + (s0 + e) * 128, st + S::A_BYTES + (e * NF + j) * 2048 + 1024);
+                if (TOKEN_HALVES<Gate...> == 2) dma16(b_src[j][1] + (s0 + e) * 128, st + S::A_BYTES + (e * NF + j) * 2048 + 1024);
             }
         if (meta_lane) dma16(m_src + s0 * 8, st + S::A_BYTES + S::B_BYTES);
     };
@@ -344,7 +349,7 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_stream_lds_kernel(const bf16_
 template <int MF, int WAVES, int NF, class... Gate>
 hipError_t launch_stream_lds(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
                              const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, const StreamXl& xl, hipStream_t s, const Gate&... gate) {
-    using S = StreamLds<MF, WAVES, NF>;
+    using S = StreamLds<MF, WAVES, NF, TOKEN_HALVES<Gate...>>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     auto kern = xl.L ? spmm_stream_lds_kernel<MF, WAVES, NF, true, Gate...> : spmm_stream_lds_kernel<MF, WAVES, NF, false, Gate...>;
     hipError_t e = xl.L ? allow_dynamic_lds<spmm_stream_lds_kernel<MF, WAVES, NF, true, Gate...>>(S::TOTAL)
@@ -376,24 +381,24 @@ hipError_t launch_stream_lds(const bf16_t* B, int64_t n, const bf16_t* Av, const
 // 36864 x 9216 at 16 tokens, rank-128 adapters: 91 -> 78 us; 9216 x 36864: 107 -> 85 us; without adapters 67 and 72 us
 // (5.7 and 5.3 TB/s of packed weight).
 constexpr int ROWS_WAVES = 3, ROWS_DEPTH = 3, ROWS_BM = 16 * ROWS_WAVES;
-template <int NF, int WAVES = ROWS_WAVES>
+template <int NF, int WAVES = ROWS_WAVES, int HALVES = 2>
 struct RowsLds {
     static constexpr int A_STAGE = 2048;                      // 16 rows x 128 B: both steps of a pair
     static constexpr int M_SLOT = 2048;                       // 16 rows x 128 B: the metadata of 8 pairs
     static constexpr int WAVE_BYTES = ROWS_DEPTH * A_STAGE + 2 * M_SLOT;
-    static constexpr int X_OPS = 4 * NF;                      // 1 KiB loads per pair: 2 steps x NF fragments x 2 halves
-    static constexpr int X_STAGE = X_OPS * 1024;
+    static constexpr int X_OPS = 2 * HALVES * NF;             // 1 KiB loads per pair: 2 steps x NF fragments x 2 halves
+    static constexpr int X_STAGE = 4 * NF * 1024;
     static constexpr int BM = 16 * WAVES, TOTAL = WAVES * WAVE_BYTES + ROWS_DEPTH * X_STAGE;
 };
 
 // The main loop of one wavefront.  XW = how many of the pair's X_OPS token loads this wavefront issues, so that the
 // number of its loads per pair, 2 + XW, is a constant the s_waitcnt immediates can be built from.
-template <int NF, int WAVES, int XW>
+template <int NF, int WAVES, int HALVES, int XW>
 __device__ __forceinline__ void rows_main_loop(const uint8_t* const (&a_src)[2], const uint8_t* const (&m_src)[2],
                                                const uint8_t* const (&b_src)[NF][2], int wave, uint8_t* mine,
                                                uint8_t* xring, int pair0, int npairs, int l16, int lq,
                                                f32x4 (&acc)[NF]) {
-    using S = RowsLds<NF, WAVES>;
+    using S = RowsLds<NF, WAVES, HALVES>;
     constexpr int L = 2 + XW;                                 // loads per pair (the metadata loads come on top, every 8th pair)
     const int sw = (l16 >> 1) & 7;
     // pair q of this slice (late ones clamped to the last, so that every call issues its L loads) into stage q % DEPTH
@@ -406,8 +411,8 @@ __device__ __forceinline__ void rows_main_loop(const uint8_t* const (&a_src)[2],
 #pragma unroll
         for (int x = 0; x < S::X_OPS; ++x)                    // load x = (step e, fragment j, half h), dealt in turn
             if (x % WAVES == wave) {
-                const int e = x / (2 * NF), j = (x / 2) % NF, h = x & 1;
-                dma16(b_src[j][h] + ((size_t)2 * p + e) * 128, xs + x * 1024);
+                const int e = x / (HALVES * NF), j = (x / HALVES) % NF, h = x % HALVES;
+                dma16(b_src[j][h] + ((size_t)2 * p + e) * 128, xs + ((e * NF + j) * 2 + h) * 1024);
             }
     };
     auto issue_meta = [&](int c) {                            // chunk c of 8 pairs of this slice (clamped) into slot c & 1
@@ -476,7 +481,8 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_rows_kernel(const bf16_t* __r
                                                                    const bf16_t* __restrict__ R, int K2,
                                                                    bf16_t* __restrict__ C, float* __restrict__ partial,
                                                                    int slice_pairs, Gate... gate) {
-    using S = RowsLds<NF, WAVES>;
+    constexpr int HALVES = TOKEN_HALVES<Gate...>;
+    using S = RowsLds<NF, WAVES, HALVES>;
     constexpr bool GATED = sizeof...(Gate) > 0;
     extern __shared__ __align__(16) uint8_t smem[];
     const int t = threadIdx.x, lane = t & 63;
@@ -515,13 +521,16 @@ __global__ void __launch_bounds__(WAVES * 64) spmm_rows_kernel(const bf16_t* __r
     for (int j = 0; j < NF; ++j) acc[j] = (f32x4){0.f, 0.f, 0.f, 0.f};
     // the token loads of a pair go to the wavefronts in turn: wavefront w issues those with x % WAVES == w
     if constexpr (S::X_OPS % WAVES == 0) {
-        rows_main_loop<NF, WAVES, S::X_OPS / WAVES>(a_src, m_src, b_src, wave, mine, xring, pair0, npairs, l16, lq, acc);
+        rows_main_loop<NF, WAVES, HALVES, S::X_OPS / WAVES>(a_src, m_src, b_src, wave, mine, xring, pair0, npairs, l16, lq, acc);
+    } else if constexpr (S::X_OPS < WAVES) {
+        if (wave < S::X_OPS) rows_main_loop<NF, WAVES, HALVES, 1>(a_src, m_src, b_src, wave, mine, xring, pair0, npairs, l16, lq, acc);
+        else rows_main_loop<NF, WAVES, HALVES, 0>(a_src, m_src, b_src, wave, mine, xring, pair0, npairs, l16, lq, acc);
     } else {
         static_assert(WAVES == 3, "each wavefront its own number of loads");
         constexpr int XW0 = (S::X_OPS + 2) / 3, XW1 = (S::X_OPS + 1) / 3, XW2 = S::X_OPS / 3;
-        if (wave == 0) rows_main_loop<NF, WAVES, XW0>(a_src, m_src, b_src, 0, mine, xring, pair0, npairs, l16, lq, acc);
-        else if (wave == 1) rows_main_loop<NF, WAVES, XW1>(a_src, m_src, b_src, 1, mine, xring, pair0, npairs, l16, lq, acc);
-        else rows_main_loop<NF, WAVES, XW2>(a_src, m_src, b_src, 2, mine, xring, pair0, npairs, l16, lq, acc);
+        if (wave == 0) rows_main_loop<NF, WAVES, HALVES, XW0>(a_src, m_src, b_src, 0, mine, xring, pair0, npairs, l16, lq, acc);
+        else if (wave == 1) rows_main_loop<NF, WAVES, HALVES, XW1>(a_src, m_src, b_src, 1, mine, xring, pair0, npairs, l16, lq, acc);
+        else rows_main_loop<NF, WAVES, HALVES, XW2>(a_src, m_src, b_src, 2, mine, xring, pair0, npairs, l16, lq, acc);
     }
     __syncthreads();                                          // the rings are free
 
@@ -842,7 +851,7 @@ template <int NF, int WAVES, class... Gate>
 static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, const uint8_t* Am, int64_t m, int64_t K,
                               const bf16_t* T, const bf16_t* R, int64_t K2, bf16_t* C, float* partial, int slices,
                               hipStream_t s, const Gate&... gate) {
-    using S = RowsLds<NF, WAVES>;
+    using S = RowsLds<NF, WAVES, TOKEN_HALVES<Gate...>>;
     static_assert(S::TOTAL <= 160 * 1024, "LDS budget");
     hipError_t e = allow_dynamic_lds<spmm_rows_kernel<NF, WAVES, Gate...>>(S::TOTAL);
     if (e != hipSuccess) return e;
@@ -879,8 +888,8 @@ static hipError_t launch_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals
     if (slices > 0) {
         if constexpr (sizeof...(Gate) > 0)
             if (gated_rows_of_64(n, m, K, slices)) return launch_rows<1, 4>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
-        return n <= 16 ? launch_rows<1, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...)
-                       : launch_rows<2, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
+        if (n <= 16) return launch_rows<1, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
+        if constexpr (TOKEN_HALVES<Gate...> == 2) return launch_rows<2, ROWS_WAVES>(B, n, A_vals, A_meta, m, K, T, R, K2, C, partial, slices, s, gate...);
     }
     const int rows = spmm_stream_rows(n, m, K);
     if (n <= 16) {
@@ -888,8 +897,11 @@ static hipError_t launch_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals
         if (rows == 48) return launch_stream_lds<3, 6, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
         return launch_stream_lds<4, 4, 1>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
     }
-    if (rows == 48) return launch_stream_lds<3, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
-    return launch_stream_lds<2, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+    if constexpr (TOKEN_HALVES<Gate...> == 2) {
+        if (rows == 48) return launch_stream_lds<3, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+        return launch_stream_lds<2, 4, 2>(B, n, A_vals, A_meta, m, K, T, R, K2, C, xl, s, gate...);
+    }
+    return hipErrorInvalidValue;
 }
 
 // n <= 32, K % 64 == 0, K >= 128; T (bf16[n][K2]) and R (bf16[K2][m]) only when K2 > 0; partial_or_null: scratch of
@@ -973,6 +985,11 @@ bool launch_spmm_stream_adapter(const bf16_t* B, int64_t n, const bf16_t* A_vals
 bool gated_stream_takes_l(int64_t n, int64_t m, int64_t K, int64_t r, bool sliced) {
     return r > 0 && spmm_rows_slices(n, m, K, sliced) == 0 && xl_by_itself(n, m, K, r);
 }
+static hipError_t launch_gated_few(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t m, int64_t K, const bf16_t* T,
+                                   const bf16_t* R, int64_t K2, bf16_t* H, float* partial, int slices, const StreamXl& xl, hipStream_t s, const GateOut& gate) {
+    if (n <= 8) return launch_stream(B, n, A_vals, A_meta, m, K, T, R, K2, H, partial, slices, xl, s, GateFew{gate});
+    return launch_stream(B, n, A_vals, A_meta, m, K, T, R, K2, H, partial, slices, xl, s, gate);
+}
 // Beside the product, as xl_beside says, where nothing is kept: sums of both, and adapter_finish_kernel (us, 13824 x 2560, X L before / so: one token, rank
 // 32 21.5 / 17.9, rank 128 22.8 / 18.7; 8, 22.4 / 18.4 and 23.6 / 19.3).
 static bool gated_beside(int64_t n, int64_t m, int64_t K, int64_t r, StreamXl& xl) {
@@ -995,7 +1012,7 @@ hipError_t launch_gated_stream_beside(const bf16_t* B, int64_t n, const bf16_t* 
     if (!gated_beside(n, m, K, r, xl)) return hipErrorInvalidValue;
     GateOut out = gate;
     out.sums = sums;
-    const hipError_t e = launch_stream(B, n, A_vals, A_meta, m, K, nullptr, nullptr, 0, H, nullptr, 0, xl, s, out);
+    const hipError_t e = launch_gated_few(B, n, A_vals, A_meta, m, K, nullptr, nullptr, 0, H, nullptr, 0, xl, s, out);
     return e != hipSuccess ? e : launch_gated_adapter_finish(sums, 1, n, gate.d_ff, Q, xl.slabs, R, r, H, gate, s);
 }
 hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* L,
@@ -1005,7 +1022,7 @@ hipError_t launch_gated_stream(const bf16_t* B, int64_t n, const bf16_t* A_vals,
     const bool leave = gate.keeps() || slices > 1;            // sums, not h
     GateOut out = gate;
     out.sums = leave ? sums_or_null : nullptr;
-    const hipError_t e = launch_stream(B, n, A_vals, A_meta, m, K, T, R, r, H, out.sums, slices, StreamXl{L, nullptr, nullptr, (int)r, 0, 0, 0}, s, out);
+    const hipError_t e = launch_gated_few(B, n, A_vals, A_meta, m, K, T, R, r, H, out.sums, slices, StreamXl{L, nullptr, nullptr, (int)r, 0, 0, 0}, s, out);
     return e != hipSuccess || !leave ? e : launch_gated_sum(out.sums, slices > 1 ? slices : 1, n, m, H, gate, s);
 }
 

@@ -191,7 +191,8 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // A tile's results, BMT virtual rows (BMT / 2 elements) x BNT tokens, by THREADS threads: like store_rows through LDS, since whole rows
-// of a tile leave in whole lines.  h and the codes together, then bf16 projections.  All threads make the call.
+// of a tile leave in whole lines.  h, then the codes, converted while h is on its way (together with h, us: 2048 tokens, 13824 x 2560 108.3 / 105.6, 16384,
+// 18432 x 2560 942 / 928), then bf16 projections.  All threads make the call.
 // What is kept is for the backward pass, long after, and passes the caches by, but for codes that fit a quarter of the last-level one beside
 // others' (us, 16384 tokens, 18432 x 2560, bf16 924 -> 875, codes 931 -> 901; 2048, 13824 x 2560, bf16 111 -> 107, codes 107 -> 105 but, with the
 // gradient right behind, 128.5 -> 131).  The tiles of a round end together, so that their results are a burst at the memory's rate, 5 us for the
@@ -234,6 +235,11 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                 *(u32x2*)(smem + (lt + j * 16) * (BMT + 16) + (le + i * 16) * 2) = four_bf16(h);
             }
     });
+    lds_barrier();
+    leave(std::integral_constant<int, BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
+        const int e = tile_e0 + p * 8;
+        if (e < count) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
+    });
     const size_t blocks = ((size_t)d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
     if constexpr (MF % 4 == 0) if (gate.q) {                  // whole blocks in a wavefront's rows: no other tile is given codes to write
 #pragma unroll
@@ -258,13 +264,9 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
                     if (lq == 0 && tok < n && e < count) gate.bytes[((size_t)tok * 2 + half) * blocks + e / Q8_BLOCK] = (uint8_t)s.byte;
                 }
     }
-    lds_barrier();
-    leave(std::integral_constant<int, BMT>{}, smem, [&](int tok, int p, const u32x4& v) {
-        const int e = tile_e0 + p * 8;
-        if (e < count) *(u32x4*)(H + (size_t)tok * d_ff + e) = v;
-    });
     const bool large = (size_t)n * d_ff > LAST_LEVEL_CACHE_BYTES / 8;
-    if constexpr (MF % 4 == 0) if (gate.q)
+    if constexpr (MF % 4 == 0) if (gate.q) {
+        lds_barrier();
         leave(std::integral_constant<int, BMT>{}, smem + CODES, [&](int tok, int p, const u32x4& v) {
             const int half = p * 16 / HALF, e = tile_e0 + p * 16 % HALF;
             uint8_t* const to = gate.q + (size_t)tok * (2 * (size_t)d_ff) + half * (size_t)d_ff + e;
@@ -273,6 +275,7 @@ __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, 
             else if (e + 8 < count) *(u32x4_a8*)to = v;
             else if (e < count) *(u32x2*)to = (u32x2){v[0], v[1]};
         });
+    }
     if (gate.gu) {                                            // uniform
         lds_barrier();
 #pragma unroll

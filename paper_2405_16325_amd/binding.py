@@ -729,8 +729,10 @@ def slope_gated_fwd(X: torch.Tensor, vals: torch.Tensor, meta: torch.Tensor, act
 
 
 def slope_gated_bwd(dH: torch.Tensor, act: int = SLOPE_ACT_SILU, gu=None, q8=None, scale=None, want_h: bool = True, out=None):
-    """Gradient of slope_gated_fwd from the projections it kept, gu bf16[b, 2 d_ff] or q8 e4m3[b, 2 d_ff] with its scale:
-    (dGU bf16[b, 2 d_ff], H bf16[b, d_ff] again or None).  out: the same two, to write into; dGU may be gu, H may be dH."""
+    """Gradient of slope_gated_fwd from the projections it kept, gu bf16[b, 2 d_ff] or q8 e4m3[b, 2 d_ff] with its scale
+    u8[b, 2, (d_ff + 31) // 32]: (dGU bf16[b, 2 d_ff], H bf16[b, d_ff] again or None).  Codes and scale may also have the shapes that
+    slope_checkpoint_q8 gives those of [2 b, d_ff]: the memory is the same.  out: the same two, to write into; dGU may be gu, H may be
+    dH."""
     if dH is None or dH.dim() != 2:
         raise ValueError("dH must be a matrix")
     b, d_ff = dH.shape
@@ -740,8 +742,8 @@ def slope_gated_bwd(dH: torch.Tensor, act: int = SLOPE_ACT_SILU, gu=None, q8=Non
     if gu is not None:
         _want(gu, BF16, (b, 2 * d_ff), "gu")
     else:
-        _want(q8, E4M3, (b, 2 * d_ff), "q8")
-        _want(scale, U8, (b, 2, _blocks(d_ff)), "scale")
+        _want(q8, E4M3, (2 * b, d_ff) if q8.shape == (2 * b, d_ff) else (b, 2 * d_ff), "q8")
+        _want(scale, U8, (2 * b, _blocks(d_ff)) if scale is not None and scale.dim() == 2 else (b, 2, _blocks(d_ff)), "scale")
     if out is None:
         dGU = dH.new_empty((b, 2 * d_ff))
         H = torch.empty_like(dH) if want_h else None

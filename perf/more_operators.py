@@ -265,11 +265,7 @@ def run(state):
         dgu, again = sl.slope_gated_bwd(s["dh"], act, q8=codes, scale=byte)
         return {"h": h, "dgu": dgu, "h_again": again}
     if kind == "gated_bwd":
-        codes, byte = s["codes"], s["byte"]
-        if codes is not None:                    # as slope_gated_fwd writes them
-            b, d_ff = s["dh"].shape
-            codes, byte = codes.view(b, 2 * d_ff), byte.view(b, 2, -1)
-        dgu, h = sl.slope_gated_bwd(s["dh"], act, gu=s["gu"], q8=codes, scale=byte)
+        dgu, h = sl.slope_gated_bwd(s["dh"], act, gu=s["gu"], q8=s["codes"], scale=s["byte"])
         return {"dgu": dgu, "h": h}
     if kind == "ckpt":
         return sl.slope_restore_q8(*sl.slope_checkpoint_q8(s["x"]))

@@ -264,10 +264,11 @@ __device__ __forceinline__ void store_sums(const f32x4 (&acc)[MF][NF], int m, in
 }
 
 // The loading wavefronts where A, k-major, comes in 8-bit blocks: `wave` of TN_LOADERS, each with the loads of EACH of eight, as they would be of
-// bf16 (DenseLoader).  Codes go through registers, restored on their way to the same places in LDS, AHEAD k-steps after their request (three where the
-// ring has room for seven: 2398 tokens, 448 x 1488 17.1 us, 15.5 so); B's loads are as ever.  All loads complete in order, and a k-step's codes are
-// requested after its rows of B, so that when its codes are there B's rows are.  For that every wavefront requests codes in every k-step (columns past the last are the
-// last eight, for rows that are not stored).
+// bf16 (DenseLoader).  Codes go through registers, restored on their way to the same places in LDS; they and B's rows, which load as ever, are requested
+// AHEAD k-steps before (three where the ring has room for seven: 2398 tokens, 448 x 1488 17.1 us, 15.5 so).  But the requests hang on whether there is such a
+// k-step, so that the compiler cannot count what is outstanding: it waits for all of them (vmcnt(0)) before the first of every AHEAD k-steps, and before no other.
+// All loads complete in order, and a k-step's codes are requested after its rows of B (`then` keeps them so), so that when its codes are there B's rows
+// are.  For that every wavefront requests codes in every k-step (columns past the last are the last eight, for rows that are not stored).
 template <int BM, int BN, int NS, bool BKM, int WROWS, int PRE>
 __device__ __forceinline__ void load_and_restore(const DenseOperand& At, const DenseOperand& Bt, const BlocksX& x, int ksteps, int k_begin, int k_end,
                                                  int m0, int n0, int wave, int lane, uint8_t* smem) {
@@ -312,6 +313,10 @@ __device__ __forceinline__ void load_and_restore(const DenseOperand& At, const D
                 c.byte[v][i] = __builtin_amdgcn_raw_buffer_load_b8(b, (int)byte_at[v][i], 0, 0);
             }
     };
+    auto then = [] {                                          // loads before it are issued before those behind it
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
     auto restore = [&](const Codes& c, int at) {
 #pragma unroll
         for (int v = 0; v < EACH; ++v)
@@ -324,6 +329,7 @@ __device__ __forceinline__ void load_and_restore(const DenseOperand& At, const D
     for (int p = 0; p < NS - 1; ++p)
         if (k_begin + p < k_end) {
             load_b(k_begin + p, p * S::STAGE, p < PRE ? MULT : 0);
+            then();
             fetch(codes[p], k_begin + p);
         }
     int at = 0;
@@ -335,8 +341,11 @@ __device__ __forceinline__ void load_and_restore(const DenseOperand& At, const D
             restore(codes[u], at);
             WAIT_HERE(waitcnt_imm(63, 0));
             wg_barrier();                                     // step ks is there, and everybody has read the one before it
-            if (ks + NS - 1 < k_end) load_b(ks + NS - 1, at == 0 ? LAST : at - S::STAGE, 0);
-            if (ks + AHEAD < k_end) fetch(codes[u], ks + AHEAD);
+            if (ks + AHEAD < k_end) {
+                load_b(ks + AHEAD, at == 0 ? LAST : at - S::STAGE, 0);
+                then();
+                fetch(codes[u], ks + AHEAD);
+            }
             at = at == LAST ? 0 : at + S::STAGE;
         }
 }

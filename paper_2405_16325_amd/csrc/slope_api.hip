@@ -673,8 +673,16 @@ static GatedPlan gated_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, bo
 
 size_t slope_gated_fwd_workspace_bytes(int64_t b, int64_t d_in, int64_t d_ff, int64_t r, int kept) {
     if (bad_gated(b, d_ff) || bad_extent(d_in, 8) || r < 0) return 0;
-    const size_t h = gated_plan(b, d_in, d_ff, r, false).total, all = kept ? gated_plan(b, d_in, d_ff, r, true).total : 0;
-    return h > all ? h : all;                                 // (room for what is kept is room for h alone)
+    // room for what is kept is room for h alone, and room for an adapter is room without one (L and R NULL), whose product may be split where the
+    // other is not
+    size_t need = 0;
+    for (int form = 0; form < 4; ++form) {
+        const bool adapter = form & 1, keeps = form & 2;
+        if ((adapter && !r) || (keeps && !kept)) continue;
+        const size_t total = gated_plan(b, d_in, d_ff, adapter ? r : 0, keeps).total;
+        if (total > need) need = total;
+    }
+    return need;
 }
 
 slope_status slope_gated_fwd(const void* X, int64_t b, const void* Wr_vals, const void* Wr_meta, int64_t d_ff, int64_t d_in, int act,

@@ -522,7 +522,8 @@ slope_status slope_spmm_fwd_q8_plan(int64_t b, int64_t d_in, int64_t d_out, int 
  * keeps GUq.  plan: host int32[6]
  *   [0] product, [1], [2] rows of the weight, gate and up projection, and tokens per workgroup, [3] slabs, slices or the tokens of
  *       the small-batch kernel: as slope_spmm_fwd_plan; or [0] 6, tiles of that size for the last rows and, in a launch before,
- *       256 x 256 ones for the first [3], which are whole rounds of them
+ *       256 x 256 ones for the first [3], which are whole rounds of them; or [0] 7, these two launches for the tokens of whole tiles and,
+ *       behind them, a small-batch kernel for the last b % 128.  Of more tokens than a launch's grid holds, the first launches' tiles
  *   [4] T = X L: 1 computed by the small-batch kernel's workgroups, 2 by others beside the product's, 0 before it (or no adapter)
  *   [5] columns of the padded copies that the call makes of its operands (0 = none)
  */

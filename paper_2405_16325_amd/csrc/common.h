@@ -164,6 +164,7 @@ hipError_t launch_adamw(const void* table, const void* device_table, double lr, 
 // the gated layer and 8-bit checkpoints (spmm.hip, spmm_stream.hip, gated.hip, wgrad_tn.hip)
 struct GateOut;
 int64_t gated_padded(int64_t n, int64_t d_ff, int64_t K);
+int64_t gated_launch_tokens(int64_t d_ff);
 int64_t gated_first_rows(int64_t n, int64_t m, int64_t K, bool blocks);
 hipError_t launch_pad_operands(const bf16_t* x, int64_t n, const bf16_t* vals, const uint8_t* meta, int64_t rows, int64_t K, int64_t Kp,
                                bf16_t* xp, bf16_t* vp, uint8_t* mp, hipStream_t s);

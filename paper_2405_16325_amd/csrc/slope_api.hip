@@ -762,20 +762,16 @@ slope_status slope_gated_fwd_plan(int64_t b, int64_t d_in, int64_t d_ff, int64_t
         plan[5] = (int32_t)p.padded;
         d_in = p.K;
     }
-    const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in);
+    const int64_t m = gated_rows(d_ff), rest = split.slabs || kept ? 0 : spmm_rest_tokens(b, m, d_in), most = gated_launch_tokens(d_ff);
+    const int64_t n = b - rest < most ? b - rest : most;
+    const int64_t first = split.slabs ? 0 : gated_first_rows(n, m, d_in, kept == 8);
     int bm, bn;
-    spmm_tile_choice(b - rest, m, d_in, r > 0, bm, bn, kept == 8);
+    spmm_tile_choice(n, m - first, d_in, r > 0, bm, bn, kept == 8);
     if (split.slabs) { plan[0] = 1; plan[1] = split.bm; plan[2] = split.bn; plan[3] = split.slabs; }
-    else if (bm == 0) { plan[0] = 3; plan[1] = plan[2] = spmm_generic_edge(b - rest, m); }
+    else if (bm == 0) { plan[0] = 3; plan[1] = plan[2] = spmm_generic_edge(n, m - first); }
     else { plan[0] = 2; plan[1] = bm; plan[2] = bn; }
-    if (rest) { plan[0] = 5; plan[3] = (int32_t)rest; }
-    else if (const int64_t first = split.slabs ? 0 : gated_first_rows(b, m, d_in, kept == 8)) {
-        spmm_tile_choice(b, m - first, d_in, r > 0, bm, bn, kept == 8);
-        plan[0] = 6;
-        plan[1] = bm ? bm : spmm_generic_edge(b, m - first);
-        plan[2] = bm ? bn : plan[1];
-        plan[3] = (int32_t)first;
-    }
+    if (first) { plan[0] = rest ? 7 : 6; plan[3] = (int32_t)first; }
+    else if (rest) { plan[0] = 5; plan[3] = (int32_t)rest; }
     return SLOPE_OK;
 }
 

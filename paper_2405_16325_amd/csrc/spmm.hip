@@ -1923,9 +1923,10 @@ hipError_t launch_gated_slabs(const bf16_t* B, int64_t n, const bf16_t* A_vals, 
 }
 
 // Tokens by as many as a launch's grid holds (d_ff is at most 2^22: at least 1024 of them, in whole tiles)
+int64_t gated_launch_tokens(int64_t d_ff) { return ((int64_t)1 << 21) / ((gated_rows(d_ff) + 63) / 64) * 64 / 256 * 256; }
 hipError_t launch_gated(const bf16_t* B, int64_t n, const bf16_t* A_vals, const uint8_t* A_meta, int64_t K, const bf16_t* T, const bf16_t* R,
                         int64_t r, bf16_t* H, const GateOut& gate, hipStream_t s) {
-    const int64_t most = ((int64_t)1 << 21) / ((gated_rows(gate.d_ff) + 63) / 64) * 64 / 256 * 256;
+    const int64_t most = gated_launch_tokens(gate.d_ff);
     const size_t d_ff = (size_t)gate.d_ff, blocks = (d_ff + Q8_BLOCK - 1) / Q8_BLOCK;
     const int64_t rest = gate.keeps() ? 0 : spmm_rest_tokens(n, gated_rows(gate.d_ff), K);
     n -= rest;                                                // the last few: one pass of the small-batch kernel, behind the others

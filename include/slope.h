@@ -456,17 +456,17 @@ slope_status slope_wgrad_masked_q8(const void* dY, const void* Xq, const void* x
  * 2 d_ff rows, the gate's first (pruned, double-pruned and updated like any other: groups along d_out stay inside a half):
  *     [g | u] = X (W^R)^T (+ (X L) R)        H = bf16(act(g) u)          g, u in fp32
  *   X in bf16[b, d_in]    Wr_vals bf16[2 d_ff, d_in/2], Wr_meta u8[2 d_ff, d_in/8]    d_ff % 8 == 0, 2 d_ff <= 2^23
- *   act   SLOPE_ACT_SILU   g s(g), s the logistic function
+ *   act   SLOPE_ACT_SILU   g s(g), s the logistic function (zero where it is below 2^-126)
  *         SLOPE_ACT_GELU   g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2
  *         SLOPE_ACT_RELU   max(g, 0)                                     (others: SLOPE_ERR_VALUE)
- *   L_or_null bf16[d_in, r], R_or_null bf16[r, 2 d_ff], r   as for slope_spmm_fwd
+ *   L_or_null bf16[d_in, r], R_or_null bf16[r, 2 d_ff], r   as for slope_spmm_fwd: X L is rounded to bf16 before it meets R
  *   H out bf16[b, d_ff]
  *   What the backward pass wants, either or both of (NULL: not kept; fp32 values of g and u rounded once):
  *     GU_or_null  out bf16[b, 2 d_ff]
  *     GUq_or_null, GU_scale_or_null  out e4m3[b, 2 d_ff], u8[b, 2, (d_ff + 31) / 32]: slope_checkpoint_q8's form of [2 b, d_ff], a token's
  *                 gate and then its up projection; both or neither
- *   workspace_or_null  slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, kept) bytes (may be 0), 256-byte aligned; kept: 0 where only H is
- *                 wanted, 8 or 16 (slope_workspace_bytes answers for these) where anything is kept.  Required with an adapter.
+ *   workspace_or_null  slope_gated_fwd_workspace_bytes(b, d_in, d_ff, r, kept) bytes (may be 0; never less than for r = 0), 256-byte aligned;
+ *                 kept: 0 where only H is wanted, 8 or 16 (slope_workspace_bytes answers for these) where anything is kept.  Required with an adapter.
  *                 Lets the call split the contraction, and copy operands whose d_in is no multiple of 64 into padded ones where that pays
  *
  * slope_gated_bwd - its gradient from what was kept, element by element:

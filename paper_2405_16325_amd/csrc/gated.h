@@ -197,7 +197,7 @@ __device__ __forceinline__ void lds_barrier() {
 // others' (us, 16384 tokens, 18432 x 2560, bf16 924 -> 875, codes 931 -> 901; 2048, 13824 x 2560, bf16 111 -> 107, codes 107 -> 105 but, with the
 // gradient right behind, 128.5 -> 131).  The tiles of a round end together, so that their results are a burst at the memory's rate, 5 us for the
 // projections of 256 tiles of 256 x 256 in bf16; codes are half of it and as long again in conversions (16384, 4096 x 768: h 86, with bf16
-// 106, with codes 107).
+// 102, with codes 104).
 template <int MF, int NF, int BMT, int BNT, int THREADS>
 __device__ __forceinline__ void store_gated(const f32x4 (&acc)[MF][NF], int f0, int t0, int n, int l16, int lq, bf16_t* __restrict__ H,
                                             uint8_t* smem, int tile_f0, int tile_t0, const GateOut& gate) {

@@ -867,9 +867,10 @@ static hipError_t launch_rows(const bf16_t* B, int64_t n, const bf16_t* Av, cons
 }
 
 // Gated layers on the row-split kernel take four wavefronts, 64 rows a workgroup, where that saves a thin last round: three workgroups are
-// resident either way.  A workgroup pulls 12.5 bytes per ns, or its share of 4.9 TB/s with many beside it, 5.3 in whole rounds.  us, 48 / 64 rows:
-// one token, 49152 x 9216 110.8 / 95.1, 40960 x 5120 57.5 / 52.4, 16 tokens, 27296 x 5120 41.3 / 37.8; but 36864 x 9216 73.5 / 80.9, 24576 x 9216
-// 54.0 / 56.4, 55296 x 10240 130 / 134.
+// resident either way.  A workgroup pulls 12.5 bytes per ns, or its share of 4.9 TB/s with many beside it, 5.3 in whole rounds.  us, 48 / 64 rows, one
+// token and 16: 49152 x 9216 109 / 94 and 113 / 101, 40960 x 5120 58 / 50 and 58 / 54; but 36864 x 9216 71.5 / 79 and 74 / 85, 24576 x 9216 50 / 51 and
+// 48 / 54, 55296 x 10240 121.5 / 125.5 and 129 / 133.  The estimate sees no difference between two numbers of workgroups that are each less than a
+// round, and 48 rows stay where 64 are faster: 27296 x 5120 32.5 / 30.5 and 38 / 34, 28672 x 4096 32.0 / 31.6 and 33.6 / 31.4.
 bool gated_rows_of_64(int64_t n, int64_t m, int64_t K, int slices) {
     if (n > 16 || slices != 1) return false;
     auto us = [&](int64_t rows) {
@@ -945,7 +946,7 @@ static bool xl_by_itself(int64_t n, int64_t m, int64_t K, int64_t r) {
 // per 32 KB (us: 1 token, 9216 x 9216, rank 128 29.1 -> 27.2; 8, 4096 x 4096, rank 64 12.8 -> 11.6; 16, 8000 x 8640, rank 64 28.5 ->
 // 25.6; 2, 17152 x 3328, rank 32 25.3 -> 22.3; without that limit 1, 512 x 26624, rank 96 26.8 -> 50.7, 32, 9216 x 9216, rank
 // 64 37.8 -> 39.3).  Not beside the row-split kernel, whose three wavefronts take 3 us and more per chunk while it saturates
-// the memory: 1, 36864 x 9216, rank 128 72.5 -> 85.3.  And not where its workgroups would begin another round of the product's:
+// the memory: 1, 36864 x 9216, rank 128 72.5 -> 85.3 (a whole round of its workgroups; less than one was not tried).  And not where its workgroups would begin another round of the product's:
 // 8, 16384 x 16256, rank 32, 512 and 4 workgroups 72.9 -> 80.9; 1, 11776 x 18624, rank 96, 246 and 12 65.9 -> 73.0.
 static bool xl_beside(int64_t n, int64_t m, int64_t K, int64_t r, int64_t max_floats, StreamXl& xl) {
     const int64_t chunks = K / 32, waves = stream_waves(n, m, K);
